@@ -156,7 +156,7 @@ def _quantise(x):
     top = b.abs().amax(-1, keepdim=True)
     mant, exp = torch.frexp(top)                 # top = mant * 2^exp, mant in [0.5, 1)
     e = exp - 3 + (mant > 0.875).int()
-    e = torch.where(top > 0, e, torch.full_like(e, -127)).clamp(-127, 127)
+    e = torch.where(top > 0, e, torch.full_like(e, -127)).clamp(-127, 125)
     a = (b / torch.ldexp(torch.ones_like(top), e)).abs()
     code = torch.zeros_like(a, dtype=torch.uint8)
     for i, edge in enumerate((0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0)):
@@ -465,8 +465,8 @@ def _exact_append(s, case):
     for x in (s.k, s.v):
         b = x.double().unflatten(-1, (-1, BLOCK))
         top = b.abs().amax(-1, keepdim=True)
-        e = torch.ceil(torch.log2(top / 7)).clamp(-127, 127)
-        e = torch.where(top > 7 * torch.exp2(e), e + 1, e)
+        e = torch.ceil(torch.log2(top / 7)).clamp(-127, 125)
+        e = torch.where((top > 7 * torch.exp2(e)) & (e < 125), e + 1, e)
         e = torch.where((top <= 7 * torch.exp2(e - 1)) & (e > -127), e - 1, e)
         unit = torch.exp2(e)
         a = (b / unit).abs()
