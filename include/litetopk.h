@@ -312,6 +312,144 @@ int lt_sample_from_topk(const int32_t* prev_idx, int64_t ld, int32_t prev_rows, 
 int lt_dsa_union(const int32_t* topk_idx, int64_t ld, int32_t num_queries, int32_t k, int32_t group,
                  int32_t* union_idx, int32_t* union_count, uint32_t* member_mask, void* stream);
 
+/* ---- serving: paged 4-bit cache, attention over it, log probabilities ------ */
+
+#define LT_MAX_PAGE_SIZE 4096       /* page sizes are powers of two up to this        */
+#define LT_PLAN_MAX_REQUESTS 16384  /* requests of one lt_paged_plan call             */
+#define LT_CACHE4_MAX_HEADS 1024    /* query and KV heads                             */
+#define LT_LOGPROB_MAX_TOP 64       /* alternatives of lt_token_logprobs              */
+#define LT_LOGPROB_MAX_VOCAB (1 << 30)
+
+/* The plan of a serving step: pages for the step's new tokens, and where each
+   token's key and value go. Request r holds context_lens[r] tokens and adds
+   new_lens[r] (both DEVICE int32; negative counts as 0). Its cache is the list
+   of pages block_table[r * table_ld + i], i < table_width; page i holds its
+   tokens [i * page_size, (i + 1) * page_size). The pages that the new tokens
+   need beyond the ceil(context / page_size) held ones are taken from
+   free_pages[*free_used ...] in request order and written into the table
+   (the only entries written). The requests are served in order until the list
+   is exhausted: one that needs pages that are no longer there gets none, nor
+   does any later one that needs pages. The call is a function of its inputs:
+   calling it again with the same free_used gives the same result.
+   cu_tokens     int32 [num_requests + 1]: prefix sums of new_lens (tokens of a
+                 step are packed in request order).
+   seq_lens      int32 [num_requests]: context + new, or context where the
+                 request was not served.
+   slots         int64 [token_capacity]: page * page_size + offset of each new
+                 token; -1 for tokens of requests that were not served, table
+                 entries that are negative and rows past the step's tokens.
+   positions     int32 [token_capacity]: position in the request, -1 past the
+                 step's tokens.
+   free_used_out int32 [1]: *free_used plus the pages taken; must not be
+                 free_used itself.
+   status        int32 [num_requests]: 0 served, 1 the table is too narrow, 2
+                 no free pages.
+   Tokens beyond token_capacity get no row. Prefix sums stop at 2^31 - 1. */
+int lt_paged_plan(const int32_t* context_lens, const int32_t* new_lens, int32_t num_requests, int32_t page_size,
+                  int32_t* block_table, int64_t table_ld, int32_t table_width, const int32_t* free_pages,
+                  int32_t num_free_pages, const int32_t* free_used, int32_t token_capacity, int32_t* cu_tokens,
+                  int32_t* seq_lens, int64_t* slots, int32_t* positions, int32_t* free_used_out, int32_t* status,
+                  void* stream);
+
+/* The 4-bit key/value cache. Per slot and KV head, 32 consecutive values of a
+   row share a scale 2^e (byte e + 127); values are E2M1 codes: 0, 0.5, 1, 1.5,
+   2, 3, 4, 6 with a sign in bit 3, two to a byte, the earlier one in the low
+   half.
+     codes  uint8 [num_pages, num_kv_heads, page_size, 2, head_dim / 2]
+     scales uint8 [num_pages, num_kv_heads, page_size, 2, head_dim / 32]
+   with the key at index 0 and the value at index 1 of the fourth axis. 16-
+   and 8-byte aligned. head_dim is 64 or 128.
+
+   lt_cache4_append writes `rows` keys and values (float32 or bfloat16,
+   [rows, num_kv_heads, head_dim] with k_stride / v_stride values between rows,
+   16-byte aligned rows) to the given slots (DEVICE int64 [rows], distinct;
+   slots outside the cache are left out). The scale is the smallest 2^e with
+   max|x| <= 7 * 2^e (never below 2^-127 nor above 2^125, whose 6 is the largest
+   value there is), values round to the nearest code (halfway: the even code).
+   A block that holds a value that is not finite gets
+   the scale byte 255 and reads as NaN. */
+int lt_cache4_append(const void* k, const void* v, lt_dtype dtype, int64_t k_stride, int64_t v_stride, int64_t rows,
+                     uint8_t* codes, uint8_t* scales, int64_t num_pages, int32_t page_size, int32_t num_kv_heads,
+                     int32_t head_dim, const int64_t* slots, void* stream);
+
+/* The keys and values that slots stand for, as bfloat16 [rows, num_kv_heads,
+   head_dim] each (exact); zeros for slots outside the cache. */
+int lt_cache4_read(const uint8_t* codes, const uint8_t* scales, int64_t num_pages, int32_t page_size,
+                   int32_t num_kv_heads, int32_t head_dim, const int64_t* slots, int64_t rows, void* k, void* v,
+                   void* stream);
+
+/* Bytes of device workspace lt_cache4_attention needs; 0 for a shape that is
+   not supported. */
+size_t lt_cache4_attention_workspace_size(int32_t num_tokens, int32_t num_requests, int32_t num_heads,
+                                          int32_t num_kv_heads, int32_t head_dim, int32_t selected_k);
+
+/* Attention of a step's tokens over their requests' cached keys:
+     out[t, h] = sum_j softmax_j(scale * q[t, h] . k_j) v_j,
+     lse[t, h] = log sum_j exp(scale * q[t, h] . k_j)
+   over the visible keys j of token t; head h reads KV head
+   h / (num_heads / num_kv_heads).
+   q          bfloat16 [num_tokens, num_heads, head_dim], q_stride values
+              between tokens (a multiple of 8), 16-byte aligned.
+   cu_tokens  int32 [num_requests + 1], ascending: request r's tokens are
+              [cu[r], cu[r + 1]). Tokens from cu[num_requests] on belong to no
+              request (a padded batch).
+   seq_lens   int32 [num_requests]: cached keys of the request, the step's own
+              among them.
+   Token t, the i-th of n of its request, sees the keys [s_t, e_t): e_t =
+   visible_end[t], or seq_len - n + i + 1 (causal) without it, clamped to
+   [0, seq_len]; s_t = visible_start[t] (0 without it), clamped to [0, e_t].
+   With selected_k > 0 it sees only those on its list: selected[t *
+   selected_ld + j], j < selected_k, minus selected_start[t] if given (lists of
+   lt_indexer_topk over sequences packed into one key array hold positions in
+   that array; selected_start is then its visible_start). Entries outside
+   [s_t, e_t), such as the -1 padding, do not count; a key listed twice counts
+   twice. Keys whose page is not in the table or not in the cache do not count.
+   A token that sees no key, or belongs to no request, gets out = 0 and lse =
+   -inf. Keys and values that a token does not see never reach its result,
+   whatever they hold.
+   out        bfloat16 [num_tokens, num_heads, head_dim], 16-byte aligned.
+   lse        float32 [num_tokens, num_heads] or NULL.
+   scale      > 0 and finite.
+   workspace  256-byte aligned; contents on entry do not matter. */
+int lt_cache4_attention(const void* q, int64_t q_stride, int32_t num_tokens, int32_t num_heads, int32_t head_dim,
+                        const uint8_t* codes, const uint8_t* scales, int64_t num_pages, int32_t page_size,
+                        int32_t num_kv_heads, const int32_t* block_table, int64_t table_ld, int32_t table_width,
+                        const int32_t* cu_tokens, const int32_t* seq_lens, int32_t num_requests,
+                        const int32_t* visible_start, const int32_t* visible_end, const int32_t* selected,
+                        int64_t selected_ld, int32_t selected_k, const int32_t* selected_start, float scale,
+                        void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of device workspace lt_token_logprobs needs; 0 for an unsupported shape. */
+size_t lt_token_logprobs_workspace_size(lt_dtype dtype, int32_t rows, int32_t vocab, int32_t top);
+
+/* What a model's logits say of given tokens. With y = scale * logits (scale =
+   1 / temperature) and p = softmax(y), per row:
+     lse = log sum exp(y),  logprob = y[token] - lse,
+     entropy = -sum p log p,
+     the `top` best entries by the total order at the head of this file (raw
+     logits; equal ones: lower index first) and their log probabilities.
+   logits     float32 or bfloat16, ld >= vocab values between rows (no
+              alignment beyond the elements').
+   tokens     int64 [rows]; a token outside [0, vocab) is not counted: logprob 0.
+   top        0..LT_LOGPROB_MAX_TOP; a vocabulary of fewer entries is padded with
+              index -1 and log probability -inf.
+   Logits of -inf are masked out: probability 0. A row of nothing else has lse
+   -inf, entropy 0 and log probabilities -inf. NaN or +inf gives NaN. */
+int lt_token_logprobs(const void* logits, lt_dtype dtype, int64_t ld, int32_t rows, int32_t vocab,
+                      const int64_t* tokens, float scale, int32_t top, float* logprob, float* entropy, float* lse,
+                      int32_t* top_index, float* top_logprob, void* workspace, size_t workspace_bytes,
+                      void* stream);
+
+/* The logits' gradient, given those of logprob and entropy (either may be
+   NULL: zero) and the forward's lse and entropy:
+     grad = scale * (g_lp * ([i = token] - p_i) - g_H * p_i * (log p_i + entropy))
+   in the logits' type, grad_ld >= vocab values between rows. A token that is
+   not counted has no g_lp term; a row of -inf alone gets zeros. */
+int lt_token_logprobs_backward(const void* logits, lt_dtype dtype, int64_t ld, int32_t rows, int32_t vocab,
+                               const int64_t* tokens, float scale, const float* lse, const float* entropy,
+                               const float* grad_logprob, const float* grad_entropy, void* grad_logits,
+                               int64_t grad_ld, void* stream);
+
 /* ---- timing helpers ------------------------------------------------------- */
 
 /* Thin wrappers over hipEventCreateWithFlags / hipEventDestroy /

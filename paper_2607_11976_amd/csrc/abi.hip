@@ -6,6 +6,7 @@
 #include <algorithm>
 #include <mutex>
 
+#include "cache4.hpp"
 #include "internal.hpp"
 #include "select_dev.hpp"
 
@@ -297,6 +298,10 @@ Resolved resolve_scores(const lt_options* o, int nq, int nk, int k, bool split) 
 }
 
 inline bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
+
+// page sizes of the serving cache: powers of two up to LT_MAX_PAGE_SIZE
+inline bool page_shift_ok(int p) { return p >= 1 && p <= LT_MAX_PAGE_SIZE && (p & (p - 1)) == 0; }
+inline int page_shift(int p) { return __builtin_ctz((unsigned)p); }
 
 inline int hip_status(hipError_t e) { return e == hipSuccess ? LT_OK : LT_EHIP; }
 
@@ -603,6 +608,214 @@ int lt_dsa_union(const int32_t* idx, int64_t ld, int32_t nq, int32_t k, int32_t 
   if (!idx || !union_idx || !union_count || !member_mask) return LT_EINVAL;
   return hip_status(launch_dsa_union(idx, ld, nq, k, group, union_idx, union_count, member_mask,
                                      (hipStream_t)stream));
+}
+
+int lt_paged_plan(const int32_t* context_lens, const int32_t* new_lens, int32_t nreq, int32_t page_size,
+                  int32_t* block_table, int64_t table_ld, int32_t table_width, const int32_t* free_pages,
+                  int32_t num_free, const int32_t* free_used, int32_t token_capacity, int32_t* cu_tokens,
+                  int32_t* seq_lens, int64_t* slots, int32_t* positions, int32_t* free_used_out, int32_t* status,
+                  void* stream) {
+  if (nreq < 0 || table_width < 0 || table_ld < table_width || num_free < 0 || token_capacity < 0) return LT_EINVAL;
+  if (!page_shift_ok(page_size)) return LT_EINVAL;
+  if (nreq > LT_PLAN_MAX_REQUESTS) return LT_EUNSUPPORTED;
+  if (!free_used || !free_used_out || free_used == free_used_out || !cu_tokens) return LT_EINVAL;
+  if (nreq > 0 && (!context_lens || !new_lens || !seq_lens || !status)) return LT_EINVAL;
+  if (nreq > 0 && table_width > 0 && !block_table) return LT_EINVAL;
+  if (num_free > 0 && !free_pages) return LT_EINVAL;
+  if (token_capacity > 0 && (!slots || !positions || !aligned(slots, 8))) return LT_EINVAL;
+  PlanArgs a{};
+  a.context = context_lens;
+  a.added = new_lens;
+  a.free_list = free_pages;
+  a.free_used = free_used;
+  a.table = block_table;
+  a.table_ld = table_ld;
+  a.cu = cu_tokens;
+  a.seq = seq_lens;
+  a.positions = positions;
+  a.status = status;
+  a.free_out = free_used_out;
+  a.slots = slots;
+  a.R = nreq;
+  a.width = table_width;
+  a.free_count = num_free;
+  a.capacity = token_capacity;
+  a.shift = page_shift(page_size);
+  return hip_status(launch_paged_plan(a, (hipStream_t)stream));
+}
+
+// Checks of a 4-bit cache; fills c.
+static int check_cache4(const void* codes, const void* scales, int64_t num_pages, int32_t page_size, int32_t hkv,
+                        int32_t d, Cache4* c) {
+  if (num_pages < 0 || hkv < 1 || d < 1) return LT_EINVAL;
+  if (!page_shift_ok(page_size)) return LT_EINVAL;
+  if (d != 64 && d != 128) return LT_EUNSUPPORTED;
+  if (hkv > LT_CACHE4_MAX_HEADS || num_pages > 0x7FFFFFFF) return LT_EUNSUPPORTED;
+  if (num_pages > 0 && (!codes || !scales || !aligned(codes, 16) || !aligned(scales, 8))) return LT_EINVAL;
+  *c = Cache4{num_pages, page_shift(page_size), hkv, d};
+  return LT_OK;
+}
+
+int lt_cache4_append(const void* k, const void* v, lt_dtype dtype, int64_t k_stride, int64_t v_stride, int64_t rows,
+                     uint8_t* codes, uint8_t* scales, int64_t num_pages, int32_t page_size, int32_t num_kv_heads,
+                     int32_t d, const int64_t* slots, void* stream) {
+  Cache4 c;
+  const int rc = check_cache4(codes, scales, num_pages, page_size, num_kv_heads, d, &c);
+  if (rc) return rc;
+  if (dtype != LT_F32 && dtype != LT_BF16) return LT_EUNSUPPORTED;
+  if (rows < 0 || rows > 0x7FFFFFFF) return LT_EINVAL;
+  if (rows == 0 || num_pages == 0) return LT_OK;
+  const int64_t width = (int64_t)num_kv_heads * d, unit = dtype == LT_F32 ? 4 : 8;
+  if (k_stride < width || v_stride < width || k_stride % unit || v_stride % unit) return LT_EINVAL;
+  if (!k || !v || !slots || !aligned(k, 16) || !aligned(v, 16) || !aligned(slots, 8)) return LT_EINVAL;
+  return hip_status(launch_cache4_append(k, v, dtype == LT_F32, k_stride, v_stride, rows, c, codes, scales, slots,
+                                         (hipStream_t)stream));
+}
+
+int lt_cache4_read(const uint8_t* codes, const uint8_t* scales, int64_t num_pages, int32_t page_size,
+                   int32_t num_kv_heads, int32_t d, const int64_t* slots, int64_t rows, void* k, void* v,
+                   void* stream) {
+  Cache4 c;
+  const int rc = check_cache4(codes, scales, num_pages, page_size, num_kv_heads, d, &c);
+  if (rc) return rc;
+  if (rows < 0 || rows > 0x7FFFFFFF) return LT_EINVAL;
+  if (rows == 0) return LT_OK;
+  if (!k || !v || !slots || !aligned(k, 16) || !aligned(v, 16) || !aligned(slots, 8)) return LT_EINVAL;
+  return hip_status(launch_cache4_read(c, codes, scales, slots, rows, k, v, (hipStream_t)stream));
+}
+
+// The shape's part of an attention call; false where it is none that is built.
+static int attn4_shape(int32_t tokens, int32_t nreq, int32_t hq, int32_t hkv, int32_t d, int32_t list_k,
+                       Attn4Args* a) {
+  if (tokens < 0 || nreq < 0 || hq < 1 || hkv < 1 || d < 1 || list_k < 0 || hq % hkv) return LT_EINVAL;
+  if (d != 64 && d != 128) return LT_EUNSUPPORTED;
+  if (hkv > LT_CACHE4_MAX_HEADS || hq > LT_CACHE4_MAX_HEADS) return LT_EUNSUPPORTED;
+  if ((int64_t)tokens * hq > 0x3FFFFFFF) return LT_EUNSUPPORTED;
+  *a = Attn4Args{};
+  a->T = tokens;
+  a->R = nreq;
+  a->hkv = hkv;
+  a->group = hq / hkv;
+  a->d = d;
+  a->list_k = list_k;
+  return LT_OK;
+}
+
+size_t lt_cache4_attention_workspace_size(int32_t tokens, int32_t nreq, int32_t hq, int32_t hkv, int32_t d,
+                                          int32_t list_k) {
+  Attn4Args a;
+  if (attn4_shape(tokens, nreq, hq, hkv, d, list_k, &a)) return 0;
+  return tokens == 0 ? 256 : attn4_workspace_bytes(a);
+}
+
+int lt_cache4_attention(const void* q, int64_t q_stride, int32_t tokens, int32_t hq, int32_t d, const uint8_t* codes,
+                        const uint8_t* scales, int64_t num_pages, int32_t page_size, int32_t hkv,
+                        const int32_t* block_table, int64_t table_ld, int32_t table_width, const int32_t* cu_tokens,
+                        const int32_t* seq_lens, int32_t nreq, const int32_t* visible_start,
+                        const int32_t* visible_end, const int32_t* selected, int64_t selected_ld, int32_t list_k,
+                        const int32_t* selected_start, float scale, void* out, float* lse, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+  Attn4Args a;
+  Cache4 c;
+  int rc = attn4_shape(tokens, nreq, hq, hkv, d, list_k, &a);
+  if (rc) return rc;
+  if ((rc = check_cache4(codes, scales, num_pages, page_size, hkv, d, &c)) != LT_OK) return rc;
+  if (table_width < 0 || table_ld < table_width || !(scale > 0.0f) || !(scale <= 3.0e38f)) return LT_EINVAL;
+  if (list_k > 0 ? selected_ld < list_k : selected != nullptr) return LT_EINVAL;
+  if (tokens == 0) return LT_OK;
+  if (num_pages == 0 || !q || !out || !cu_tokens) return LT_EINVAL;
+  if (!aligned(q, 16) || !aligned(out, 16) || q_stride < (int64_t)hq * d || q_stride % 8) return LT_EINVAL;
+  if (nreq > 0 && (!seq_lens || (table_width > 0 && !block_table))) return LT_EINVAL;
+  if (list_k > 0 && !selected) return LT_EINVAL;
+  if (!workspace || !aligned(workspace, 256)) return LT_EINVAL;
+  const size_t need = attn4_workspace_bytes(a);
+  if (need == 0) return LT_EUNSUPPORTED;
+  if (workspace_bytes < need) return LT_EWORKSPACE;
+  a.q = static_cast<const uint16_t*>(q);
+  a.q_stride = q_stride;
+  a.codes = codes;
+  a.scales = scales;
+  a.num_pages = num_pages;
+  a.table = block_table;
+  a.table_ld = table_ld;
+  a.table_width = table_width;
+  a.shift = c.shift;
+  a.cu = cu_tokens;
+  a.seq = seq_lens;
+  a.start = visible_start;
+  a.end = visible_end;
+  a.list = selected;
+  a.list_ld = selected_ld;
+  a.list_base = selected_start;
+  a.scale_log2 = scale * 1.44269504088896340736f;
+  a.out = static_cast<uint16_t*>(out);
+  a.lse = lse;
+  return hip_status(launch_attn4(a, workspace, (hipStream_t)stream));
+}
+
+static int check_logprobs(const void* logits, lt_dtype dtype, int64_t ld, int32_t rows, int32_t vocab,
+                          const int64_t* tokens, float scale) {
+  if (dtype != LT_F32 && dtype != LT_BF16) return LT_EUNSUPPORTED;
+  if (rows < 0 || vocab < 0 || ld < vocab || !(scale > 0.0f) || !(scale <= 3.0e38f)) return LT_EINVAL;
+  if (vocab > LT_LOGPROB_MAX_VOCAB) return LT_EUNSUPPORTED;
+  if (rows == 0) return LT_OK;
+  if ((vocab > 0 && !logits) || !aligned(logits, dtype == LT_F32 ? 4 : 2)) return LT_EINVAL;
+  if (!tokens || !aligned(tokens, 8)) return LT_EINVAL;
+  return LT_OK;
+}
+
+size_t lt_token_logprobs_workspace_size(lt_dtype dtype, int32_t rows, int32_t vocab, int32_t top) {
+  if ((dtype != LT_F32 && dtype != LT_BF16) || rows < 0 || vocab < 0 || vocab > LT_LOGPROB_MAX_VOCAB || top < 0 ||
+      top > LT_LOGPROB_MAX_TOP)
+    return 0;
+  LogprobArgs a{};
+  a.bf16 = dtype == LT_BF16;
+  a.rows = rows;
+  a.vocab = vocab;
+  a.top = top;
+  return logprob_workspace_bytes(a);
+}
+
+int lt_token_logprobs(const void* logits, lt_dtype dtype, int64_t ld, int32_t rows, int32_t vocab,
+                      const int64_t* tokens, float scale, int32_t top, float* logprob, float* entropy, float* lse,
+                      int32_t* top_index, float* top_logprob, void* workspace, size_t workspace_bytes,
+                      void* stream) {
+  const int rc = check_logprobs(logits, dtype, ld, rows, vocab, tokens, scale);
+  if (rc) return rc;
+  if (top < 0) return LT_EINVAL;
+  if (top > LT_LOGPROB_MAX_TOP) return LT_EUNSUPPORTED;
+  if (rows == 0) return LT_OK;
+  if (!logprob || !entropy || !lse || (top > 0 && (!top_index || !top_logprob))) return LT_EINVAL;
+  if (!workspace || !aligned(workspace, 256)) return LT_EINVAL;
+  LogprobArgs a{};
+  a.logits = logits;
+  a.ld = ld;
+  a.bf16 = dtype == LT_BF16;
+  a.rows = rows;
+  a.vocab = vocab;
+  a.top = top;
+  a.tokens = tokens;
+  a.scale = scale;
+  a.logprob = logprob;
+  a.entropy = entropy;
+  a.lse = lse;
+  a.top_index = top_index;
+  a.top_logprob = top_logprob;
+  if (workspace_bytes < logprob_workspace_bytes(a)) return LT_EWORKSPACE;
+  return hip_status(launch_logprobs(a, workspace, (hipStream_t)stream));
+}
+
+int lt_token_logprobs_backward(const void* logits, lt_dtype dtype, int64_t ld, int32_t rows, int32_t vocab,
+                               const int64_t* tokens, float scale, const float* lse, const float* entropy,
+                               const float* grad_logprob, const float* grad_entropy, void* grad_logits,
+                               int64_t grad_ld, void* stream) {
+  const int rc = check_logprobs(logits, dtype, ld, rows, vocab, tokens, scale);
+  if (rc) return rc;
+  if (grad_ld < vocab) return LT_EINVAL;
+  if (rows == 0 || vocab == 0) return LT_OK;
+  if (!lse || !entropy || !grad_logits || !aligned(grad_logits, dtype == LT_F32 ? 4 : 2)) return LT_EINVAL;
+  return hip_status(launch_logprobs_backward(logits, ld, dtype == LT_BF16, rows, vocab, tokens, scale, lse, entropy,
+                                             grad_logprob, grad_entropy, grad_logits, grad_ld, (hipStream_t)stream));
 }
 
 int lt_event_create(void** ev) {

@@ -210,4 +210,73 @@ constexpr uint32_t kSelIlv = 1u << 29;
 constexpr uint32_t kSelRefilter = 1u << 28;
 constexpr uint32_t kSelSecond = 1u << 27;
 
+// ---- paged serving cache (paged.hip) ----
+struct PlanArgs {
+  const int32_t *context, *added, *free_list, *free_used;
+  int32_t* table;
+  int64_t table_ld;
+  int32_t *cu, *seq, *positions, *status, *free_out;
+  int64_t* slots;
+  int R, width, free_count, capacity, shift;
+};
+hipError_t launch_paged_plan(const PlanArgs& a, hipStream_t st);
+struct Cache4;
+hipError_t launch_cache4_append(const void* k, const void* v, bool f32, int64_t k_stride, int64_t v_stride,
+                                int64_t rows, const Cache4& c, uint8_t* codes, uint8_t* scales, const int64_t* slots,
+                                hipStream_t st);
+hipError_t launch_cache4_read(const Cache4& c, const uint8_t* codes, const uint8_t* scales, const int64_t* slots,
+                              int64_t rows, void* k, void* v, hipStream_t st);
+
+// ---- attention over the 4-bit cache (attn4.hip) ----
+struct Attn4Args {
+  const uint16_t* q;        // [T, hkv * group, d], q_stride values between tokens
+  int64_t q_stride;
+  const uint8_t *codes, *scales;
+  int64_t num_pages;
+  const int32_t* table;
+  int64_t table_ld;
+  int table_width, shift;
+  const int32_t *cu, *seq, *start, *end;
+  const int32_t* list;      // [T, list_k] rows of list_ld, or NULL
+  int64_t list_ld;
+  const int32_t* list_base;
+  int list_k;
+  int R, T, hkv, group, d;
+  float scale_log2;         // softmax scale * log2 e
+  uint16_t* out;
+  float* lse;
+  // resolved by launch_attn4
+  float slack;
+  int rt, row_tiles, chunks, chunk_keys, target, lds_join;
+  int64_t items;
+  bool split;
+  uint32_t* sched;
+  float* part_o;
+  float2* part_ml;
+};
+// 0: more tiles than a launch can hold.
+size_t attn4_workspace_bytes(Attn4Args a);
+hipError_t launch_attn4(Attn4Args a, void* workspace, hipStream_t st);
+
+// ---- token log probabilities (logprob.hip) ----
+struct LogprobArgs {
+  const void* logits;       // [rows, vocab], ld values between rows
+  int64_t ld;
+  bool bf16;
+  int rows, vocab, top;
+  const int64_t* tokens;
+  float scale;
+  float *logprob, *entropy, *lse;
+  int32_t* top_index;       // [rows, top]
+  float* top_logprob;
+  int splits, split_len;    // resolved by logprob_shape
+};
+void logprob_shape(LogprobArgs& a);
+size_t logprob_workspace_bytes(LogprobArgs a);
+hipError_t launch_logprobs(LogprobArgs a, void* workspace, hipStream_t st);
+hipError_t launch_logprobs_backward(const void* logits, int64_t ld, bool bf16, int rows, int vocab,
+                                    const int64_t* tokens, float scale, const float* lse, const float* entropy,
+                                    const float* g_logprob, const float* g_entropy, void* out, int64_t out_ld,
+                                    hipStream_t st);
+
 }  // namespace lt

@@ -1,0 +1,471 @@
+// Log probabilities of given tokens, entropy and best alternatives of rows of
+// logits, and the logits' gradient.
+//
+//   y_i = scale * x_i,  lse = log sum exp(y_i),  lp = y_tok - lse,
+//   H = lse - sum p_i y_i,  p_i = exp(y_i - lse)
+//   dx_i = scale * (g_lp * (1[i = tok] - p_i) - g_H * p_i * (log p_i + H))
+//
+// Forward reads the logits once. With a running reference logit m, in powers of
+// two (t = (x - m) scale log2 e), a thread sums s = sum 2^t and u = sum t 2^t in
+// float32: lse = scale m + log2 s ln 2, lp = scale (x_tok - m) - log2 s ln 2 and
+// H = (log2 s - u / s) ln 2, none with a large difference; logits at their type's
+// lowest value are values like any other. The best `top` entries are kept by each wave, sorted over its
+// lanes (one 64-bit key a lane: value, then the lower index), behind a
+// threshold that the waves of a block share.
+#include "internal.hpp"
+
+namespace lt {
+namespace {
+
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kUnroll = 4;            // 16-byte loads a thread has in flight
+constexpr float kSlack = 8.0f;        // log2 by which a value may pass the reference
+constexpr float kStart = -3.402823466e38f;  // reference before the first value: the lowest there is
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+__device__ __forceinline__ float ninf() { return -__builtin_inff(); }
+
+template <class T>
+struct Vec;
+template <>
+struct Vec<uint16_t> {
+  static constexpr int N = 8;
+  __device__ static __forceinline__ void unpack(const uint4& a, float (&x)[8]) {
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+  }
+  __device__ static __forceinline__ float one(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
+  static constexpr uint32_t kFill = 0xFF80FF80u;  // -inf
+};
+template <>
+struct Vec<float> {
+  static constexpr int N = 4;
+  __device__ static __forceinline__ void unpack(const uint4& a, float (&x)[4]) {
+    x[0] = __uint_as_float(a.x), x[1] = __uint_as_float(a.y);
+    x[2] = __uint_as_float(a.z), x[3] = __uint_as_float(a.w);
+  }
+  __device__ static __forceinline__ float one(const float* p) { return *p; }
+  static constexpr uint32_t kFill = 0xFF800000u;
+};
+
+// 16 bytes of a row at its elements' alignment (rows need no other).
+template <class T>
+__device__ __forceinline__ uint4 load16(const T* p) {
+  uint4 v;
+  __builtin_memcpy(&v, p, 16);
+  return v;
+}
+
+// ---- sums ----
+struct Sums {
+  float m, s, u;
+};
+__device__ __forceinline__ void rebase(Sums& a, float m, float c) {
+  const float d = (a.m - m) * c, f = __builtin_amdgcn_exp2f(d);
+  a.u = f * fmaf(a.s, fmaxf(d, -1.0e4f), a.u);  // f is 0 long before that
+  a.s *= f;
+  a.m = m;
+}
+__device__ __forceinline__ Sums join(Sums a, Sums b, float c) {
+  const float m = fmaxf(a.m, b.m);
+  rebase(a, m, c);
+  rebase(b, m, c);
+  return Sums{m, a.s + b.s, a.u + b.u};
+}
+__device__ __forceinline__ Sums wave_join(Sums a, float c) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) a = join(a, Sums{__shfl_xor(a.m, o), __shfl_xor(a.s, o), __shfl_xor(a.u, o)}, c);
+  return a;
+}
+
+// ---- the best entries ----
+__device__ __forceinline__ uint64_t shfl64(uint64_t v, int lane) {
+  return ((uint64_t)(uint32_t)__shfl((int)(v >> 32), lane) << 32) | (uint32_t)__shfl((int)(uint32_t)v, lane);
+}
+__device__ __forceinline__ uint64_t shfl64_xor(uint64_t v, int o) {
+  return ((uint64_t)(uint32_t)__shfl_xor((int)(v >> 32), o) << 32) | (uint32_t)__shfl_xor((int)(uint32_t)v, o);
+}
+// A list of 64 keys over the lanes, descending; 0 = no entry (below every key:
+// a key's low word is never 0).
+// Entry i of the union's best 64 of two such lists.
+__device__ __forceinline__ uint64_t merge_lists(uint64_t a, uint64_t b) {
+  const int lane = threadIdx.x & 63;
+  const uint64_t r = shfl64(b, 63 - lane);
+  uint64_t v = a > r ? a : r;  // bitonic: the best 64 of both
+#pragma unroll
+  for (int o = 32; o; o >>= 1) {
+    const uint64_t w = shfl64_xor(v, o);
+    v = ((lane & o) == 0) == (v > w) ? v : w;
+  }
+  return v;
+}
+// 64 unordered keys, descending.
+__device__ __forceinline__ uint64_t sort_list(uint64_t v) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int k = 2; k <= 64; k <<= 1)
+#pragma unroll
+    for (int o = k >> 1; o; o >>= 1) {
+      const uint64_t w = shfl64_xor(v, o);
+      const bool first = ((lane & o) == 0) == ((lane & k) == 0);  // takes the larger
+      v = first == (v > w) ? v : w;
+    }
+  return v;
+}
+__device__ __forceinline__ void insert(uint64_t& list, uint64_t key) {  // key is wave-uniform
+  const int lane = threadIdx.x & 63;
+  const int at = __popcll(__ballot(list > key));
+  const uint64_t up = shfl64(list, lane - 1);
+  list = lane < at ? list : lane == at ? key : up;
+}
+__device__ __forceinline__ uint64_t read_lane64(uint64_t v, int lane) {
+  return ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32) |
+         (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
+}
+// The score of a key's value part; keys of NaN and "no entry" give -inf.
+__device__ __forceinline__ float key_floor(uint64_t key) {
+  const uint32_t o = (uint32_t)(key >> 32);
+  return o ? __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o) : ninf();
+}
+
+struct Best {
+  uint64_t list, thr;  // thr: a key that top keys of the row are known to reach
+  float floor;
+  __device__ __forceinline__ void raise(uint64_t key) {
+    if (key > thr) {
+      thr = key;
+      floor = key_floor(key);
+    }
+  }
+};
+
+template <class T>
+__device__ __forceinline__ void take(Best& b, const float (&x)[Vec<T>::N], int first, int count, int top) {
+#pragma unroll
+  for (int j = 0; j < Vec<T>::N; ++j) {
+    const uint64_t key = j < count && !(x[j] < b.floor) ? comp_key(x[j], (uint32_t)(first + j)) : 0u;
+    uint64_t who = __ballot(key > b.thr);
+    while (who) {
+      const int lane = __ffsll((unsigned long long)who) - 1;
+      who &= who - 1;
+      const uint64_t k = read_lane64(key, lane);
+      if (k <= b.thr) continue;
+      insert(b.list, k);
+      b.raise(read_lane64(b.list, top - 1));
+    }
+  }
+}
+
+// What a row's sums and list say; the list and sums are wave-uniform resp. one
+// entry a lane. Called by one wave.
+template <class T>
+__device__ __forceinline__ void finish(const LogprobArgs& a, int row, Sums s, uint64_t list) {
+  const int lane = threadIdx.x & 63;
+  const T* x = reinterpret_cast<const T*>(a.logits) + (int64_t)row * a.ld;
+  const bool none = s.s == 0.0f;  // no value above -inf
+  const float l2 = __builtin_amdgcn_logf(s.s);
+  const float lse = none ? ninf() : fmaf(s.m, a.scale, l2 * kLn2);
+  if (lane == 0) {
+    const int64_t tok = a.tokens[row];
+    float lp = 0.0f;
+    if (tok >= 0 && tok < a.vocab) {
+      lp = none ? ninf() : fmaf(Vec<T>::one(x + tok) - s.m, a.scale, -l2 * kLn2);
+    }
+    a.logprob[row] = lp;
+    a.entropy[row] = none ? 0.0f : (l2 - s.u / s.s) * kLn2;
+    a.lse[row] = lse;
+  }
+  if (lane < a.top) {
+    const bool real = list != 0;
+    const int i = real ? (int)comp_pos(list) : -1;
+    float lp = ninf();
+    if (real && !none) lp = fmaf(Vec<T>::one(x + i) - s.m, a.scale, -l2 * kLn2);
+    a.top_index[(int64_t)row * a.top + lane] = i;
+    a.top_logprob[(int64_t)row * a.top + lane] = lp;
+  }
+}
+
+struct Partial {
+  Sums* sums;      // [rows * splits]
+  uint64_t* keys;  // [rows * splits][top]
+};
+
+template <class T, bool TOP>
+__global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a, Partial part) {
+  constexpr int N = Vec<T>::N;
+  __shared__ Sums wsum[kWaves];
+  __shared__ uint64_t wlist[kWaves][64];
+  __shared__ unsigned long long shared_thr;
+  const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
+  const int row = blockIdx.x / a.splits, split = blockIdx.x - row * a.splits;
+  const T* x = reinterpret_cast<const T*>(a.logits) + (int64_t)row * a.ld;
+  const int b = split * a.split_len, e = min(a.vocab - b, a.split_len) + b;  // elements [b, e)
+  const float c = a.scale * kLog2e, slack = fminf(kSlack / c, 1.0e30f);
+  if constexpr (TOP) {
+    if (t == 0) shared_thr = 0;
+    __syncthreads();
+  }
+
+  Sums s{kStart, 0.0f, 0.0f};
+  Best best{0, 0, ninf()};
+  bool primed = false;
+  auto fetch = [&](int base, uint4 (&v)[kUnroll]) {
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) {
+      const int i = base + (k * kThreads + t) * N;
+      if (i + N <= e) {
+        v[k] = load16(x + i);
+      } else {  // the row's end, or beyond it
+        uint32_t w[4] = {Vec<T>::kFill, Vec<T>::kFill, Vec<T>::kFill, Vec<T>::kFill};
+        for (int j = 0; j < N && i + j < e; ++j) {
+          if constexpr (N == 8) {
+            const uint32_t h = x[i + j];
+            w[j >> 1] = j & 1 ? (w[j >> 1] & 0xFFFFu) | (h << 16) : (w[j >> 1] & 0xFFFF0000u) | h;
+          } else {
+            w[j] = __float_as_uint(x[i + j]);
+          }
+        }
+        v[k] = uint4{w[0], w[1], w[2], w[3]};
+      }
+    }
+  };
+  constexpr int kStep = kThreads * kUnroll * N;
+  uint4 nxt[kUnroll];
+  fetch(b, nxt);
+  for (int base = b; base < e; base += kStep) {
+    float v[kUnroll][N], vmax[kUnroll];
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) {
+      Vec<T>::unpack(nxt[k], v[k]);
+      vmax[k] = v[k][0];
+#pragma unroll
+      for (int j = 1; j < N; ++j) vmax[k] = fmaxf(vmax[k], v[k][j]);
+    }
+    if (base + kStep < e) fetch(base + kStep, nxt);
+    float top = fmaxf(fmaxf(vmax[0], vmax[1]), fmaxf(vmax[2], vmax[3]));
+    if (__any(top > s.m + slack)) rebase(s, fmaxf(s.m, top), c);
+    // four chains of sums
+    float ss[4] = {}, uu[4] = {};
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k)
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const float d = (v[k][j] - s.m) * c, p = __builtin_amdgcn_exp2f(d);
+        ss[j & 3] += p;
+        // 2^d is 0 long before -200; -inf must not meet it
+        uu[j & 3] = fmaf(p, fmaxf(d, -200.0f), uu[j & 3]);
+      }
+    s.s += (ss[0] + ss[1]) + (ss[2] + ss[3]);
+    s.u += (uu[0] + uu[1]) + (uu[2] + uu[3]);
+    if constexpr (TOP) {
+      if (!primed) {
+        // the top-th largest of 64 lanes' own largest values bounds the row's
+        primed = true;
+        const int i0 = base + t * N;
+        uint64_t mine = 0;
+        if (i0 + N <= e) mine = comp_key(vmax[0], 0xFFFFFFFEu);  // below every entry of that value
+        const uint64_t bound = read_lane64(sort_list(mine), a.top - 1);
+        if (bound) best.raise(bound - 1);
+      }
+      best.raise(*(volatile unsigned long long*)&shared_thr);
+      const uint64_t was = best.thr;
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k) {
+        const int i = base + (k * kThreads + t) * N;
+        if (__any(i < e && !(vmax[k] < best.floor))) take<T>(best, v[k], i, e - i, a.top);
+      }
+      if (best.thr > was && lane == 0) atomicMax(&shared_thr, (unsigned long long)best.thr);
+    }
+  }
+
+  s = wave_join(s, c);
+  if (lane == 0) wsum[wave] = s;
+  if constexpr (TOP) wlist[wave][lane] = best.list;
+  __syncthreads();
+  if (wave) return;
+  for (int i = 1; i < kWaves; ++i) {
+    s = join(s, wsum[i], c);
+    if constexpr (TOP) best.list = merge_lists(best.list, wlist[i][lane]);
+  }
+  if (a.splits == 1) {
+    finish<T>(a, row, s, best.list);
+  } else {
+    if (lane == 0) part.sums[blockIdx.x] = s;
+    if (TOP && lane < a.top) part.keys[(int64_t)blockIdx.x * a.top + lane] = best.list;
+  }
+}
+
+// Joins a row's splits: a block a row, each wave a share of them.
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_logprobs_join(LogprobArgs a, Partial part) {
+  __shared__ Sums wsum[kWaves];
+  __shared__ uint64_t wlist[kWaves][64];
+  const int t = threadIdx.x, wave = t >> 6, lane = t & 63, row = blockIdx.x;
+  const float c = a.scale * kLog2e;
+  Sums s{kStart, 0.0f, 0.0f};
+  for (int i = t; i < a.splits; i += kThreads) s = join(s, part.sums[(int64_t)row * a.splits + i], c);
+  s = wave_join(s, c);
+  uint64_t list = 0;
+  if (a.top > 0)
+    for (int i = wave; i < a.splits; i += kWaves) {
+      const uint64_t k = lane < a.top ? part.keys[((int64_t)row * a.splits + i) * a.top + lane] : 0;
+      list = merge_lists(list, k);
+    }
+  if (lane == 0) wsum[wave] = s;
+  wlist[wave][lane] = list;
+  __syncthreads();
+  if (wave) return;
+  for (int i = 1; i < kWaves; ++i) {
+    s = join(s, wsum[i], c);
+    list = merge_lists(list, wlist[i][lane]);
+  }
+  finish<T>(a, row, s, list);
+}
+
+// ---- gradient: one pass, bound by reading and writing the logits once ----
+// p = w exp(scale (x - a) - b) with a = 0, b = lse, w = 1. Where lse is too large
+// for its last bit to be small (kFarLse and beyond; in earnest only rows whose
+// logits are all at their type's lowest value), a block first finds the row's own
+// maximum and sum again: a = max, b = 0, w = 1 / sum.
+constexpr float kFarLse = 1024.0f;
+
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_logprobs_backward(const T* logits, int64_t ld, int vocab,
+                                                                const int64_t* tokens, float scale, const float* lse,
+                                                                const float* entropy, const float* g_lp,
+                                                                const float* g_ent, T* out, int64_t out_ld) {
+  constexpr int N = Vec<T>::N;
+  const int row = blockIdx.x, t = threadIdx.x;
+  const T* x = logits + (int64_t)row * ld;
+  T* o = out + (int64_t)row * out_ld;
+  const int64_t tok = tokens[row];
+  const bool counts = tok >= 0 && tok < vocab;
+  const float z = lse[row];
+  const bool none = z == ninf();
+  float from = 0.0f, minus = z, w = 1.0f;
+  if (fabsf(z) >= kFarLse && !none) {
+    __shared__ float red[kWaves], red2[kWaves];
+    float top = ninf(), sum = 0.0f;
+    for (int i = t; i < vocab; i += kThreads) top = fmaxf(top, Vec<T>::one(x + i));
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+    if ((t & 63) == 0) red[t >> 6] = top;
+    __syncthreads();
+    for (int i = 0; i < kWaves; ++i) top = fmaxf(top, red[i]);
+    for (int i = t; i < vocab; i += kThreads) sum += __builtin_amdgcn_exp2f((Vec<T>::one(x + i) - top) * scale * kLog2e);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+    if ((t & 63) == 0) red2[t >> 6] = sum;
+    __syncthreads();
+    from = top;
+    minus = 0.0f;
+    w = 1.0f / ((red2[0] + red2[1]) + (red2[2] + red2[3]));
+  }
+  const float gl = counts && g_lp ? g_lp[row] * scale : 0.0f, gh = g_ent ? g_ent[row] * scale : 0.0f;
+  // -g_lp p - g_H p (log p + H) = 2^d (k0 - k1w d), d = log2 (p / w)
+  const float k1 = gh * kLn2;
+  const float k0 = w * (-gl - gh * entropy[row] - k1 * __builtin_amdgcn_logf(w)), k1w = k1 * w;
+  for (int i = (blockIdx.y * kThreads + t) * N; i < vocab; i += gridDim.y * kThreads * N) {
+    const int n = min(N, vocab - i);
+    float v[N];
+    if (n == N) {
+      Vec<T>::unpack(load16(x + i), v);
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j) v[j] = j < n ? Vec<T>::one(x + i + j) : 0.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      // log p first: it is small where p is large
+      const float d = fmaf(v[j] - from, scale, -minus) * kLog2e, p = __builtin_amdgcn_exp2f(d);
+      float g = p * fmaf(-k1w, fmaxf(d, -200.0f), k0);
+      if (i + j == tok) g += gl;
+      v[j] = none ? 0.0f : g;
+    }
+    if constexpr (N == 8) {
+      typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+      const bf16x8_t r{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3],
+                       (__bf16)v[4], (__bf16)v[5], (__bf16)v[6], (__bf16)v[7]};
+      if (n == N) {
+        __builtin_memcpy(o + i, &r, 16);
+      } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+          if (j < n) reinterpret_cast<__bf16*>(o)[i + j] = r[j];
+      }
+    } else {
+      if (n == N) {
+        __builtin_memcpy(o + i, v, 16);
+      } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+          if (j < n) o[i + j] = v[j];
+      }
+    }
+  }
+}
+
+template <class T>
+hipError_t run_forward(const LogprobArgs& a, const Partial& p, hipStream_t st) {
+  const dim3 grid((unsigned)(a.rows * a.splits));
+  if (a.top > 0) k_logprobs<T, true><<<grid, kThreads, 0, st>>>(a, p);
+  else k_logprobs<T, false><<<grid, kThreads, 0, st>>>(a, p);
+  if (a.splits > 1) k_logprobs_join<T><<<dim3((unsigned)a.rows), kThreads, 0, st>>>(a, p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+void logprob_shape(LogprobArgs& a) {
+  // Rows are split until there are four blocks a CU, down to one load a thread.
+  const int n = a.bf16 ? 8 : 4, unit = kThreads * n;
+  const int64_t most = ((int64_t)a.vocab + unit - 1) / unit;
+  int64_t s = a.rows > 0 ? (1024 + a.rows - 1) / a.rows : 1;
+  s = s > most ? most : s;
+  s = s < 1 ? 1 : s;
+  a.split_len = (int)((most + s - 1) / s) * unit;
+  if ((int64_t)a.split_len > a.vocab) a.split_len = a.vocab > 0 ? a.vocab : 1;
+  a.splits = a.vocab > 0 ? (int)(((int64_t)a.vocab + a.split_len - 1) / a.split_len) : 1;
+}
+
+size_t logprob_workspace_bytes(LogprobArgs a) {
+  logprob_shape(a);
+  if (a.splits == 1) return 256;
+  const size_t n = (size_t)a.rows * a.splits;
+  return 256 + (n * sizeof(Sums) + 255) / 256 * 256 + n * a.top * 8;
+}
+
+hipError_t launch_logprobs(LogprobArgs a, void* workspace, hipStream_t st) {
+  logprob_shape(a);
+  Partial p{};
+  if (a.splits > 1) {
+    const size_t n = (size_t)a.rows * a.splits;
+    p.sums = static_cast<Sums*>(workspace);
+    p.keys = reinterpret_cast<uint64_t*>(static_cast<uint8_t*>(workspace) + (n * sizeof(Sums) + 255) / 256 * 256);
+  }
+  return a.bf16 ? run_forward<uint16_t>(a, p, st) : run_forward<float>(a, p, st);
+}
+
+hipError_t launch_logprobs_backward(const void* logits, int64_t ld, bool bf16, int rows, int vocab,
+                                    const int64_t* tokens, float scale, const float* lse, const float* entropy,
+                                    const float* g_logprob, const float* g_entropy, void* out, int64_t out_ld,
+                                    hipStream_t st) {
+  const int unit = kThreads * (bf16 ? 8 : 4);
+  int64_t y = ((int64_t)vocab + unit - 1) / unit;
+  const int64_t want = (4096 + rows - 1) / rows;
+  y = y > want ? want : y;
+  const dim3 grid((unsigned)rows, (unsigned)(y < 1 ? 1 : y));
+  if (bf16)
+    k_logprobs_backward<uint16_t><<<grid, kThreads, 0, st>>>((const uint16_t*)logits, ld, vocab, tokens, scale, lse,
+                                                             entropy, g_logprob, g_entropy, (uint16_t*)out, out_ld);
+  else
+    k_logprobs_backward<float><<<grid, kThreads, 0, st>>>((const float*)logits, ld, vocab, tokens, scale, lse, entropy,
+                                                          g_logprob, g_entropy, (float*)out, out_ld);
+  return hipGetLastError();
+}
+
+}  // namespace lt

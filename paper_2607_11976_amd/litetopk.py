@@ -16,7 +16,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional, Sequence
+from typing import NamedTuple, Optional, Sequence
 
 import torch
 
@@ -35,13 +35,21 @@ LT_UNION_MAX = 32768
 LT_ROW_STATS = 12
 LT_STATIC_SCRATCH_BYTES = 256 << 20
 LT_NUM_STAGE_EVENTS = 6
+LT_MAX_PAGE_SIZE = 4096
+LT_PLAN_MAX_REQUESTS = 16384
+LT_CACHE4_MAX_HEADS = 1024
+LT_LOGPROB_MAX_TOP = 64
+LT_LOGPROB_MAX_VOCAB = 1 << 30
 STAGES = ("sample", "range", "filter", "select", "fallback")
 
 EXPORTED = (
     "lt_options_default", "lt_indexer_topk_workspace_size", "lt_indexer_topk", "lt_indexer_topk_static",
     "lt_indexer_scores",
     "lt_topk_select_workspace_size", "lt_topk_select", "lt_topk_radix",
-    "lt_sample_from_topk_workspace_size", "lt_sample_from_topk", "lt_dsa_union", "lt_event_create",
+    "lt_sample_from_topk_workspace_size", "lt_sample_from_topk", "lt_dsa_union",
+    "lt_paged_plan", "lt_cache4_append", "lt_cache4_read", "lt_cache4_attention_workspace_size",
+    "lt_cache4_attention", "lt_token_logprobs_workspace_size", "lt_token_logprobs", "lt_token_logprobs_backward",
+    "lt_event_create",
     "lt_event_destroy", "lt_event_record", "lt_event_elapsed_ms", "lt_strerror",
 )
 
@@ -70,6 +78,7 @@ _P = ctypes.c_void_p
 _I32 = ctypes.c_int32
 _I64 = ctypes.c_int64
 _SZ = ctypes.c_size_t
+_F32 = ctypes.c_float
 
 
 def load(path: str = LIB_PATH):
@@ -106,6 +115,25 @@ def load(path: str = LIB_PATH):
     lib.lt_sample_from_topk.restype = ctypes.c_int
     lib.lt_dsa_union.argtypes = [_P, _I64, _I32, _I32, _I32, _P, _P, _P, _P]
     lib.lt_dsa_union.restype = ctypes.c_int
+    lib.lt_paged_plan.argtypes = [_P, _P, _I32, _I32, _P, _I64, _I32, _P, _I32, _P, _I32, _P, _P, _P, _P, _P, _P, _P]
+    lib.lt_paged_plan.restype = ctypes.c_int
+    lib.lt_cache4_append.argtypes = [_P, _P, ctypes.c_int, _I64, _I64, _I64, _P, _P, _I64, _I32, _I32, _I32, _P, _P]
+    lib.lt_cache4_append.restype = ctypes.c_int
+    lib.lt_cache4_read.argtypes = [_P, _P, _I64, _I32, _I32, _I32, _P, _I64, _P, _P, _P]
+    lib.lt_cache4_read.restype = ctypes.c_int
+    lib.lt_cache4_attention_workspace_size.argtypes = [_I32, _I32, _I32, _I32, _I32, _I32]
+    lib.lt_cache4_attention_workspace_size.restype = _SZ
+    lib.lt_cache4_attention.argtypes = [_P, _I64, _I32, _I32, _I32, _P, _P, _I64, _I32, _I32, _P, _I64, _I32, _P, _P,
+                                        _I32, _P, _P, _P, _I64, _I32, _P, _F32, _P, _P, _P, _SZ, _P]
+    lib.lt_cache4_attention.restype = ctypes.c_int
+    lib.lt_token_logprobs_workspace_size.argtypes = [ctypes.c_int, _I32, _I32, _I32]
+    lib.lt_token_logprobs_workspace_size.restype = _SZ
+    lib.lt_token_logprobs.argtypes = [_P, ctypes.c_int, _I64, _I32, _I32, _P, _F32, _I32, _P, _P, _P, _P, _P, _P, _SZ,
+                                      _P]
+    lib.lt_token_logprobs.restype = ctypes.c_int
+    lib.lt_token_logprobs_backward.argtypes = [_P, ctypes.c_int, _I64, _I32, _I32, _P, _F32, _P, _P, _P, _P, _P, _I64,
+                                               _P]
+    lib.lt_token_logprobs_backward.restype = ctypes.c_int
     lib.lt_event_create.argtypes = [ctypes.POINTER(ctypes.c_void_p)]
     lib.lt_event_create.restype = ctypes.c_int
     lib.lt_event_destroy.argtypes = [_P]
@@ -185,6 +213,38 @@ def lt_sample_from_topk(prev_idx, ld, prev_rows, prev_k, nk, sample_size, sample
 
 def lt_dsa_union(topk_idx, ld, nq, k, group, union_idx, union_count, member_mask, stream) -> int:
     return load().lt_dsa_union(topk_idx, ld, nq, k, group, union_idx, union_count, member_mask, stream)
+
+
+def lt_paged_plan(*args) -> int:
+    return load().lt_paged_plan(*args)
+
+
+def lt_cache4_append(*args) -> int:
+    return load().lt_cache4_append(*args)
+
+
+def lt_cache4_read(*args) -> int:
+    return load().lt_cache4_read(*args)
+
+
+def lt_cache4_attention_workspace_size(tokens, requests, heads, kv_heads, head_dim, selected_k=0) -> int:
+    return load().lt_cache4_attention_workspace_size(tokens, requests, heads, kv_heads, head_dim, selected_k)
+
+
+def lt_cache4_attention(*args) -> int:
+    return load().lt_cache4_attention(*args)
+
+
+def lt_token_logprobs_workspace_size(dtype, rows, vocab, top) -> int:
+    return load().lt_token_logprobs_workspace_size(dtype, rows, vocab, top)
+
+
+def lt_token_logprobs(*args) -> int:
+    return load().lt_token_logprobs(*args)
+
+
+def lt_token_logprobs_backward(*args) -> int:
+    return load().lt_token_logprobs_backward(*args)
 
 
 def lt_strerror(status: int) -> str:
@@ -492,3 +552,241 @@ def dsa_union(topk_idx: torch.Tensor, group: int, stream=None):
                       _ptr(ucnt), _ptr(mask), _stream(stream))
     _check(st, "lt_dsa_union")
     return uidx, ucnt, mask
+
+
+# ---------------------------------------------------------------------------
+# serving: page plan, 4-bit cache, attention over it, log probabilities
+# ---------------------------------------------------------------------------
+
+def _int32(t: Optional[torch.Tensor], n: Optional[int], name: str):
+    if t is None:
+        return
+    _on_gpu(t)
+    _need(t.dtype == torch.int32 and t.dim() == 1 and (n is None or t.numel() == n),
+          "%s must be a contiguous int32 vector%s on the GPU" % (name, "" if n is None else " of %d entries" % n))
+
+
+def _table(t: torch.Tensor, rows: int):
+    """block_table int32 [rows, width] with unit column stride."""
+    _need(t.is_cuda and t.dtype == torch.int32 and t.dim() == 2 and t.shape[0] == rows
+          and (t.numel() == 0 or t.shape[1] == 1 or t.stride(1) == 1),
+          "block_table must be an int32 [requests, pages] GPU matrix with unit column stride")
+    return max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1], t.shape[1]
+
+
+def _used_on(stream, *ts):
+    """Memory allocated here on the current stream and used on `stream`: keep
+    the allocator from handing it out before that work has run."""
+    if stream is not None and stream.cuda_stream != torch.cuda.current_stream().cuda_stream:
+        for t in ts:
+            if t is not None and t.numel():
+                t.record_stream(stream)
+
+
+class PagedPlan(NamedTuple):
+    """What paged_plan returns; see lt_paged_plan in the header."""
+    cu_tokens: torch.Tensor   # int32 [R + 1]
+    seq_lens: torch.Tensor    # int32 [R]
+    slots: torch.Tensor       # int64 [token_capacity]
+    positions: torch.Tensor   # int32 [token_capacity]
+    free_used: torch.Tensor   # int32 [1]: pages of the free list now in use
+    status: torch.Tensor      # int32 [R]: 0 served, 1 table too narrow, 2 out of pages
+
+
+def paged_plan(context_lens: torch.Tensor, new_lens: torch.Tensor, block_table: torch.Tensor,
+               free_pages: torch.Tensor, free_used: torch.Tensor, page_size: int, token_capacity: int,
+               stream=None) -> PagedPlan:
+    """Block tables and slot maps of a step, built on the GPU from the
+    requests' lengths (int32 [R] each): pages for the new tokens are taken from
+    free_pages [free_used[0]:] in request order and entered into block_table
+    [R, W] (in place), and every new token gets its slot and position."""
+    n = context_lens.numel()
+    _int32(context_lens, None, "context_lens")
+    _int32(new_lens, n, "new_lens")
+    _int32(free_pages, None, "free_pages")
+    _int32(free_used, 1, "free_used")
+    _need(token_capacity >= 0, "token_capacity must not be negative")
+    ld, width = _table(block_table, n)
+    dev = context_lens.device
+    p = PagedPlan(torch.empty(n + 1, dtype=torch.int32, device=dev), torch.empty(n, dtype=torch.int32, device=dev),
+                  torch.empty(token_capacity, dtype=torch.int64, device=dev),
+                  torch.empty(token_capacity, dtype=torch.int32, device=dev),
+                  torch.empty(1, dtype=torch.int32, device=dev), torch.empty(n, dtype=torch.int32, device=dev))
+    st = lt_paged_plan(_ptr(context_lens), _ptr(new_lens), n, page_size, _ptr(block_table), ld, width,
+                       _ptr(free_pages), free_pages.numel(), _ptr(free_used), token_capacity, _ptr(p.cu_tokens),
+                       _ptr(p.seq_lens), _ptr(p.slots), _ptr(p.positions), _ptr(p.free_used), _ptr(p.status),
+                       _stream(stream))
+    _check(st, "lt_paged_plan")
+    _used_on(stream, *p)
+    return p
+
+
+def cache4_empty(num_pages: int, page_size: int, kv_heads: int, head_dim: int, device=None):
+    """An empty 4-bit cache: (codes uint8 [pages, kv_heads, page_size, 2,
+    head_dim / 2], scales uint8 [pages, kv_heads, page_size, 2, head_dim / 32])."""
+    dev = device or "cuda"
+    return (torch.zeros((num_pages, kv_heads, page_size, 2, head_dim // 2), dtype=torch.uint8, device=dev),
+            torch.zeros((num_pages, kv_heads, page_size, 2, head_dim // 32), dtype=torch.uint8, device=dev))
+
+
+def _cache4(codes: torch.Tensor, scales: torch.Tensor):
+    """(pages, page size, KV heads, head dim) of a 4-bit cache."""
+    _on_gpu(codes, scales)
+    _need(codes.dtype == torch.uint8 and scales.dtype == torch.uint8 and codes.dim() == 5 and scales.dim() == 5
+          and codes.shape[3] == 2 and codes.shape[:4] == scales.shape[:4] and codes.shape[4] == 16 * scales.shape[4],
+          "a cache is codes uint8 [pages, heads, page_size, 2, d / 2] and scales uint8 [pages, heads, page_size, 2, "
+          "d / 32]")
+    return codes.shape[0], codes.shape[2], codes.shape[1], 2 * codes.shape[4]
+
+
+def _rows_of(t: torch.Tensor, heads: int, d: int, name: str) -> int:
+    """Stride between the rows of a [rows, heads, d] tensor whose rows are contiguous."""
+    _need(t.is_cuda and t.dim() == 3 and tuple(t.shape[1:]) == (heads, d)
+          and (t.numel() == 0 or ((d == 1 or t.stride(2) == 1) and (heads == 1 or t.stride(1) == d))),
+          "%s must be [rows, %d, %d] on the GPU with contiguous rows" % (name, heads, d))
+    return t.stride(0) if t.shape[0] > 1 else heads * d
+
+
+def cache4_append(k: torch.Tensor, v: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, slots: torch.Tensor,
+                  stream=None) -> None:
+    """Quantises the keys and values [rows, kv_heads, head_dim] (float32 or
+    bfloat16) into the cache's slots (int64 [rows], distinct; -1 = leave out)."""
+    pages, page, heads, d = _cache4(codes, scales)
+    ks, vs = _rows_of(k, heads, d, "k"), _rows_of(v, heads, d, "v")
+    _need(k.dtype == v.dtype and k.dtype in (torch.float32, torch.bfloat16) and k.shape[0] == v.shape[0],
+          "k and v must have as many rows of one type, float32 or bfloat16")
+    _on_gpu(slots)
+    _need(slots.dtype == torch.int64 and slots.dim() == 1 and slots.numel() == k.shape[0],
+          "slots must be int64 [rows]")
+    st = lt_cache4_append(_ptr(k), _ptr(v), _dtype_code(k), ks, vs, k.shape[0], _ptr(codes), _ptr(scales), pages,
+                          page, heads, d, _ptr(slots), _stream(stream))
+    _check(st, "lt_cache4_append")
+
+
+def cache4_read(codes: torch.Tensor, scales: torch.Tensor, slots: torch.Tensor, stream=None):
+    """The (keys, values) that slots (int64 [rows]) hold, bfloat16 [rows,
+    kv_heads, head_dim] each; zeros for slots outside the cache."""
+    pages, page, heads, d = _cache4(codes, scales)
+    _on_gpu(slots)
+    _need(slots.dtype == torch.int64 and slots.dim() == 1, "slots must be int64 [rows]")
+    n = slots.numel()
+    k = torch.empty((n, heads, d), dtype=torch.bfloat16, device=slots.device)
+    v = torch.empty_like(k)
+    st = lt_cache4_read(_ptr(codes), _ptr(scales), pages, page, heads, d, _ptr(slots), n, _ptr(k), _ptr(v),
+                        _stream(stream))
+    _check(st, "lt_cache4_read")
+    _used_on(stream, k, v)
+    return k, v
+
+
+def cache4_attention(q: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, block_table: torch.Tensor,
+                     cu_tokens: torch.Tensor, seq_lens: torch.Tensor, scale: Optional[float] = None,
+                     visible_start: Optional[torch.Tensor] = None, visible_end: Optional[torch.Tensor] = None,
+                     selected: Optional[torch.Tensor] = None, selected_start: Optional[torch.Tensor] = None,
+                     return_lse: bool = True, workspace: Optional[torch.Tensor] = None, stream=None):
+    """Attention of q [T, heads, head_dim] (bfloat16) over the 4-bit cache:
+    tokens [cu_tokens[r], cu_tokens[r + 1]) belong to request r, which has
+    seq_lens[r] cached keys on the pages of block_table[r]. Token t sees the keys
+    [visible_start[t], visible_end[t]) (defaults: 0, and causal), and with
+    `selected` int32 [T, k] only those on its list (indexer_topk's result; minus
+    selected_start[t] for sequences packed into one key array). Scale defaults to
+    head_dim ** -0.5. Returns (out bfloat16 like q, lse float32 [T, heads] or
+    None)."""
+    pages, page, hkv, d = _cache4(codes, scales)
+    _need(q.dim() == 3 and q.dtype == torch.bfloat16, "q must be bfloat16 [T, heads, head_dim]")
+    tokens, hq = q.shape[0], q.shape[1]
+    qs = _rows_of(q, hq, d, "q")
+    _int32(seq_lens, None, "seq_lens")
+    n = seq_lens.numel()
+    _int32(cu_tokens, n + 1, "cu_tokens")
+    _int32(visible_start, tokens, "visible_start")
+    _int32(visible_end, tokens, "visible_end")
+    _int32(selected_start, tokens, "selected_start")
+    ld, width = _table(block_table, n)
+    k, sel_ld = 0, 0
+    if selected is not None:
+        _need(selected.is_cuda and selected.dtype == torch.int32 and selected.dim() == 2
+              and selected.shape[0] == tokens and selected.shape[1] >= 1
+              and (selected.shape[1] == 1 or selected.stride(1) == 1 or tokens == 0),
+              "selected must be an int32 [T, k] GPU matrix with unit column stride")
+        k = selected.shape[1]
+        sel_ld = max(selected.stride(0), k) if tokens > 1 else k
+    out = torch.empty((tokens, hq, d), dtype=torch.bfloat16, device=q.device)
+    lse = torch.empty((tokens, hq), dtype=torch.float32, device=q.device) if return_lse else None
+    need = lt_cache4_attention_workspace_size(tokens, n, hq, hkv, d, k)
+    _need(need > 0, "unsupported shape for lt_cache4_attention")
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    st = lt_cache4_attention(_ptr(q), qs, tokens, hq, d, _ptr(codes), _ptr(scales), pages, page, hkv,
+                             _ptr(block_table), ld, width, _ptr(cu_tokens), _ptr(seq_lens), n, _ptr(visible_start),
+                             _ptr(visible_end), _ptr(selected), sel_ld, k, _ptr(selected_start),
+                             d ** -0.5 if scale is None else scale, _ptr(out), _ptr(lse), _ptr(workspace),
+                             workspace.numel(), _stream(stream))
+    _check(st, "lt_cache4_attention")
+    _used_on(stream, out, lse, workspace)
+    return out, lse
+
+
+class TokenLogprobs(NamedTuple):
+    """What token_logprobs returns; see lt_token_logprobs in the header."""
+    logprob: torch.Tensor      # float32 [rows]
+    entropy: torch.Tensor      # float32 [rows]
+    lse: torch.Tensor          # float32 [rows]
+    top_index: torch.Tensor    # int32 [rows, top]
+    top_logprob: torch.Tensor  # float32 [rows, top]
+
+
+def _logits(logits: torch.Tensor, tokens: torch.Tensor) -> int:
+    _need(logits.is_cuda and logits.dim() == 2 and logits.dtype in (torch.float32, torch.bfloat16)
+          and (logits.numel() == 0 or logits.shape[1] == 1 or logits.stride(1) == 1),
+          "logits must be a float32 or bfloat16 [rows, vocab] GPU matrix with unit column stride")
+    _on_gpu(tokens)
+    _need(tokens.dtype == torch.int64 and tokens.dim() == 1 and tokens.numel() == logits.shape[0],
+          "tokens must be int64 [rows]")
+    return max(logits.stride(0), logits.shape[1]) if logits.shape[0] > 1 else logits.shape[1]
+
+
+def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0, scale: float = 1.0,
+                   workspace: Optional[torch.Tensor] = None, stream=None) -> TokenLogprobs:
+    """Log probability of each row's token under softmax(scale * logits), the
+    row's entropy, log normaliser and `top` best alternatives with their log
+    probabilities (higher logit first, equal ones by index). A token outside the
+    vocabulary (-1) is not counted: its log probability is 0."""
+    ld = _logits(logits, tokens)
+    rows, vocab = logits.shape
+    dt, dev = _dtype_code(logits), logits.device
+    need = lt_token_logprobs_workspace_size(dt, rows, vocab, top)
+    _need(need > 0, "unsupported shape for lt_token_logprobs (top must be 0..%d)" % LT_LOGPROB_MAX_TOP)
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    f = torch.empty((3, rows), dtype=torch.float32, device=dev)
+    r = TokenLogprobs(f[0], f[1], f[2], torch.empty((rows, min(top, vocab)), dtype=torch.int32, device=dev),
+                      torch.empty((rows, min(top, vocab)), dtype=torch.float32, device=dev))
+    st = lt_token_logprobs(_ptr(logits), dt, ld, rows, vocab, _ptr(tokens), scale, min(top, vocab), _ptr(r.logprob),
+                           _ptr(r.entropy), _ptr(r.lse), _ptr(r.top_index), _ptr(r.top_logprob), _ptr(workspace),
+                           workspace.numel(), _stream(stream))
+    _check(st, "lt_token_logprobs")
+    _used_on(stream, f, r.top_index, r.top_logprob, workspace)
+    return r
+
+
+def token_logprobs_backward(logits: torch.Tensor, tokens: torch.Tensor, lse: torch.Tensor, entropy: torch.Tensor,
+                            grad_logprob: Optional[torch.Tensor] = None, grad_entropy: Optional[torch.Tensor] = None,
+                            scale: float = 1.0, stream=None) -> torch.Tensor:
+    """The logits' gradient (in their type) from those of token_logprobs'
+    logprob and entropy (float32 [rows], None = zero) and its lse and entropy."""
+    ld = _logits(logits, tokens)
+    rows, vocab = logits.shape
+    for t in (lse, entropy, grad_logprob, grad_entropy):
+        _on_gpu(t)
+        _need(t is None or (t.dtype == torch.float32 and t.dim() == 1 and t.numel() == rows),
+              "lse, entropy and the gradients must be float32 [rows]")
+    # rows start on a line: full-width stores whatever the vocabulary's size
+    pad = (vocab + 63) // 64 * 64
+    out = torch.empty((rows, pad), dtype=logits.dtype, device=logits.device)[:, :vocab]
+    st = lt_token_logprobs_backward(_ptr(logits), _dtype_code(logits), ld, rows, vocab, _ptr(tokens), scale, _ptr(lse),
+                                    _ptr(entropy), _ptr(grad_logprob), _ptr(grad_entropy), _ptr(out), pad,
+                                    _stream(stream))
+    _check(st, "lt_token_logprobs_backward")
+    _used_on(stream, out)
+    return out
