@@ -11,9 +11,9 @@
 // output's own rounding.
 //
 // Rows are (token, head of the group) pairs that share a KV head. A tile is up
-// to 16 * RT rows of one request; its key range is cut into chunks so that the
-// work of all tiles, long and short, fills the GPU evenly; chunks of a tile
-// are joined by a second kernel.
+// to 16 (k_attn4_few), 64 or 128 (k_attn4_many) rows of one request; its key
+// range is cut into chunks so that the work of all tiles, long and short, fills
+// the GPU evenly; the chunks of a tile are joined by a second kernel.
 #include "cache4.hpp"
 #include "internal.hpp"
 
@@ -21,12 +21,15 @@ namespace lt {
 namespace {
 
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4_t* lds_s16x4_t;
 
 constexpr float kLn2 = 0.69314718055994530942f;
 constexpr int kInlineRequests = 64;  // requests that a wave schedules by itself
-constexpr int kMinChunk = 128;       // shortest chunk: one step of 32 keys for each wave
+constexpr int kMinChunk = 128;       // shortest chunk
+constexpr uint32_t kNoSplit = 0x80000000u;  // chunk length that no request reaches
 
 __device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -41,6 +44,9 @@ __device__ __forceinline__ uint32_t lane_bcast(uint32_t v, int lane) {
 // items, and C = sum tiles_r * span_r / target keeps the items within
 // target + tiles. span_r only balances: a tile's last chunk takes what is left.
 // ---------------------------------------------------------------------------
+// Keys of a request; positions and steps past them stay within 31 bits.
+__device__ __forceinline__ int key_count(int n) { return min(max(n, 0), LT_CACHE4_MAX_KEYS); }
+
 struct Req {
   int t0, nt, len, tiles;  // first token, tokens, cached keys, tiles
   uint32_t span;
@@ -52,7 +58,7 @@ __device__ __forceinline__ Req load_req(const Attn4Args& a, int r) {
   const int t0 = min(max(a.cu[r], 0), a.T), t1 = min(max(a.cu[r + 1], t0), a.T);
   q.t0 = t0;
   q.nt = t1 - t0;
-  q.len = max(a.seq[r], 0);
+  q.len = key_count(a.seq[r]);
   q.tiles = q.nt > 0 ? a.hkv * (int)(((int64_t)q.nt * a.group + ROWS - 1) / ROWS) : 0;
   int lo = 0, hi = q.len;
   if (q.nt > 0 && a.end) hi = min(max(a.end[t1 - 1], 0), hi);
@@ -87,18 +93,19 @@ __device__ __forceinline__ uint32_t chunk_len(uint64_t work, int target) {
 
 struct Item {
   int r, t0, nt, len;       // request, its first token, tokens and keys
-  int head, row0;           // KV head; first row of the tile within the request
+  int head, row0, rows;     // KV head; the tile's rows [row0, rows) within the request, at most ROWS
   int chunk, chunks;
-  uint32_t C;
+  uint32_t C, item;
   bool any;
 };
 
 // The schedule of more than kInlineRequests requests: the items' prefix sums
-// sched[0..R] and the chunk length sched[R + 1].
+// sched[0..R], the chunk length sched[R + 1] and the tiles' prefix sums from
+// sched[R + 2] on.
 template <int ROWS>
 __global__ __launch_bounds__(1024) void k_attn4_schedule(Attn4Args a) {
   __shared__ uint64_t sum[16];
-  __shared__ uint32_t part[16];
+  __shared__ uint32_t part[16], tpart[16];
   const int t = threadIdx.x, w = t >> 6, lane = t & 63;
   uint64_t work = 0;
   for (int r = t; r < a.R; r += 1024) {
@@ -110,117 +117,141 @@ __global__ __launch_bounds__(1024) void k_attn4_schedule(Attn4Args a) {
   __syncthreads();
   work = 0;
   for (int i = 0; i < 16; ++i) work += sum[i];
-  const uint32_t C = a.target > 0 ? chunk_len(work, a.target) : 0x80000000u;
-  uint32_t base = 0;
+  const uint32_t C = a.target > 0 ? chunk_len(work, a.target) : kNoSplit;
+  uint32_t base = 0, tbase = 0;
   for (int r0 = 0; r0 < a.R; r0 += 1024) {
     const int r = r0 + t;
-    uint32_t n = 0;
+    uint32_t n = 0, nt = 0;
     if (r < a.R) {
       const Req q = load_req<ROWS>(a, r);
-      n = (uint32_t)q.tiles * ((q.span + C - 1) / C);
+      nt = (uint32_t)q.tiles;
+      n = nt * ((q.span + C - 1) / C);
     }
-    const uint32_t in = wave_prefix(n);
+    const uint32_t in = wave_prefix(n), tin = wave_prefix(nt);
     __syncthreads();
-    if (lane == 63) part[w] = in;
+    if (lane == 63) part[w] = in, tpart[w] = tin;
     __syncthreads();
-    uint32_t before = base, all = base;
+    uint32_t before = base, tbefore = tbase;
     for (int i = 0; i < 16; ++i) {
-      if (i < w) before += part[i];
-      all += part[i];
+      if (i < w) before += part[i], tbefore += tpart[i];
+      base += part[i];
+      tbase += tpart[i];
     }
-    if (r < a.R) a.sched[r] = before + in - n;
-    base = all;
+    if (r < a.R) {
+      a.sched[r] = before + in - n;
+      a.sched[a.R + 2 + r] = tbefore + tin - nt;
+    }
   }
   if (t == 0) {
     a.sched[a.R] = base;
     a.sched[a.R + 1] = C;
+    a.sched[2 * a.R + 2] = tbase;
   }
 }
 
-// The item a block works on; wave-uniform.
-template <int ROWS>
-__device__ __forceinline__ Item find_item(const Attn4Args& a, uint32_t item) {
+// The last of n >= 1 ascending entries (the first is taken to be <= x) that is <= x; wave-uniform.
+template <class T>
+__device__ __forceinline__ int last_le(const T* v, int n, T x) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0;
+  while (n > 1) {
+    const int step = (n + 63) / 64, o = lane * step;
+    const uint64_t le = __ballot(o == 0 || (o < n && v[lo + o] <= x));
+    const int at = (63 - __clzll((long long)le)) * step;
+    lo += at;
+    n = step > 1 ? min(step, n - at) : 1;
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// The item a block works on, or with TILE the first item of a tile; wave-uniform.
+template <int ROWS, bool TILE>
+__device__ __forceinline__ Item find_item(const Attn4Args& a, uint32_t id) {
   const int lane = threadIdx.x & 63;
   Item it{};
   Req q{};
-  uint32_t first = 0;
+  uint32_t first = 0, tfirst = 0;
   if (a.R <= kInlineRequests) {
     if (lane < a.R) q = load_req<ROWS>(a, lane);
-    it.C = a.target > 0 ? chunk_len(wave_sum64((uint64_t)q.tiles * q.span), a.target) : 0x80000000u;
+    it.C = a.target > 0 ? chunk_len(wave_sum64((uint64_t)q.tiles * q.span), a.target) : kNoSplit;
     const uint32_t n = lane < a.R ? (uint32_t)q.tiles * ((q.span + it.C - 1) / it.C) : 0u;
-    const uint32_t in = wave_prefix(n);
-    const uint64_t hit = __ballot(in > item);
+    const uint32_t in = wave_prefix(n), tin = TILE ? wave_prefix((uint32_t)q.tiles) : 0u;
+    const uint64_t hit = __ballot((TILE ? tin : in) > id);
     if (!hit) return it;
     it.r = __ffsll((unsigned long long)hit) - 1;
     first = lane_bcast(in - n, it.r);
+    tfirst = lane_bcast(tin - q.tiles, it.r);
     q.t0 = lane_bcast(q.t0, it.r);
     q.nt = lane_bcast(q.nt, it.r);
     q.len = lane_bcast(q.len, it.r);
     q.tiles = lane_bcast(q.tiles, it.r);
     q.span = lane_bcast(q.span, it.r);
   } else {
-    if (item >= a.sched[a.R]) return it;
+    const uint32_t* s = TILE ? a.sched + a.R + 2 : a.sched;
+    if (id >= s[a.R]) return it;
     it.C = a.sched[a.R + 1];
-    // last r with sched[r] <= item, 64 at a time (sched[0] = 0)
-    int lo = 0, n = a.R;
-    while (n > 0) {
-      const int step = (n + 63) / 64, r = lo + lane * step;
-      const uint64_t le = __ballot(lane * step < n && a.sched[min(r, a.R)] <= item);
-      lo += (63 - __clzll((long long)le)) * step;
-      n = step > 1 ? min(step, a.R - lo) : 0;
-    }
-    it.r = __builtin_amdgcn_readfirstlane(lo);
+    it.r = last_le<uint32_t>(s, a.R, id);
     first = a.sched[it.r];
+    tfirst = a.sched[a.R + 2 + it.r];
     q = load_req<ROWS>(a, it.r);
   }
   it.any = true;
   it.t0 = __builtin_amdgcn_readfirstlane(q.t0);
   it.nt = __builtin_amdgcn_readfirstlane(q.nt);
   it.len = __builtin_amdgcn_readfirstlane(q.len);
-  it.chunks = (int)((q.span + it.C - 1) / it.C);
-  const uint32_t at = item - first, tile = at / (uint32_t)it.chunks;
-  it.chunk = (int)(at - tile * it.chunks);
+  it.chunks = __builtin_amdgcn_readfirstlane((int)((q.span + it.C - 1) / it.C));
+  uint32_t tile;
+  if constexpr (TILE) {
+    tile = id - tfirst;
+    it.item = first + tile * it.chunks;
+  } else {
+    const uint32_t at = id - first;
+    tile = at / (uint32_t)it.chunks;
+    it.chunk = (int)(at - tile * it.chunks);
+    it.item = id;
+  }
   const int per_head = q.tiles / a.hkv;
   it.head = (int)tile / per_head;
-  it.row0 = ((int)tile - it.head * per_head) * ROWS;
+  // the last rows first: with a causal mask they see the most keys
+  it.row0 = (per_head - 1 - ((int)tile - it.head * per_head)) * ROWS;
+  it.rows = it.nt * a.group;
   return it;
 }
 
-// Items of list attention: every token of the batch, KV head and row tile over
-// a.chunks chunks of the list.
-template <int ROWS>
-__device__ __forceinline__ Item find_list_item(const Attn4Args& a, uint32_t item) {
-  const int lane = threadIdx.x & 63;
+// The same for list attention: every token of the batch, KV head and row tile
+// over a.chunks chunks of the list.
+template <int ROWS, bool TILE>
+__device__ __forceinline__ Item find_list_item(const Attn4Args& a, uint32_t id) {
   Item it{};
   if (a.R == 0) return it;
-  const uint32_t per_tok = (uint32_t)(a.hkv * a.row_tiles * a.chunks);
-  const int t = (int)(item / per_tok);
-  const uint32_t in = item - t * per_tok;
-  // the request whose tokens hold t: the last r with cu[r] <= t
-  int lo = 0, n = a.R;
-  while (n > 0) {
-    const int step = (n + 63) / 64, r = lo + lane * step;
-    const uint64_t le = __ballot(lane * step < n && (r == 0 || a.cu[min(r, a.R)] <= t));
-    lo += (63 - __clzll((long long)le)) * step;
-    n = step > 1 ? min(step, a.R - lo) : 0;
-  }
-  it.r = __builtin_amdgcn_readfirstlane(lo);
+  const uint32_t chunks = TILE ? 1u : (uint32_t)a.chunks, tile = id / chunks;
+  const uint32_t per_tok = (uint32_t)(a.hkv * a.row_tiles);
+  const int t = (int)(tile / per_tok);
+  it.r = last_le<int32_t>(a.cu, a.R, t);
   const int c0 = a.cu[it.r], c1 = a.cu[it.r + 1];
   if (t < c0 || t >= c1) return it;
   it.any = true;
   it.t0 = c0;
   it.nt = min(c1, a.T) - c0;
-  it.len = max(a.seq[it.r], 0);
+  it.len = key_count(a.seq[it.r]);
   it.chunks = a.chunks;
-  it.chunk = (int)(in % (uint32_t)a.chunks);
-  const uint32_t tile = in / (uint32_t)a.chunks;
-  it.head = (int)tile / a.row_tiles;
-  it.row0 = (t - c0) * a.group + ((int)tile - it.head * a.row_tiles) * ROWS;
+  it.chunk = (int)(id - tile * chunks);
+  it.item = TILE ? tile * a.chunks : id;
   it.C = (uint32_t)a.chunk_keys;
+  const int in = (int)(tile - t * per_tok);
+  it.head = in / a.row_tiles;
+  it.row0 = (t - c0) * a.group + (in - it.head * a.row_tiles) * ROWS;
+  it.rows = (t - c0 + 1) * a.group;  // of this token
   return it;
 }
 
-// Visible keys of token t (the i-th of its request).
+template <int ROWS, bool LIST, bool TILE>
+__device__ __forceinline__ Item find(const Attn4Args& a, uint32_t id) {
+  if constexpr (LIST) return find_list_item<ROWS, TILE>(a, id);
+  else return find_item<ROWS, TILE>(a, id);
+}
+
+// Visible keys of the i-th token of an item's request.
 __device__ __forceinline__ RowRange token_range(const Attn4Args& a, const Item& it, int i) {
   int e = a.end ? a.end[it.t0 + i] : it.len - it.nt + i + 1;
   e = min(max(e, 0), it.len);
@@ -228,6 +259,80 @@ __device__ __forceinline__ RowRange token_range(const Attn4Args& a, const Item& 
   s = min(max(s, 0), e);
   return RowRange{s, e};
 }
+
+// What the rows of a tile see together: [lo, hi) holds every visible key,
+// [smax, emin) the keys that all of them see.
+struct Reach {
+  int lo, hi, smax, emin;
+};
+template <int ROWS>
+__device__ __forceinline__ Reach tile_reach(const Attn4Args& a, const Item& it) {
+  Reach r{0x7FFFFFFF, 0, 0, 0x7FFFFFFF};
+  for (int x = it.row0 + (threadIdx.x & 63); x < min(it.row0 + ROWS, it.rows); x += 64) {
+    const RowRange rr = token_range(a, it, x / a.group);
+    if (rr.s < rr.e) {
+      r.lo = min(r.lo, rr.s);
+      r.hi = max(r.hi, rr.e);
+    }
+    r.smax = max(r.smax, rr.s);
+    r.emin = min(r.emin, rr.e);
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    r.lo = min(r.lo, __shfl_xor(r.lo, o));
+    r.hi = max(r.hi, __shfl_xor(r.hi, o));
+    r.smax = max(r.smax, __shfl_xor(r.smax, o));
+    r.emin = min(r.emin, __shfl_xor(r.emin, o));
+  }
+  r.lo = __builtin_amdgcn_readfirstlane(min(r.lo, r.hi));
+  r.hi = __builtin_amdgcn_readfirstlane(r.hi);
+  r.smax = __builtin_amdgcn_readfirstlane(r.smax);
+  r.emin = __builtin_amdgcn_readfirstlane(r.emin);
+  return r;
+}
+
+// The places of an item's chunk, positions or entries of the token's list, and
+// the keys that they name.
+template <bool LIST>
+struct Keys {
+  const int32_t *list, *table;
+  int base, lo, hi, k0, k1, head;
+  __device__ __forceinline__ void init(const Attn4Args& a, const Item& it, const Reach& r) {
+    table = a.table + (int64_t)it.r * a.table_ld;
+    head = it.head;
+    lo = r.lo;
+    hi = r.hi;
+    list = nullptr;
+    base = 0;
+    if constexpr (LIST) {
+      const int t = it.t0 + it.row0 / a.group;
+      list = a.list + (int64_t)t * a.list_ld;
+      base = a.list_base ? a.list_base[t] : 0;
+      k0 = (int)min((int64_t)it.chunk * it.C, (int64_t)a.list_k);
+      k1 = lo == hi ? k0 : (int)min((int64_t)k0 + it.C, (int64_t)a.list_k);
+    } else {
+      // a chunk's length comes from the request's estimate: the last one takes the rest
+      k0 = (int)min(lo + (int64_t)it.chunk * it.C, (int64_t)hi);
+      k1 = it.chunk == it.chunks - 1 ? hi : (int)min((int64_t)k0 + it.C, (int64_t)hi);
+    }
+  }
+  // the position of place j, or -1
+  __device__ __forceinline__ int position(int j) const {
+    if constexpr (LIST) {
+      if (j >= k1) return -1;
+      const int64_t p = (int64_t)list[j] - base;
+      return p >= lo && p < hi ? (int)p : -1;
+    } else {
+      return j < k1 ? j : -1;
+    }
+  }
+  // its page, or -1
+  __device__ __forceinline__ int page(const Attn4Args& a, int pos) const {
+    const int b = pos >> a.shift;
+    const int p = pos >= 0 && b < a.table_width ? table[b] : -1;
+    return p < a.num_pages ? p : -1;
+  }
+};
 
 __device__ __forceinline__ float max_groups(float x) {  // over the four lanes of a column
   x = fmaxf(x, __shfl_xor(x, 16));
@@ -238,20 +343,18 @@ __device__ __forceinline__ float sum_groups(float x) {
   return x + __shfl_xor(x, 32);
 }
 
-// The codes and scales of a lane's part of one key and its value.
+// A quarter (`part`) of one key's codes and of its value's, and the scales of both rows.
 template <int D>
 struct KeyRegs {
   uint32_t k[D / 32], v[D / 32];
-  uint32_t ks, vs;  // the row's scale bytes (D = 64: the key's and the value's in ks)
+  uint32_t ks, vs;  // scale bytes (D = 64: the key's and the value's in ks)
 };
 
-// Lane (c = lane % 16, g = lane / 16) takes dims [g D/4, (g + 1) D/4) of key c.
 template <int D>
-__device__ __forceinline__ void load_key(const Attn4Args& a, int page, int pos, int head, bool ok, KeyRegs<D>& x) {
-  const int g = (threadIdx.x & 63) >> 4;
+__device__ __forceinline__ void load_key(const Attn4Args& a, int page, int pos, int head, int part, KeyRegs<D>& x) {
   const int64_t row =
-      ok ? (((int64_t)page * a.hkv + head) << a.shift) + (pos & ((1 << a.shift) - 1)) : 0;  // any row serves
-  const uint8_t* c = a.codes + row * D + g * (D / 8);
+      page >= 0 ? (((int64_t)page * a.hkv + head) << a.shift) + (pos & ((1 << a.shift) - 1)) : 0;  // any row serves
+  const uint8_t* c = a.codes + row * D + part * (D / 8);
   const uint8_t* s = a.scales + row * (D / 16);
   if constexpr (D == 128) {
     const uint4 k = *reinterpret_cast<const uint4*>(c), v = *reinterpret_cast<const uint4*>(c + D / 2);
@@ -267,174 +370,232 @@ __device__ __forceinline__ void load_key(const Attn4Args& a, int page, int pos, 
   }
 }
 
-// The exponents of a lane's part of a key and of its value; 0 for a key that
-// does not count, whose codes are then finite whatever they are.
+// The exponents of a quarter of a key and of its value; 0 for a key that does
+// not count, whose codes are then finite whatever they are.
 template <int D>
-__device__ __forceinline__ uint32_t key_byte(const KeyRegs<D>& x, int g, bool ok) {
-  const uint32_t b = D == 128 ? x.ks >> (8 * g) : x.ks >> (8 * (g >> 1));
+__device__ __forceinline__ uint32_t key_byte(const KeyRegs<D>& x, int part, bool ok) {
+  const uint32_t b = D == 128 ? x.ks >> (8 * part) : x.ks >> (8 * (part >> 1));
   return ok ? b & 255u : 0u;
 }
 template <int D>
-__device__ __forceinline__ uint32_t value_byte(const KeyRegs<D>& x, int g, bool ok) {
-  const uint32_t b = D == 128 ? x.vs >> (8 * g) : x.ks >> (16 + 8 * (g >> 1));
+__device__ __forceinline__ uint32_t value_byte(const KeyRegs<D>& x, int part, bool ok) {
+  const uint32_t b = D == 128 ? x.vs >> (8 * part) : x.ks >> (16 + 8 * (part >> 1));
   return ok ? b & 255u : 0u;
 }
 
+// Rows of decoded keys (k_attn4_many) and values (k_attn4_few) in LDS, in bytes.
+// 16 lanes that read 16 bytes of 16 key rows, and 32 that read 8 bytes of 8
+// value rows in fours, meet every bank once.
 template <int D>
-constexpr int kVRow = 2 * D + 32;  // bytes of a decoded value row in LDS: 8 rows cover all banks once
+constexpr int kKRow = 2 * D + 16;
+template <int D>
+constexpr int kVRow = 2 * D + 32;
 
 // ---------------------------------------------------------------------------
-// Few rows a tile: the four waves of a block share the chunk's keys, 32 at a
-// time in turn, and join their sums at the end. Keys are decoded straight into
-// the matrix operand; values pass through the wave's own LDS rows, whose
-// transposing reads give the other operand. The products are taken as
-// S^T = K Q^T and O^T = V^T P^T, so that a lane's probabilities are already
-// the operand of the second product.
+// A column of rows: lane (c = lane % 16, g = lane / 16) holds row c's maximum
+// m (and mc = m * scale), its share of the sum l and, as O^T tiles, the outputs
+// 16 n + 4 g .. + 3. The products are taken as S^T = K Q^T and O^T = V^T P^T, so
+// a lane's probabilities are already the operand of the second product.
 // ---------------------------------------------------------------------------
-template <int D, int RT, bool LIST>
-__global__ __launch_bounds__(256) void k_attn4_few(Attn4Args a) {
-  constexpr int ROWS = 16 * RT, NI = D / 32, NT = D / 16;
-  extern __shared__ __align__(16) uint8_t lds[];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
-  const Item it = LIST ? find_list_item<ROWS>(a, blockIdx.x) : find_item<ROWS>(a, blockIdx.x);
+template <int D>
+struct Column {
+  f32x4_t acc[D / 16];
+  float m, mc, l;
+  int s, e;  // the row's visible range; empty for no row
+  bool row;
 
-  // rows of tokens that belong to no request
-  {
-    const int used = a.R > 0 ? min(max(a.cu[a.R], 0), a.T) : 0;
-    const int per = a.hkv * a.group * D / 2;
-    for (int t = used + blockIdx.x; t < a.T; t += gridDim.x) {
-      uint32_t* o = reinterpret_cast<uint32_t*>(a.out + (int64_t)t * per * 2);
-      for (int i = threadIdx.x; i < per; i += 256) o[i] = 0u;
-      if (a.lse)
-        for (int i = threadIdx.x; i < a.hkv * a.group; i += 256) a.lse[(int64_t)t * a.hkv * a.group + i] = neg_inf();
-    }
-  }
-  if (!it.any) return;
-
-  // this lane's rows (column c of every row tile) and their ranges
-  const int rows = LIST ? min((it.row0 / a.group + 1) * a.group, it.nt * a.group) : it.nt * a.group;
-  bf16x8_t q[RT][NI];
-  int rs[RT], re[RT];
-  int lo = 0x7FFFFFFF, hi = 0, smax = 0, emin = 0x7FFFFFFF;
+  __device__ __forceinline__ void init(const Attn4Args& a, const Item& it, int x, bf16x8_t (&q)[D / 32], int stride,
+                                       int step) {
+    m = neg_inf();
+    mc = l = 0.0f;
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    const int x = it.row0 + rt * 16 + c;
-    rs[rt] = re[rt] = 0;
-    if (x < rows) {
-      const int i = x / a.group, h = it.head * a.group + (x - i * a.group);
-      const uint16_t* p = a.q + (int64_t)(it.t0 + i) * a.q_stride + (int64_t)h * D + g * (D / 4);
+    for (int n = 0; n < D / 16; ++n) acc[n] = f32x4_t{};
+    s = e = 0;
+    row = x < it.rows;
+    if (row) {
+      const int i = x / a.group, h = it.head * a.group + (x - i * a.group), g = (threadIdx.x & 63) >> 4;
+      const uint16_t* p = a.q + (int64_t)(it.t0 + i) * a.q_stride + (int64_t)h * D + g * stride;
 #pragma unroll
-      for (int n = 0; n < NI; ++n) q[rt][n] = *reinterpret_cast<const bf16x8_t*>(p + 8 * n);
+      for (int n = 0; n < D / 32; ++n) q[n] = *reinterpret_cast<const bf16x8_t*>(p + n * step);
       const RowRange rr = token_range(a, it, i);
-      rs[rt] = rr.s;
-      re[rt] = rr.e;
-      if (rr.s < rr.e) {
-        lo = min(lo, rr.s);
-        hi = max(hi, rr.e);
+      s = rr.s;
+      e = rr.e;
+    } else {
+#pragma unroll
+      for (int n = 0; n < D / 32; ++n) q[n] = bf16x8_t{};
+    }
+  }
+
+  // Scores of KT tiles of 16 keys, place j0 on, to probabilities. valid: a bit
+  // a key, looked at (with the row's range) unless every row sees all of them.
+  template <int KT, bool LIST>
+  __device__ __forceinline__ void weigh(f32x4_t (&x)[KT], bool whole, uint64_t valid, int j0, float sc, float slack,
+                                        bf16x8_t (&p)[KT / 2]) {
+    const int g = (threadIdx.x & 63) >> 4;
+    if (!whole) {
+#pragma unroll
+      for (int u = 0; u < KT; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int kk = 16 * u + 4 * g + i;
+          bool v = (valid >> kk) & 1u;
+          if constexpr (!LIST) v = v && j0 + kk >= s && j0 + kk < e;
+          x[u][i] = v ? x[u][i] : neg_inf();
+        }
+    }
+    float top = fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3]));
+#pragma unroll
+    for (int u = 1; u < KT; ++u) top = fmaxf(top, fmaxf(fmaxf(x[u][0], x[u][1]), fmaxf(x[u][2], x[u][3])));
+    // the maximum is renewed only where it would grow by more than 2^8: the
+    // sums keep their precision at any power of two
+    if (__any(top > m + slack)) {
+      const float mn = fmaxf(m, max_groups(top));
+      const float nc = mn == neg_inf() ? 0.0f : mn * sc;
+      const float f = m == neg_inf() ? 0.0f : exp2_fast(mc - nc);
+      m = mn;
+      mc = nc;
+      l *= f;
+#pragma unroll
+      for (int n = 0; n < D / 16; ++n) acc[n] *= f;
+    }
+#pragma unroll
+    for (int u = 0; u < KT; ++u) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[u][i] = exp2_fast(fmaf(x[u][i], sc, -mc));
+      l += (x[u][0] + x[u][1]) + (x[u][2] + x[u][3]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[u >> 1][4 * (u & 1) + i] = (__bf16)x[u][i];
+    }
+  }
+
+  // Values that are not finite, into the rows that see them: bad has a bit for
+  // each (quarter, key of 16) of the tile of keys at place j0.
+  template <bool LIST>
+  __device__ __forceinline__ void spoil(uint64_t bad, int j0) {
+    while (bad) {
+      const int from = __ffsll((unsigned long long)bad) - 1;
+      bad &= bad - 1;
+      const int j = j0 + (from & 15);
+      if (row && (LIST || (j >= s && j < e))) {
+#pragma unroll
+        for (int n = 0; n < D / 16; ++n)
+          if (n / (D / 64) == from >> 4) acc[n] += __builtin_nanf("");
       }
-      smax = max(smax, rr.s);
-      emin = min(emin, rr.e);
-    } else {
-#pragma unroll
-      for (int n = 0; n < NI; ++n) q[rt][n] = bf16x8_t{};
     }
   }
-#pragma unroll
-  for (int o = 1; o < 16; o <<= 1) {
-    lo = min(lo, __shfl_xor(lo, o));
-    hi = max(hi, __shfl_xor(hi, o));
-    smax = max(smax, __shfl_xor(smax, o));
-    emin = min(emin, __shfl_xor(emin, o));
-  }
-  lo = __builtin_amdgcn_readfirstlane(lo);
-  hi = __builtin_amdgcn_readfirstlane(hi);
-  smax = __builtin_amdgcn_readfirstlane(smax);
-  emin = __builtin_amdgcn_readfirstlane(emin);
-  if (lo > hi) lo = hi;
 
-  // the chunk's keys: positions, or places on the token's list
-  int64_t k0, k1;
-  const int32_t* list = nullptr;
-  int base = 0;
-  if constexpr (LIST) {
-    const int t = it.t0 + it.row0 / a.group;
-    list = a.list + (int64_t)t * a.list_ld;
-    base = a.list_base ? a.list_base[t] : 0;
-    k0 = (int64_t)it.chunk * it.C;
-    k1 = min(k0 + (int64_t)it.C, (int64_t)a.list_k);
-    if (lo == hi) k1 = k0;
-  } else {
-    k0 = lo + (int64_t)it.chunk * it.C;
-    k1 = it.chunk == it.chunks - 1 ? hi : min(k0 + (int64_t)it.C, (int64_t)hi);
+  // One row's result, or its part of it. M, L: the row's maximum (times scale) and sum.
+  __device__ __forceinline__ void store(const Attn4Args& a, const Item& it, int x, int rows_per_tile, float M,
+                                        float L) const {
+    if (!row) return;
+    const int g = (threadIdx.x & 63) >> 4;
+    if (it.chunks == 1) {
+      const int i = x / a.group, h = it.head * a.group + (x - i * a.group);
+      const int64_t at = (int64_t)(it.t0 + i) * a.hkv * a.group + h;
+      const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+      __bf16* o = reinterpret_cast<__bf16*>(a.out) + at * D + 4 * g;
+#pragma unroll
+      for (int n = 0; n < D / 16; ++n) {
+        const f32x4_t y = acc[n] * inv;
+        *reinterpret_cast<bf16x4_t*>(o + n * 16) = bf16x4_t{(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
+      }
+      if (a.lse && g == 0) a.lse[at] = L == 0.0f ? neg_inf() : (M + __builtin_amdgcn_logf(L)) * kLn2;
+    } else {
+      const int64_t at = (int64_t)it.item * rows_per_tile + (x - it.row0);
+      f32x4_t* o = reinterpret_cast<f32x4_t*>(a.part_o + at * D) + g;
+#pragma unroll
+      for (int n = 0; n < D / 16; ++n) o[n * 4] = acc[n];
+      if (g == 0) a.part_ml[at] = float2{M, L};
+    }
   }
-  const int32_t* table = a.table + (int64_t)it.r * a.table_ld;
+};
 
-  f32x4_t acc[RT][NT];
-  float m[RT], mc[RT], l[RT];
+// O^T += V^T P^T for 32 keys whose decoded values are in LDS rows at v.
+template <int D, int RW>
+__device__ __forceinline__ void add_values(const uint8_t* v, const bf16x8_t (&p)[RW], Column<D> (&col)[RW]) {
+  const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+  const uint8_t* vr = v + (4 * g + (c >> 2)) * kVRow<D> + (c & 3) * 8;
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    m[rt] = neg_inf();
-    mc[rt] = 0.0f;
-    l[rt] = 0.0f;
+  for (int n = 0; n < D / 16; ++n) {
+    const s16x4_t v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(vr + n * 32));
+    const s16x4_t v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(vr + 16 * kVRow<D> + n * 32));
+    const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-    for (int n = 0; n < NT; ++n) acc[rt][n] = f32x4_t{};
+    for (int w = 0; w < RW; ++w)
+      col[w].acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[w], col[w].acc[n], 0, 0, 0);
   }
+}
+
+// Rows of tokens that belong to no request: zero, by all blocks of a launch.
+template <int D>
+__device__ __forceinline__ void clear_padding(const Attn4Args& a) {
+  const int used = a.R > 0 ? min(max(a.cu[a.R], 0), a.T) : 0;
+  const int heads = a.hkv * a.group, per = heads * D / 2;
+  for (int t = used + blockIdx.x; t < a.T; t += gridDim.x) {
+    uint32_t* o = reinterpret_cast<uint32_t*>(a.out) + (int64_t)t * per;
+    for (int i = threadIdx.x; i < per; i += 256) o[i] = 0u;
+    if (a.lse)
+      for (int i = threadIdx.x; i < heads; i += 256) a.lse[(int64_t)t * heads + i] = neg_inf();
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Up to 16 rows a tile: the four waves of a block share the chunk's keys, 32 at
+// a time in turn, and join their sums at the end. Keys are decoded straight
+// into the matrix operand; values pass through the wave's own LDS rows, whose
+// transposing reads give the other operand. No barrier inside the loop.
+// ---------------------------------------------------------------------------
+template <int D, bool LIST>
+__global__ __launch_bounds__(256, 3) void k_attn4_few(Attn4Args a) {
+  constexpr int ROWS = 16, NI = D / 32, NT = D / 16;
+  __shared__ __align__(16) uint8_t lds[4 * 32 * kVRow<D>];
+  __shared__ float ml[4][2][ROWS];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+  const Item it = find<ROWS, LIST, false>(a, blockIdx.x);
+  clear_padding<D>(a);
+  if (!it.any) return;
+  const Reach reach = tile_reach<ROWS>(a, it);
+  Keys<LIST> keys;
+  keys.init(a, it, reach);
+
+  // lane group g takes the dims [g D/4, (g + 1) D/4) of every key, 8 at a time
+  bf16x8_t q[NI];
+  Column<D> col[1];
+  col[0].init(a, it, it.row0 + c, q, D / 4, 8);
   uint8_t* vrows = lds + wave * 32 * kVRow<D>;
-  const float sc = a.scale_log2;
-
-  const int steps = k1 > k0 ? (int)((k1 - k0 + 31) / 32) : 0;
-
-  // position of place j, or -1
-  auto place = [&](int64_t j) -> int {
-    if (j >= k1) return -1;
-    if constexpr (LIST) {
-      const int p = list[j] - base;
-      return p >= lo && p < hi ? p : -1;
-    } else {
-      return (int)j;
-    }
-  };
-  auto page_of = [&](int pos) -> int {
-    const int b = pos >> a.shift;
-    return pos >= 0 && b < a.table_width ? table[b] : -1;
-  };
+  const int steps = (keys.k1 - keys.k0 + 31) / 32;
 
   // software pipeline: codes one step ahead, pages two, list entries three
   KeyRegs<D> kv[2];
-  int pos[2] = {-1, -1}, pos1[2] = {-1, -1}, page1[2] = {-1, -1}, pos2[2] = {-1, -1};
-  bool ok[2] = {false, false};
-  auto place_of_step = [&](int s, int (&p)[2]) {
-    const int64_t j = k0 + (int64_t)s * 32 + c;
-    p[0] = s < steps ? place(j) : -1;
-    p[1] = s < steps ? place(j + 16) : -1;
+  int page0[2], page1[2], pos1[2], pos2[2];
+  auto positions = [&](int s, int (&p)[2]) {
+    const int j = keys.k0 + s * 32 + c;
+    p[0] = s < steps ? keys.position(j) : -1;
+    p[1] = s < steps ? keys.position(j + 16) : -1;
   };
   {
     int p0[2];
-    place_of_step(wave, p0);
-    place_of_step(wave + 4, pos1);
-    place_of_step(wave + 8, pos2);
+    positions(wave, p0);
+    positions(wave + 4, pos1);
+    positions(wave + 8, pos2);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const int pg = page_of(p0[u]);
-      page1[u] = page_of(pos1[u]);
-      pos[u] = p0[u];
-      ok[u] = pg >= 0 && pg < a.num_pages;
-      load_key<D>(a, pg, p0[u], it.head, ok[u], kv[u]);
+      page0[u] = keys.page(a, p0[u]);
+      page1[u] = keys.page(a, pos1[u]);
+      load_key<D>(a, page0[u], p0[u], it.head, g, kv[u]);
     }
   }
-
   for (int s = wave; s < steps; s += 4) {
-    // decode this step
-    bf16x8_t kf[2][NI];
-    const uint32_t valid0 = (uint32_t)__ballot(ok[0]) & 0xFFFFu, valid1 = (uint32_t)__ballot(ok[1]) & 0xFFFFu;
-    const int64_t j0 = k0 + (int64_t)s * 32;
-    bool whole = (valid0 & valid1) == 0xFFFFu;
-    if constexpr (!LIST) whole = whole && j0 >= smax && j0 + 32 <= emin;
+    const uint64_t valid = (__ballot(page0[0] >= 0) & 0xFFFFu) | (__ballot(page0[1] >= 0) & 0xFFFFu) << 16;
+    const int j0 = keys.k0 + s * 32;
+    bool whole = valid == 0xFFFFFFFFu;
+    if constexpr (!LIST) whole = whole && j0 >= reach.smax && j0 + 32 <= reach.emin;
     uint64_t bad[2] = {0, 0};
+    f32x4_t x[2] = {};
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const float ks = __uint_as_float(key_byte<D>(kv[u], g, ok[u]) << 23);
-      uint32_t vb = value_byte<D>(kv[u], g, ok[u]);
+      const float ks = __uint_as_float(key_byte<D>(kv[u], g, page0[u] >= 0) << 23);
+      uint32_t vb = value_byte<D>(kv[u], g, page0[u] >= 0);
       // a value that is not finite must not reach rows that do not see it
       if (!whole) {
         bad[u] = __ballot(vb == 255u);
@@ -444,287 +605,491 @@ __global__ __launch_bounds__(256) void k_attn4_few(Attn4Args a) {
       uint8_t* w = vrows + (u * 16 + c) * kVRow<D> + g * (D / 2);
 #pragma unroll
       for (int n = 0; n < NI; ++n) {
-        kf[u][n] = decode8(kv[u].k[n], ks);
+        x[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8(kv[u].k[n], ks), q[n], x[u], 0, 0, 0);
         *reinterpret_cast<bf16x8_t*>(w + 16 * n) = decode8(kv[u].v[n], vs);
       }
     }
-    // start the next one
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      pos[u] = pos1[u];
-      const int pg = page1[u];
-      ok[u] = pg >= 0 && pg < a.num_pages;
-      load_key<D>(a, pg, pos[u], it.head, ok[u], kv[u]);
+      page0[u] = page1[u];
+      load_key<D>(a, page0[u], pos1[u], it.head, g, kv[u]);
       pos1[u] = pos2[u];
-      page1[u] = page_of(pos1[u]);
+      page1[u] = keys.page(a, pos1[u]);
     }
-    place_of_step(s + 12, pos2);
-
-    // S^T, then probabilities
-    bf16x8_t p[RT];
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      f32x4_t s0 = {}, s1 = {};
-#pragma unroll
-      for (int n = 0; n < NI; ++n) {
-        s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[0][n], q[rt][n], s0, 0, 0, 0);
-        s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[1][n], q[rt][n], s1, 0, 0, 0);
-      }
-      if (!whole) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int kk = 4 * g + i;
-          bool v0 = (valid0 >> kk) & 1u, v1 = (valid1 >> kk) & 1u;
-          if constexpr (!LIST) {
-            const int64_t j = j0 + kk;
-            v0 = v0 && j >= rs[rt] && j < re[rt];
-            v1 = v1 && j + 16 >= rs[rt] && j + 16 < re[rt];
-          }
-          s0[i] = v0 ? s0[i] : neg_inf();
-          s1[i] = v1 ? s1[i] : neg_inf();
-        }
-      }
-      const float top = fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])),
-                              fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
-      // the maximum is renewed only where it would grow by more than 2^8: the
-      // sums keep their precision at any power of two
-      if (__any(top > m[rt] + a.slack)) {
-        const float mn = fmaxf(m[rt], max_groups(top));
-        const float nc = mn == neg_inf() ? 0.0f : mn * sc;
-        const float f = m[rt] == neg_inf() ? 0.0f : exp2_fast(mc[rt] - nc);
-        m[rt] = mn;
-        mc[rt] = nc;
-        l[rt] *= f;
-#pragma unroll
-        for (int n = 0; n < NT; ++n) acc[rt][n] *= f;
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        s0[i] = exp2_fast(fmaf(s0[i], sc, -mc[rt]));
-        s1[i] = exp2_fast(fmaf(s1[i], sc, -mc[rt]));
-      }
-      l[rt] += (s0[0] + s0[1]) + (s0[2] + s0[3]) + ((s1[0] + s1[1]) + (s1[2] + s1[3]));
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        p[rt][i] = (__bf16)s0[i];
-        p[rt][4 + i] = (__bf16)s1[i];
-      }
-    }
-    // O^T += V^T P^T
+    positions(s + 12, pos2);
+    bf16x8_t p[1];
+    col[0].template weigh<2, LIST>(x, whole, valid, j0, a.scale_log2, a.slack, p);
     __builtin_amdgcn_wave_barrier();
-    const uint8_t* vr = vrows + (4 * g + (c >> 2)) * kVRow<D> + (c & 3) * 8;
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const s16x4_t v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(vr + n * 32));
-      const s16x4_t v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(vr + 16 * kVRow<D> + n * 32));
-      const bf16x8_t vf = __builtin_bit_cast(
-          bf16x8_t, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) acc[rt][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, p[rt], acc[rt][n], 0, 0, 0);
-    }
+    add_values<D, 1>(vrows, p, col);
     __builtin_amdgcn_wave_barrier();
-    // values that are not finite, into the rows that see them
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      uint64_t b = bad[u];
-      while (b) {
-        const int from = __ffsll((unsigned long long)b) - 1;
-        b &= b - 1;
-        const int kk = from & 15, gg = from >> 4;  // key, quarter of the dims
-        const int64_t j = j0 + u * 16 + kk;
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-          bool sees = it.row0 + rt * 16 + c < rows;
-          if constexpr (!LIST) sees = sees && j >= rs[rt] && j < re[rt];
-          if (sees) {
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-              if (n / (NT / 4) == gg) acc[rt][n] += __builtin_nanf("");
-          }
-        }
-      }
-    }
+    col[0].template spoil<LIST>(bad[0], j0);
+    col[0].template spoil<LIST>(bad[1], j0 + 16);
   }
 
   // join the four waves: maxima and sums first, then the outputs by halves
-  float* ml = reinterpret_cast<float*>(lds + a.lds_join);  // [4][2][ROWS]
-  float w[RT];
   __syncthreads();
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    l[rt] = sum_groups(l[rt]);
-    if (g == 0) {
-      ml[(wave * 2) * ROWS + rt * 16 + c] = m[rt] == neg_inf() ? neg_inf() : mc[rt];
-      ml[(wave * 2 + 1) * ROWS + rt * 16 + c] = l[rt];
-    }
+  col[0].l = sum_groups(col[0].l);
+  if (g == 0) {
+    ml[wave][0][c] = col[0].m == neg_inf() ? neg_inf() : col[0].mc;
+    ml[wave][1][c] = col[0].l;
   }
   __syncthreads();
-  float M[RT], L[RT];
+  float M = neg_inf(), L = 0.0f;
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    M[rt] = neg_inf();
+  for (int i = 0; i < 4; ++i) M = fmaxf(M, ml[i][0][c]);
+  const float ref = M == neg_inf() ? 0.0f : M;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) M[rt] = fmaxf(M[rt], ml[(i * 2) * ROWS + rt * 16 + c]);
-    const float ref = M[rt] == neg_inf() ? 0.0f : M[rt];
-    L[rt] = 0.0f;
+  for (int i = 0; i < 4; ++i) L += exp2_fast(ml[i][0][c] - ref) * ml[i][1][c];
+  const float w = col[0].m == neg_inf() ? 0.0f : exp2_fast(col[0].mc - ref);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      L[rt] += exp2_fast(ml[(i * 2) * ROWS + rt * 16 + c] - ref) * ml[(i * 2 + 1) * ROWS + rt * 16 + c];
-    w[rt] = m[rt] == neg_inf() ? 0.0f : exp2_fast(mc[rt] - ref);
-#pragma unroll
-    for (int n = 0; n < NT; ++n) acc[rt][n] *= w[rt];
-  }
-  f32x4_t* box = reinterpret_cast<f32x4_t*>(lds);  // [2][RT * NT][64]
+  for (int n = 0; n < NT; ++n) col[0].acc[n] *= w;
+  f32x4_t* box = reinterpret_cast<f32x4_t*>(lds);  // [2][NT][64]
 #pragma unroll
   for (int half = 2; half >= 1; half >>= 1) {
     if (wave >= half && wave < 2 * half) {
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) box[((wave - half) * RT * NT + rt * NT + n) * 64 + lane] = acc[rt][n];
+      for (int n = 0; n < NT; ++n) box[((wave - half) * NT + n) * 64 + lane] = col[0].acc[n];
     }
     __syncthreads();
     if (wave < half) {
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) acc[rt][n] += box[(wave * RT * NT + rt * NT + n) * 64 + lane];
+      for (int n = 0; n < NT; ++n) col[0].acc[n] += box[(wave * NT + n) * 64 + lane];
     }
     __syncthreads();
   }
-  if (wave) return;
-
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    const int x = it.row0 + rt * 16 + c;
-    if (x >= rows) continue;
-    if (it.chunks == 1) {
-      const int i = x / a.group, h = it.head * a.group + (x - i * a.group);
-      const int64_t row = (int64_t)(it.t0 + i) * a.hkv * a.group + h;
-      const float inv = L[rt] == 0.0f ? 0.0f : 1.0f / L[rt];
-      __bf16* o = reinterpret_cast<__bf16*>(a.out) + row * D + 4 * g;
-      typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const f32x4_t y = acc[rt][n] * inv;
-        *reinterpret_cast<bf16x4_t*>(o + n * 16) = bf16x4_t{(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
-      }
-      if (a.lse && g == 0)
-        a.lse[row] = L[rt] == 0.0f ? neg_inf() : (M[rt] + __builtin_amdgcn_logf(L[rt])) * kLn2;
-    } else {
-      const int64_t at = (int64_t)blockIdx.x * ROWS + rt * 16 + c;
-      f32x4_t* o = reinterpret_cast<f32x4_t*>(a.part_o + at * D) + g;
-#pragma unroll
-      for (int n = 0; n < NT; ++n) o[n * 4] = acc[rt][n];
-      if (g == 0) a.part_ml[at] = float2{M[rt], L[rt]};
-    }
-  }
+  if (wave == 0) col[0].store(a, it, it.row0 + c, ROWS, M, L);
 }
 
-// Joins the chunks of a tile: one block for each item and 4 of its rows (only
-// the items that are a tile's first chunk of several do anything), a wave a
-// row.
+// ---------------------------------------------------------------------------
+// Many rows a tile: each wave holds 32 rows, all four share the keys, 64 at a
+// time. The block decodes them once into LDS (two buffers, one barrier a step):
+// the decoding and the cache's bytes are spent once for all rows, and what is
+// left is bound by the matrix products and the exponentials. With 64 rows a
+// tile (WR = 2) two waves share their rows and take half of a step's keys each.
+//
+// 32 x 32 products: one occupies the matrix pipe for 32 cycles and the issue
+// port for few, so up to six other instructions run beside it (16 x 16 ones
+// leave room for two); measured with both in a loop of its own.
+// ---------------------------------------------------------------------------
+
+// 32 rows: lane (r = lane % 32, h = lane / 32) holds row r's maximum and sum as
+// a Column does and the outputs 32 n + 8 (i / 4) + 4 h + i % 4.
+template <int D>
+struct Wide {
+  f32x16_t acc[D / 32];
+  float m, mc, l;
+  int s, e;
+  bool row;
+
+  __device__ __forceinline__ void init(const Attn4Args& a, const Item& it, int x, bf16x8_t (&q)[D / 16]) {
+    m = neg_inf();
+    mc = l = 0.0f;
+#pragma unroll
+    for (int n = 0; n < D / 32; ++n) acc[n] = f32x16_t{};
+    s = e = 0;
+    row = x < it.rows;
+    if (row) {
+      const int i = x / a.group, head = it.head * a.group + (x - i * a.group), h = (threadIdx.x & 63) >> 5;
+      const uint16_t* p = a.q + (int64_t)(it.t0 + i) * a.q_stride + (int64_t)head * D + h * 8;
+#pragma unroll
+      for (int n = 0; n < D / 16; ++n) q[n] = *reinterpret_cast<const bf16x8_t*>(p + n * 16);
+      const RowRange rr = token_range(a, it, i);
+      s = rr.s;
+      e = rr.e;
+    } else {
+#pragma unroll
+      for (int n = 0; n < D / 16; ++n) q[n] = bf16x8_t{};
+    }
+  }
+
+  // The scores of 32 * KT keys from place j0 on become weights; see Column::weigh.
+  template <int KT, bool LIST>
+  __device__ __forceinline__ void mask(f32x16_t (&x)[KT], uint64_t valid, int j0) const {
+    const int h = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int u = 0; u < KT; ++u) {
+      const uint32_t bits = (uint32_t)(valid >> (32 * u)) >> (4 * h);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int kk = 8 * (i / 4) + i % 4, j = j0 + 32 * u + kk + 4 * h;
+        bool v = (bits >> kk) & 1u;
+        if constexpr (!LIST) v = v && j >= s && j < e;
+        x[u][i] = v ? x[u][i] : neg_inf();
+      }
+    }
+  }
+  template <int KT>
+  __device__ __forceinline__ void renew(const f32x16_t (&x)[KT], float sc, float slack) {
+    float top = x[0][0];
+#pragma unroll
+    for (int u = 0; u < KT; ++u)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, x[u][i]);
+    if (__any(top > m + slack)) {
+      const float mn = fmaxf(m, fmaxf(top, __shfl_xor(top, 32)));
+      const float nc = mn == neg_inf() ? 0.0f : mn * sc;
+      const float f = m == neg_inf() ? 0.0f : exp2_fast(mc - nc);
+      m = mn;
+      mc = nc;
+      l *= f;
+#pragma unroll
+      for (int n = 0; n < D / 32; ++n) acc[n] *= f;
+    }
+  }
+  // weights of half a tile (16 keys): values 8 u .. 8 u + 7 of x
+  __device__ __forceinline__ bf16x8_t weights(const f32x16_t& x, int u, float sc) {
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = exp2_fast(fmaf(x[8 * u + i], sc, -mc));
+    l += ((y[0] + y[1]) + (y[2] + y[3])) + ((y[4] + y[5]) + (y[6] + y[7]));
+    return bf16x8_t{(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3],
+                    (__bf16)y[4], (__bf16)y[5], (__bf16)y[6], (__bf16)y[7]};
+  }
+
+  // Values that are not finite, into the rows that see them: bad has the bit 4 k + quarter for each of 16 keys.
+  template <bool LIST>
+  __device__ __forceinline__ void spoil(uint64_t bad, int j0) {
+    while (bad) {
+      const int from = __ffsll((unsigned long long)bad) - 1;
+      bad &= bad - 1;
+      const int j = j0 + (from >> 2);
+      if (row && (LIST || (j >= s && j < e))) {
+#pragma unroll
+        for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if ((D == 128 ? n : 2 * n + i / 8) == (from & 3)) acc[n][i] += __builtin_nanf("");
+      }
+    }
+  }
+
+  __device__ __forceinline__ void store(const Attn4Args& a, const Item& it, int x, int rows_per_tile, float M,
+                                        float L) const {
+    if (!row) return;
+    const int h = (threadIdx.x & 63) >> 5;
+    if (it.chunks == 1) {
+      const int i = x / a.group, head = it.head * a.group + (x - i * a.group);
+      const int64_t at = (int64_t)(it.t0 + i) * a.hkv * a.group + head;
+      const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+      __bf16* o = reinterpret_cast<__bf16*>(a.out) + at * D + 4 * h;
+#pragma unroll
+      for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+          *reinterpret_cast<bf16x4_t*>(o + n * 32 + b * 8) =
+              bf16x4_t{(__bf16)(acc[n][4 * b] * inv), (__bf16)(acc[n][4 * b + 1] * inv),
+                       (__bf16)(acc[n][4 * b + 2] * inv), (__bf16)(acc[n][4 * b + 3] * inv)};
+      if (a.lse && h == 0) a.lse[at] = L == 0.0f ? neg_inf() : (M + __builtin_amdgcn_logf(L)) * kLn2;
+    } else {
+      const int64_t at = (int64_t)it.item * rows_per_tile + (x - it.row0);
+      float* o = a.part_o + at * D + 4 * h;
+#pragma unroll
+      for (int n = 0; n < D / 32; ++n)
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+          *reinterpret_cast<f32x4_t*>(o + n * 32 + b * 8) =
+              f32x4_t{acc[n][4 * b], acc[n][4 * b + 1], acc[n][4 * b + 2], acc[n][4 * b + 3]};
+      if (h == 0) a.part_ml[at] = float2{M, L};
+    }
+  }
+};
+
+// Decoded values in LDS: rows of 2 D bytes whose 16-byte chunks are permuted by
+// the key, chunk ^ swizzle(key). Sixteen lanes that write a chunk of four keys'
+// quarters, and 32 that read 64 bytes of four keys, then meet every bank once.
+template <int D>
+__device__ __forceinline__ int swizzle(int key) {
+  return D == 128 ? 5 * (key & 3) : 5 * ((key >> 1) & 1);
+}
+
+template <int D, int WR, bool LIST>
+__global__ __launch_bounds__(256, 2) void k_attn4_many(Attn4Args a) {
+  constexpr int ROWS = 32 * WR, NK = D / 16, NV = D / 32, KEYS = 64, KT = WR / 2;
+  constexpr int kBuf = KEYS * (kKRow<D> + 2 * D);
+  extern __shared__ __align__(16) uint8_t lds[];  // two buffers of decoded keys, then values
+  __shared__ uint64_t bad_of[2][4];               // per 16 keys: quarters of values that are not finite
+  __shared__ uint32_t valid_of[2][4];             // per 16 keys: those that count; bit 16: bad_of is not 0
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 31, h = lane >> 5;
+  const int wr = WR == 4 ? wave : wave >> 1, wk = WR == 4 ? 0 : wave & 1;  // the wave's rows, its keys of a step
+  const Item it = find<ROWS, LIST, false>(a, blockIdx.x);
+  clear_padding<D>(a);
+  if (!it.any) return;
+  const Reach reach = tile_reach<ROWS>(a, it);
+  Keys<LIST> keys;
+  keys.init(a, it, reach);
+
+  bf16x8_t q[NK];
+  Wide<D> col;
+  col.init(a, it, it.row0 + wr * 32 + r, q);
+  // of this wave's rows
+  int smin = col.row ? col.s : 0x7FFFFFFF, smax = col.row ? col.s : 0, emin = col.row ? col.e : 0x7FFFFFFF,
+      emax = col.row ? col.e : 0;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    smin = min(smin, __shfl_xor(smin, o));
+    smax = max(smax, __shfl_xor(smax, o));
+    emin = min(emin, __shfl_xor(emin, o));
+    emax = max(emax, __shfl_xor(emax, o));
+  }
+  smin = __builtin_amdgcn_readfirstlane(smin);
+  smax = __builtin_amdgcn_readfirstlane(smax);
+  emin = __builtin_amdgcn_readfirstlane(emin);
+  emax = __builtin_amdgcn_readfirstlane(emax);
+
+  // the loading side: four threads a key
+  const int part = tid & 3, mine = tid >> 2;
+  const int steps = (keys.k1 - keys.k0 + KEYS - 1) / KEYS;
+  const int kw = mine * kKRow<D> + part * (D / 2);
+  const int vw = KEYS * kKRow<D> + mine * 2 * D + ((part * (D / 32)) ^ swizzle<D>(mine)) * 16;
+  KeyRegs<D> kv;
+  int page0, page1, pos1, pos2;
+  auto position = [&](int s) { return s < steps ? keys.position(keys.k0 + s * KEYS + mine) : -1; };
+  {
+    const int p0 = position(0);
+    pos1 = position(1);
+    pos2 = position(2);
+    page0 = keys.page(a, p0);
+    page1 = keys.page(a, pos1);
+    load_key<D>(a, page0, p0, it.head, part, kv);
+  }
+  auto stage = [&](int s, int b) {  // decode step s into buffer b, start loading the next
+    const bool ok = page0 >= 0;
+    const float ks = __uint_as_float(key_byte<D>(kv, part, ok) << 23);
+    uint32_t vb = value_byte<D>(kv, part, ok);
+    const int j0 = keys.k0 + s * KEYS;
+    const uint64_t oks = __ballot(ok);
+    bool whole = oks == ~0ull;
+    if constexpr (!LIST) whole = whole && j0 >= reach.smax && j0 + KEYS <= reach.emin;
+    // a value that is not finite must not reach rows that do not see it
+    const uint64_t bad = __ballot(!whole && vb == 255u);
+    vb = !whole && vb == 255u ? 0u : vb;
+    if (lane == 0) {
+      bad_of[b][wave] = bad;
+      uint64_t v = oks & 0x1111111111111111ull;  // a key's four threads agree
+      v = (v | v >> 3) & 0x0303030303030303ull;
+      v = (v | v >> 6) & 0x000F000F000F000Full;
+      v = (v | v >> 12) & 0x000000FF000000FFull;
+      valid_of[b][wave] = ((uint32_t)(v | v >> 24) & 0xFFFFu) | (bad ? 0x10000u : 0u);
+    }
+    const float vs = __uint_as_float(vb << 23);
+    uint8_t* buf = lds + b * kBuf;
+#pragma unroll
+    for (int n = 0; n < D / 32; ++n) {
+      *reinterpret_cast<bf16x8_t*>(buf + kw + 16 * n) = decode8(kv.k[n], ks);
+      *reinterpret_cast<bf16x8_t*>(buf + (vw ^ (16 * n))) = decode8(kv.v[n], vs);
+    }
+    page0 = page1;
+    load_key<D>(a, page0, pos1, it.head, part, kv);
+    pos1 = pos2;
+    page1 = keys.page(a, pos1);
+    pos2 = position(s + 3);
+  };
+
+  // the reading side: a key's row of 16 dims, and 8 bytes of a value's chunk
+  const int kr = (wk * 32 + r) * kKRow<D> + h * 16;
+  const int vk = 4 * h + ((lane & 15) >> 2);  // key of a lane's transposing read
+  int vr[NV];
+#pragma unroll
+  for (int n = 0; n < NV; ++n)
+    vr[n] = KEYS * kKRow<D> + (wk * 32 + vk) * 2 * D +
+            ((4 * n + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ swizzle<D>(vk)) * 16 + (lane & 1) * 8;
+
+  stage(0, 0);
+  __syncthreads();
+  for (int s = 0; s < steps; ++s) {
+    const int b = s & 1, j0 = keys.k0 + s * KEYS + wk * 32;
+    stage(s + 1, b ^ 1);  // past the last step: keys that do not count
+    if (LIST ? emax > 0 : (j0 < emax && j0 + 32 * KT > smin)) {
+      const uint8_t* buf = lds + b * kBuf;
+      f32x16_t x[KT];
+#pragma unroll
+      for (int u = 0; u < KT; ++u) x[u] = f32x16_t{};
+#pragma unroll
+      for (int n = 0; n < NK; ++n)
+#pragma unroll
+        for (int u = 0; u < KT; ++u) {
+          const bf16x8_t kf = *reinterpret_cast<const bf16x8_t*>(buf + kr + u * 32 * kKRow<D> + n * 32);
+          x[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[n], x[u], 0, 0, 0);
+        }
+      uint64_t valid = 0;
+      uint32_t any_bad = 0;
+#pragma unroll
+      for (int u = 0; u < 2 * KT; ++u) {
+        const uint32_t v = valid_of[b][2 * wk + u];
+        valid |= (uint64_t)(v & 0xFFFFu) << (16 * u);
+        any_bad |= v >> 16;
+      }
+      bool whole = valid == (KT == 1 ? 0xFFFFFFFFull : ~0ull);
+      if constexpr (!LIST) whole = whole && j0 >= smax && j0 + 32 * KT <= emin;
+      if (!whole) {
+        asm volatile("");  // a branch, not selects: most steps need no mask
+        col.template mask<KT, LIST>(x, valid, j0);
+      }
+      col.template renew<KT>(x, a.scale_log2, a.slack);
+#pragma unroll
+      for (int u = 0; u < 2 * KT; ++u) {
+        const bf16x8_t p = col.weights(x[u >> 1], u & 1, a.scale_log2);
+#pragma unroll
+        for (int n = 0; n < NV; ++n) {
+          const uint8_t* v = buf + vr[n] + u * 16 * 2 * D;
+          const s16x4_t v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)v);
+          const s16x4_t v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(v + 8 * 2 * D));
+          const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+          col.acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p, col.acc[n], 0, 0, 0);
+        }
+      }
+      if (any_bad) {
+#pragma unroll 1
+        for (int u = 0; u < 2 * KT; ++u) {
+          const uint64_t bad = bad_of[b][2 * wk + u];
+          col.template spoil<LIST>(bad, j0 + 16 * u);
+        }
+      }
+    }
+    __syncthreads();
+  }
+  float L = col.l + __shfl_xor(col.l, 32), M = col.m == neg_inf() ? neg_inf() : col.mc;
+  if constexpr (WR == 2) {
+    // the two waves of the same rows
+    f32x4_t* box = reinterpret_cast<f32x4_t*>(lds) + wr * (4 * NV * 64 + 32);
+    float2* ml = reinterpret_cast<float2*>(box + 4 * NV * 64);
+    if (wk == 1) {
+#pragma unroll
+      for (int n = 0; n < NV; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          box[(4 * n + i) * 64 + lane] =
+              f32x4_t{col.acc[n][4 * i], col.acc[n][4 * i + 1], col.acc[n][4 * i + 2], col.acc[n][4 * i + 3]};
+      if (h == 0) ml[r] = float2{M, L};
+    }
+    __syncthreads();
+    if (wk == 1) return;
+    const float2 o = ml[r];
+    const float top = fmaxf(M, o.x), ref = top == neg_inf() ? 0.0f : top;
+    const float f0 = exp2_fast(M - ref), f1 = exp2_fast(o.x - ref);
+    M = top;
+    L = L * f0 + o.y * f1;
+#pragma unroll
+    for (int n = 0; n < NV; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        col.acc[n][i] = col.acc[n][i] * f0 + box[(4 * n + i / 4) * 64 + lane][i % 4] * f1;
+  }
+  col.store(a, it, it.row0 + wr * 32 + r, ROWS, M, L);
+}
+
+// Joins the chunks of a tile: a thread takes four outputs of a row, a block
+// 1024 / D rows at a time, eight chunks' loads in flight.
 template <int D, int ROWS, bool LIST>
 __global__ __launch_bounds__(256) void k_attn4_join(Attn4Args a) {
-  const Item it = LIST ? find_list_item<ROWS>(a, blockIdx.x) : find_item<ROWS>(a, blockIdx.x);
-  if (!it.any || it.chunks == 1 || it.chunk != 0) return;
-  const int lane = threadIdx.x & 63, in = blockIdx.y * 4 + (threadIdx.x >> 6), x = it.row0 + in;
-  const int rows = LIST ? min((it.row0 / a.group + 1) * a.group, it.nt * a.group) : it.nt * a.group;
-  if (x >= rows) return;
-  const int64_t at = (int64_t)blockIdx.x * ROWS + in;
-  float M = neg_inf();
-  for (int i = lane; i < it.chunks; i += 64) M = fmaxf(M, a.part_ml[at + (int64_t)i * ROWS].x);
+  constexpr int kRowThreads = D / 4, kAtOnce = 256 / kRowThreads;
+  const Item it = find<ROWS, LIST, true>(a, blockIdx.x);
+  if (!it.any || it.chunks == 1) return;
+  const int c = threadIdx.x % kRowThreads;
+  const int n = min(ROWS, it.rows - it.row0);
+  for (int in = blockIdx.y * kAtOnce + threadIdx.x / kRowThreads; in < n; in += gridDim.y * kAtOnce) {
+    const float2* ml = a.part_ml + (int64_t)it.item * ROWS + in;
+    const f32x4_t* po = reinterpret_cast<const f32x4_t*>(a.part_o + ((int64_t)it.item * ROWS + in) * D) + c;
+    float M = neg_inf(), L = 0.0f;
+    f32x4_t o = {};
+    for (int i0 = 0; i0 < it.chunks; i0 += 8) {
+      float2 w[8];
+      f32x4_t v[8];
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) M = fmaxf(M, __shfl_xor(M, o));
-  const float ref = M == neg_inf() ? 0.0f : M;
-  float L = 0.0f, o0 = 0.0f, o1 = 0.0f;
-  for (int i = 0; i < it.chunks; ++i) {
-    const float2 ml = a.part_ml[at + (int64_t)i * ROWS];
-    const float w = exp2_fast(ml.x - ref);
-    L = fmaf(w, ml.y, L);
-    const float* o = a.part_o + (at + (int64_t)i * ROWS) * D;
-    if (ml.x != neg_inf()) {
-      if constexpr (D == 128) {
-        const float2 v = reinterpret_cast<const float2*>(o)[lane];
-        o0 = fmaf(w, v.x, o0);
-        o1 = fmaf(w, v.y, o1);
-      } else {
-        o0 = fmaf(w, o[lane], o0);
+      for (int u = 0; u < 8; ++u) {
+        const int64_t at = (int64_t)min(i0 + u, it.chunks - 1) * ROWS;
+        w[u] = ml[at];
+        v[u] = po[at * kRowThreads];
+      }
+      float top = M;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) top = fmaxf(top, w[u].x);
+      const float ref = top == neg_inf() ? 0.0f : top, f = exp2_fast(M - ref);
+      M = top;
+      L *= f;
+      o *= f;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const float g = i0 + u < it.chunks ? exp2_fast(w[u].x - ref) : 0.0f;
+        if (i0 + u < it.chunks) {
+          L = fmaf(g, w[u].y, L);
+          o += g * v[u];
+        }
       }
     }
+    const int x = it.row0 + in, i = x / a.group, h = it.head * a.group + (x - i * a.group);
+    const int64_t row = (int64_t)(it.t0 + i) * a.hkv * a.group + h;
+    const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+    o *= inv;
+    reinterpret_cast<bf16x4_t*>(reinterpret_cast<__bf16*>(a.out) + row * D)[c] =
+        bf16x4_t{(__bf16)o[0], (__bf16)o[1], (__bf16)o[2], (__bf16)o[3]};
+    if (a.lse && c == 0) a.lse[row] = L == 0.0f ? neg_inf() : (M + __builtin_amdgcn_logf(L)) * kLn2;
   }
-  const int i = x / a.group, h = it.head * a.group + (x - i * a.group);
-  const int64_t row = (int64_t)(it.t0 + i) * a.hkv * a.group + h;
-  const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-  __bf16* out = reinterpret_cast<__bf16*>(a.out) + row * D;
-  if constexpr (D == 128) {
-    typedef __bf16 pair __attribute__((ext_vector_type(2)));
-    reinterpret_cast<pair*>(out)[lane] = pair{(__bf16)(o0 * inv), (__bf16)(o1 * inv)};
-  } else {
-    out[lane] = (__bf16)(o0 * inv);
-  }
-  if (a.lse && lane == 0) a.lse[row] = L == 0.0f ? neg_inf() : (M + __builtin_amdgcn_logf(L)) * kLn2;
 }
 
-template <int D, int RT, bool LIST>
-hipError_t run_few(Attn4Args a, hipStream_t st) {
-  constexpr int ROWS = 16 * RT;
-  constexpr int stage = 4 * 32 * kVRow<D>, box = 2 * RT * (D / 16) * 64 * 16;
-  a.lds_join = stage > box ? stage : box;
-  const size_t lds = (size_t)a.lds_join + 4 * 2 * ROWS * 4;
-  if (lds > 64 * 1024) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_attn4_few<D, RT, LIST>),
-                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-    if (e != hipSuccess) return e;
-  }
+template <int D, int ROWS, bool LIST>
+hipError_t run(const Attn4Args& a, hipStream_t st) {
   if (!LIST && a.R > kInlineRequests) k_attn4_schedule<ROWS><<<1, 1024, 0, st>>>(a);
-  k_attn4_few<D, RT, LIST><<<dim3((unsigned)a.items), 256, lds, st>>>(a);
-  if (a.split) k_attn4_join<D, ROWS, LIST><<<dim3((unsigned)a.items, ROWS / 4), 256, 0, st>>>(a);
+  const dim3 grid((unsigned)a.items);
+  if constexpr (ROWS == 16) {
+    k_attn4_few<D, LIST><<<grid, 256, 0, st>>>(a);
+  } else {
+    constexpr int WR = ROWS / 32;
+    constexpr size_t lds = 2 * 64 * (kKRow<D> + 2 * D);
+    if (lds > 64 * 1024) {
+      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_attn4_many<D, WR, LIST>),
+                                               hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+      if (e != hipSuccess) return e;
+    }
+    k_attn4_many<D, WR, LIST><<<grid, 256, lds, st>>>(a);
+  }
+  if (a.split) k_attn4_join<D, ROWS, LIST><<<dim3((unsigned)a.tiles, ROWS == 16 ? 2 : ROWS / 32), 256, 0, st>>>(a);
   return hipGetLastError();
 }
 
 template <int D, bool LIST>
-hipError_t run_rt(const Attn4Args& a, hipStream_t st) {
-  if (a.rt == 1) return run_few<D, 1, LIST>(a, st);
-  if (a.rt == 2) return run_few<D, 2, LIST>(a, st);
-  return run_few<D, 4, LIST>(a, st);
+hipError_t run_rows(const Attn4Args& a, hipStream_t st) {
+  if (a.rows_per_tile == 16) return run<D, 16, LIST>(a, st);
+  if (a.rows_per_tile == 64) return run<D, 64, LIST>(a, st);
+  return run<D, 128, LIST>(a, st);
 }
 
-constexpr int kTargetItems = 1024;
+constexpr int kTargetItems = 1024, kTargetFew = 2048, kTargetMany = 2048;
 
 // Shape of the launch: everything that depends on host values alone.
 bool shape_of(Attn4Args& a) {
   const int64_t rows = a.list_k > 0 ? a.group : ((int64_t)a.T * a.group + a.R - 1) / (a.R > 0 ? a.R : 1);
-  a.rt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-  const int ROWS = 16 * a.rt;
-  int64_t items;
+  a.rows_per_tile = rows <= 16 ? 16 : rows <= 64 ? 64 : 128;
   if (a.list_k > 0) {
-    a.row_tiles = (a.group + ROWS - 1) / ROWS;
-    const int64_t tiles = (int64_t)a.T * a.hkv * a.row_tiles;
+    // few tokens: narrow tiles rather than many chunks
+    if ((int64_t)a.T * a.hkv < 256) a.rows_per_tile = 16;
+    const int R = a.rows_per_tile;
+    a.row_tiles = (a.group + R - 1) / R;
+    a.tiles = (int64_t)a.T * a.hkv * a.row_tiles;
     const int64_t most = (a.list_k + kMinChunk - 1) / kMinChunk;
-    int64_t n = (kTargetItems + tiles - 1) / tiles;
+    int64_t n = a.tiles >= kTargetItems / 4 ? 1 : kTargetItems / 2 / a.tiles;
     n = n < 1 ? 1 : n > most ? most : n;
-    a.chunk_keys = (int)(((a.list_k + n - 1) / n + 31) / 32 * 32);
+    a.chunk_keys = (int)(((a.list_k + n - 1) / n + 63) / 64 * 64);
     a.chunks = (a.list_k + a.chunk_keys - 1) / a.chunk_keys;
     a.split = a.chunks > 1;
     a.target = 0;
-    items = tiles * a.chunks;
+    a.items = a.tiles * a.chunks;
   } else {
-    const int64_t tiles = (int64_t)a.hkv * (((int64_t)a.T * a.group + ROWS - 1) / ROWS + a.R);
+    const int R = a.rows_per_tile;
+    a.tiles = (int64_t)a.hkv * (((int64_t)a.T * a.group + R - 1) / R + a.R);
     a.split = (int64_t)a.T * a.group * a.hkv <= 131072;
-    a.target = a.split ? kTargetItems : 0;
-    items = tiles + a.target;
+    a.target = a.split ? (a.rows_per_tile == 16 ? kTargetFew : kTargetMany) : 0;
+    a.items = a.tiles + a.target;
   }
-  a.items = items;
-  return items <= 0x3FFFFFFF;
+  return a.items <= 0x3FFFFFFF;
 }
 
 }  // namespace
 
 size_t attn4_workspace_bytes(Attn4Args a) {
   if (!shape_of(a)) return 0;
-  size_t n = 256 + (((size_t)a.R + 2) * 4 + 255) / 256 * 256;
-  if (a.split) n += (size_t)a.items * 16 * a.rt * ((size_t)a.d * 4 + 8);
+  size_t n = 256 + ((2 * (size_t)a.R + 3) * 4 + 255) / 256 * 256;
+  if (a.split) n += (size_t)a.items * a.rows_per_tile * ((size_t)a.d * 4 + 8);
   return n;
 }
 
@@ -732,13 +1097,13 @@ hipError_t launch_attn4(Attn4Args a, void* workspace, hipStream_t st) {
   if (!shape_of(a)) return hipErrorInvalidValue;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   a.sched = reinterpret_cast<uint32_t*>(ws);
-  ws += (((size_t)a.R + 2) * 4 + 255) / 256 * 256;
+  ws += ((2 * (size_t)a.R + 3) * 4 + 255) / 256 * 256;
   a.part_o = reinterpret_cast<float*>(ws);
-  a.part_ml = reinterpret_cast<float2*>(ws + (a.split ? (size_t)a.items * 16 * a.rt * a.d * 4 : 0));
+  a.part_ml = reinterpret_cast<float2*>(ws + (a.split ? (size_t)a.items * a.rows_per_tile * a.d * 4 : 0));
   a.slack = 8.0f / a.scale_log2;
   if (!(a.slack < 1e30f)) a.slack = 1e30f;
-  if (a.list_k > 0) return a.d == 128 ? run_rt<128, true>(a, st) : run_rt<64, true>(a, st);
-  return a.d == 128 ? run_rt<128, false>(a, st) : run_rt<64, false>(a, st);
+  if (a.list_k > 0) return a.d == 128 ? run_rows<128, true>(a, st) : run_rows<64, true>(a, st);
+  return a.d == 128 ? run_rows<128, false>(a, st) : run_rows<64, false>(a, st);
 }
 
 }  // namespace lt

@@ -247,8 +247,8 @@ struct Attn4Args {
   float* lse;
   // resolved by launch_attn4
   float slack;
-  int rt, row_tiles, chunks, chunk_keys, target, lds_join;
-  int64_t items;
+  int rows_per_tile, row_tiles, chunks, chunk_keys, target;
+  int64_t tiles, items;
   bool split;
   uint32_t* sched;
   float* part_o;
