@@ -41,7 +41,7 @@ __device__ __forceinline__ uint32_t lane_bcast(uint32_t v, int lane) {
 // ---------------------------------------------------------------------------
 // Schedule. Request r has tiles_r = heads * ceil(rows_r / ROWS) tiles over
 // about span_r keys; with a chunk length C it makes tiles_r * ceil(span_r / C)
-// items, and C = sum tiles_r * span_r / target keeps the items within
+// items, and C >= sum tiles_r * span_r / target keeps the items within
 // target + tiles. span_r only balances: a tile's last chunk takes what is left.
 // ---------------------------------------------------------------------------
 // Keys of a request; positions and steps past them stay within 31 bits.
@@ -85,10 +85,20 @@ __device__ __forceinline__ uint32_t wave_prefix(uint32_t v) {  // inclusive
   return v;
 }
 
-__device__ __forceinline__ uint32_t chunk_len(uint64_t work, int target) {
-  const uint64_t c = (work + target - 1) / target;
-  const uint64_t r = (c + kMinChunk - 1) / kMinChunk * kMinChunk;
-  return r < kMinChunk ? kMinChunk : r > 0x40000000u ? 0x40000000u : (uint32_t)r;
+// As many items as blocks are resident at once (kSlots), and where that makes
+// chunks longer than kFullChunk, up to kTarget: then the last blocks to finish
+// keep the GPU busy for a shorter time, and a chunk's own start is small
+// beside its keys.
+template <int ROWS>
+constexpr int kSlots = ROWS == 16 ? 768 : 512;
+constexpr int kTarget = 2048, kFullChunk = 1024;
+
+template <int ROWS>
+__device__ __forceinline__ uint32_t chunk_len(uint64_t work) {
+  const uint64_t few = (work + kSlots<ROWS> - 1) / kSlots<ROWS>, many = (work + kTarget - 1) / kTarget;
+  uint64_t c = max(many, min(few, (uint64_t)kFullChunk));
+  c = (c + kMinChunk - 1) / kMinChunk * kMinChunk;
+  return c < kMinChunk ? kMinChunk : c > 0x40000000u ? 0x40000000u : (uint32_t)c;
 }
 
 struct Item {
@@ -117,7 +127,7 @@ __global__ __launch_bounds__(1024) void k_attn4_schedule(Attn4Args a) {
   __syncthreads();
   work = 0;
   for (int i = 0; i < 16; ++i) work += sum[i];
-  const uint32_t C = a.target > 0 ? chunk_len(work, a.target) : kNoSplit;
+  const uint32_t C = a.split ? chunk_len<ROWS>(work) : kNoSplit;
   uint32_t base = 0, tbase = 0;
   for (int r0 = 0; r0 < a.R; r0 += 1024) {
     const int r = r0 + t;
@@ -173,7 +183,7 @@ __device__ __forceinline__ Item find_item(const Attn4Args& a, uint32_t id) {
   uint32_t first = 0, tfirst = 0;
   if (a.R <= kInlineRequests) {
     if (lane < a.R) q = load_req<ROWS>(a, lane);
-    it.C = a.target > 0 ? chunk_len(wave_sum64((uint64_t)q.tiles * q.span), a.target) : kNoSplit;
+    it.C = a.split ? chunk_len<ROWS>(wave_sum64((uint64_t)q.tiles * q.span)) : kNoSplit;
     const uint32_t n = lane < a.R ? (uint32_t)q.tiles * ((q.span + it.C - 1) / it.C) : 0u;
     const uint32_t in = wave_prefix(n), tin = TILE ? wave_prefix((uint32_t)q.tiles) : 0u;
     const uint64_t hit = __ballot((TILE ? tin : in) > id);
@@ -802,6 +812,11 @@ __device__ __forceinline__ int swizzle(int key) {
   return D == 128 ? 5 * (key & 3) : 5 * ((key >> 1) & 1);
 }
 
+template <int N>
+struct Int {
+  static constexpr int value = N;
+};
+
 template <int D, int WR, bool LIST>
 __global__ __launch_bounds__(256, 2) void k_attn4_many(Attn4Args a) {
   constexpr int ROWS = 32 * WR, NK = D / 16, NV = D / 32, KEYS = 64, KT = WR / 2;
@@ -841,19 +856,24 @@ __global__ __launch_bounds__(256, 2) void k_attn4_many(Attn4Args a) {
   const int steps = (keys.k1 - keys.k0 + KEYS - 1) / KEYS;
   const int kw = mine * kKRow<D> + part * (D / 2);
   const int vw = KEYS * kKRow<D> + mine * 2 * D + ((part * (D / 32)) ^ swizzle<D>(mine)) * 16;
-  KeyRegs<D> kv;
-  int page0, page1, pos1, pos2;
+  // in flight: the codes of two steps, the pages of a third, the places of a fourth
+  KeyRegs<D> kvs[2];
+  int page[2], page2, pos2, pos3;
   auto position = [&](int s) { return s < steps ? keys.position(keys.k0 + s * KEYS + mine) : -1; };
   {
-    const int p0 = position(0);
-    pos1 = position(1);
+    const int p0 = position(0), p1 = position(1);
     pos2 = position(2);
-    page0 = keys.page(a, p0);
-    page1 = keys.page(a, pos1);
-    load_key<D>(a, page0, p0, it.head, part, kv);
+    pos3 = position(3);
+    page[0] = keys.page(a, p0);
+    page[1] = keys.page(a, p1);
+    page2 = keys.page(a, pos2);
+    load_key<D>(a, page[0], p0, it.head, part, kvs[0]);
+    load_key<D>(a, page[1], p1, it.head, part, kvs[1]);
   }
-  auto stage = [&](int s, int b) {  // decode step s into buffer b, start loading the next
-    const bool ok = page0 >= 0;
+  auto stage = [&](int s, auto bc) {  // decode step s into buffer b, start loading step s + 2
+    constexpr int b = decltype(bc)::value;
+    KeyRegs<D>& kv = kvs[b];
+    const bool ok = page[b] >= 0;
     const float ks = __uint_as_float(key_byte<D>(kv, part, ok) << 23);
     uint32_t vb = value_byte<D>(kv, part, ok);
     const int j0 = keys.k0 + s * KEYS;
@@ -878,11 +898,11 @@ __global__ __launch_bounds__(256, 2) void k_attn4_many(Attn4Args a) {
       *reinterpret_cast<bf16x8_t*>(buf + kw + 16 * n) = decode8(kv.k[n], ks);
       *reinterpret_cast<bf16x8_t*>(buf + (vw ^ (16 * n))) = decode8(kv.v[n], vs);
     }
-    page0 = page1;
-    load_key<D>(a, page0, pos1, it.head, part, kv);
-    pos1 = pos2;
-    page1 = keys.page(a, pos1);
-    pos2 = position(s + 3);
+    page[b] = page2;
+    load_key<D>(a, page2, pos2, it.head, part, kv);
+    pos2 = pos3;
+    page2 = keys.page(a, pos2);
+    pos3 = position(s + 4);
   };
 
   // the reading side: a key's row of 16 dims, and 8 bytes of a value's chunk
@@ -894,11 +914,10 @@ __global__ __launch_bounds__(256, 2) void k_attn4_many(Attn4Args a) {
     vr[n] = KEYS * kKRow<D> + (wk * 32 + vk) * 2 * D +
             ((4 * n + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ swizzle<D>(vk)) * 16 + (lane & 1) * 8;
 
-  stage(0, 0);
-  __syncthreads();
-  for (int s = 0; s < steps; ++s) {
-    const int b = s & 1, j0 = keys.k0 + s * KEYS + wk * 32;
-    stage(s + 1, b ^ 1);  // past the last step: keys that do not count
+  auto work = [&](int s, auto bc) {
+    constexpr int b = decltype(bc)::value;
+    const int j0 = keys.k0 + s * KEYS + wk * 32;
+    stage(s + 1, Int<b ^ 1>{});  // past the last step: keys that do not count
     if (LIST ? emax > 0 : (j0 < emax && j0 + 32 * KT > smin)) {
       const uint8_t* buf = lds + b * kBuf;
       f32x16_t x[KT];
@@ -947,6 +966,12 @@ __global__ __launch_bounds__(256, 2) void k_attn4_many(Attn4Args a) {
       }
     }
     __syncthreads();
+  };
+  stage(0, Int<0>{});
+  __syncthreads();
+  for (int s = 0; s < steps; s += 2) {
+    work(s, Int<0>{});
+    if (s + 1 < steps) work(s + 1, Int<1>{});
   }
   float L = col.l + __shfl_xor(col.l, 32), M = col.m == neg_inf() ? neg_inf() : col.mc;
   if constexpr (WR == 2) {
@@ -1054,8 +1079,6 @@ hipError_t run_rows(const Attn4Args& a, hipStream_t st) {
   return run<D, 128, LIST>(a, st);
 }
 
-constexpr int kTargetItems = 1024, kTargetFew = 2048, kTargetMany = 2048;
-
 // Shape of the launch: everything that depends on host values alone.
 bool shape_of(Attn4Args& a) {
   const int64_t rows = a.list_k > 0 ? a.group : ((int64_t)a.T * a.group + a.R - 1) / (a.R > 0 ? a.R : 1);
@@ -1067,19 +1090,17 @@ bool shape_of(Attn4Args& a) {
     a.row_tiles = (a.group + R - 1) / R;
     a.tiles = (int64_t)a.T * a.hkv * a.row_tiles;
     const int64_t most = (a.list_k + kMinChunk - 1) / kMinChunk;
-    int64_t n = a.tiles >= kTargetItems / 4 ? 1 : kTargetItems / 2 / a.tiles;
+    int64_t n = a.tiles >= 256 ? 1 : 512 / a.tiles;
     n = n < 1 ? 1 : n > most ? most : n;
     a.chunk_keys = (int)(((a.list_k + n - 1) / n + 63) / 64 * 64);
     a.chunks = (a.list_k + a.chunk_keys - 1) / a.chunk_keys;
     a.split = a.chunks > 1;
-    a.target = 0;
     a.items = a.tiles * a.chunks;
   } else {
     const int R = a.rows_per_tile;
     a.tiles = (int64_t)a.hkv * (((int64_t)a.T * a.group + R - 1) / R + a.R);
     a.split = (int64_t)a.T * a.group * a.hkv <= 131072;
-    a.target = a.split ? (a.rows_per_tile == 16 ? kTargetFew : kTargetMany) : 0;
-    a.items = a.tiles + a.target;
+    a.items = a.tiles + (a.split ? kTarget : 0);
   }
   return a.items <= 0x3FFFFFFF;
 }

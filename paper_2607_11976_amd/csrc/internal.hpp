@@ -247,7 +247,7 @@ struct Attn4Args {
   float* lse;
   // resolved by launch_attn4
   float slack;
-  int rows_per_tile, row_tiles, chunks, chunk_keys, target;
+  int rows_per_tile, row_tiles, chunks, chunk_keys;
   int64_t tiles, items;
   bool split;
   uint32_t* sched;
