@@ -739,6 +739,7 @@ int lt_cache4_attention(const void* q, int64_t q_stride, int32_t tokens, int32_t
   a.table = block_table;
   a.table_ld = table_ld;
   a.table_width = table_width;
+  if (table_width == 0) a.table = cu_tokens, a.table_ld = 0;  // read, never used
   a.shift = c.shift;
   a.cu = cu_tokens;
   a.seq = seq_lens;

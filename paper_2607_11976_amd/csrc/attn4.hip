@@ -31,6 +31,7 @@ constexpr int kInlineRequests = 64;  // requests that a wave schedules by itself
 constexpr int kMinChunk = 128;       // shortest chunk
 constexpr uint32_t kNoSplit = 0x80000000u;  // chunk length that no request reaches
 
+__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
 __device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -183,7 +184,8 @@ __device__ __forceinline__ Item find_item(const Attn4Args& a, uint32_t id) {
   uint32_t first = 0, tfirst = 0;
   if (a.R <= kInlineRequests) {
     if (lane < a.R) q = load_req<ROWS>(a, lane);
-    it.C = a.split ? chunk_len<ROWS>(wave_sum64((uint64_t)q.tiles * q.span)) : kNoSplit;
+    it.C = __builtin_amdgcn_readfirstlane(
+        a.split ? chunk_len<ROWS>(wave_sum64((uint64_t)q.tiles * q.span)) : kNoSplit);
     const uint32_t n = lane < a.R ? (uint32_t)q.tiles * ((q.span + it.C - 1) / it.C) : 0u;
     const uint32_t in = wave_prefix(n), tin = TILE ? wave_prefix((uint32_t)q.tiles) : 0u;
     const uint64_t hit = __ballot((TILE ? tin : in) > id);
@@ -326,21 +328,27 @@ struct Keys {
       k1 = it.chunk == it.chunks - 1 ? hi : (int)min((int64_t)k0 + it.C, (int64_t)hi);
     }
   }
+  // Each lookup in two halves, so that a loop can keep its load in flight: the
+  // load, at some entry that there is, and what its result says.
+  __device__ __forceinline__ int fetch(const Attn4Args& a, int j) const {
+    if constexpr (LIST) return list[min(j, a.list_k - 1)];
+    else return 0;
+  }
   // the position of place j, or -1
-  __device__ __forceinline__ int position(int j) const {
+  __device__ __forceinline__ int position(int j, int raw) const {
     if constexpr (LIST) {
-      if (j >= k1) return -1;
-      const int64_t p = (int64_t)list[j] - base;
-      return p >= lo && p < hi ? (int)p : -1;
+      const int64_t p = (int64_t)raw - base;
+      return ((j < k1) & (p >= lo) & (p < hi)) ? (int)p : -1;
     } else {
       return j < k1 ? j : -1;
     }
   }
+  __device__ __forceinline__ int look(const Attn4Args& a, int pos) const {
+    return table[min(max(pos, 0) >> a.shift, max(a.table_width - 1, 0))];
+  }
   // its page, or -1
-  __device__ __forceinline__ int page(const Attn4Args& a, int pos) const {
-    const int b = pos >> a.shift;
-    const int p = pos >= 0 && b < a.table_width ? table[b] : -1;
-    return p < a.num_pages ? p : -1;
+  __device__ __forceinline__ int page(const Attn4Args& a, int pos, int raw) const {
+    return ((pos >= 0) & ((pos >> a.shift) < a.table_width) & (raw < a.num_pages)) ? max(raw, -1) : -1;
   }
 };
 
@@ -560,7 +568,7 @@ __global__ __launch_bounds__(256, 3) void k_attn4_few(Attn4Args a) {
   constexpr int ROWS = 16, NI = D / 32, NT = D / 16;
   __shared__ __align__(16) uint8_t lds[4 * 32 * kVRow<D>];
   __shared__ float ml[4][2][ROWS];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = wave_id(), c = lane & 15, g = lane >> 4;
   const Item it = find<ROWS, LIST, false>(a, blockIdx.x);
   clear_padding<D>(a);
   if (!it.any) return;
@@ -575,23 +583,28 @@ __global__ __launch_bounds__(256, 3) void k_attn4_few(Attn4Args a) {
   uint8_t* vrows = lds + wave * 32 * kVRow<D>;
   const int steps = (keys.k1 - keys.k0 + 31) / 32;
 
-  // software pipeline: codes one step ahead, pages two, list entries three
+  // in flight: the codes of the next step, the pages of the one after, the places of a third
   KeyRegs<D> kv[2];
-  int page0[2], page1[2], pos1[2], pos2[2];
-  auto positions = [&](int s, int (&p)[2]) {
-    const int j = keys.k0 + s * 32 + c;
-    p[0] = s < steps ? keys.position(j) : -1;
-    p[1] = s < steps ? keys.position(j + 16) : -1;
-  };
+  int page0[2], pos1[2], raw1[2], raw2[2];
+  auto at_step = [&](int s, int u) { return keys.k0 + s * 32 + u * 16 + c; };
   {
-    int p0[2];
-    positions(wave, p0);
-    positions(wave + 4, pos1);
-    positions(wave + 8, pos2);
+    int p0[2], r0[2], r1[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      page0[u] = keys.page(a, p0[u]);
-      page1[u] = keys.page(a, pos1[u]);
+      r0[u] = keys.fetch(a, at_step(wave, u));
+      r1[u] = keys.fetch(a, at_step(wave + 4, u));
+      raw2[u] = keys.fetch(a, at_step(wave + 8, u));
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      p0[u] = keys.position(at_step(wave, u), r0[u]);
+      pos1[u] = keys.position(at_step(wave + 4, u), r1[u]);
+      r0[u] = keys.look(a, p0[u]);
+      raw1[u] = keys.look(a, pos1[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      page0[u] = keys.page(a, p0[u], r0[u]);
       load_key<D>(a, page0[u], p0[u], it.head, g, kv[u]);
     }
   }
@@ -619,14 +632,18 @@ __global__ __launch_bounds__(256, 3) void k_attn4_few(Attn4Args a) {
         *reinterpret_cast<bf16x8_t*>(w + 16 * n) = decode8(kv[u].v[n], vs);
       }
     }
+    // loads come back in order: pages and places first, codes last
+    int at[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      page0[u] = page1[u];
-      load_key<D>(a, page0[u], pos1[u], it.head, g, kv[u]);
-      pos1[u] = pos2[u];
-      page1[u] = keys.page(a, pos1[u]);
+      page0[u] = keys.page(a, pos1[u], raw1[u]);
+      at[u] = pos1[u];
+      pos1[u] = keys.position(at_step(s + 8, u), raw2[u]);
+      raw1[u] = keys.look(a, pos1[u]);
+      raw2[u] = keys.fetch(a, at_step(s + 12, u));
     }
-    positions(s + 12, pos2);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) load_key<D>(a, page0[u], at[u], it.head, g, kv[u]);
     bf16x8_t p[1];
     col[0].template weigh<2, LIST>(x, whole, valid, j0, a.scale_log2, a.slack, p);
     __builtin_amdgcn_wave_barrier();
@@ -824,7 +841,7 @@ __global__ __launch_bounds__(256, 2) void k_attn4_many(Attn4Args a) {
   extern __shared__ __align__(16) uint8_t lds[];  // two buffers of decoded keys, then values
   __shared__ uint64_t bad_of[2][4];               // per 16 keys: quarters of values that are not finite
   __shared__ uint32_t valid_of[2][4];             // per 16 keys: those that count; bit 16: bad_of is not 0
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 31, h = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, wave = wave_id(), r = lane & 31, h = lane >> 5;
   const int wr = WR == 4 ? wave : wave >> 1, wk = WR == 4 ? 0 : wave & 1;  // the wave's rows, its keys of a step
   const Item it = find<ROWS, LIST, false>(a, blockIdx.x);
   clear_padding<D>(a);
@@ -836,20 +853,15 @@ __global__ __launch_bounds__(256, 2) void k_attn4_many(Attn4Args a) {
   bf16x8_t q[NK];
   Wide<D> col;
   col.init(a, it, it.row0 + wr * 32 + r, q);
-  // of this wave's rows
-  int smin = col.row ? col.s : 0x7FFFFFFF, smax = col.row ? col.s : 0, emin = col.row ? col.e : 0x7FFFFFFF,
-      emax = col.row ? col.e : 0;
+  // what all of this wave's rows see
+  int smax = col.row ? col.s : 0, emin = col.row ? col.e : 0x7FFFFFFF;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    smin = min(smin, __shfl_xor(smin, o));
     smax = max(smax, __shfl_xor(smax, o));
     emin = min(emin, __shfl_xor(emin, o));
-    emax = max(emax, __shfl_xor(emax, o));
   }
-  smin = __builtin_amdgcn_readfirstlane(smin);
   smax = __builtin_amdgcn_readfirstlane(smax);
   emin = __builtin_amdgcn_readfirstlane(emin);
-  emax = __builtin_amdgcn_readfirstlane(emax);
 
   // the loading side: four threads a key
   const int part = tid & 3, mine = tid >> 2;
@@ -858,39 +870,52 @@ __global__ __launch_bounds__(256, 2) void k_attn4_many(Attn4Args a) {
   const int vw = KEYS * kKRow<D> + mine * 2 * D + ((part * (D / 32)) ^ swizzle<D>(mine)) * 16;
   // in flight: the codes of two steps, the pages of a third, the places of a fourth
   KeyRegs<D> kvs[2];
-  int page[2], page2, pos2, pos3;
-  auto position = [&](int s) { return s < steps ? keys.position(keys.k0 + s * KEYS + mine) : -1; };
+  int page[2], pos2, raw2, raw3;
+  auto at_step = [&](int s) { return keys.k0 + s * KEYS + mine; };
   {
-    const int p0 = position(0), p1 = position(1);
-    pos2 = position(2);
-    pos3 = position(3);
-    page[0] = keys.page(a, p0);
-    page[1] = keys.page(a, p1);
-    page2 = keys.page(a, pos2);
-    load_key<D>(a, page[0], p0, it.head, part, kvs[0]);
-    load_key<D>(a, page[1], p1, it.head, part, kvs[1]);
+    int p[3], raw[3];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) raw[i] = keys.fetch(a, at_step(i));
+    raw3 = keys.fetch(a, at_step(3));
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      p[i] = keys.position(at_step(i), raw[i]);
+      raw[i] = keys.look(a, p[i]);
+    }
+    pos2 = p[2];
+    raw2 = raw[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      page[i] = keys.page(a, p[i], raw[i]);
+      load_key<D>(a, page[i], p[i], it.head, part, kvs[i]);
+    }
   }
   auto stage = [&](int s, auto bc) {  // decode step s into buffer b, start loading step s + 2
     constexpr int b = decltype(bc)::value;
     KeyRegs<D>& kv = kvs[b];
+    // loads come back in order: the next page and place are asked for before
+    // the codes, so that waiting for them does not wait for those
+    const int now = keys.page(a, pos2, raw2), at = pos2;
+    pos2 = keys.position(at_step(s + 3), raw3);
+    raw2 = keys.look(a, pos2);
+    raw3 = keys.fetch(a, at_step(s + 4));
     const bool ok = page[b] >= 0;
     const float ks = __uint_as_float(key_byte<D>(kv, part, ok) << 23);
     uint32_t vb = value_byte<D>(kv, part, ok);
     const int j0 = keys.k0 + s * KEYS;
     const uint64_t oks = __ballot(ok);
     bool whole = oks == ~0ull;
-    if constexpr (!LIST) whole = whole && j0 >= reach.smax && j0 + KEYS <= reach.emin;
+    if constexpr (!LIST) whole = whole & (j0 >= reach.smax) & (j0 + KEYS <= reach.emin);
     // a value that is not finite must not reach rows that do not see it
-    const uint64_t bad = __ballot(!whole && vb == 255u);
-    vb = !whole && vb == 255u ? 0u : vb;
-    if (lane == 0) {
-      bad_of[b][wave] = bad;
-      uint64_t v = oks & 0x1111111111111111ull;  // a key's four threads agree
-      v = (v | v >> 3) & 0x0303030303030303ull;
-      v = (v | v >> 6) & 0x000F000F000F000Full;
-      v = (v | v >> 12) & 0x000000FF000000FFull;
-      valid_of[b][wave] = ((uint32_t)(v | v >> 24) & 0xFFFFu) | (bad ? 0x10000u : 0u);
-    }
+    const bool drop = !whole & (vb == 255u);
+    const uint64_t bad = __ballot(drop);
+    vb = drop ? 0u : vb;
+    bad_of[b][wave] = bad;  // wave-uniform, no branch
+    uint64_t v = oks & 0x1111111111111111ull;  // a key's four threads agree
+    v = (v | v >> 3) & 0x0303030303030303ull;
+    v = (v | v >> 6) & 0x000F000F000F000Full;
+    v = (v | v >> 12) & 0x000000FF000000FFull;
+    valid_of[b][wave] = ((uint32_t)(v | v >> 24) & 0xFFFFu) | (bad ? 0x10000u : 0u);
     const float vs = __uint_as_float(vb << 23);
     uint8_t* buf = lds + b * kBuf;
 #pragma unroll
@@ -898,11 +923,8 @@ __global__ __launch_bounds__(256, 2) void k_attn4_many(Attn4Args a) {
       *reinterpret_cast<bf16x8_t*>(buf + kw + 16 * n) = decode8(kv.k[n], ks);
       *reinterpret_cast<bf16x8_t*>(buf + (vw ^ (16 * n))) = decode8(kv.v[n], vs);
     }
-    page[b] = page2;
-    load_key<D>(a, page2, pos2, it.head, part, kv);
-    pos2 = pos3;
-    page2 = keys.page(a, pos2);
-    pos3 = position(s + 4);
+    page[b] = now;
+    load_key<D>(a, now, at, it.head, part, kv);
   };
 
   // the reading side: a key's row of 16 dims, and 8 bytes of a value's chunk
@@ -917,62 +939,69 @@ __global__ __launch_bounds__(256, 2) void k_attn4_many(Attn4Args a) {
   auto work = [&](int s, auto bc) {
     constexpr int b = decltype(bc)::value;
     const int j0 = keys.k0 + s * KEYS + wk * 32;
+    // The decoding of the next step runs beside the first products, the weights
+    // of each 16 keys beside the second products of the 16 before.
+    // (Rows or keys that there are not take part like any other: a branch around
+    // them would make every path wait for all loads in flight.)
+    const uint8_t* buf = lds + b * kBuf;
+    f32x16_t x[KT];
+#pragma unroll
+    for (int u = 0; u < KT; ++u) x[u] = f32x16_t{};
+#pragma unroll
+    for (int n = 0; n < NK; ++n)
+#pragma unroll
+      for (int u = 0; u < KT; ++u) {
+        const bf16x8_t kf = *reinterpret_cast<const bf16x8_t*>(buf + kr + u * 32 * kKRow<D> + n * 32);
+        x[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[n], x[u], 0, 0, 0);
+      }
     stage(s + 1, Int<b ^ 1>{});  // past the last step: keys that do not count
-    if (LIST ? emax > 0 : (j0 < emax && j0 + 32 * KT > smin)) {
-      const uint8_t* buf = lds + b * kBuf;
-      f32x16_t x[KT];
+    uint64_t valid = 0;
+    uint32_t any_bad = 0;
 #pragma unroll
-      for (int u = 0; u < KT; ++u) x[u] = f32x16_t{};
+    for (int u = 0; u < 2 * KT; ++u) {
+      const uint32_t v = valid_of[b][2 * wk + u];
+      valid |= (uint64_t)(v & 0xFFFFu) << (16 * u);
+      any_bad |= v >> 16;
+    }
+    bool whole = valid == (KT == 1 ? 0xFFFFFFFFull : ~0ull);
+    if constexpr (!LIST) whole = whole & (j0 >= smax) & (j0 + 32 * KT <= emin);
+    if (!whole) {
+      asm volatile("");  // a branch, not selects: most steps need no mask
+      col.template mask<KT, LIST>(x, valid, j0);
+    }
+    col.template renew<KT>(x, a.scale_log2, a.slack);
+    bf16x8_t p = col.weights(x[0], 0, a.scale_log2);
 #pragma unroll
-      for (int n = 0; n < NK; ++n)
+    for (int u = 0; u < 2 * KT; ++u) {
+      bf16x8_t next;
+      if (u + 1 < 2 * KT) next = col.weights(x[(u + 1) >> 1], (u + 1) & 1, a.scale_log2);
 #pragma unroll
-        for (int u = 0; u < KT; ++u) {
-          const bf16x8_t kf = *reinterpret_cast<const bf16x8_t*>(buf + kr + u * 32 * kKRow<D> + n * 32);
-          x[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[n], x[u], 0, 0, 0);
-        }
-      uint64_t valid = 0;
-      uint32_t any_bad = 0;
-#pragma unroll
-      for (int u = 0; u < 2 * KT; ++u) {
-        const uint32_t v = valid_of[b][2 * wk + u];
-        valid |= (uint64_t)(v & 0xFFFFu) << (16 * u);
-        any_bad |= v >> 16;
+      for (int n = 0; n < NV; ++n) {
+        const uint8_t* v = buf + vr[n] + u * 16 * 2 * D;
+        const s16x4_t v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)v);
+        const s16x4_t v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(v + 8 * 2 * D));
+        const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+        col.acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p, col.acc[n], 0, 0, 0);
       }
-      bool whole = valid == (KT == 1 ? 0xFFFFFFFFull : ~0ull);
-      if constexpr (!LIST) whole = whole && j0 >= smax && j0 + 32 * KT <= emin;
-      if (!whole) {
-        asm volatile("");  // a branch, not selects: most steps need no mask
-        col.template mask<KT, LIST>(x, valid, j0);
-      }
-      col.template renew<KT>(x, a.scale_log2, a.slack);
-#pragma unroll
-      for (int u = 0; u < 2 * KT; ++u) {
-        const bf16x8_t p = col.weights(x[u >> 1], u & 1, a.scale_log2);
-#pragma unroll
-        for (int n = 0; n < NV; ++n) {
-          const uint8_t* v = buf + vr[n] + u * 16 * 2 * D;
-          const s16x4_t v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)v);
-          const s16x4_t v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(v + 8 * 2 * D));
-          const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-          col.acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p, col.acc[n], 0, 0, 0);
-        }
-      }
-      if (any_bad) {
+      p = next;
+    }
+    if (any_bad) {
 #pragma unroll 1
-        for (int u = 0; u < 2 * KT; ++u) {
-          const uint64_t bad = bad_of[b][2 * wk + u];
-          col.template spoil<LIST>(bad, j0 + 16 * u);
-        }
+      for (int u = 0; u < 2 * KT; ++u) {
+        const uint64_t bad = bad_of[b][2 * wk + u];
+        col.template spoil<LIST>(bad, j0 + 16 * u);
       }
     }
     __syncthreads();
   };
   stage(0, Int<0>{});
   __syncthreads();
-  for (int s = 0; s < steps; s += 2) {
+  int s = 0;
+  for (; s + 1 < steps; s += 2) {
     work(s, Int<0>{});
-    if (s + 1 < steps) work(s + 1, Int<1>{});
+    work(s + 1, Int<1>{});
   }
+  if (s < steps) work(s, Int<0>{});
   float L = col.l + __shfl_xor(col.l, 32), M = col.m == neg_inf() ? neg_inf() : col.mc;
   if constexpr (WR == 2) {
     // the two waves of the same rows
