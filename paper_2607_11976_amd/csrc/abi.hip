@@ -728,9 +728,7 @@ int lt_cache4_attention(const void* q, int64_t q_stride, int32_t tokens, int32_t
   if (nreq > 0 && (!seq_lens || (table_width > 0 && !block_table))) return LT_EINVAL;
   if (list_k > 0 && !selected) return LT_EINVAL;
   if (!workspace || !aligned(workspace, 256)) return LT_EINVAL;
-  const size_t need = attn4_workspace_bytes(a);
-  if (need == 0) return LT_EUNSUPPORTED;
-  if (workspace_bytes < need) return LT_EWORKSPACE;
+  if (workspace_bytes < attn4_workspace_bytes(a)) return LT_EWORKSPACE;
   a.q = static_cast<const uint16_t*>(q);
   a.q_stride = q_stride;
   a.codes = codes;

@@ -11,9 +11,11 @@
 // output's own rounding.
 //
 // Rows are (token, head of the group) pairs that share a KV head. A tile is up
-// to 16 (k_attn4_few), 64 or 128 (k_attn4_many) rows of one request; its key
-// range is cut into chunks so that the work of all tiles, long and short, fills
-// the GPU evenly; the chunks of a tile are joined by a second kernel.
+// to 16 (k_attn4_few), 64 or 128 (k_attn4_many) rows of one request; the keys
+// of all tiles are shared out evenly over the blocks, and the parts of a tile
+// that falls to several are joined by a second kernel.
+#include <algorithm>
+
 #include "cache4.hpp"
 #include "internal.hpp"
 
@@ -28,8 +30,6 @@ typedef __attribute__((address_space(3))) s16x4_t* lds_s16x4_t;
 
 constexpr float kLn2 = 0.69314718055994530942f;
 constexpr int kInlineRequests = 64;  // requests that a wave schedules by itself
-constexpr int kMinChunk = 128;       // shortest chunk
-constexpr uint32_t kNoSplit = 0x80000000u;  // chunk length that no request reaches
 
 __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
 __device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
@@ -40,17 +40,40 @@ __device__ __forceinline__ uint32_t lane_bcast(uint32_t v, int lane) {
 }
 
 // ---------------------------------------------------------------------------
-// Schedule. Request r has tiles_r = heads * ceil(rows_r / ROWS) tiles over
-// about span_r keys; with a chunk length C it makes tiles_r * ceil(span_r / C)
-// items, and C >= sum tiles_r * span_r / target keeps the items within
-// target + tiles. span_r only balances: a tile's last chunk takes what is left.
+// Schedule. All tiles, laid end to end by the keys they see, are one line of
+// work, cut into equal shares for the blocks: whatever the lengths of the
+// requests, every block has as much to do, and only tiles that a cut falls into
+// are joined afterwards (at most two parts a block).
+//
+// A tile's length on that line is an estimate: request r has n row tiles a KV
+// head, the j-th from the end sees about u_j = top - j * slope keys, the line
+// between its last and its first token's ranges (exact for a causal mask and for
+// a window), and its start costs as much time as kStart keys. The estimate only
+// balances: the last part of a tile takes the keys that are left. A cut falls on
+// a multiple of 64 keys of the tile.
+//
+// One share for each block that is resident at once, two a CU: a decode step of
+// 48 requests of 1K to 128K keys (1.31 GB) takes 246 us, 256 with two shares a
+// block and 302 with eight (each pays its start again), and with three blocks a
+// CU (fewer registers for loads in flight) 293.
 // ---------------------------------------------------------------------------
+constexpr int kShares = 512;
+template <int ROWS>
+constexpr int kStart = ROWS == 16 ? 384 : 128;
+constexpr int kMinShare = 128;
+constexpr int kCut = 64;
+
 // Keys of a request; positions and steps past them stay within 31 bits.
 __device__ __forceinline__ int key_count(int n) { return min(max(n, 0), LT_CACHE4_MAX_KEYS); }
 
 struct Req {
-  int t0, nt, len, tiles;  // first token, tokens, cached keys, tiles
-  uint32_t span;
+  int t0, nt, len, tiles;  // first token, tokens, cached keys, row tiles
+  uint32_t top, slope;
+  // keys of the tiles before the j-th, one head
+  __device__ __forceinline__ uint64_t before(uint32_t j) const {
+    return (uint64_t)j * top - (uint64_t)j * (j - 1) / 2 * slope;
+  }
+  __device__ __forceinline__ uint32_t keys(uint32_t j) const { return top - j * slope; }
 };
 
 template <int ROWS>
@@ -60,104 +83,59 @@ __device__ __forceinline__ Req load_req(const Attn4Args& a, int r) {
   q.t0 = t0;
   q.nt = t1 - t0;
   q.len = key_count(a.seq[r]);
-  q.tiles = q.nt > 0 ? a.hkv * (int)(((int64_t)q.nt * a.group + ROWS - 1) / ROWS) : 0;
-  int lo = 0, hi = q.len;
-  if (q.nt > 0 && a.end) hi = min(max(a.end[t1 - 1], 0), hi);
-  if (q.nt > 0 && a.start) lo = min(max(a.start[t0], 0), hi);
-  q.span = (uint32_t)max(hi - lo, 1);
+  q.tiles = (int)(((int64_t)q.nt * a.group + ROWS - 1) / ROWS);
+  int e0 = q.len - q.nt + 1, e1 = q.len, s0 = 0, s1 = 0;
+  if (q.nt > 0 && a.end) e0 = a.end[t0], e1 = a.end[t1 - 1];
+  if (q.nt > 0 && a.start) s0 = a.start[t0], s1 = a.start[t1 - 1];
+  e0 = min(max(e0, 0), q.len), e1 = min(max(e1, 0), q.len);
+  const int first = max(e0 - max(s0, 0), 0), last = max(e1 - max(s1, 0), 0);
+  q.slope = q.tiles > 1 && last > first ? (uint32_t)(last - first) / (uint32_t)(q.tiles - 1) : 0u;
+  q.top = (uint32_t)max(first, last) + kStart<ROWS>;
   return q;
 }
 
-__device__ __forceinline__ uint64_t wave_sum64(uint64_t v) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const uint32_t lo = (uint32_t)__shfl_xor((int)(uint32_t)v, o), hi = (uint32_t)__shfl_xor((int)(v >> 32), o);
-    v += ((uint64_t)hi << 32) | lo;
-  }
-  return v;
+__device__ __forceinline__ uint64_t shfl64_up(uint64_t v, int o) {
+  return ((uint64_t)(uint32_t)__shfl_up((int)(v >> 32), o) << 32) | (uint32_t)__shfl_up((int)(uint32_t)v, o);
 }
-__device__ __forceinline__ uint32_t wave_prefix(uint32_t v) {  // inclusive
+__device__ __forceinline__ uint64_t wave_prefix64(uint64_t v) {  // inclusive
   const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const uint32_t u = (uint32_t)__shfl_up((int)v, o);
+    const uint64_t u = shfl64_up(v, o);
     if (lane >= o) v += u;
   }
   return v;
 }
-
-// As many items as blocks are resident at once (kSlots), and where that makes
-// chunks longer than kFullChunk, up to kTarget: then the last blocks to finish
-// keep the GPU busy for a shorter time, and a chunk's own start is small
-// beside its keys.
-template <int ROWS>
-constexpr int kSlots = ROWS == 16 ? 768 : 512;
-constexpr int kTarget = 2048, kFullChunk = 1024;
-
-template <int ROWS>
-__device__ __forceinline__ uint32_t chunk_len(uint64_t work) {
-  const uint64_t few = (work + kSlots<ROWS> - 1) / kSlots<ROWS>, many = (work + kTarget - 1) / kTarget;
-  uint64_t c = max(many, min(few, (uint64_t)kFullChunk));
-  c = (c + kMinChunk - 1) / kMinChunk * kMinChunk;
-  return c < kMinChunk ? kMinChunk : c > 0x40000000u ? 0x40000000u : (uint32_t)c;
+__device__ __forceinline__ uint64_t lane_bcast64(uint64_t v, int lane) {
+  return ((uint64_t)lane_bcast((uint32_t)(v >> 32), lane) << 32) | lane_bcast((uint32_t)v, lane);
 }
+__device__ __forceinline__ uint64_t uniform64(uint64_t v) { return lane_bcast64(v, 0); }
 
-struct Item {
-  int r, t0, nt, len;       // request, its first token, tokens and keys
-  int head, row0, rows;     // KV head; the tile's rows [row0, rows) within the request, at most ROWS
-  int chunk, chunks;
-  uint32_t C, item;
-  bool any;
-};
-
-// The schedule of more than kInlineRequests requests: the items' prefix sums
-// sched[0..R], the chunk length sched[R + 1] and the tiles' prefix sums from
-// sched[R + 2] on.
+// The lines' beginnings of more than kInlineRequests requests, and their end.
 template <int ROWS>
 __global__ __launch_bounds__(1024) void k_attn4_schedule(Attn4Args a) {
-  __shared__ uint64_t sum[16];
-  __shared__ uint32_t part[16], tpart[16];
+  __shared__ uint64_t part[16];
   const int t = threadIdx.x, w = t >> 6, lane = t & 63;
-  uint64_t work = 0;
-  for (int r = t; r < a.R; r += 1024) {
-    const Req q = load_req<ROWS>(a, r);
-    work += (uint64_t)q.tiles * q.span;
-  }
-  work = wave_sum64(work);
-  if (lane == 0) sum[w] = work;
-  __syncthreads();
-  work = 0;
-  for (int i = 0; i < 16; ++i) work += sum[i];
-  const uint32_t C = a.split ? chunk_len<ROWS>(work) : kNoSplit;
-  uint32_t base = 0, tbase = 0;
+  uint64_t base = 0;
   for (int r0 = 0; r0 < a.R; r0 += 1024) {
     const int r = r0 + t;
-    uint32_t n = 0, nt = 0;
+    uint64_t n = 0;
     if (r < a.R) {
       const Req q = load_req<ROWS>(a, r);
-      nt = (uint32_t)q.tiles;
-      n = nt * ((q.span + C - 1) / C);
+      n = a.hkv * q.before(q.tiles);
     }
-    const uint32_t in = wave_prefix(n), tin = wave_prefix(nt);
+    const uint64_t in = wave_prefix64(n);
     __syncthreads();
-    if (lane == 63) part[w] = in, tpart[w] = tin;
+    if (lane == 63) part[w] = in;
     __syncthreads();
-    uint32_t before = base, tbefore = tbase;
+    uint64_t before = base;
     for (int i = 0; i < 16; ++i) {
-      if (i < w) before += part[i], tbefore += tpart[i];
+      if (i < w) before += part[i];
       base += part[i];
-      tbase += tpart[i];
     }
-    if (r < a.R) {
-      a.sched[r] = before + in - n;
-      a.sched[a.R + 2 + r] = tbefore + tin - nt;
-    }
+    if (r < a.R) a.sched[r] = before + in - n;
   }
-  if (t == 0) {
-    a.sched[a.R] = base;
-    a.sched[a.R + 1] = C;
-    a.sched[2 * a.R + 2] = tbase;
-  }
+  if (t == 0) a.sched[a.R] = base;
 }
 
 // The last of n >= 1 ascending entries (the first is taken to be <= x) that is <= x; wave-uniform.
@@ -175,96 +153,147 @@ __device__ __forceinline__ int last_le(const T* v, int n, T x) {
   return __builtin_amdgcn_readfirstlane(lo);
 }
 
-// The item a block works on, or with TILE the first item of a tile; wave-uniform.
-template <int ROWS, bool TILE>
-__device__ __forceinline__ Item find_item(const Attn4Args& a, uint32_t id) {
-  const int lane = threadIdx.x & 63;
-  Item it{};
+// A tile (or a part of one): its request, KV head and rows, and its place on the line.
+struct Tile {
+  int r, t0, nt, len;    // request, its first token, tokens and keys
+  int head, row0, rows;  // KV head; the tile's rows [row0, rows) within the request, at most ROWS
+  uint32_t keys;         // its length
+  uint64_t at;           // where it begins
+  int k0, k1;            // the part: keys [k0, k1) of the tile, k1 < 0: to its end
+  int slot;              // where the part's sums go, -1: it is the whole tile
+};
+
+// Length of the line and of a share.
+struct Line {
+  uint64_t end, share;
+};
+__device__ __forceinline__ Line line_of(uint64_t end) {
+  const uint64_t s = ((end + kShares - 1) / kShares + kCut - 1) / kCut * kCut;
+  return Line{end, max(s, (uint64_t)kMinShare)};
+}
+
+template <int ROWS, bool LIST>
+__device__ __forceinline__ Line measure(const Attn4Args& a) {
+  if constexpr (LIST) {
+    return Line{a.R > 0 ? (uint64_t)a.T * a.hkv * a.row_tiles * a.list_parts * a.list_share : 0, (uint64_t)a.list_share};
+  } else if (a.R > kInlineRequests) {
+    return line_of(uniform64(a.sched[a.R]));
+  } else {
+    const int lane = threadIdx.x & 63;
+    uint64_t n = 0;
+    if (lane < a.R) {
+      const Req q = load_req<ROWS>(a, lane);
+      n = a.hkv * q.before(q.tiles);
+    }
+    return line_of(lane_bcast64(wave_prefix64(n), 63));
+  }
+}
+
+// The tile that holds the place x < end of the line; wave-uniform.
+template <int ROWS>
+__device__ __forceinline__ Tile tile_at(const Attn4Args& a, uint64_t x) {
+  Tile it;
   Req q{};
-  uint32_t first = 0, tfirst = 0;
+  uint64_t base;
   if (a.R <= kInlineRequests) {
-    if (lane < a.R) q = load_req<ROWS>(a, lane);
-    it.C = __builtin_amdgcn_readfirstlane(
-        a.split ? chunk_len<ROWS>(wave_sum64((uint64_t)q.tiles * q.span)) : kNoSplit);
-    const uint32_t n = lane < a.R ? (uint32_t)q.tiles * ((q.span + it.C - 1) / it.C) : 0u;
-    const uint32_t in = wave_prefix(n), tin = TILE ? wave_prefix((uint32_t)q.tiles) : 0u;
-    const uint64_t hit = __ballot((TILE ? tin : in) > id);
-    if (!hit) return it;
-    it.r = __ffsll((unsigned long long)hit) - 1;
-    first = lane_bcast(in - n, it.r);
-    tfirst = lane_bcast(tin - q.tiles, it.r);
+    const int lane = threadIdx.x & 63;
+    uint64_t n = 0;
+    if (lane < a.R) {
+      q = load_req<ROWS>(a, lane);
+      n = a.hkv * q.before(q.tiles);
+    }
+    const uint64_t in = wave_prefix64(n);
+    it.r = __ffsll((unsigned long long)__ballot(in > x)) - 1;
+    base = lane_bcast64(in - n, it.r);
     q.t0 = lane_bcast(q.t0, it.r);
     q.nt = lane_bcast(q.nt, it.r);
     q.len = lane_bcast(q.len, it.r);
     q.tiles = lane_bcast(q.tiles, it.r);
-    q.span = lane_bcast(q.span, it.r);
+    q.top = lane_bcast(q.top, it.r);
+    q.slope = lane_bcast(q.slope, it.r);
   } else {
-    const uint32_t* s = TILE ? a.sched + a.R + 2 : a.sched;
-    if (id >= s[a.R]) return it;
-    it.C = a.sched[a.R + 1];
-    it.r = last_le<uint32_t>(s, a.R, id);
-    first = a.sched[it.r];
-    tfirst = a.sched[a.R + 2 + it.r];
+    it.r = last_le<uint64_t>(a.sched, a.R, x);
+    base = uniform64(a.sched[it.r]);
     q = load_req<ROWS>(a, it.r);
+    q.t0 = __builtin_amdgcn_readfirstlane(q.t0);
+    q.nt = __builtin_amdgcn_readfirstlane(q.nt);
+    q.len = __builtin_amdgcn_readfirstlane(q.len);
+    q.tiles = __builtin_amdgcn_readfirstlane(q.tiles);
+    q.top = __builtin_amdgcn_readfirstlane(q.top);
+    q.slope = __builtin_amdgcn_readfirstlane(q.slope);
   }
-  it.any = true;
-  it.t0 = __builtin_amdgcn_readfirstlane(q.t0);
-  it.nt = __builtin_amdgcn_readfirstlane(q.nt);
-  it.len = __builtin_amdgcn_readfirstlane(q.len);
-  it.chunks = __builtin_amdgcn_readfirstlane((int)((q.span + it.C - 1) / it.C));
-  uint32_t tile;
-  if constexpr (TILE) {
-    tile = id - tfirst;
-    it.item = first + tile * it.chunks;
-  } else {
-    const uint32_t at = id - first;
-    tile = at / (uint32_t)it.chunks;
-    it.chunk = (int)(at - tile * it.chunks);
-    it.item = id;
+  x -= base;
+  // row tiles from the end of the request, each with all its heads
+  uint32_t j = 0, n = (uint32_t)q.tiles;
+  while (n > 1) {  // the last j with heads * before(j) <= x
+    const uint32_t half = n / 2;
+    if (a.hkv * q.before(j + half) <= x) {
+      j += half;
+      n -= half;
+    } else {
+      n = half;
+    }
   }
-  const int per_head = q.tiles / a.hkv;
-  it.head = (int)tile / per_head;
-  // the last rows first: with a causal mask they see the most keys
-  it.row0 = (per_head - 1 - ((int)tile - it.head * per_head)) * ROWS;
-  it.rows = it.nt * a.group;
+  it.keys = q.keys(j);
+  x -= a.hkv * q.before(j);
+  it.head = (int)((uint32_t)(x / it.keys));
+  it.at = base + a.hkv * q.before(j) + (uint64_t)it.head * it.keys;
+  it.t0 = q.t0;
+  it.nt = q.nt;
+  it.len = q.len;
+  it.row0 = (q.tiles - 1 - (int)j) * ROWS;
+  it.rows = q.nt * a.group;
   return it;
 }
 
-// The same for list attention: every token of the batch, KV head and row tile
-// over a.chunks chunks of the list.
-template <int ROWS, bool TILE>
-__device__ __forceinline__ Item find_list_item(const Attn4Args& a, uint32_t id) {
-  Item it{};
-  if (a.R == 0) return it;
-  const uint32_t chunks = TILE ? 1u : (uint32_t)a.chunks, tile = id / chunks;
-  const uint32_t per_tok = (uint32_t)(a.hkv * a.row_tiles);
-  const int t = (int)(tile / per_tok);
+// The same for list attention: every token, KV head and row tile has list_parts
+// shares of its own. rows = 0: the token belongs to no request.
+template <int ROWS>
+__device__ __forceinline__ Tile list_tile_at(const Attn4Args& a, uint64_t x) {
+  Tile it;
+  it.keys = (uint32_t)(a.list_parts * a.list_share);
+  const uint32_t tile = (uint32_t)(x / it.keys), per_tok = (uint32_t)(a.hkv * a.row_tiles);
+  const int t = (int)(tile / per_tok), in = (int)(tile - t * per_tok);
+  it.at = (uint64_t)tile * it.keys;
   it.r = last_le<int32_t>(a.cu, a.R, t);
-  const int c0 = a.cu[it.r], c1 = a.cu[it.r + 1];
-  if (t < c0 || t >= c1) return it;
-  it.any = true;
+  const int c0 = __builtin_amdgcn_readfirstlane(a.cu[it.r]), c1 = __builtin_amdgcn_readfirstlane(a.cu[it.r + 1]);
   it.t0 = c0;
   it.nt = min(c1, a.T) - c0;
-  it.len = key_count(a.seq[it.r]);
-  it.chunks = a.chunks;
-  it.chunk = (int)(id - tile * chunks);
-  it.item = TILE ? tile * a.chunks : id;
-  it.C = (uint32_t)a.chunk_keys;
-  const int in = (int)(tile - t * per_tok);
+  it.len = key_count(__builtin_amdgcn_readfirstlane(a.seq[it.r]));
   it.head = in / a.row_tiles;
   it.row0 = (t - c0) * a.group + (in - it.head * a.row_tiles) * ROWS;
-  it.rows = (t - c0 + 1) * a.group;  // of this token
+  it.rows = t < c0 || t >= c1 ? 0 : (t - c0 + 1) * a.group;  // of this token
   return it;
 }
 
-template <int ROWS, bool LIST, bool TILE>
-__device__ __forceinline__ Item find(const Attn4Args& a, uint32_t id) {
-  if constexpr (LIST) return find_list_item<ROWS, TILE>(a, id);
-  else return find_item<ROWS, TILE>(a, id);
+template <int ROWS, bool LIST>
+__device__ __forceinline__ Tile find(const Attn4Args& a, uint64_t x) {
+  if constexpr (LIST) return list_tile_at<ROWS>(a, x);
+  else return tile_at<ROWS>(a, x);
 }
 
-// Visible keys of the i-th token of an item's request.
-__device__ __forceinline__ RowRange token_range(const Attn4Args& a, const Item& it, int i) {
+// The keys of a tile before a cut at the place x of the line.
+template <int ROWS, bool LIST>
+__device__ __forceinline__ int cut_in(const Tile& it, uint64_t x) {
+  const uint64_t from = it.at + (LIST ? 0 : kStart<ROWS>);
+  return x <= from ? 0 : (int)((uint32_t)(x - from) / kCut * kCut);
+}
+
+// The part of a tile that a share beginning at `begin` has from x on; returns
+// where the next one begins. A part without keys is left out (false in `any`).
+template <int ROWS, bool LIST>
+__device__ __forceinline__ uint64_t take_part(Tile& it, uint64_t begin, uint64_t end, uint64_t x, int block,
+                                              bool& any) {
+  const uint64_t tile_end = it.at + it.keys, stop = min(end, tile_end);
+  it.k0 = cut_in<ROWS, LIST>(it, x);
+  it.k1 = stop == tile_end ? -1 : cut_in<ROWS, LIST>(it, stop);
+  it.slot = it.k0 == 0 && it.k1 < 0 ? -1 : 2 * block + (x == begin ? 0 : 1);
+  any = it.k1 < 0 || it.k0 < it.k1;
+  return stop;
+}
+
+// Visible keys of the i-th token of a tile's request.
+__device__ __forceinline__ RowRange token_range(const Attn4Args& a, const Tile& it, int i) {
   int e = a.end ? a.end[it.t0 + i] : it.len - it.nt + i + 1;
   e = min(max(e, 0), it.len);
   int s = a.start ? a.start[it.t0 + i] : 0;
@@ -278,7 +307,7 @@ struct Reach {
   int lo, hi, smax, emin;
 };
 template <int ROWS>
-__device__ __forceinline__ Reach tile_reach(const Attn4Args& a, const Item& it) {
+__device__ __forceinline__ Reach tile_reach(const Attn4Args& a, const Tile& it) {
   Reach r{0x7FFFFFFF, 0, 0, 0x7FFFFFFF};
   for (int x = it.row0 + (threadIdx.x & 63); x < min(it.row0 + ROWS, it.rows); x += 64) {
     const RowRange rr = token_range(a, it, x / a.group);
@@ -303,13 +332,13 @@ __device__ __forceinline__ Reach tile_reach(const Attn4Args& a, const Item& it) 
   return r;
 }
 
-// The places of an item's chunk, positions or entries of the token's list, and
-// the keys that they name.
+// The places of a part, positions or entries of the token's list, and the keys
+// that they name.
 template <bool LIST>
 struct Keys {
   const int32_t *list, *table;
   int base, lo, hi, k0, k1, head;
-  __device__ __forceinline__ void init(const Attn4Args& a, const Item& it, const Reach& r) {
+  __device__ __forceinline__ void init(const Attn4Args& a, const Tile& it, const Reach& r) {
     table = a.table + (int64_t)it.r * a.table_ld;
     head = it.head;
     lo = r.lo;
@@ -320,12 +349,11 @@ struct Keys {
       const int t = it.t0 + it.row0 / a.group;
       list = a.list + (int64_t)t * a.list_ld;
       base = a.list_base ? a.list_base[t] : 0;
-      k0 = (int)min((int64_t)it.chunk * it.C, (int64_t)a.list_k);
-      k1 = lo == hi ? k0 : (int)min((int64_t)k0 + it.C, (int64_t)a.list_k);
+      k0 = min(it.k0, a.list_k);
+      k1 = lo == hi ? k0 : it.k1 < 0 ? a.list_k : min(it.k1, a.list_k);
     } else {
-      // a chunk's length comes from the request's estimate: the last one takes the rest
-      k0 = (int)min(lo + (int64_t)it.chunk * it.C, (int64_t)hi);
-      k1 = it.chunk == it.chunks - 1 ? hi : (int)min((int64_t)k0 + it.C, (int64_t)hi);
+      k0 = min(lo + min(it.k0, hi - lo), hi);
+      k1 = it.k1 < 0 ? hi : lo + min(it.k1, hi - lo);
     }
   }
   // Each lookup in two halves, so that a loop can keep its load in flight: the
@@ -422,7 +450,7 @@ struct Column {
   int s, e;  // the row's visible range; empty for no row
   bool row;
 
-  __device__ __forceinline__ void init(const Attn4Args& a, const Item& it, int x, bf16x8_t (&q)[D / 32], int stride,
+  __device__ __forceinline__ void init(const Attn4Args& a, const Tile& it, int x, bf16x8_t (&q)[D / 32], int stride,
                                        int step) {
     m = neg_inf();
     mc = l = 0.0f;
@@ -503,11 +531,11 @@ struct Column {
   }
 
   // One row's result, or its part of it. M, L: the row's maximum (times scale) and sum.
-  __device__ __forceinline__ void store(const Attn4Args& a, const Item& it, int x, int rows_per_tile, float M,
+  __device__ __forceinline__ void store(const Attn4Args& a, const Tile& it, int x, int rows_per_tile, float M,
                                         float L) const {
     if (!row) return;
     const int g = (threadIdx.x & 63) >> 4;
-    if (it.chunks == 1) {
+    if (it.slot < 0) {
       const int i = x / a.group, h = it.head * a.group + (x - i * a.group);
       const int64_t at = (int64_t)(it.t0 + i) * a.hkv * a.group + h;
       const float inv = L == 0.0f ? 0.0f : 1.0f / L;
@@ -519,7 +547,7 @@ struct Column {
       }
       if (a.lse && g == 0) a.lse[at] = L == 0.0f ? neg_inf() : (M + __builtin_amdgcn_logf(L)) * kLn2;
     } else {
-      const int64_t at = (int64_t)it.item * rows_per_tile + (x - it.row0);
+      const int64_t at = (int64_t)it.slot * rows_per_tile + (x - it.row0);
       f32x4_t* o = reinterpret_cast<f32x4_t*>(a.part_o + at * D) + g;
 #pragma unroll
       for (int n = 0; n < D / 16; ++n) o[n * 4] = acc[n];
@@ -564,14 +592,19 @@ __device__ __forceinline__ void clear_padding(const Attn4Args& a) {
 // transposing reads give the other operand. No barrier inside the loop.
 // ---------------------------------------------------------------------------
 template <int D, bool LIST>
-__global__ __launch_bounds__(256, 3) void k_attn4_few(Attn4Args a) {
+__global__ __launch_bounds__(256, 2) void k_attn4_few(Attn4Args a) {
   constexpr int ROWS = 16, NI = D / 32, NT = D / 16;
   __shared__ __align__(16) uint8_t lds[4 * 32 * kVRow<D>];
   __shared__ float ml[4][2][ROWS];
   const int lane = threadIdx.x & 63, wave = wave_id(), c = lane & 15, g = lane >> 4;
-  const Item it = find<ROWS, LIST, false>(a, blockIdx.x);
   clear_padding<D>(a);
-  if (!it.any) return;
+  const Line line = measure<ROWS, LIST>(a);
+  const uint64_t begin = blockIdx.x * line.share, end = min(begin + line.share, line.end);
+  for (uint64_t at = begin; at < end;) {
+  Tile it = find<ROWS, LIST>(a, at);
+  bool any;
+  at = take_part<ROWS, LIST>(it, begin, end, at, blockIdx.x, any);
+  if (!any || it.rows == 0) continue;
   const Reach reach = tile_reach<ROWS>(a, it);
   Keys<LIST> keys;
   keys.init(a, it, reach);
@@ -685,6 +718,7 @@ __global__ __launch_bounds__(256, 3) void k_attn4_few(Attn4Args a) {
     __syncthreads();
   }
   if (wave == 0) col[0].store(a, it, it.row0 + c, ROWS, M, L);
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -708,7 +742,7 @@ struct Wide {
   int s, e;
   bool row;
 
-  __device__ __forceinline__ void init(const Attn4Args& a, const Item& it, int x, bf16x8_t (&q)[D / 16]) {
+  __device__ __forceinline__ void init(const Attn4Args& a, const Tile& it, int x, bf16x8_t (&q)[D / 16]) {
     m = neg_inf();
     mc = l = 0.0f;
 #pragma unroll
@@ -790,11 +824,11 @@ struct Wide {
     }
   }
 
-  __device__ __forceinline__ void store(const Attn4Args& a, const Item& it, int x, int rows_per_tile, float M,
+  __device__ __forceinline__ void store(const Attn4Args& a, const Tile& it, int x, int rows_per_tile, float M,
                                         float L) const {
     if (!row) return;
     const int h = (threadIdx.x & 63) >> 5;
-    if (it.chunks == 1) {
+    if (it.slot < 0) {
       const int i = x / a.group, head = it.head * a.group + (x - i * a.group);
       const int64_t at = (int64_t)(it.t0 + i) * a.hkv * a.group + head;
       const float inv = L == 0.0f ? 0.0f : 1.0f / L;
@@ -808,7 +842,7 @@ struct Wide {
                        (__bf16)(acc[n][4 * b + 2] * inv), (__bf16)(acc[n][4 * b + 3] * inv)};
       if (a.lse && h == 0) a.lse[at] = L == 0.0f ? neg_inf() : (M + __builtin_amdgcn_logf(L)) * kLn2;
     } else {
-      const int64_t at = (int64_t)it.item * rows_per_tile + (x - it.row0);
+      const int64_t at = (int64_t)it.slot * rows_per_tile + (x - it.row0);
       float* o = a.part_o + at * D + 4 * h;
 #pragma unroll
       for (int n = 0; n < D / 32; ++n)
@@ -843,9 +877,14 @@ __global__ __launch_bounds__(256, 2) void k_attn4_many(Attn4Args a) {
   __shared__ uint32_t valid_of[2][4];             // per 16 keys: those that count; bit 16: bad_of is not 0
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_id(), r = lane & 31, h = lane >> 5;
   const int wr = WR == 4 ? wave : wave >> 1, wk = WR == 4 ? 0 : wave & 1;  // the wave's rows, its keys of a step
-  const Item it = find<ROWS, LIST, false>(a, blockIdx.x);
   clear_padding<D>(a);
-  if (!it.any) return;
+  const Line line = measure<ROWS, LIST>(a);
+  const uint64_t begin = blockIdx.x * line.share, end = min(begin + line.share, line.end);
+  for (uint64_t at = begin; at < end;) {
+  Tile it = find<ROWS, LIST>(a, at);
+  bool any;
+  at = take_part<ROWS, LIST>(it, begin, end, at, blockIdx.x, any);
+  if (!any || it.rows == 0) continue;
   const Reach reach = tile_reach<ROWS>(a, it);
   Keys<LIST> keys;
   keys.init(a, it, reach);
@@ -1017,43 +1056,52 @@ __global__ __launch_bounds__(256, 2) void k_attn4_many(Attn4Args a) {
       if (h == 0) ml[r] = float2{M, L};
     }
     __syncthreads();
-    if (wk == 1) return;
-    const float2 o = ml[r];
-    const float top = fmaxf(M, o.x), ref = top == neg_inf() ? 0.0f : top;
-    const float f0 = exp2_fast(M - ref), f1 = exp2_fast(o.x - ref);
-    M = top;
-    L = L * f0 + o.y * f1;
+    if (wk == 0) {
+      const float2 o = ml[r];
+      const float top = fmaxf(M, o.x), ref = top == neg_inf() ? 0.0f : top;
+      const float f0 = exp2_fast(M - ref), f1 = exp2_fast(o.x - ref);
+      M = top;
+      L = L * f0 + o.y * f1;
 #pragma unroll
-    for (int n = 0; n < NV; ++n)
+      for (int n = 0; n < NV; ++n)
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        col.acc[n][i] = col.acc[n][i] * f0 + box[(4 * n + i / 4) * 64 + lane][i % 4] * f1;
+        for (int i = 0; i < 16; ++i)
+          col.acc[n][i] = col.acc[n][i] * f0 + box[(4 * n + i / 4) * 64 + lane][i % 4] * f1;
+    }
   }
-  col.store(a, it, it.row0 + wr * 32 + r, ROWS, M, L);
+  if (wk == 0) col.store(a, it, it.row0 + wr * 32 + r, ROWS, M, L);
+  __syncthreads();  // the buffers are free again
+  }
 }
 
-// Joins the chunks of a tile: a thread takes four outputs of a row, a block
-// 1024 / D rows at a time, eight chunks' loads in flight.
+// Joins the parts of a tile, by the block of the first cut inside it: parts c =
+// b - 1, b, ... of the shares that reach into it. A thread takes four outputs of
+// a row, a block 1024 / D rows at a time, eight parts' loads in flight.
 template <int D, int ROWS, bool LIST>
 __global__ __launch_bounds__(256) void k_attn4_join(Attn4Args a) {
   constexpr int kRowThreads = D / 4, kAtOnce = 256 / kRowThreads;
-  const Item it = find<ROWS, LIST, true>(a, blockIdx.x);
-  if (!it.any || it.chunks == 1) return;
+  const Line line = measure<ROWS, LIST>(a);
+  const int b = blockIdx.x + 1;
+  const uint64_t cut = b * line.share, before = cut - line.share;
+  if (cut >= line.end) return;
+  const Tile it = find<ROWS, LIST>(a, cut);
+  if (it.rows == 0 || cut_in<ROWS, LIST>(it, cut) == 0 || cut_in<ROWS, LIST>(it, before) > 0) return;
+  const int parts = 1 + (int)((it.at + it.keys - cut + line.share - 1) / line.share);
+  const int slot0 = 2 * (b - 1) + (it.at > before ? 1 : 0);
   const int c = threadIdx.x % kRowThreads;
   const int n = min(ROWS, it.rows - it.row0);
   for (int in = blockIdx.y * kAtOnce + threadIdx.x / kRowThreads; in < n; in += gridDim.y * kAtOnce) {
-    const float2* ml = a.part_ml + (int64_t)it.item * ROWS + in;
-    const f32x4_t* po = reinterpret_cast<const f32x4_t*>(a.part_o + ((int64_t)it.item * ROWS + in) * D) + c;
     float M = neg_inf(), L = 0.0f;
     f32x4_t o = {};
-    for (int i0 = 0; i0 < it.chunks; i0 += 8) {
+    for (int i0 = 0; i0 < parts; i0 += 8) {
       float2 w[8];
       f32x4_t v[8];
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        const int64_t at = (int64_t)min(i0 + u, it.chunks - 1) * ROWS;
-        w[u] = ml[at];
-        v[u] = po[at * kRowThreads];
+        const int i = min(i0 + u, parts - 1);
+        const int64_t row = (int64_t)(i == 0 ? slot0 : 2 * (b - 1 + i)) * ROWS + in;
+        w[u] = a.part_ml[row];
+        v[u] = reinterpret_cast<const f32x4_t*>(a.part_o)[row * kRowThreads + c];
       }
       float top = M;
 #pragma unroll
@@ -1064,8 +1112,8 @@ __global__ __launch_bounds__(256) void k_attn4_join(Attn4Args a) {
       o *= f;
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        const float g = i0 + u < it.chunks ? exp2_fast(w[u].x - ref) : 0.0f;
-        if (i0 + u < it.chunks) {
+        const float g = exp2_fast(w[u].x - ref);
+        if (i0 + u < parts) {
           L = fmaf(g, w[u].y, L);
           o += g * v[u];
         }
@@ -1084,7 +1132,8 @@ __global__ __launch_bounds__(256) void k_attn4_join(Attn4Args a) {
 template <int D, int ROWS, bool LIST>
 hipError_t run(const Attn4Args& a, hipStream_t st) {
   if (!LIST && a.R > kInlineRequests) k_attn4_schedule<ROWS><<<1, 1024, 0, st>>>(a);
-  const dim3 grid((unsigned)a.items);
+  const unsigned shares = LIST ? (unsigned)((int64_t)a.T * a.hkv * a.row_tiles * a.list_parts) : kShares;
+  const dim3 grid(shares);
   if constexpr (ROWS == 16) {
     k_attn4_few<D, LIST><<<grid, 256, 0, st>>>(a);
   } else {
@@ -1097,7 +1146,8 @@ hipError_t run(const Attn4Args& a, hipStream_t st) {
     }
     k_attn4_many<D, WR, LIST><<<grid, 256, lds, st>>>(a);
   }
-  if (a.split) k_attn4_join<D, ROWS, LIST><<<dim3((unsigned)a.tiles, ROWS == 16 ? 2 : ROWS / 32), 256, 0, st>>>(a);
+  if (!LIST || a.list_parts > 1)
+    k_attn4_join<D, ROWS, LIST><<<dim3(shares - 1, ROWS == 16 ? 2 : ROWS / 32), 256, 0, st>>>(a);
   return hipGetLastError();
 }
 
@@ -1108,48 +1158,42 @@ hipError_t run_rows(const Attn4Args& a, hipStream_t st) {
   return run<D, 128, LIST>(a, st);
 }
 
-// Shape of the launch: everything that depends on host values alone.
-bool shape_of(Attn4Args& a) {
+// What depends on host values alone: the rows of a tile, and for lists, which are
+// all as long, the parts of a tile: none but where there are too few tiles.
+void shape_of(Attn4Args& a) {
   const int64_t rows = a.list_k > 0 ? a.group : ((int64_t)a.T * a.group + a.R - 1) / (a.R > 0 ? a.R : 1);
   a.rows_per_tile = rows <= 16 ? 16 : rows <= 64 ? 64 : 128;
-  if (a.list_k > 0) {
-    // few tokens: narrow tiles rather than many chunks
-    if ((int64_t)a.T * a.hkv < 256) a.rows_per_tile = 16;
-    const int R = a.rows_per_tile;
-    a.row_tiles = (a.group + R - 1) / R;
-    a.tiles = (int64_t)a.T * a.hkv * a.row_tiles;
-    const int64_t most = (a.list_k + kMinChunk - 1) / kMinChunk;
-    int64_t n = a.tiles >= 256 ? 1 : 512 / a.tiles;
-    n = n < 1 ? 1 : n > most ? most : n;
-    a.chunk_keys = (int)(((a.list_k + n - 1) / n + 63) / 64 * 64);
-    a.chunks = (a.list_k + a.chunk_keys - 1) / a.chunk_keys;
-    a.split = a.chunks > 1;
-    a.items = a.tiles * a.chunks;
-  } else {
-    const int R = a.rows_per_tile;
-    a.tiles = (int64_t)a.hkv * (((int64_t)a.T * a.group + R - 1) / R + a.R);
-    a.split = (int64_t)a.T * a.group * a.hkv <= 131072;
-    a.items = a.tiles + (a.split ? kTarget : 0);
-  }
-  return a.items <= 0x3FFFFFFF;
+  if (a.list_k == 0) return;
+  // few tokens: more, narrower tiles rather than more parts
+  if ((int64_t)a.T * a.hkv < 256) a.rows_per_tile = 16;
+  a.row_tiles = (a.group + a.rows_per_tile - 1) / a.rows_per_tile;
+  const int64_t tiles = (int64_t)a.T * a.hkv * a.row_tiles, most = ((int64_t)a.list_k + kMinShare - 1) / kMinShare;
+  const int64_t parts = tiles >= 256 || tiles == 0 ? 1 : std::min(512 / tiles, most);
+  a.list_share = (int)((((int64_t)a.list_k + parts - 1) / parts + kCut - 1) / kCut * kCut);
+  a.list_parts = (int)(((int64_t)a.list_k + a.list_share - 1) / a.list_share);
+}
+
+// Parts that may have to be kept.
+size_t slots_of(const Attn4Args& a) {
+  if (a.list_k > 0) return a.list_parts > 1 ? 2 * (size_t)a.T * a.hkv * a.row_tiles * a.list_parts : 0;
+  return 2 * kShares;
 }
 
 }  // namespace
 
 size_t attn4_workspace_bytes(Attn4Args a) {
-  if (!shape_of(a)) return 0;
-  size_t n = 256 + ((2 * (size_t)a.R + 3) * 4 + 255) / 256 * 256;
-  if (a.split) n += (size_t)a.items * a.rows_per_tile * ((size_t)a.d * 4 + 8);
-  return n;
+  shape_of(a);
+  return 256 + (((size_t)a.R + 1) * 8 + 255) / 256 * 256 +
+         slots_of(a) * a.rows_per_tile * ((size_t)a.d * 4 + 8);
 }
 
 hipError_t launch_attn4(Attn4Args a, void* workspace, hipStream_t st) {
-  if (!shape_of(a)) return hipErrorInvalidValue;
+  shape_of(a);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
-  a.sched = reinterpret_cast<uint32_t*>(ws);
-  ws += ((2 * (size_t)a.R + 3) * 4 + 255) / 256 * 256;
+  a.sched = reinterpret_cast<uint64_t*>(ws);
+  ws += (((size_t)a.R + 1) * 8 + 255) / 256 * 256;
   a.part_o = reinterpret_cast<float*>(ws);
-  a.part_ml = reinterpret_cast<float2*>(ws + (a.split ? (size_t)a.items * a.rows_per_tile * a.d * 4 : 0));
+  a.part_ml = reinterpret_cast<float2*>(ws + slots_of(a) * a.rows_per_tile * a.d * 4);
   a.slack = 8.0f / a.scale_log2;
   if (!(a.slack < 1e30f)) a.slack = 1e30f;
   if (a.list_k > 0) return a.d == 128 ? run_rows<128, true>(a, st) : run_rows<64, true>(a, st);

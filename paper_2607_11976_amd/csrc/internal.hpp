@@ -247,14 +247,11 @@ struct Attn4Args {
   float* lse;
   // resolved by launch_attn4
   float slack;
-  int rows_per_tile, row_tiles, chunks, chunk_keys;
-  int64_t tiles, items;
-  bool split;
-  uint32_t* sched;
+  int rows_per_tile, row_tiles, list_parts, list_share;
+  uint64_t* sched;
   float* part_o;
   float2* part_ml;
 };
-// 0: more tiles than a launch can hold.
 size_t attn4_workspace_bytes(Attn4Args a);
 hipError_t launch_attn4(Attn4Args a, void* workspace, hipStream_t st);
 
