@@ -267,6 +267,7 @@ struct LogprobArgs {
   int32_t* top_index;       // [rows, top]
   float* top_logprob;
   int splits, split_len;    // resolved by logprob_shape
+  bool parts;
 };
 void logprob_shape(LogprobArgs& a);
 size_t logprob_workspace_bytes(LogprobArgs a);

@@ -60,6 +60,25 @@ __device__ __forceinline__ uint4 load16(const T* p) {
   return v;
 }
 
+// The same of elements [i, i + N), those from e on as -inf.
+template <class T>
+__device__ __forceinline__ uint4 fetch16(const T* x, int i, int e) {
+  constexpr int N = Vec<T>::N;
+  if (i + N <= e) return load16(x + i);
+  uint32_t w[4] = {Vec<T>::kFill, Vec<T>::kFill, Vec<T>::kFill, Vec<T>::kFill};
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    if (i + j >= e) continue;
+    if constexpr (N == 8) {
+      const uint32_t h = x[i + j];
+      w[j >> 1] = j & 1 ? (w[j >> 1] & 0xFFFFu) | (h << 16) : (w[j >> 1] & 0xFFFF0000u) | h;
+    } else {
+      w[j] = __float_as_uint(x[i + j]);
+    }
+  }
+  return uint4{w[0], w[1], w[2], w[3]};
+}
+
 // ---- sums ----
 struct Sums {
   float m, s, u;
@@ -160,39 +179,42 @@ __device__ __forceinline__ void take(Best& b, const float (&x)[Vec<T>::N], int f
   }
 }
 
-// What a row's sums and list say; the list and sums are wave-uniform resp. one
-// entry a lane. Called by one wave.
+// What a row's sums say of its token; one thread.
 template <class T>
-__device__ __forceinline__ void finish(const LogprobArgs& a, int row, Sums s, uint64_t list) {
-  const int lane = threadIdx.x & 63;
+__device__ __forceinline__ void finish_row(const LogprobArgs& a, int row, const Sums& s) {
   const T* x = reinterpret_cast<const T*>(a.logits) + (int64_t)row * a.ld;
   const bool none = s.s == 0.0f;  // no value above -inf
   const float l2 = __builtin_amdgcn_logf(s.s);
-  const float lse = none ? ninf() : fmaf(s.m, a.scale, l2 * kLn2);
-  if (lane == 0) {
-    const int64_t tok = a.tokens[row];
-    float lp = 0.0f;
-    if (tok >= 0 && tok < a.vocab) {
-      lp = none ? ninf() : fmaf(Vec<T>::one(x + tok) - s.m, a.scale, -l2 * kLn2);
-    }
-    a.logprob[row] = lp;
-    a.entropy[row] = none ? 0.0f : (l2 - s.u / s.s) * kLn2;
-    a.lse[row] = lse;
+  const int64_t tok = a.tokens[row];
+  float lp = 0.0f;
+  if (tok >= 0 && tok < a.vocab) lp = none ? ninf() : fmaf(Vec<T>::one(x + tok) - s.m, a.scale, -l2 * kLn2);
+  a.logprob[row] = lp;
+  a.entropy[row] = none ? 0.0f : (l2 - s.u / s.s) * kLn2;
+  a.lse[row] = none ? ninf() : fmaf(s.m, a.scale, l2 * kLn2);
+}
+// The row's best entry number `place`; key 0: there is none.
+__device__ __forceinline__ void finish_top(const LogprobArgs& a, int row, const Sums& s, int place, uint64_t key) {
+  float lp = ninf();
+  if (key && s.s != 0.0f) {
+    // a NaN among the logits makes the sums NaN, whatever the key's value
+    lp = fmaf(key_floor(key) - s.m, a.scale, -__builtin_amdgcn_logf(s.s) * kLn2);
   }
-  if (lane < a.top) {
-    const bool real = list != 0;
-    const int i = real ? (int)comp_pos(list) : -1;
-    float lp = ninf();
-    if (real && !none) lp = fmaf(Vec<T>::one(x + i) - s.m, a.scale, -l2 * kLn2);
-    a.top_index[(int64_t)row * a.top + lane] = i;
-    a.top_logprob[(int64_t)row * a.top + lane] = lp;
-  }
+  a.top_index[(int64_t)row * a.top + place] = key ? (int)comp_pos(key) : -1;
+  a.top_logprob[(int64_t)row * a.top + place] = lp;
 }
 
+// What a split of a row leaves: its sums, and keys among which its best `top`
+// are (0: no entry).
+constexpr int kList = 128;
 struct Partial {
   Sums* sums;      // [rows * splits]
-  uint64_t* keys;  // [rows * splits][top]
+  uint64_t* keys;  // [rows * splits][kList]
 };
+__device__ __forceinline__ void put_list(uint64_t* out, uint64_t list) {  // one wave
+  const int lane = threadIdx.x & 63;
+  out[lane] = list;
+  out[64 + lane] = 0;
+}
 
 template <class T, bool TOP>
 __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a, Partial part) {
@@ -215,23 +237,7 @@ __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a, Partial pa
   bool primed = false;
   auto fetch = [&](int base, uint4 (&v)[kUnroll]) {
 #pragma unroll
-    for (int k = 0; k < kUnroll; ++k) {
-      const int i = base + (k * kThreads + t) * N;
-      if (i + N <= e) {
-        v[k] = load16(x + i);
-      } else {  // the row's end, or beyond it
-        uint32_t w[4] = {Vec<T>::kFill, Vec<T>::kFill, Vec<T>::kFill, Vec<T>::kFill};
-        for (int j = 0; j < N && i + j < e; ++j) {
-          if constexpr (N == 8) {
-            const uint32_t h = x[i + j];
-            w[j >> 1] = j & 1 ? (w[j >> 1] & 0xFFFFu) | (h << 16) : (w[j >> 1] & 0xFFFF0000u) | h;
-          } else {
-            w[j] = __float_as_uint(x[i + j]);
-          }
-        }
-        v[k] = uint4{w[0], w[1], w[2], w[3]};
-      }
-    }
+    for (int k = 0; k < kUnroll; ++k) v[k] = fetch16<T>(x, base + (k * kThreads + t) * N, e);
   };
   constexpr int kStep = kThreads * kUnroll * N;
   uint4 nxt[kUnroll];
@@ -292,38 +298,200 @@ __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a, Partial pa
     if constexpr (TOP) best.list = merge_lists(best.list, wlist[i][lane]);
   }
   if (a.splits == 1) {
-    finish<T>(a, row, s, best.list);
+    if (lane == 0) finish_row<T>(a, row, s);
+    if (TOP && lane < a.top) finish_top(a, row, s, lane, best.list);
   } else {
     if (lane == 0) part.sums[blockIdx.x] = s;
-    if (TOP && lane < a.top) part.keys[(int64_t)blockIdx.x * a.top + lane] = best.list;
+    if (TOP) put_list(part.keys + (int64_t)blockIdx.x * kList, lane < a.top ? best.list : 0);
   }
 }
 
-// Joins a row's splits: a block a row, each wave a share of them.
+// ---- few rows: latency ----
+// The largest value, cut to its upper 16 bits, that at least n of a block's
+// threads reach. One barrier; mine: LDS of a word a thread.
+__device__ __forceinline__ uint32_t nth_floor(uint32_t v, int n, uint32_t* mine) {
+  mine[threadIdx.x] = v;
+  __syncthreads();
+  const uint4 w = reinterpret_cast<const uint4*>(mine)[threadIdx.x & 63];  // each wave looks at all of them
+  uint32_t t = 0;
+#pragma unroll
+  for (int bit = 31; bit >= 16; --bit) {
+    const uint32_t c = t | 1u << bit;
+    const int reach = __popcll(__ballot(w.x >= c)) + __popcll(__ballot(w.y >= c)) + __popcll(__ballot(w.z >= c)) +
+                      __popcll(__ballot(w.w >= c));
+    if (reach >= n) t = c;
+  }
+  return t;
+}
+
+// A part of a row in registers, kHeld loads a thread. The block's best lie at or
+// above a value that the largest entries of `top` threads reach: hardly more
+// entries than that (21 for 20, 73 for 64 of 4096 normal values), which go out in
+// any order. (More than kList: sorted lists as above.)
+constexpr int kHeld = 2;
+template <class T, bool TOP>
+__global__ __launch_bounds__(kThreads) void k_logprobs_part(LogprobArgs a, Partial part) {
+  constexpr int N = Vec<T>::N;
+  __shared__ Sums wsum[kWaves];
+  __shared__ __align__(16) uint32_t tops[kThreads];
+  __shared__ int count;
+  __shared__ uint64_t wlist[kWaves][64];
+  const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
+  const int row = blockIdx.x / a.splits, split = blockIdx.x - row * a.splits;
+  const T* x = reinterpret_cast<const T*>(a.logits) + (int64_t)row * a.ld;
+  const int b = split * a.split_len, e = min(a.vocab - b, a.split_len) + b;
+  const float c = a.scale * kLog2e;
+  if (t == 0) count = 0;
+  uint4 raw[kHeld];
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k) raw[k] = fetch16<T>(x, b + (k * kThreads + t) * N, e);
+  float v[kHeld][N], top = ninf();
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k) {
+    Vec<T>::unpack(raw[k], v[k]);
+#pragma unroll
+    for (int j = 0; j < N; ++j) top = fmaxf(top, v[k][j]);
+  }
+  uint32_t o[kHeld][N], mine = 0;
+  if constexpr (TOP) {
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k)
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        o[k][j] = b + (k * kThreads + t) * N + j < e ? ord_key(v[k][j]) : 0u;
+        mine = max(mine, o[k][j]);
+      }
+  }
+#pragma unroll
+  for (int i = 1; i < 64; i <<= 1) top = fmaxf(top, __shfl_xor(top, i));
+  Sums s{fmaxf(top, kStart), 0.0f, 0.0f};
+  float ss[4] = {}, uu[4] = {};
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k)
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const float d = (v[k][j] - s.m) * c, p = __builtin_amdgcn_exp2f(d);
+      ss[j & 3] += p;
+      uu[j & 3] = fmaf(p, fmaxf(d, -200.0f), uu[j & 3]);
+    }
+  s.s = (ss[0] + ss[1]) + (ss[2] + ss[3]);
+  s.u = (uu[0] + uu[1]) + (uu[2] + uu[3]);
+#pragma unroll
+  for (int i = 1; i < 64; i <<= 1) {
+    s.s += __shfl_xor(s.s, i);
+    s.u += __shfl_xor(s.u, i);
+  }
+  if (lane == 0) wsum[wave] = s;
+  uint32_t f = 0;
+  if constexpr (TOP) f = nth_floor(mine, a.top, tops);
+  else __syncthreads();
+  if (t == 0) {
+    for (int i = 1; i < kWaves; ++i) s = join(s, wsum[i], c);
+    part.sums[blockIdx.x] = s;
+  }
+  if constexpr (TOP) {
+    int n = 0;
+    uint64_t who[kHeld][N];
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k)
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        who[k][j] = __ballot(o[k][j] >= f && b + (k * kThreads + t) * N + j < e);
+        n += __popcll(who[k][j]);
+      }
+    int at = 0;
+    if (lane == 0) at = atomicAdd(&count, n);
+    at = __builtin_amdgcn_readfirstlane(at);
+    const uint64_t below = (1ull << lane) - 1;
+    uint64_t* list = wlist[0];
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k)
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const int p = at + __popcll(who[k][j] & below);
+        if (((who[k][j] >> lane) & 1u) && p < kList)
+          list[p] = comp_key(v[k][j], (uint32_t)(b + (k * kThreads + t) * N + j));
+        at += __popcll(who[k][j]);
+      }
+    __syncthreads();
+    const int total = count;
+    uint64_t* out = part.keys + (int64_t)blockIdx.x * kList;
+    if (total <= kList) {
+      if (t < kList) out[t] = t < total ? list[t] : 0;
+      return;
+    }
+    __syncthreads();  // (wlist is read by no one any more)
+    Best best{0, 0, ninf()};
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) {
+      const int i = b + (k * kThreads + t) * N;
+      take<T>(best, v[k], i, e - i, a.top);
+    }
+    wlist[wave][lane] = best.list;
+    __syncthreads();
+    if (wave) return;
+    for (int i = 1; i < kWaves; ++i) best.list = merge_lists(best.list, wlist[i][lane]);
+    put_list(out, lane < a.top ? best.list : 0);
+  }
+}
+
+// Joins a row's splits: a block a row. The best entries lie at or above a value
+// that `top` threads' own reach; of those, each counts how many come before it.
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_logprobs_join(LogprobArgs a, Partial part) {
+  constexpr int kMost = 512;
   __shared__ Sums wsum[kWaves];
-  __shared__ uint64_t wlist[kWaves][64];
+  __shared__ __align__(16) uint32_t tops[kThreads];
+  __shared__ int count;
+  __shared__ uint64_t wlist[kMost];
   const int t = threadIdx.x, wave = t >> 6, lane = t & 63, row = blockIdx.x;
   const float c = a.scale * kLog2e;
+  const uint64_t* keys = part.keys + (int64_t)row * a.splits * kList;
+  const int slots = a.top > 0 ? a.splits * kList : 0;
+  if (t == 0) count = 0;
+  uint32_t mine = 0;
+#pragma unroll 8
+  for (int i = t; i < slots; i += kThreads) mine = max(mine, (uint32_t)(keys[i] >> 32));
   Sums s{kStart, 0.0f, 0.0f};
   for (int i = t; i < a.splits; i += kThreads) s = join(s, part.sums[(int64_t)row * a.splits + i], c);
   s = wave_join(s, c);
-  uint64_t list = 0;
-  if (a.top > 0)
-    for (int i = wave; i < a.splits; i += kWaves) {
-      const uint64_t k = lane < a.top ? part.keys[((int64_t)row * a.splits + i) * a.top + lane] : 0;
-      list = merge_lists(list, k);
-    }
   if (lane == 0) wsum[wave] = s;
-  wlist[wave][lane] = list;
+  const uint32_t f = nth_floor(mine, a.top, tops);
+  s = wsum[0];
+  for (int i = 1; i < kWaves; ++i) s = join(s, wsum[i], c);
+  if (t == 0) finish_row<T>(a, row, s);
+  if (a.top == 0) return;
+
+  for (int i = t; i < slots; i += kThreads) {  // whole waves: slots is a multiple of 64
+    const uint64_t k = keys[i];
+    const uint64_t who = __ballot(k != 0 && (uint32_t)(k >> 32) >= f);
+    if (!who) continue;
+    int at = 0;
+    if (lane == 0) at = atomicAdd(&count, __popcll(who));
+    at = __builtin_amdgcn_readfirstlane(at) + __popcll(who & ((1ull << lane) - 1));
+    if (((who >> lane) & 1u) && at < kMost) wlist[at] = k;
+  }
+  __syncthreads();
+  const int total = count;
+  if (total <= kMost) {
+    for (int i = t; i < total; i += kThreads) {
+      const uint64_t k = wlist[i];
+      int before = 0;
+      for (int j = 0; j < total; ++j) before += wlist[j] > k ? 1 : 0;
+      if (before < a.top) finish_top(a, row, s, before, k);
+    }
+    if (t >= total && t < a.top) finish_top(a, row, s, t, 0);
+    return;
+  }
+  // many equal values: sorted lists
+  __syncthreads();
+  uint64_t list = 0;
+  for (int i = wave; i < slots / 64; i += kWaves) list = merge_lists(list, sort_list(keys[i * 64 + lane]));
+  wlist[wave * 64 + lane] = list;
   __syncthreads();
   if (wave) return;
-  for (int i = 1; i < kWaves; ++i) {
-    s = join(s, wsum[i], c);
-    list = merge_lists(list, wlist[i][lane]);
-  }
-  finish<T>(a, row, s, list);
+  for (int i = 1; i < kWaves; ++i) list = merge_lists(list, wlist[i * 64 + lane]);
+  if (lane < a.top) finish_top(a, row, s, lane, list);
 }
 
 // ---- gradient: one pass, bound by reading and writing the logits once ----
@@ -412,7 +580,10 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_backward(const T* logits,
 template <class T>
 hipError_t run_forward(const LogprobArgs& a, const Partial& p, hipStream_t st) {
   const dim3 grid((unsigned)(a.rows * a.splits));
-  if (a.top > 0) k_logprobs<T, true><<<grid, kThreads, 0, st>>>(a, p);
+  if (a.parts) {
+    if (a.top > 0) k_logprobs_part<T, true><<<grid, kThreads, 0, st>>>(a, p);
+    else k_logprobs_part<T, false><<<grid, kThreads, 0, st>>>(a, p);
+  } else if (a.top > 0) k_logprobs<T, true><<<grid, kThreads, 0, st>>>(a, p);
   else k_logprobs<T, false><<<grid, kThreads, 0, st>>>(a, p);
   if (a.splits > 1) k_logprobs_join<T><<<dim3((unsigned)a.rows), kThreads, 0, st>>>(a, p);
   return hipGetLastError();
@@ -421,8 +592,17 @@ hipError_t run_forward(const LogprobArgs& a, const Partial& p, hipStream_t st) {
 }  // namespace
 
 void logprob_shape(LogprobArgs& a) {
-  // Rows are split until there are four blocks a CU, down to one load a thread.
+  // Few rows: parts that a block holds in registers, eight blocks a CU at most
+  // (8 rows of 131072: 32 parts each). More rows are split until there are four
+  // blocks a CU, down to one load a thread.
   const int n = a.bf16 ? 8 : 4, unit = kThreads * n;
+  const int64_t parts = ((int64_t)a.vocab + kHeld * unit - 1) / (kHeld * unit);
+  a.parts = parts > 1 && parts * a.rows <= 2048;
+  if (a.parts) {
+    a.split_len = kHeld * unit;
+    a.splits = (int)parts;
+    return;
+  }
   const int64_t most = ((int64_t)a.vocab + unit - 1) / unit;
   int64_t s = a.rows > 0 ? (1024 + a.rows - 1) / a.rows : 1;
   s = s > most ? most : s;
@@ -436,7 +616,7 @@ size_t logprob_workspace_bytes(LogprobArgs a) {
   logprob_shape(a);
   if (a.splits == 1) return 256;
   const size_t n = (size_t)a.rows * a.splits;
-  return 256 + (n * sizeof(Sums) + 255) / 256 * 256 + n * a.top * 8;
+  return 256 + (n * sizeof(Sums) + 255) / 256 * 256 + (a.top > 0 ? n * kList * 8 : 0);
 }
 
 hipError_t launch_logprobs(LogprobArgs a, void* workspace, hipStream_t st) {

@@ -1,5 +1,7 @@
 // Paged serving cache: the plan of a step (block tables and slot maps from the
 // requests' lengths) and the 4-bit key/value pages (writing and reading rows).
+#include <algorithm>
+
 #include "cache4.hpp"
 #include "internal.hpp"
 
@@ -15,11 +17,12 @@ namespace {
 // One launch: every block repeats the two prefix sums in LDS (8 bytes a
 // request) and then takes its slice of the tokens, of the new pages and of the
 // requests; a search in the sums tells whose they are. Blocks share nothing, so
-// there is no second launch, no flag between blocks and no atomic. The call is
-// bound by its latency: the loads of the lengths, the sums and a token's
-// dependent load of its page.
+// there is no second launch, no flag between blocks and no atomic. The first
+// blocks do the tokens, the others the pages and requests, side by side. With
+// TOKENS = 4 a thread takes four consecutive tokens, which then mostly share their
+// request and page: one search and one dependent load for all. The call is bound
+// by its latency: the loads of the lengths, the sums and the load of the page.
 // ---------------------------------------------------------------------------
-constexpr int kPlanThreads = 256;
 constexpr uint32_t kPlanTop = 0x7FFFFFFFu;
 
 // Both operands are at most kPlanTop; sums stop there (associative, monotone).
@@ -52,8 +55,10 @@ __device__ __forceinline__ Need need_of(const PlanArgs& a, int r) {
 }
 
 // In-place exclusive prefix sums of two arrays of n entries, the totals at [n].
-__device__ void plan_sums(uint32_t* x, uint32_t* y, int n, uint32_t* part) {
-  const int t = threadIdx.x, per = (n + kPlanThreads - 1) / kPlanThreads;
+template <int THREADS>
+__device__ __forceinline__ void plan_sums(uint32_t* x, uint32_t* y, int n, uint32_t* part) {
+  constexpr int kWaves = THREADS / 64;
+  const int t = threadIdx.x, per = (n + THREADS - 1) / THREADS;
   const int b = min(t * per, n), e = min(b + per, n);
   uint32_t sx = 0, sy = 0;
   for (int i = b; i < e; ++i) {
@@ -72,7 +77,7 @@ __device__ void plan_sums(uint32_t* x, uint32_t* y, int n, uint32_t* part) {
   }
   if (lane == 63) {
     part[w] = ix;
-    part[4 + w] = iy;
+    part[kWaves + w] = iy;
   }
   // exclusive inside the wave
   uint32_t bx = __shfl_up(ix, 1), by = __shfl_up(iy, 1);
@@ -80,7 +85,7 @@ __device__ void plan_sums(uint32_t* x, uint32_t* y, int n, uint32_t* part) {
   __syncthreads();
   for (int i = 0; i < w; ++i) {
     bx = sat_add(bx, part[i]);
-    by = sat_add(by, part[4 + i]);
+    by = sat_add(by, part[kWaves + i]);
   }
   for (int i = b; i < e; ++i) {
     const uint32_t vx = x[i], vy = y[i];
@@ -89,34 +94,37 @@ __device__ void plan_sums(uint32_t* x, uint32_t* y, int n, uint32_t* part) {
     bx = sat_add(bx, vx);
     by = sat_add(by, vy);
   }
-  if (t == kPlanThreads - 1) {
+  if (t == THREADS - 1) {
     x[n] = bx;
     y[n] = by;
   }
   __syncthreads();
 }
 
-__global__ __launch_bounds__(kPlanThreads) void k_paged_plan(PlanArgs a) {
+template <int THREADS, int TOKENS>
+__global__ __launch_bounds__(THREADS) void k_paged_plan(PlanArgs a, int token_blocks) {
   extern __shared__ uint32_t lds[];
-  __shared__ uint32_t part[8];
+  __shared__ uint32_t part[2 * THREADS / 64];
   uint32_t* tok = lds;                  // [R + 1] prefix sums of the new tokens
   uint32_t* pag = lds + a.R + 1;        // [R + 1] prefix sums of the new pages
   const int t = threadIdx.x;
-  for (int r = t; r < a.R; r += kPlanThreads) {
+#pragma unroll 4
+  for (int r = t; r < a.R; r += THREADS) {
     const Need n = need_of(a, r);
     tok[r] = n.add;
     pag[r] = n.pages;
   }
   const int used = min(max(*a.free_used, 0), a.free_count);
   __syncthreads();
-  plan_sums(tok, pag, a.R, part);
+  plan_sums<THREADS>(tok, pag, a.R, part);
 
   // Pages are handed out in request order until one request's do not fit: the
   // sums pass the number of free pages there for good, so the pages taken are
   // the largest sum within it.
   const uint32_t avail = (uint32_t)(a.free_count - used);
   const uint32_t taken = pag[upper(pag, 0, a.R + 1, avail) - 1];
-  const int stride = gridDim.x * kPlanThreads, at = blockIdx.x * kPlanThreads + t;
+  if ((int)blockIdx.x >= token_blocks) {
+  const int stride = ((int)gridDim.x - token_blocks) * THREADS, at = ((int)blockIdx.x - token_blocks) * THREADS + t;
   if (at == 0) *a.free_out = used + (int)taken;
   for (int r = at; r <= a.R; r += stride) {
     a.cu[r] = (int)tok[r];
@@ -131,23 +139,48 @@ __global__ __launch_bounds__(kPlanThreads) void k_paged_plan(PlanArgs a) {
     const Need n = need_of(a, r);
     a.table[(int64_t)r * a.table_ld + n.held + (i - pag[r])] = a.free_list[used + i];
   }
+  return;
+  }
   const uint32_t tokens = tok[a.R];
-  for (int i = at; i < a.capacity; i += stride) {
-    int64_t slot = -1;
-    int pos = -1;
-    if ((uint32_t)i < tokens) {
-      const int r = upper(tok, 0, a.R, i) - 1;
-      const Need n = need_of(a, r);
-      const uint32_t p = sat_add(n.ctx, i - tok[r]);
-      pos = (int)p;
-      if (!n.longer && (n.pages == 0 || pag[r + 1] <= avail)) {
-        const uint32_t b = p >> a.shift;
-        const int page = b < n.held ? a.table[(int64_t)r * a.table_ld + b] : a.free_list[used + pag[r] + (b - n.held)];
-        if (page >= 0) slot = ((int64_t)page << a.shift) + (p & ((1u << a.shift) - 1u));
+  const int64_t stride = (int64_t)token_blocks * THREADS * TOKENS;
+  for (int64_t i0 = ((int64_t)blockIdx.x * THREADS + t) * TOKENS; i0 < a.capacity; i0 += stride) {
+    int64_t slot[TOKENS];
+    int pos[TOKENS];
+    uint32_t first = 0, end = 0, block = 0;  // the request's tokens, and the page looked up
+    int r = 0, page = -1;
+    Need n{};
+    bool served = false;
+#pragma unroll
+    for (int j = 0; j < TOKENS; ++j) {
+      const uint32_t i = (uint32_t)i0 + j;
+      slot[j] = -1;
+      pos[j] = -1;
+      if (i >= tokens) continue;
+      const bool next = i >= end;
+      if (next) {
+        r = upper(tok, 0, a.R, i) - 1;
+        n = need_of(a, r);
+        first = tok[r];
+        end = tok[r + 1];
+        served = !n.longer && (n.pages == 0 || pag[r + 1] <= avail);
       }
+      const uint32_t p = sat_add(n.ctx, i - first), b = p >> a.shift;
+      pos[j] = (int)p;
+      if (!served) continue;
+      if (next || b != block) {
+        block = b;
+        page = b < n.held ? a.table[(int64_t)r * a.table_ld + b] : a.free_list[used + pag[r] + (b - n.held)];
+      }
+      if (page >= 0) slot[j] = ((int64_t)page << a.shift) + (p & ((1u << a.shift) - 1u));
     }
-    a.slots[i] = slot;
-    a.positions[i] = pos;
+    if (i0 + TOKENS <= a.capacity) {
+      __builtin_memcpy(a.slots + i0, slot, sizeof(slot));
+      __builtin_memcpy(a.positions + i0, pos, sizeof(pos));
+    } else {
+#pragma unroll
+      for (int j = 0; j < TOKENS; ++j)
+        if (i0 + j < a.capacity) a.slots[i0 + j] = slot[j], a.positions[i0 + j] = pos[j];
+    }
   }
 }
 
@@ -230,18 +263,29 @@ __global__ __launch_bounds__(256) void k_cache4_read(Cache4 c, const uint8_t* co
 
 }  // namespace
 
-hipError_t launch_paged_plan(const PlanArgs& a, hipStream_t st) {
-  const int64_t work = a.capacity > a.R ? a.capacity : a.R;
-  int64_t blocks = (work + 2 * kPlanThreads - 1) / (2 * kPlanThreads);
-  blocks = blocks < 1 ? 1 : blocks > 512 ? 512 : blocks;
+template <int THREADS, int TOKENS>
+static hipError_t run_plan(const PlanArgs& a, hipStream_t st) {
+  constexpr int64_t per = THREADS * TOKENS;
+  const int64_t tokens = std::min(((int64_t)a.capacity + per - 1) / per, (int64_t)512);
+  const int64_t others = std::min(((int64_t)a.R + THREADS) / THREADS, (int64_t)32);
   const size_t lds = 8 * ((size_t)a.R + 1);
   if (lds > 64 * 1024) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_paged_plan),
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_paged_plan<THREADS, TOKENS>),
                                              hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
   }
-  k_paged_plan<<<dim3((unsigned)blocks), kPlanThreads, lds, st>>>(a);
+  k_paged_plan<THREADS, TOKENS><<<dim3((unsigned)(tokens + others)), THREADS, lds, st>>>(a, (int)tokens);
   return hipGetLastError();
+}
+
+hipError_t launch_paged_plan(const PlanArgs& a, hipStream_t st) {
+  // Every block sums all requests: wide blocks where there are many, narrow
+  // ones for few, whose barriers cost less. Several tokens a thread only where
+  // requests have several (64 decoding requests: 6.5 us with four, 4.2 with one;
+  // 4096 requests and 540K tokens: 24 us with one and narrow blocks).
+  const bool several = a.capacity > 4 * (int64_t)a.R;
+  if (a.R > 512) return several ? run_plan<1024, 4>(a, st) : run_plan<1024, 1>(a, st);
+  return several ? run_plan<256, 4>(a, st) : run_plan<256, 1>(a, st);
 }
 
 hipError_t launch_cache4_append(const void* k, const void* v, bool f32, int64_t k_stride, int64_t v_stride,

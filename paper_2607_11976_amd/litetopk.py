@@ -558,20 +558,35 @@ def dsa_union(topk_idx: torch.Tensor, group: int, stream=None):
 # serving: page plan, 4-bit cache, attention over it, log probabilities
 # ---------------------------------------------------------------------------
 
+# These calls are short beside what surrounds them in a decode step, so their
+# checks build no message before one is needed, and the stream handle is read
+# without making a Stream object.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream_of(stream, t: torch.Tensor) -> int:
+    """The HIP stream to work on: `stream`, or the current one of t's device."""
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is not None:
+        return _raw_stream(t.device.index)
+    return torch.cuda.current_stream(t.device).cuda_stream
+
+
 def _int32(t: Optional[torch.Tensor], n: Optional[int], name: str):
-    if t is None:
-        return
-    _on_gpu(t)
-    _need(t.dtype == torch.int32 and t.dim() == 1 and (n is None or t.numel() == n),
-          "%s must be a contiguous int32 vector%s on the GPU" % (name, "" if n is None else " of %d entries" % n))
+    if t is not None and not (t.is_cuda and t.dtype is torch.int32 and t.dim() == 1 and t.is_contiguous()
+                              and (n is None or t.numel() == n)):
+        raise LiteTopKError("%s must be a contiguous int32 vector%s on the GPU"
+                            % (name, "" if n is None else " of %d entries" % n))
 
 
 def _table(t: torch.Tensor, rows: int):
     """block_table int32 [rows, width] with unit column stride."""
-    _need(t.is_cuda and t.dtype == torch.int32 and t.dim() == 2 and t.shape[0] == rows
-          and (t.numel() == 0 or t.shape[1] == 1 or t.stride(1) == 1),
+    width = t.shape[-1]
+    _need(t.is_cuda and t.dtype is torch.int32 and t.dim() == 2 and t.shape[0] == rows
+          and (t.numel() == 0 or width == 1 or t.stride(1) == 1),
           "block_table must be an int32 [requests, pages] GPU matrix with unit column stride")
-    return max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1], t.shape[1]
+    return t.stride(0) if rows > 1 and width > 0 else width, width
 
 
 def _used_on(stream, *ts):
@@ -608,14 +623,14 @@ def paged_plan(context_lens: torch.Tensor, new_lens: torch.Tensor, block_table: 
     _need(token_capacity >= 0, "token_capacity must not be negative")
     ld, width = _table(block_table, n)
     dev = context_lens.device
-    p = PagedPlan(torch.empty(n + 1, dtype=torch.int32, device=dev), torch.empty(n, dtype=torch.int32, device=dev),
-                  torch.empty(token_capacity, dtype=torch.int64, device=dev),
-                  torch.empty(token_capacity, dtype=torch.int32, device=dev),
-                  torch.empty(1, dtype=torch.int32, device=dev), torch.empty(n, dtype=torch.int32, device=dev))
+    # the 32-bit results in one allocation
+    cu, seq, used, status, positions = torch.empty(
+        3 * n + 2 + token_capacity, dtype=torch.int32, device=dev).split((n + 1, n, 1, n, token_capacity))
+    p = PagedPlan(cu, seq, torch.empty(token_capacity, dtype=torch.int64, device=dev), positions, used, status)
     st = lt_paged_plan(_ptr(context_lens), _ptr(new_lens), n, page_size, _ptr(block_table), ld, width,
                        _ptr(free_pages), free_pages.numel(), _ptr(free_used), token_capacity, _ptr(p.cu_tokens),
                        _ptr(p.seq_lens), _ptr(p.slots), _ptr(p.positions), _ptr(p.free_used), _ptr(p.status),
-                       _stream(stream))
+                       _stream_of(stream, context_lens))
     _check(st, "lt_paged_plan")
     _used_on(stream, *p)
     return p
@@ -641,9 +656,9 @@ def _cache4(codes: torch.Tensor, scales: torch.Tensor):
 
 def _rows_of(t: torch.Tensor, heads: int, d: int, name: str) -> int:
     """Stride between the rows of a [rows, heads, d] tensor whose rows are contiguous."""
-    _need(t.is_cuda and t.dim() == 3 and tuple(t.shape[1:]) == (heads, d)
-          and (t.numel() == 0 or ((d == 1 or t.stride(2) == 1) and (heads == 1 or t.stride(1) == d))),
-          "%s must be [rows, %d, %d] on the GPU with contiguous rows" % (name, heads, d))
+    if not (t.is_cuda and t.dim() == 3 and t.shape[1] == heads and t.shape[2] == d
+            and (t.is_contiguous() or (t.stride(2) == 1 and (heads == 1 or t.stride(1) == d)))):
+        raise LiteTopKError("%s must be [rows, %d, %d] on the GPU with contiguous rows" % (name, heads, d))
     return t.stride(0) if t.shape[0] > 1 else heads * d
 
 
@@ -659,7 +674,7 @@ def cache4_append(k: torch.Tensor, v: torch.Tensor, codes: torch.Tensor, scales:
     _need(slots.dtype == torch.int64 and slots.dim() == 1 and slots.numel() == k.shape[0],
           "slots must be int64 [rows]")
     st = lt_cache4_append(_ptr(k), _ptr(v), _dtype_code(k), ks, vs, k.shape[0], _ptr(codes), _ptr(scales), pages,
-                          page, heads, d, _ptr(slots), _stream(stream))
+                          page, heads, d, _ptr(slots), _stream_of(stream, k))
     _check(st, "lt_cache4_append")
 
 
@@ -673,7 +688,7 @@ def cache4_read(codes: torch.Tensor, scales: torch.Tensor, slots: torch.Tensor, 
     k = torch.empty((n, heads, d), dtype=torch.bfloat16, device=slots.device)
     v = torch.empty_like(k)
     st = lt_cache4_read(_ptr(codes), _ptr(scales), pages, page, heads, d, _ptr(slots), n, _ptr(k), _ptr(v),
-                        _stream(stream))
+                        _stream_of(stream, slots))
     _check(st, "lt_cache4_read")
     _used_on(stream, k, v)
     return k, v
@@ -710,7 +725,7 @@ def cache4_attention(q: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
               and (selected.shape[1] == 1 or selected.stride(1) == 1 or tokens == 0),
               "selected must be an int32 [T, k] GPU matrix with unit column stride")
         k = selected.shape[1]
-        sel_ld = max(selected.stride(0), k) if tokens > 1 else k
+        sel_ld = selected.stride(0) if tokens > 1 else k
     out = torch.empty((tokens, hq, d), dtype=torch.bfloat16, device=q.device)
     lse = torch.empty((tokens, hq), dtype=torch.float32, device=q.device) if return_lse else None
     need = lt_cache4_attention_workspace_size(tokens, n, hq, hkv, d, k)
@@ -721,7 +736,7 @@ def cache4_attention(q: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
                              _ptr(block_table), ld, width, _ptr(cu_tokens), _ptr(seq_lens), n, _ptr(visible_start),
                              _ptr(visible_end), _ptr(selected), sel_ld, k, _ptr(selected_start),
                              d ** -0.5 if scale is None else scale, _ptr(out), _ptr(lse), _ptr(workspace),
-                             workspace.numel(), _stream(stream))
+                             workspace.numel(), _stream_of(stream, q))
     _check(st, "lt_cache4_attention")
     _used_on(stream, out, lse, workspace)
     return out, lse
@@ -743,7 +758,7 @@ def _logits(logits: torch.Tensor, tokens: torch.Tensor) -> int:
     _on_gpu(tokens)
     _need(tokens.dtype == torch.int64 and tokens.dim() == 1 and tokens.numel() == logits.shape[0],
           "tokens must be int64 [rows]")
-    return max(logits.stride(0), logits.shape[1]) if logits.shape[0] > 1 else logits.shape[1]
+    return logits.stride(0) if logits.shape[0] > 1 and logits.shape[1] > 0 else logits.shape[1]
 
 
 def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0, scale: float = 1.0,
@@ -759,12 +774,14 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0, sca
     _need(need > 0, "unsupported shape for lt_token_logprobs (top must be 0..%d)" % LT_LOGPROB_MAX_TOP)
     if workspace is None:
         workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-    f = torch.empty((3, rows), dtype=torch.float32, device=dev)
-    r = TokenLogprobs(f[0], f[1], f[2], torch.empty((rows, min(top, vocab)), dtype=torch.int32, device=dev),
-                      torch.empty((rows, min(top, vocab)), dtype=torch.float32, device=dev))
-    st = lt_token_logprobs(_ptr(logits), dt, ld, rows, vocab, _ptr(tokens), scale, min(top, vocab), _ptr(r.logprob),
+    n = min(top, vocab)
+    f = torch.empty(rows * (3 + n), dtype=torch.float32, device=dev)
+    logprob, entropy, lse, best = f.split((rows, rows, rows, rows * n))
+    r = TokenLogprobs(logprob, entropy, lse, torch.empty((rows, n), dtype=torch.int32, device=dev),
+                      best.view(rows, n))
+    st = lt_token_logprobs(_ptr(logits), dt, ld, rows, vocab, _ptr(tokens), scale, n, _ptr(r.logprob),
                            _ptr(r.entropy), _ptr(r.lse), _ptr(r.top_index), _ptr(r.top_logprob), _ptr(workspace),
-                           workspace.numel(), _stream(stream))
+                           workspace.numel(), _stream_of(stream, logits))
     _check(st, "lt_token_logprobs")
     _used_on(stream, f, r.top_index, r.top_logprob, workspace)
     return r
@@ -786,7 +803,7 @@ def token_logprobs_backward(logits: torch.Tensor, tokens: torch.Tensor, lse: tor
     out = torch.empty((rows, pad), dtype=logits.dtype, device=logits.device)[:, :vocab]
     st = lt_token_logprobs_backward(_ptr(logits), _dtype_code(logits), ld, rows, vocab, _ptr(tokens), scale, _ptr(lse),
                                     _ptr(entropy), _ptr(grad_logprob), _ptr(grad_entropy), _ptr(out), pad,
-                                    _stream(stream))
+                                    _stream_of(stream, logits))
     _check(st, "lt_token_logprobs_backward")
     _used_on(stream, out)
     return out
