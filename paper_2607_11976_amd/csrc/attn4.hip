@@ -907,38 +907,40 @@ __global__ __launch_bounds__(256, 2) void k_attn4_many(Attn4Args a) {
   const int steps = (keys.k1 - keys.k0 + KEYS - 1) / KEYS;
   const int kw = mine * kKRow<D> + part * (D / 2);
   const int vw = KEYS * kKRow<D> + mine * 2 * D + ((part * (D / 32)) ^ swizzle<D>(mine)) * 16;
-  // in flight: the codes of two steps, the pages of a third, the places of a fourth
-  KeyRegs<D> kvs[2];
-  int page[2], pos2, raw2, raw3;
+  // in flight: the codes of kAhead steps, the pages of one more, the places of a
+  // second. Listed keys lie anywhere: two steps ahead.
+  constexpr int kAhead = LIST ? 2 : 1;
+  KeyRegs<D> kvs[kAhead];
+  int page[kAhead], pos1, raw1, raw2;
   auto at_step = [&](int s) { return keys.k0 + s * KEYS + mine; };
   {
-    int p[3], raw[3];
+    int p[kAhead + 1], raw[kAhead + 1];
 #pragma unroll
-    for (int i = 0; i < 3; ++i) raw[i] = keys.fetch(a, at_step(i));
-    raw3 = keys.fetch(a, at_step(3));
+    for (int i = 0; i <= kAhead; ++i) raw[i] = keys.fetch(a, at_step(i));
+    raw2 = keys.fetch(a, at_step(kAhead + 1));
 #pragma unroll
-    for (int i = 0; i < 3; ++i) {
+    for (int i = 0; i <= kAhead; ++i) {
       p[i] = keys.position(at_step(i), raw[i]);
       raw[i] = keys.look(a, p[i]);
     }
-    pos2 = p[2];
-    raw2 = raw[2];
+    pos1 = p[kAhead];
+    raw1 = raw[kAhead];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < kAhead; ++i) {
       page[i] = keys.page(a, p[i], raw[i]);
       load_key<D>(a, page[i], p[i], it.head, part, kvs[i]);
     }
   }
-  auto stage = [&](int s, auto bc) {  // decode step s into buffer b, start loading step s + 2
-    constexpr int b = decltype(bc)::value;
-    KeyRegs<D>& kv = kvs[b];
+  auto stage = [&](int s, auto bc) {  // decode step s into buffer b, start loading step s + kAhead
+    constexpr int b = decltype(bc)::value, c = b % kAhead;
+    KeyRegs<D>& kv = kvs[c];
     // loads come back in order: the next page and place are asked for before
     // the codes, so that waiting for them does not wait for those
-    const int now = keys.page(a, pos2, raw2), at = pos2;
-    pos2 = keys.position(at_step(s + 3), raw3);
-    raw2 = keys.look(a, pos2);
-    raw3 = keys.fetch(a, at_step(s + 4));
-    const bool ok = page[b] >= 0;
+    const int now = keys.page(a, pos1, raw1), at = pos1;
+    pos1 = keys.position(at_step(s + kAhead + 1), raw2);
+    raw1 = keys.look(a, pos1);
+    raw2 = keys.fetch(a, at_step(s + kAhead + 2));
+    const bool ok = page[c] >= 0;
     const float ks = __uint_as_float(key_byte<D>(kv, part, ok) << 23);
     uint32_t vb = value_byte<D>(kv, part, ok);
     const int j0 = keys.k0 + s * KEYS;
@@ -962,7 +964,7 @@ __global__ __launch_bounds__(256, 2) void k_attn4_many(Attn4Args a) {
       *reinterpret_cast<bf16x8_t*>(buf + kw + 16 * n) = decode8(kv.k[n], ks);
       *reinterpret_cast<bf16x8_t*>(buf + (vw ^ (16 * n))) = decode8(kv.v[n], vs);
     }
-    page[b] = now;
+    page[c] = now;
     load_key<D>(a, now, at, it.head, part, kv);
   };
 
@@ -979,10 +981,12 @@ __global__ __launch_bounds__(256, 2) void k_attn4_many(Attn4Args a) {
     constexpr int b = decltype(bc)::value;
     const int j0 = keys.k0 + s * KEYS + wk * 32;
     // The decoding of the next step runs beside the first products, the weights
-    // of each 16 keys beside the second products of the 16 before.
+    // of each 16 keys beside the second products of the 16 before. A wave in its
+    // first products goes before one that weighs (prefill 975 -> 950 us).
     // (Rows or keys that there are not take part like any other: a branch around
     // them would make every path wait for all loads in flight.)
     const uint8_t* buf = lds + b * kBuf;
+    __builtin_amdgcn_s_setprio(1);
     f32x16_t x[KT];
 #pragma unroll
     for (int u = 0; u < KT; ++u) x[u] = f32x16_t{};
@@ -1008,6 +1012,7 @@ __global__ __launch_bounds__(256, 2) void k_attn4_many(Attn4Args a) {
       asm volatile("");  // a branch, not selects: most steps need no mask
       col.template mask<KT, LIST>(x, valid, j0);
     }
+    __builtin_amdgcn_s_setprio(0);
     col.template renew<KT>(x, a.scale_log2, a.slack);
     bf16x8_t p = col.weights(x[0], 0, a.scale_log2);
 #pragma unroll
