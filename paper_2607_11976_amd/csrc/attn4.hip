@@ -175,7 +175,8 @@ __device__ __forceinline__ Line line_of(uint64_t end) {
 template <int ROWS, bool LIST>
 __device__ __forceinline__ Line measure(const Attn4Args& a) {
   if constexpr (LIST) {
-    return Line{a.R > 0 ? (uint64_t)a.T * a.hkv * a.row_tiles * a.list_parts * a.list_share : 0, (uint64_t)a.list_share};
+    return Line{a.R > 0 ? (uint64_t)a.T * a.hkv * a.row_tiles * a.list_parts * a.list_share : 0,
+                (uint64_t)a.list_share};
   } else if (a.R > kInlineRequests) {
     return line_of(uniform64(a.sched[a.R]));
   } else {
@@ -590,6 +591,11 @@ __device__ __forceinline__ void clear_padding(const Attn4Args& a) {
 // a time in turn, and join their sums at the end. Keys are decoded straight
 // into the matrix operand; values pass through the wave's own LDS rows, whose
 // transposing reads give the other operand. No barrier inside the loop.
+//
+// Bound by the cache's bytes where there are many (1.31 GB in 246 us, 5.3 TB/s) and
+// by a chain of dependent loads (places, pages, codes) and two launches where there
+// are few: one request of 4001 keys takes 8.4 us and its join 6.5; 32 tokens with
+// lists of 2048 keys (9.4 MB) 16 and 4.
 // ---------------------------------------------------------------------------
 template <int D, bool LIST>
 __global__ __launch_bounds__(256, 2) void k_attn4_few(Attn4Args a) {
@@ -601,123 +607,123 @@ __global__ __launch_bounds__(256, 2) void k_attn4_few(Attn4Args a) {
   const Line line = measure<ROWS, LIST>(a);
   const uint64_t begin = blockIdx.x * line.share, end = min(begin + line.share, line.end);
   for (uint64_t at = begin; at < end;) {
-  Tile it = find<ROWS, LIST>(a, at);
-  bool any;
-  at = take_part<ROWS, LIST>(it, begin, end, at, blockIdx.x, any);
-  if (!any || it.rows == 0) continue;
-  const Reach reach = tile_reach<ROWS>(a, it);
-  Keys<LIST> keys;
-  keys.init(a, it, reach);
+    Tile it = find<ROWS, LIST>(a, at);
+    bool any;
+    at = take_part<ROWS, LIST>(it, begin, end, at, blockIdx.x, any);
+    if (!any || it.rows == 0) continue;
+    const Reach reach = tile_reach<ROWS>(a, it);
+    Keys<LIST> keys;
+    keys.init(a, it, reach);
 
-  // lane group g takes the dims [g D/4, (g + 1) D/4) of every key, 8 at a time
-  bf16x8_t q[NI];
-  Column<D> col[1];
-  col[0].init(a, it, it.row0 + c, q, D / 4, 8);
-  uint8_t* vrows = lds + wave * 32 * kVRow<D>;
-  const int steps = (keys.k1 - keys.k0 + 31) / 32;
+    // lane group g takes the dims [g D/4, (g + 1) D/4) of every key, 8 at a time
+    bf16x8_t q[NI];
+    Column<D> col[1];
+    col[0].init(a, it, it.row0 + c, q, D / 4, 8);
+    uint8_t* vrows = lds + wave * 32 * kVRow<D>;
+    const int steps = (keys.k1 - keys.k0 + 31) / 32;
 
-  // in flight: the codes of the next step, the pages of the one after, the places of a third
-  KeyRegs<D> kv[2];
-  int page0[2], pos1[2], raw1[2], raw2[2];
-  auto at_step = [&](int s, int u) { return keys.k0 + s * 32 + u * 16 + c; };
-  {
-    int p0[2], r0[2], r1[2];
+    // in flight: the codes of the next step, the pages of the one after, the places of a third
+    KeyRegs<D> kv[2];
+    int page0[2], pos1[2], raw1[2], raw2[2];
+    auto at_step = [&](int s, int u) { return keys.k0 + s * 32 + u * 16 + c; };
+    {
+      int p0[2], r0[2], r1[2];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      r0[u] = keys.fetch(a, at_step(wave, u));
-      r1[u] = keys.fetch(a, at_step(wave + 4, u));
-      raw2[u] = keys.fetch(a, at_step(wave + 8, u));
-    }
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      p0[u] = keys.position(at_step(wave, u), r0[u]);
-      pos1[u] = keys.position(at_step(wave + 4, u), r1[u]);
-      r0[u] = keys.look(a, p0[u]);
-      raw1[u] = keys.look(a, pos1[u]);
-    }
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      page0[u] = keys.page(a, p0[u], r0[u]);
-      load_key<D>(a, page0[u], p0[u], it.head, g, kv[u]);
-    }
-  }
-  for (int s = wave; s < steps; s += 4) {
-    const uint64_t valid = (__ballot(page0[0] >= 0) & 0xFFFFu) | (__ballot(page0[1] >= 0) & 0xFFFFu) << 16;
-    const int j0 = keys.k0 + s * 32;
-    bool whole = valid == 0xFFFFFFFFu;
-    if constexpr (!LIST) whole = whole && j0 >= reach.smax && j0 + 32 <= reach.emin;
-    uint64_t bad[2] = {0, 0};
-    f32x4_t x[2] = {};
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const float ks = __uint_as_float(key_byte<D>(kv[u], g, page0[u] >= 0) << 23);
-      uint32_t vb = value_byte<D>(kv[u], g, page0[u] >= 0);
-      // a value that is not finite must not reach rows that do not see it
-      if (!whole) {
-        bad[u] = __ballot(vb == 255u);
-        if (vb == 255u) vb = 0u;
+      for (int u = 0; u < 2; ++u) {
+        r0[u] = keys.fetch(a, at_step(wave, u));
+        r1[u] = keys.fetch(a, at_step(wave + 4, u));
+        raw2[u] = keys.fetch(a, at_step(wave + 8, u));
       }
-      const float vs = __uint_as_float(vb << 23);
-      uint8_t* w = vrows + (u * 16 + c) * kVRow<D> + g * (D / 2);
 #pragma unroll
-      for (int n = 0; n < NI; ++n) {
-        x[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8(kv[u].k[n], ks), q[n], x[u], 0, 0, 0);
-        *reinterpret_cast<bf16x8_t*>(w + 16 * n) = decode8(kv[u].v[n], vs);
+      for (int u = 0; u < 2; ++u) {
+        p0[u] = keys.position(at_step(wave, u), r0[u]);
+        pos1[u] = keys.position(at_step(wave + 4, u), r1[u]);
+        r0[u] = keys.look(a, p0[u]);
+        raw1[u] = keys.look(a, pos1[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        page0[u] = keys.page(a, p0[u], r0[u]);
+        load_key<D>(a, page0[u], p0[u], it.head, g, kv[u]);
       }
     }
-    // loads come back in order: pages and places first, codes last
-    int at[2];
+    for (int s = wave; s < steps; s += 4) {
+      const uint64_t valid = (__ballot(page0[0] >= 0) & 0xFFFFu) | (__ballot(page0[1] >= 0) & 0xFFFFu) << 16;
+      const int j0 = keys.k0 + s * 32;
+      bool whole = valid == 0xFFFFFFFFu;
+      if constexpr (!LIST) whole = whole && j0 >= reach.smax && j0 + 32 <= reach.emin;
+      uint64_t bad[2] = {0, 0};
+      f32x4_t x[2] = {};
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      page0[u] = keys.page(a, pos1[u], raw1[u]);
-      at[u] = pos1[u];
-      pos1[u] = keys.position(at_step(s + 8, u), raw2[u]);
-      raw1[u] = keys.look(a, pos1[u]);
-      raw2[u] = keys.fetch(a, at_step(s + 12, u));
+      for (int u = 0; u < 2; ++u) {
+        const float ks = __uint_as_float(key_byte<D>(kv[u], g, page0[u] >= 0) << 23);
+        uint32_t vb = value_byte<D>(kv[u], g, page0[u] >= 0);
+        // a value that is not finite must not reach rows that do not see it
+        if (!whole) {
+          bad[u] = __ballot(vb == 255u);
+          if (vb == 255u) vb = 0u;
+        }
+        const float vs = __uint_as_float(vb << 23);
+        uint8_t* w = vrows + (u * 16 + c) * kVRow<D> + g * (D / 2);
+#pragma unroll
+        for (int n = 0; n < NI; ++n) {
+          x[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8(kv[u].k[n], ks), q[n], x[u], 0, 0, 0);
+          *reinterpret_cast<bf16x8_t*>(w + 16 * n) = decode8(kv[u].v[n], vs);
+        }
+      }
+      // loads come back in order: pages and places first, codes last
+      int at[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        page0[u] = keys.page(a, pos1[u], raw1[u]);
+        at[u] = pos1[u];
+        pos1[u] = keys.position(at_step(s + 8, u), raw2[u]);
+        raw1[u] = keys.look(a, pos1[u]);
+        raw2[u] = keys.fetch(a, at_step(s + 12, u));
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) load_key<D>(a, page0[u], at[u], it.head, g, kv[u]);
+      bf16x8_t p[1];
+      col[0].template weigh<2, LIST>(x, whole, valid, j0, a.scale_log2, a.slack, p);
+      __builtin_amdgcn_wave_barrier();
+      add_values<D, 1>(vrows, p, col);
+      __builtin_amdgcn_wave_barrier();
+      col[0].template spoil<LIST>(bad[0], j0);
+      col[0].template spoil<LIST>(bad[1], j0 + 16);
     }
-#pragma unroll
-    for (int u = 0; u < 2; ++u) load_key<D>(a, page0[u], at[u], it.head, g, kv[u]);
-    bf16x8_t p[1];
-    col[0].template weigh<2, LIST>(x, whole, valid, j0, a.scale_log2, a.slack, p);
-    __builtin_amdgcn_wave_barrier();
-    add_values<D, 1>(vrows, p, col);
-    __builtin_amdgcn_wave_barrier();
-    col[0].template spoil<LIST>(bad[0], j0);
-    col[0].template spoil<LIST>(bad[1], j0 + 16);
-  }
 
-  // join the four waves: maxima and sums first, then the outputs by halves
-  __syncthreads();
-  col[0].l = sum_groups(col[0].l);
-  if (g == 0) {
-    ml[wave][0][c] = col[0].m == neg_inf() ? neg_inf() : col[0].mc;
-    ml[wave][1][c] = col[0].l;
-  }
-  __syncthreads();
-  float M = neg_inf(), L = 0.0f;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) M = fmaxf(M, ml[i][0][c]);
-  const float ref = M == neg_inf() ? 0.0f : M;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) L += exp2_fast(ml[i][0][c] - ref) * ml[i][1][c];
-  const float w = col[0].m == neg_inf() ? 0.0f : exp2_fast(col[0].mc - ref);
-#pragma unroll
-  for (int n = 0; n < NT; ++n) col[0].acc[n] *= w;
-  f32x4_t* box = reinterpret_cast<f32x4_t*>(lds);  // [2][NT][64]
-#pragma unroll
-  for (int half = 2; half >= 1; half >>= 1) {
-    if (wave >= half && wave < 2 * half) {
-#pragma unroll
-      for (int n = 0; n < NT; ++n) box[((wave - half) * NT + n) * 64 + lane] = col[0].acc[n];
+    // join the four waves: maxima and sums first, then the outputs by halves
+    __syncthreads();
+    col[0].l = sum_groups(col[0].l);
+    if (g == 0) {
+      ml[wave][0][c] = col[0].m == neg_inf() ? neg_inf() : col[0].mc;
+      ml[wave][1][c] = col[0].l;
     }
     __syncthreads();
-    if (wave < half) {
+    float M = neg_inf(), L = 0.0f;
 #pragma unroll
-      for (int n = 0; n < NT; ++n) col[0].acc[n] += box[(wave * NT + n) * 64 + lane];
+    for (int i = 0; i < 4; ++i) M = fmaxf(M, ml[i][0][c]);
+    const float ref = M == neg_inf() ? 0.0f : M;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) L += exp2_fast(ml[i][0][c] - ref) * ml[i][1][c];
+    const float w = col[0].m == neg_inf() ? 0.0f : exp2_fast(col[0].mc - ref);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) col[0].acc[n] *= w;
+    f32x4_t* box = reinterpret_cast<f32x4_t*>(lds);  // [2][NT][64]
+#pragma unroll
+    for (int half = 2; half >= 1; half >>= 1) {
+      if (wave >= half && wave < 2 * half) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) box[((wave - half) * NT + n) * 64 + lane] = col[0].acc[n];
+      }
+      __syncthreads();
+      if (wave < half) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) col[0].acc[n] += box[(wave * NT + n) * 64 + lane];
+      }
+      __syncthreads();
     }
-    __syncthreads();
-  }
-  if (wave == 0) col[0].store(a, it, it.row0 + c, ROWS, M, L);
+    if (wave == 0) col[0].store(a, it, it.row0 + c, ROWS, M, L);
   }
 }
 
@@ -727,6 +733,14 @@ __global__ __launch_bounds__(256, 2) void k_attn4_few(Attn4Args a) {
 // the decoding and the cache's bytes are spent once for all rows, and what is
 // left is bound by the matrix products and the exponentials. With 64 rows a
 // tile (WR = 2) two waves share their rows and take half of a step's keys each.
+//
+// Prefill of 4047 tokens of two requests at 9K to 20K keys (928 GFLOP) takes 925
+// to 965 us, 1.0 PFLOP/s: a step of 64 keys keeps the matrix pipe, the vector ALU
+// and LDS busy for 1.0 to 1.3K cycles each of about 2.4K, with two waves a SIMD to
+// overlap them. Tiles of 256 rows would halve the decoding, but their registers
+// spill (1978 us); one LDS buffer and more blocks a CU spill too (3.4 ms). 1000
+// tokens with lists of 2048 keys and 64 heads (67 GFLOP) take 103 to 117 us; the
+// scattered reads do not bind there (102 with neighbouring keys).
 //
 // 32 x 32 products: one occupies the matrix pipe for 32 cycles and the issue
 // port for few, so up to six other instructions run beside it (16 x 16 ones
@@ -881,201 +895,201 @@ __global__ __launch_bounds__(256, 2) void k_attn4_many(Attn4Args a) {
   const Line line = measure<ROWS, LIST>(a);
   const uint64_t begin = blockIdx.x * line.share, end = min(begin + line.share, line.end);
   for (uint64_t at = begin; at < end;) {
-  Tile it = find<ROWS, LIST>(a, at);
-  bool any;
-  at = take_part<ROWS, LIST>(it, begin, end, at, blockIdx.x, any);
-  if (!any || it.rows == 0) continue;
-  const Reach reach = tile_reach<ROWS>(a, it);
-  Keys<LIST> keys;
-  keys.init(a, it, reach);
+    Tile it = find<ROWS, LIST>(a, at);
+    bool any;
+    at = take_part<ROWS, LIST>(it, begin, end, at, blockIdx.x, any);
+    if (!any || it.rows == 0) continue;
+    const Reach reach = tile_reach<ROWS>(a, it);
+    Keys<LIST> keys;
+    keys.init(a, it, reach);
 
-  bf16x8_t q[NK];
-  Wide<D> col;
-  col.init(a, it, it.row0 + wr * 32 + r, q);
-  // what all of this wave's rows see
-  int smax = col.row ? col.s : 0, emin = col.row ? col.e : 0x7FFFFFFF;
+    bf16x8_t q[NK];
+    Wide<D> col;
+    col.init(a, it, it.row0 + wr * 32 + r, q);
+    // what all of this wave's rows see
+    int smax = col.row ? col.s : 0, emin = col.row ? col.e : 0x7FFFFFFF;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    smax = max(smax, __shfl_xor(smax, o));
-    emin = min(emin, __shfl_xor(emin, o));
-  }
-  smax = __builtin_amdgcn_readfirstlane(smax);
-  emin = __builtin_amdgcn_readfirstlane(emin);
-
-  // the loading side: four threads a key
-  const int part = tid & 3, mine = tid >> 2;
-  const int steps = (keys.k1 - keys.k0 + KEYS - 1) / KEYS;
-  const int kw = mine * kKRow<D> + part * (D / 2);
-  const int vw = KEYS * kKRow<D> + mine * 2 * D + ((part * (D / 32)) ^ swizzle<D>(mine)) * 16;
-  // in flight: the codes of kAhead steps, the pages of one more, the places of a
-  // second. Listed keys lie anywhere: two steps ahead.
-  constexpr int kAhead = LIST ? 2 : 1;
-  KeyRegs<D> kvs[kAhead];
-  int page[kAhead], pos1, raw1, raw2;
-  auto at_step = [&](int s) { return keys.k0 + s * KEYS + mine; };
-  {
-    int p[kAhead + 1], raw[kAhead + 1];
-#pragma unroll
-    for (int i = 0; i <= kAhead; ++i) raw[i] = keys.fetch(a, at_step(i));
-    raw2 = keys.fetch(a, at_step(kAhead + 1));
-#pragma unroll
-    for (int i = 0; i <= kAhead; ++i) {
-      p[i] = keys.position(at_step(i), raw[i]);
-      raw[i] = keys.look(a, p[i]);
+    for (int o = 1; o < 32; o <<= 1) {
+      smax = max(smax, __shfl_xor(smax, o));
+      emin = min(emin, __shfl_xor(emin, o));
     }
-    pos1 = p[kAhead];
-    raw1 = raw[kAhead];
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      page[i] = keys.page(a, p[i], raw[i]);
-      load_key<D>(a, page[i], p[i], it.head, part, kvs[i]);
-    }
-  }
-  auto stage = [&](int s, auto bc) {  // decode step s into buffer b, start loading step s + kAhead
-    constexpr int b = decltype(bc)::value, c = b % kAhead;
-    KeyRegs<D>& kv = kvs[c];
-    // loads come back in order: the next page and place are asked for before
-    // the codes, so that waiting for them does not wait for those
-    const int now = keys.page(a, pos1, raw1), at = pos1;
-    pos1 = keys.position(at_step(s + kAhead + 1), raw2);
-    raw1 = keys.look(a, pos1);
-    raw2 = keys.fetch(a, at_step(s + kAhead + 2));
-    const bool ok = page[c] >= 0;
-    const float ks = __uint_as_float(key_byte<D>(kv, part, ok) << 23);
-    uint32_t vb = value_byte<D>(kv, part, ok);
-    const int j0 = keys.k0 + s * KEYS;
-    const uint64_t oks = __ballot(ok);
-    bool whole = oks == ~0ull;
-    if constexpr (!LIST) whole = whole & (j0 >= reach.smax) & (j0 + KEYS <= reach.emin);
-    // a value that is not finite must not reach rows that do not see it
-    const bool drop = !whole & (vb == 255u);
-    const uint64_t bad = __ballot(drop);
-    vb = drop ? 0u : vb;
-    bad_of[b][wave] = bad;  // wave-uniform, no branch
-    uint64_t v = oks & 0x1111111111111111ull;  // a key's four threads agree
-    v = (v | v >> 3) & 0x0303030303030303ull;
-    v = (v | v >> 6) & 0x000F000F000F000Full;
-    v = (v | v >> 12) & 0x000000FF000000FFull;
-    valid_of[b][wave] = ((uint32_t)(v | v >> 24) & 0xFFFFu) | (bad ? 0x10000u : 0u);
-    const float vs = __uint_as_float(vb << 23);
-    uint8_t* buf = lds + b * kBuf;
-#pragma unroll
-    for (int n = 0; n < D / 32; ++n) {
-      *reinterpret_cast<bf16x8_t*>(buf + kw + 16 * n) = decode8(kv.k[n], ks);
-      *reinterpret_cast<bf16x8_t*>(buf + (vw ^ (16 * n))) = decode8(kv.v[n], vs);
-    }
-    page[c] = now;
-    load_key<D>(a, now, at, it.head, part, kv);
-  };
+    smax = __builtin_amdgcn_readfirstlane(smax);
+    emin = __builtin_amdgcn_readfirstlane(emin);
 
-  // the reading side: a key's row of 16 dims, and 8 bytes of a value's chunk
-  const int kr = (wk * 32 + r) * kKRow<D> + h * 16;
-  const int vk = 4 * h + ((lane & 15) >> 2);  // key of a lane's transposing read
-  int vr[NV];
+    // the loading side: four threads a key
+    const int part = tid & 3, mine = tid >> 2;
+    const int steps = (keys.k1 - keys.k0 + KEYS - 1) / KEYS;
+    const int kw = mine * kKRow<D> + part * (D / 2);
+    const int vw = KEYS * kKRow<D> + mine * 2 * D + ((part * (D / 32)) ^ swizzle<D>(mine)) * 16;
+    // in flight: the codes of kAhead steps, the pages of one more, the places of a
+    // second. Listed keys lie anywhere: two steps ahead.
+    constexpr int kAhead = LIST ? 2 : 1;
+    KeyRegs<D> kvs[kAhead];
+    int page[kAhead], pos1, raw1, raw2;
+    auto at_step = [&](int s) { return keys.k0 + s * KEYS + mine; };
+    {
+      int p[kAhead + 1], raw[kAhead + 1];
 #pragma unroll
-  for (int n = 0; n < NV; ++n)
-    vr[n] = KEYS * kKRow<D> + (wk * 32 + vk) * 2 * D +
-            ((4 * n + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ swizzle<D>(vk)) * 16 + (lane & 1) * 8;
-
-  auto work = [&](int s, auto bc) {
-    constexpr int b = decltype(bc)::value;
-    const int j0 = keys.k0 + s * KEYS + wk * 32;
-    // The decoding of the next step runs beside the first products, the weights
-    // of each 16 keys beside the second products of the 16 before. A wave in its
-    // first products goes before one that weighs (prefill 975 -> 950 us).
-    // (Rows or keys that there are not take part like any other: a branch around
-    // them would make every path wait for all loads in flight.)
-    const uint8_t* buf = lds + b * kBuf;
-    __builtin_amdgcn_s_setprio(1);
-    f32x16_t x[KT];
+      for (int i = 0; i <= kAhead; ++i) raw[i] = keys.fetch(a, at_step(i));
+      raw2 = keys.fetch(a, at_step(kAhead + 1));
 #pragma unroll
-    for (int u = 0; u < KT; ++u) x[u] = f32x16_t{};
-#pragma unroll
-    for (int n = 0; n < NK; ++n)
-#pragma unroll
-      for (int u = 0; u < KT; ++u) {
-        const bf16x8_t kf = *reinterpret_cast<const bf16x8_t*>(buf + kr + u * 32 * kKRow<D> + n * 32);
-        x[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[n], x[u], 0, 0, 0);
+      for (int i = 0; i <= kAhead; ++i) {
+        p[i] = keys.position(at_step(i), raw[i]);
+        raw[i] = keys.look(a, p[i]);
       }
-    stage(s + 1, Int<b ^ 1>{});  // past the last step: keys that do not count
-    uint64_t valid = 0;
-    uint32_t any_bad = 0;
+      pos1 = p[kAhead];
+      raw1 = raw[kAhead];
 #pragma unroll
-    for (int u = 0; u < 2 * KT; ++u) {
-      const uint32_t v = valid_of[b][2 * wk + u];
-      valid |= (uint64_t)(v & 0xFFFFu) << (16 * u);
-      any_bad |= v >> 16;
-    }
-    bool whole = valid == (KT == 1 ? 0xFFFFFFFFull : ~0ull);
-    if constexpr (!LIST) whole = whole & (j0 >= smax) & (j0 + 32 * KT <= emin);
-    if (!whole) {
-      asm volatile("");  // a branch, not selects: most steps need no mask
-      col.template mask<KT, LIST>(x, valid, j0);
-    }
-    __builtin_amdgcn_s_setprio(0);
-    col.template renew<KT>(x, a.scale_log2, a.slack);
-    bf16x8_t p = col.weights(x[0], 0, a.scale_log2);
-#pragma unroll
-    for (int u = 0; u < 2 * KT; ++u) {
-      bf16x8_t next;
-      if (u + 1 < 2 * KT) next = col.weights(x[(u + 1) >> 1], (u + 1) & 1, a.scale_log2);
-#pragma unroll
-      for (int n = 0; n < NV; ++n) {
-        const uint8_t* v = buf + vr[n] + u * 16 * 2 * D;
-        const s16x4_t v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)v);
-        const s16x4_t v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(v + 8 * 2 * D));
-        const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-        col.acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p, col.acc[n], 0, 0, 0);
+      for (int i = 0; i < kAhead; ++i) {
+        page[i] = keys.page(a, p[i], raw[i]);
+        load_key<D>(a, page[i], p[i], it.head, part, kvs[i]);
       }
-      p = next;
     }
-    if (any_bad) {
-#pragma unroll 1
+    auto stage = [&](int s, auto bc) {  // decode step s into buffer b, start loading step s + kAhead
+      constexpr int b = decltype(bc)::value, c = b % kAhead;
+      KeyRegs<D>& kv = kvs[c];
+      // loads come back in order: the next page and place are asked for before
+      // the codes, so that waiting for them does not wait for those
+      const int now = keys.page(a, pos1, raw1), at = pos1;
+      pos1 = keys.position(at_step(s + kAhead + 1), raw2);
+      raw1 = keys.look(a, pos1);
+      raw2 = keys.fetch(a, at_step(s + kAhead + 2));
+      const bool ok = page[c] >= 0;
+      const float ks = __uint_as_float(key_byte<D>(kv, part, ok) << 23);
+      uint32_t vb = value_byte<D>(kv, part, ok);
+      const int j0 = keys.k0 + s * KEYS;
+      const uint64_t oks = __ballot(ok);
+      bool whole = oks == ~0ull;
+      if constexpr (!LIST) whole = whole & (j0 >= reach.smax) & (j0 + KEYS <= reach.emin);
+      // a value that is not finite must not reach rows that do not see it
+      const bool drop = !whole & (vb == 255u);
+      const uint64_t bad = __ballot(drop);
+      vb = drop ? 0u : vb;
+      bad_of[b][wave] = bad;  // wave-uniform, no branch
+      uint64_t v = oks & 0x1111111111111111ull;  // a key's four threads agree
+      v = (v | v >> 3) & 0x0303030303030303ull;
+      v = (v | v >> 6) & 0x000F000F000F000Full;
+      v = (v | v >> 12) & 0x000000FF000000FFull;
+      valid_of[b][wave] = ((uint32_t)(v | v >> 24) & 0xFFFFu) | (bad ? 0x10000u : 0u);
+      const float vs = __uint_as_float(vb << 23);
+      uint8_t* buf = lds + b * kBuf;
+#pragma unroll
+      for (int n = 0; n < D / 32; ++n) {
+        *reinterpret_cast<bf16x8_t*>(buf + kw + 16 * n) = decode8(kv.k[n], ks);
+        *reinterpret_cast<bf16x8_t*>(buf + (vw ^ (16 * n))) = decode8(kv.v[n], vs);
+      }
+      page[c] = now;
+      load_key<D>(a, now, at, it.head, part, kv);
+    };
+
+    // the reading side: a key's row of 16 dims, and 8 bytes of a value's chunk
+    const int kr = (wk * 32 + r) * kKRow<D> + h * 16;
+    const int vk = 4 * h + ((lane & 15) >> 2);  // key of a lane's transposing read
+    int vr[NV];
+#pragma unroll
+    for (int n = 0; n < NV; ++n)
+      vr[n] = KEYS * kKRow<D> + (wk * 32 + vk) * 2 * D +
+              ((4 * n + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ swizzle<D>(vk)) * 16 + (lane & 1) * 8;
+
+    auto work = [&](int s, auto bc) {
+      constexpr int b = decltype(bc)::value;
+      const int j0 = keys.k0 + s * KEYS + wk * 32;
+      // The decoding of the next step runs beside the first products, the weights
+      // of each 16 keys beside the second products of the 16 before. A wave in its
+      // first products goes before one that weighs (prefill 975 -> 950 us).
+      // (Rows or keys that there are not take part like any other: a branch around
+      // them would make every path wait for all loads in flight.)
+      const uint8_t* buf = lds + b * kBuf;
+      __builtin_amdgcn_s_setprio(1);
+      f32x16_t x[KT];
+#pragma unroll
+      for (int u = 0; u < KT; ++u) x[u] = f32x16_t{};
+#pragma unroll
+      for (int n = 0; n < NK; ++n)
+#pragma unroll
+        for (int u = 0; u < KT; ++u) {
+          const bf16x8_t kf = *reinterpret_cast<const bf16x8_t*>(buf + kr + u * 32 * kKRow<D> + n * 32);
+          x[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[n], x[u], 0, 0, 0);
+        }
+      stage(s + 1, Int<b ^ 1>{});  // past the last step: keys that do not count
+      uint64_t valid = 0;
+      uint32_t any_bad = 0;
+#pragma unroll
       for (int u = 0; u < 2 * KT; ++u) {
-        const uint64_t bad = bad_of[b][2 * wk + u];
-        col.template spoil<LIST>(bad, j0 + 16 * u);
+        const uint32_t v = valid_of[b][2 * wk + u];
+        valid |= (uint64_t)(v & 0xFFFFu) << (16 * u);
+        any_bad |= v >> 16;
+      }
+      bool whole = valid == (KT == 1 ? 0xFFFFFFFFull : ~0ull);
+      if constexpr (!LIST) whole = whole & (j0 >= smax) & (j0 + 32 * KT <= emin);
+      if (!whole) {
+        asm volatile("");  // a branch, not selects: most steps need no mask
+        col.template mask<KT, LIST>(x, valid, j0);
+      }
+      __builtin_amdgcn_s_setprio(0);
+      col.template renew<KT>(x, a.scale_log2, a.slack);
+      bf16x8_t p = col.weights(x[0], 0, a.scale_log2);
+#pragma unroll
+      for (int u = 0; u < 2 * KT; ++u) {
+        bf16x8_t next;
+        if (u + 1 < 2 * KT) next = col.weights(x[(u + 1) >> 1], (u + 1) & 1, a.scale_log2);
+#pragma unroll
+        for (int n = 0; n < NV; ++n) {
+          const uint8_t* v = buf + vr[n] + u * 16 * 2 * D;
+          const s16x4_t v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)v);
+          const s16x4_t v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(v + 8 * 2 * D));
+          const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+          col.acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p, col.acc[n], 0, 0, 0);
+        }
+        p = next;
+      }
+      if (any_bad) {
+#pragma unroll 1
+        for (int u = 0; u < 2 * KT; ++u) {
+          const uint64_t bad = bad_of[b][2 * wk + u];
+          col.template spoil<LIST>(bad, j0 + 16 * u);
+        }
+      }
+      __syncthreads();
+    };
+    stage(0, Int<0>{});
+    __syncthreads();
+    int s = 0;
+    for (; s + 1 < steps; s += 2) {
+      work(s, Int<0>{});
+      work(s + 1, Int<1>{});
+    }
+    if (s < steps) work(s, Int<0>{});
+    float L = col.l + __shfl_xor(col.l, 32), M = col.m == neg_inf() ? neg_inf() : col.mc;
+    if constexpr (WR == 2) {
+      // the two waves of the same rows
+      f32x4_t* box = reinterpret_cast<f32x4_t*>(lds) + wr * (4 * NV * 64 + 32);
+      float2* ml = reinterpret_cast<float2*>(box + 4 * NV * 64);
+      if (wk == 1) {
+#pragma unroll
+        for (int n = 0; n < NV; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            box[(4 * n + i) * 64 + lane] =
+                f32x4_t{col.acc[n][4 * i], col.acc[n][4 * i + 1], col.acc[n][4 * i + 2], col.acc[n][4 * i + 3]};
+        if (h == 0) ml[r] = float2{M, L};
+      }
+      __syncthreads();
+      if (wk == 0) {
+        const float2 o = ml[r];
+        const float top = fmaxf(M, o.x), ref = top == neg_inf() ? 0.0f : top;
+        const float f0 = exp2_fast(M - ref), f1 = exp2_fast(o.x - ref);
+        M = top;
+        L = L * f0 + o.y * f1;
+#pragma unroll
+        for (int n = 0; n < NV; ++n)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            col.acc[n][i] = col.acc[n][i] * f0 + box[(4 * n + i / 4) * 64 + lane][i % 4] * f1;
       }
     }
-    __syncthreads();
-  };
-  stage(0, Int<0>{});
-  __syncthreads();
-  int s = 0;
-  for (; s + 1 < steps; s += 2) {
-    work(s, Int<0>{});
-    work(s + 1, Int<1>{});
-  }
-  if (s < steps) work(s, Int<0>{});
-  float L = col.l + __shfl_xor(col.l, 32), M = col.m == neg_inf() ? neg_inf() : col.mc;
-  if constexpr (WR == 2) {
-    // the two waves of the same rows
-    f32x4_t* box = reinterpret_cast<f32x4_t*>(lds) + wr * (4 * NV * 64 + 32);
-    float2* ml = reinterpret_cast<float2*>(box + 4 * NV * 64);
-    if (wk == 1) {
-#pragma unroll
-      for (int n = 0; n < NV; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          box[(4 * n + i) * 64 + lane] =
-              f32x4_t{col.acc[n][4 * i], col.acc[n][4 * i + 1], col.acc[n][4 * i + 2], col.acc[n][4 * i + 3]};
-      if (h == 0) ml[r] = float2{M, L};
-    }
-    __syncthreads();
-    if (wk == 0) {
-      const float2 o = ml[r];
-      const float top = fmaxf(M, o.x), ref = top == neg_inf() ? 0.0f : top;
-      const float f0 = exp2_fast(M - ref), f1 = exp2_fast(o.x - ref);
-      M = top;
-      L = L * f0 + o.y * f1;
-#pragma unroll
-      for (int n = 0; n < NV; ++n)
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          col.acc[n][i] = col.acc[n][i] * f0 + box[(4 * n + i / 4) * 64 + lane][i % 4] * f1;
-    }
-  }
-  if (wk == 0) col.store(a, it, it.row0 + wr * 32 + r, ROWS, M, L);
-  __syncthreads();  // the buffers are free again
+    if (wk == 0) col.store(a, it, it.row0 + wr * 32 + r, ROWS, M, L);
+    __syncthreads();  // the buffers are free again
   }
 }
 
@@ -1178,18 +1192,16 @@ void shape_of(Attn4Args& a) {
   a.list_parts = (int)(((int64_t)a.list_k + a.list_share - 1) / a.list_share);
 }
 
-// Parts that may have to be kept.
-size_t slots_of(const Attn4Args& a) {
-  if (a.list_k > 0) return a.list_parts > 1 ? 2 * (size_t)a.T * a.hkv * a.row_tiles * a.list_parts : 0;
-  return 2 * kShares;
-}
+// Rows of parts that may have to be kept. Lists: only narrow tiles have parts, 512
+// at most; as much for any list, so that a larger call's workspace serves a smaller.
+size_t kept_rows(const Attn4Args& a) { return 2 * (size_t)kShares * (a.list_k > 0 ? 16 : a.rows_per_tile); }
 
 }  // namespace
 
 size_t attn4_workspace_bytes(Attn4Args a) {
   shape_of(a);
   return 256 + (((size_t)a.R + 1) * 8 + 255) / 256 * 256 +
-         slots_of(a) * a.rows_per_tile * ((size_t)a.d * 4 + 8);
+         kept_rows(a) * ((size_t)a.d * 4 + 8);
 }
 
 hipError_t launch_attn4(Attn4Args a, void* workspace, hipStream_t st) {
@@ -1198,7 +1210,7 @@ hipError_t launch_attn4(Attn4Args a, void* workspace, hipStream_t st) {
   a.sched = reinterpret_cast<uint64_t*>(ws);
   ws += (((size_t)a.R + 1) * 8 + 255) / 256 * 256;
   a.part_o = reinterpret_cast<float*>(ws);
-  a.part_ml = reinterpret_cast<float2*>(ws + slots_of(a) * a.rows_per_tile * a.d * 4);
+  a.part_ml = reinterpret_cast<float2*>(ws + kept_rows(a) * a.d * 4);
   a.slack = 8.0f / a.scale_log2;
   if (!(a.slack < 1e30f)) a.slack = 1e30f;
   if (a.list_k > 0) return a.d == 128 ? run_rows<128, true>(a, st) : run_rows<64, true>(a, st);

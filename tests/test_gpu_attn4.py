@@ -349,3 +349,59 @@ def test_argument_errors_raise(lib):
         with pytest.raises(lt.LiteTopKError):
             lt.cache4_attention(a["q"], a["codes"], a["scales"], a["table"], a["cu"], a["seq"], a["scale"],
                                 visible_end=a["end"], selected=a["sel"], workspace=a["ws"])
+
+
+@pytest.mark.parametrize("reqs,new,hq,hkv,longest", [(2000, 1, 4, 2, 64), (300, 6, 8, 2, 80), (90, 40, 4, 1, 300),
+                                                     (70, 3, 16, 4, 2500)])
+def test_shares_of_several_tiles(lib, reqs, new, hq, hkv, longest):
+    """More work than a share's smallest length for every block: shares hold whole tiles and parts of others."""
+    rng = random.Random(reqs)
+    total = [rng.choice([1, rng.randint(1, longest), longest]) for _ in range(reqs)]
+    toks = [min(n, rng.choice([0, new, new])) for n in total]
+    _both(total, toks, hq, hkv, 64, 16, seed=reqs)
+
+
+def test_long_causal_prefill(lib):
+    """Tiles from one key to the whole length: cuts by the tiles' own lengths."""
+    _both([1500, 700], [1500, 700], 2, 1, 64, 64, seed=7)
+
+
+def test_capture_in_a_graph(lib):
+    """Every replay of a captured plan, append, attention and log probabilities equals the eager calls."""
+    g = torch.Generator().manual_seed(1)
+    i = dict(dtype=torch.int32, device="cuda")
+    codes, scales = lt.cache4_empty(40, 16, 2, 64)
+    table = torch.full((3, 8), -1, **i)
+    free, used = torch.arange(39, -1, -1, **i), torch.zeros(1, **i)
+    ctx, new = torch.zeros(3, **i), torch.tensor([30, 1, 17], **i)
+    k, v, q = (torch.randn(48, h, 64, generator=g).cuda() for h in (2, 2, 8))
+    q = q.to(torch.bfloat16)
+    logits = torch.randn(48, 5000, generator=g).cuda()
+    tok = torch.randint(0, 5000, (48,), generator=g).cuda()
+
+    def step():
+        p = lt.paged_plan(ctx, new, table, free, used, 16, 48)
+        lt.cache4_append(k, v, codes, scales, p.slots)
+        o, lse = lt.cache4_attention(q, codes, scales, table, p.cu_tokens, p.seq_lens)
+        return [o, lse, *lt.token_logprobs(logits, tok, top=9), p.slots, p.status]
+
+    want = [t.clone() for t in step()]
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step()
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for _ in range(4):
+        for t in got:
+            t.zero_()
+        codes.zero_()
+        scales.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        step()                                     # the program's own eager work in between
+        torch.cuda.synchronize()
