@@ -580,9 +580,9 @@ __device__ __forceinline__ void clear_padding(const Attn4Args& a) {
   const int heads = a.hkv * a.group, per = heads * D / 2;
   for (int t = used + blockIdx.x; t < a.T; t += gridDim.x) {
     uint32_t* o = reinterpret_cast<uint32_t*>(a.out) + (int64_t)t * per;
-    for (int i = threadIdx.x; i < per; i += 256) o[i] = 0u;
+    for (int i = threadIdx.x; i < per; i += blockDim.x) o[i] = 0u;
     if (a.lse)
-      for (int i = threadIdx.x; i < heads; i += 256) a.lse[(int64_t)t * heads + i] = neg_inf();
+      for (int i = threadIdx.x; i < heads; i += blockDim.x) a.lse[(int64_t)t * heads + i] = neg_inf();
   }
 }
 
@@ -728,19 +728,19 @@ __global__ __launch_bounds__(256, 2) void k_attn4_few(Attn4Args a) {
 }
 
 // ---------------------------------------------------------------------------
-// Many rows a tile: each wave holds 32 rows, all four share the keys, 64 at a
-// time. The block decodes them once into LDS (two buffers, one barrier a step):
-// the decoding and the cache's bytes are spent once for all rows, and what is
-// left is bound by the matrix products and the exponentials. With 64 rows a
-// tile (WR = 2) two waves share their rows and take half of a step's keys each.
+// Many rows a tile: WR waves hold 32 rows each, and with WK = 2 two waves share
+// their rows and take half of a step's keys each. The block decodes a step's keys,
+// 16 a wave, once into LDS (two buffers, one barrier a step): the decoding and the
+// cache's bytes are spent once for all rows, and what is left is bound by the
+// matrix products and the exponentials.
 //
 // Prefill of 4047 tokens of two requests at 9K to 20K keys (928 GFLOP) takes 925
 // to 965 us, 1.0 PFLOP/s: a step of 64 keys keeps the matrix pipe, the vector ALU
 // and LDS busy for 1.0 to 1.3K cycles each of about 2.4K, with two waves a SIMD to
 // overlap them. Tiles of 256 rows would halve the decoding, but their registers
 // spill (1978 us); one LDS buffer and more blocks a CU spill too (3.4 ms). 1000
-// tokens with lists of 2048 keys and 64 heads (67 GFLOP) take 103 to 117 us; the
-// scattered reads do not bind there (102 with neighbouring keys).
+// tokens with lists of 2048 keys and 64 heads (67 GFLOP) take 96 us with two waves
+// a tile, 106 with four; the scattered reads do not bind there.
 //
 // 32 x 32 products: one occupies the matrix pipe for 32 cycles and the issue
 // port for few, so up to six other instructions run beside it (16 x 16 ones
@@ -882,15 +882,15 @@ struct Int {
   static constexpr int value = N;
 };
 
-template <int D, int WR, bool LIST>
-__global__ __launch_bounds__(256, 2) void k_attn4_many(Attn4Args a) {
-  constexpr int ROWS = 32 * WR, NK = D / 16, NV = D / 32, KEYS = 64, KT = WR / 2;
+template <int D, int WR, int WK, bool LIST>
+__global__ __launch_bounds__(64 * WR * WK, 2) void k_attn4_many(Attn4Args a) {
+  constexpr int ROWS = 32 * WR, NK = D / 16, NV = D / 32, WAVES = WR * WK, KEYS = 16 * WAVES, KT = WR / 2;
   constexpr int kBuf = KEYS * (kKRow<D> + 2 * D);
   extern __shared__ __align__(16) uint8_t lds[];  // two buffers of decoded keys, then values
-  __shared__ uint64_t bad_of[2][4];               // per 16 keys: quarters of values that are not finite
-  __shared__ uint32_t valid_of[2][4];             // per 16 keys: those that count; bit 16: bad_of is not 0
+  __shared__ uint64_t bad_of[2][WAVES];           // per 16 keys: quarters of values that are not finite
+  __shared__ uint32_t valid_of[2][WAVES];         // per 16 keys: those that count; bit 16: bad_of is not 0
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_id(), r = lane & 31, h = lane >> 5;
-  const int wr = WR == 4 ? wave : wave >> 1, wk = WR == 4 ? 0 : wave & 1;  // the wave's rows, its keys of a step
+  const int wr = wave / WK, wk = wave % WK;  // the wave's rows, its keys of a step
   clear_padding<D>(a);
   const Line line = measure<ROWS, LIST>(a);
   const uint64_t begin = blockIdx.x * line.share, end = min(begin + line.share, line.end);
@@ -1061,7 +1061,7 @@ __global__ __launch_bounds__(256, 2) void k_attn4_many(Attn4Args a) {
     }
     if (s < steps) work(s, Int<0>{});
     float L = col.l + __shfl_xor(col.l, 32), M = col.m == neg_inf() ? neg_inf() : col.mc;
-    if constexpr (WR == 2) {
+    if constexpr (WK == 2) {
       // the two waves of the same rows
       f32x4_t* box = reinterpret_cast<f32x4_t*>(lds) + wr * (4 * NV * 64 + 32);
       float2* ml = reinterpret_cast<float2*>(box + 4 * NV * 64);
@@ -1148,6 +1148,18 @@ __global__ __launch_bounds__(256) void k_attn4_join(Attn4Args a) {
   }
 }
 
+template <int D, int WR, int WK, bool LIST>
+hipError_t run_many(const Attn4Args& a, dim3 grid, hipStream_t st) {
+  constexpr size_t lds = 2 * 16 * WR * WK * (kKRow<D> + 2 * D);
+  if (lds > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_attn4_many<D, WR, WK, LIST>),
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  k_attn4_many<D, WR, WK, LIST><<<grid, 64 * WR * WK, lds, st>>>(a);
+  return hipSuccess;
+}
+
 template <int D, int ROWS, bool LIST>
 hipError_t run(const Attn4Args& a, hipStream_t st) {
   if (!LIST && a.R > kInlineRequests) k_attn4_schedule<ROWS><<<1, 1024, 0, st>>>(a);
@@ -1156,14 +1168,20 @@ hipError_t run(const Attn4Args& a, hipStream_t st) {
   if constexpr (ROWS == 16) {
     k_attn4_few<D, LIST><<<grid, 256, 0, st>>>(a);
   } else {
-    constexpr int WR = ROWS / 32;
-    constexpr size_t lds = 2 * 64 * (kKRow<D> + 2 * D);
-    if (lds > 64 * 1024) {
-      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_attn4_many<D, WR, LIST>),
-                                               hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-      if (e != hipSuccess) return e;
+    hipError_t e;
+    if constexpr (ROWS == 128) {
+      e = run_many<D, 4, 1, LIST>(a, grid, st);
+    } else if constexpr (LIST) {
+      // Four waves a tile, 512 tiles at once, or two, 1024 at once, which has fewer
+      // starts: a round of lists of 2048 keys takes 53 us or 95 (1000 tokens 106 and
+      // 96, 1500 tokens 155 and 168, 512 tokens 57 and 80).
+      const int64_t tiles = grid.x;
+      e = 9 * ((tiles + 1023) / 1024) <= 5 * ((tiles + 511) / 512) ? run_many<D, 2, 1, LIST>(a, grid, st)
+                                                                   : run_many<D, 2, 2, LIST>(a, grid, st);
+    } else {
+      e = run_many<D, 2, 2, LIST>(a, grid, st);
     }
-    k_attn4_many<D, WR, LIST><<<grid, 256, lds, st>>>(a);
+    if (e != hipSuccess) return e;
   }
   if (!LIST || a.list_parts > 1)
     k_attn4_join<D, ROWS, LIST><<<dim3(shares - 1, ROWS == 16 ? 2 : ROWS / 32), 256, 0, st>>>(a);

@@ -405,3 +405,28 @@ def test_capture_in_a_graph(lib):
         assert all(torch.equal(a, b) for a, b in zip(got, want))
         step()                                     # the program's own eager work in between
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("tokens,hq,hkv,d,k", [(280, 64, 1, 128, 97), (600, 40, 1, 64, 64), (520, 64, 1, 128, 130),
+                                               (1030, 33, 1, 64, 1), (270, 100, 1, 128, 70), (130, 160, 2, 64, 129)])
+def test_lists_of_many_tokens(lib, tokens, hq, hkv, d, k):
+    """Wide tiles of one token each, with entries that do not count, empty lists and keys that are NaN."""
+    total, new = [tokens - 23, 190], [tokens - 30, 30]
+    sel = _lists(total, new, k, seed=k)
+    sel[5] = -1
+    sel[7, 0], sel[8, -1], sel[9, k // 2] = 2**31 - 1, -2**31, 10**6
+    sel[10, :k // 2] = sel[10, k - k // 2:]         # listed twice
+    codes, scales, table = _cache(total, 16, hkv, d, seed=k + 1)
+    for r, pos, what, blk in ((0, 3, 1, 0), (0, 100, 1, 1), (1, 150, 0, 1), (1, 170, 1, d // 32 - 1)):
+        scales[table[r, pos // 16], 0, pos % 16, what, blk] = 255
+    table[0, 9] = -1                                # a page that is not there
+    g = torch.Generator().manual_seed(tokens)
+    q = torch.randn(tokens + 3, hq, d, generator=g).to(torch.bfloat16)
+    sel = torch.cat((sel, torch.zeros(3, k, dtype=torch.int32)))
+    cu = [0, tokens - 30, tokens]
+    print("attn4 lists", tokens, hq, hkv, d, k, flush=True)
+    out, lse = _run(q, codes, scales, table, cu, total, selected=sel)
+    ref = orc.attention(q, codes, scales, table, cu, total, d ** -0.5, selected=sel)
+    assert torch.isnan(ref[0]).any() and not torch.isnan(ref[0]).all()
+    _check(out, lse, ref)
+    assert (out[tokens:] == 0).all() and (lse[tokens:] == NEG_INF).all()
