@@ -181,15 +181,24 @@ __device__ __forceinline__ void take(Best& b, const float (&x)[Vec<T>::N], int f
   }
 }
 
-// What a row's sums say of its token; one thread.
+// A row's token's logit, asked for early: two loads, one after the other.
+struct Token {
+  bool in;  // inside the vocabulary
+  float x;
+};
 template <class T>
-__device__ __forceinline__ void finish_row(const LogprobArgs& a, int row, const Sums& s) {
-  const T* x = reinterpret_cast<const T*>(a.logits) + (int64_t)row * a.ld;
+__device__ __forceinline__ Token token_of(const LogprobArgs& a, int row) {
+  const int64_t tok = a.tokens[row];
+  const bool in = tok >= 0 && tok < a.vocab;
+  return Token{in, in ? Vec<T>::one(reinterpret_cast<const T*>(a.logits) + (int64_t)row * a.ld + tok) : 0.0f};
+}
+
+// What a row's sums say of its token; one thread.
+__device__ __forceinline__ void finish_row(const LogprobArgs& a, int row, const Sums& s, const Token& k) {
   const bool none = s.s == 0.0f;  // no value above -inf
   const float l2 = __builtin_amdgcn_logf(s.s);
-  const int64_t tok = a.tokens[row];
   float lp = 0.0f;
-  if (tok >= 0 && tok < a.vocab) lp = none ? ninf() : fmaf(Vec<T>::one(x + tok) - s.m, a.scale, -l2 * kLn2);
+  if (k.in) lp = none ? ninf() : fmaf(k.x - s.m, a.scale, -l2 * kLn2);
   a.logprob[row] = lp;
   a.entropy[row] = none ? 0.0f : (l2 - s.u / s.s) * kLn2;
   a.lse[row] = none ? ninf() : fmaf(s.m, a.scale, l2 * kLn2);
@@ -300,7 +309,7 @@ __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a, Partial pa
     if constexpr (TOP) best.list = merge_lists(best.list, wlist[i][lane]);
   }
   if (a.splits == 1) {
-    if (lane == 0) finish_row<T>(a, row, s);
+    if (lane == 0) finish_row(a, row, s, token_of<T>(a, row));
     if (TOP && lane < a.top) finish_top(a, row, s, lane, best.list);
   } else {
     if (lane == 0) part.sums[blockIdx.x] = s;
@@ -309,8 +318,8 @@ __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a, Partial pa
 }
 
 // ---- few rows: latency ----
-// 8 rows of 131072 in bfloat16 and their best 20: 6.3 us for the parts, 9 for the
-// join (a launch alone takes 3.8). Sorted lists of every wave took 12.3 and 12.4.
+// 8 rows of 131072 in bfloat16 and their best 20: 12.2 us in a captured graph,
+// parts and join (a launch alone takes 3.8). Sorted lists of every wave took 24.7.
 // The largest value, cut to its upper 16 bits, that at least n of a block's
 // threads reach. One barrier; mine: LDS of a word a thread.
 __device__ __forceinline__ uint32_t nth_floor(uint32_t v, int n, uint32_t* mine) {
@@ -443,7 +452,7 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_part(LogprobArgs a, Parti
 // that `top` threads' own reach; of those, each counts how many come before it.
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_logprobs_join(LogprobArgs a, Partial part) {
-  constexpr int kMost = 512;
+  constexpr int kMost = 512, kKept = 16;
   __shared__ Sums wsum[kWaves];
   __shared__ __align__(16) uint32_t tops[kThreads];
   __shared__ int count;
@@ -453,9 +462,16 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_join(LogprobArgs a, Parti
   const uint64_t* keys = part.keys + (int64_t)row * a.splits * kList;
   const int slots = a.top > 0 ? a.splits * kList : 0;
   if (t == 0) count = 0;
+  const Token token = token_of<T>(a, row);
+  // the first keys stay in registers, loaded together; more are read twice
+  uint64_t held[kKept];
+#pragma unroll
+  for (int u = 0; u < kKept; ++u) held[u] = u * kThreads + t < slots ? keys[u * kThreads + t] : 0;
   uint32_t mine = 0;
 #pragma unroll 8
-  for (int i = t; i < slots; i += kThreads) mine = max(mine, (uint32_t)(keys[i] >> 32));
+  for (int i = kKept * kThreads + t; i < slots; i += kThreads) mine = max(mine, (uint32_t)(keys[i] >> 32));
+#pragma unroll
+  for (int u = 0; u < kKept; ++u) mine = max(mine, (uint32_t)(held[u] >> 32));
   Sums s{kStart, 0.0f, 0.0f};
   for (int i = t; i < a.splits; i += kThreads) s = join(s, part.sums[(int64_t)row * a.splits + i], c);
   s = wave_join(s, c);
@@ -463,18 +479,20 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_join(LogprobArgs a, Parti
   const uint32_t f = nth_floor(mine, a.top, tops);
   s = wsum[0];
   for (int i = 1; i < kWaves; ++i) s = join(s, wsum[i], c);
-  if (t == 0) finish_row<T>(a, row, s);
+  if (t == 0) finish_row(a, row, s, token);
   if (a.top == 0) return;
 
-  for (int i = t; i < slots; i += kThreads) {  // whole waves: slots is a multiple of 64
-    const uint64_t k = keys[i];
+  auto list = [&](uint64_t k) {
     const uint64_t who = __ballot(k != 0 && (uint32_t)(k >> 32) >= f);
-    if (!who) continue;
+    if (!who) return;
     int at = 0;
     if (lane == 0) at = atomicAdd(&count, __popcll(who));
     at = __builtin_amdgcn_readfirstlane(at) + __popcll(who & ((1ull << lane) - 1));
     if (((who >> lane) & 1u) && at < kMost) wlist[at] = k;
-  }
+  };
+#pragma unroll
+  for (int u = 0; u < kKept; ++u) list(held[u]);
+  for (int i = kKept * kThreads + t; i < slots; i += kThreads) list(keys[i]);  // whole waves: a multiple of 64
   __syncthreads();
   const int total = count;
   if (total <= kMost) {
@@ -489,13 +507,13 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_join(LogprobArgs a, Parti
   }
   // many equal values: sorted lists
   __syncthreads();
-  uint64_t list = 0;
-  for (int i = wave; i < slots / 64; i += kWaves) list = merge_lists(list, sort_list(keys[i * 64 + lane]));
-  wlist[wave * 64 + lane] = list;
+  uint64_t best = 0;
+  for (int i = wave; i < slots / 64; i += kWaves) best = merge_lists(best, sort_list(keys[i * 64 + lane]));
+  wlist[wave * 64 + lane] = best;
   __syncthreads();
   if (wave) return;
-  for (int i = 1; i < kWaves; ++i) list = merge_lists(list, wlist[i * 64 + lane]);
-  if (lane < a.top) finish_top(a, row, s, lane, list);
+  for (int i = 1; i < kWaves; ++i) best = merge_lists(best, wlist[i * 64 + lane]);
+  if (lane < a.top) finish_top(a, row, s, lane, best);
 }
 
 // ---- gradient: one pass, bound by reading and writing the logits once ----
