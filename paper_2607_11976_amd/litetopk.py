@@ -582,11 +582,11 @@ def _int32(t: Optional[torch.Tensor], n: Optional[int], name: str):
 
 def _table(t: torch.Tensor, rows: int):
     """block_table int32 [rows, width] with unit column stride."""
-    width = t.shape[-1]
-    _need(t.is_cuda and t.dtype is torch.int32 and t.dim() == 2 and t.shape[0] == rows
-          and (t.numel() == 0 or width == 1 or t.stride(1) == 1),
-          "block_table must be an int32 [requests, pages] GPU matrix with unit column stride")
-    return t.stride(0) if rows > 1 and width > 0 else width, width
+    s = t.shape
+    if not (t.is_cuda and t.dtype is torch.int32 and len(s) == 2 and s[0] == rows
+            and (rows == 0 or s[1] <= 1 or t.stride(1) == 1)):
+        raise LiteTopKError("block_table must be an int32 [requests, pages] GPU matrix with unit column stride")
+    return t.stride(0) if rows > 1 and s[1] > 0 else s[1], s[1]
 
 
 def _used_on(stream, *ts):
@@ -625,7 +625,7 @@ def paged_plan(context_lens: torch.Tensor, new_lens: torch.Tensor, block_table: 
     dev = context_lens.device
     # the 32-bit results in one allocation
     cu, seq, used, status, positions = torch.empty(
-        3 * n + 2 + token_capacity, dtype=torch.int32, device=dev).split((n + 1, n, 1, n, token_capacity))
+        3 * n + 2 + token_capacity, dtype=torch.int32, device=dev).split_with_sizes((n + 1, n, 1, n, token_capacity))
     p = PagedPlan(cu, seq, torch.empty(token_capacity, dtype=torch.int64, device=dev), positions, used, status)
     st = lt_paged_plan(_ptr(context_lens), _ptr(new_lens), n, page_size, _ptr(block_table), ld, width,
                        _ptr(free_pages), free_pages.numel(), _ptr(free_used), token_capacity, _ptr(p.cu_tokens),
@@ -647,19 +647,22 @@ def cache4_empty(num_pages: int, page_size: int, kv_heads: int, head_dim: int, d
 def _cache4(codes: torch.Tensor, scales: torch.Tensor):
     """(pages, page size, KV heads, head dim) of a 4-bit cache."""
     _on_gpu(codes, scales)
-    _need(codes.dtype == torch.uint8 and scales.dtype == torch.uint8 and codes.dim() == 5 and scales.dim() == 5
-          and codes.shape[3] == 2 and codes.shape[:4] == scales.shape[:4] and codes.shape[4] == 16 * scales.shape[4],
-          "a cache is codes uint8 [pages, heads, page_size, 2, d / 2] and scales uint8 [pages, heads, page_size, 2, "
-          "d / 32]")
-    return codes.shape[0], codes.shape[2], codes.shape[1], 2 * codes.shape[4]
+    a, b = codes.shape, scales.shape    # each use of .shape builds it anew
+    if not (codes.dtype is torch.uint8 and scales.dtype is torch.uint8 and len(a) == 5 and len(b) == 5
+            and a[0] == b[0] and a[1] == b[1] and a[2] == b[2] and a[3] == b[3] == 2 and a[4] == 16 * b[4]):
+        raise LiteTopKError("a cache is codes uint8 [pages, heads, page_size, 2, d / 2] and scales uint8 [pages, "
+                            "heads, page_size, 2, d / 32]")
+    return a[0], a[2], a[1], 2 * a[4]
 
 
 def _rows_of(t: torch.Tensor, heads: int, d: int, name: str) -> int:
     """Stride between the rows of a [rows, heads, d] tensor whose rows are contiguous."""
-    if not (t.is_cuda and t.dim() == 3 and t.shape[1] == heads and t.shape[2] == d
-            and (t.is_contiguous() or (t.stride(2) == 1 and (heads == 1 or t.stride(1) == d)))):
+    s = t.shape
+    whole = t.is_contiguous()
+    if not (t.is_cuda and len(s) == 3 and s[1] == heads and s[2] == d
+            and (whole or (t.stride(2) == 1 and (heads == 1 or t.stride(1) == d)))):
         raise LiteTopKError("%s must be [rows, %d, %d] on the GPU with contiguous rows" % (name, heads, d))
-    return t.stride(0) if t.shape[0] > 1 else heads * d
+    return heads * d if whole or s[0] <= 1 else t.stride(0)
 
 
 def cache4_append(k: torch.Tensor, v: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, slots: torch.Tensor,
@@ -708,8 +711,9 @@ def cache4_attention(q: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
     head_dim ** -0.5. Returns (out bfloat16 like q, lse float32 [T, heads] or
     None)."""
     pages, page, hkv, d = _cache4(codes, scales)
-    _need(q.dim() == 3 and q.dtype == torch.bfloat16, "q must be bfloat16 [T, heads, head_dim]")
-    tokens, hq = q.shape[0], q.shape[1]
+    shape = q.shape
+    _need(len(shape) == 3 and q.dtype is torch.bfloat16, "q must be bfloat16 [T, heads, head_dim]")
+    tokens, hq = shape[0], shape[1]
     qs = _rows_of(q, hq, d, "q")
     _int32(seq_lens, None, "seq_lens")
     n = seq_lens.numel()
@@ -776,7 +780,7 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0, sca
         workspace = torch.empty(need, dtype=torch.uint8, device=dev)
     n = min(top, vocab)
     f = torch.empty(rows * (3 + n), dtype=torch.float32, device=dev)
-    logprob, entropy, lse, best = f.split((rows, rows, rows, rows * n))
+    logprob, entropy, lse, best = f.split_with_sizes((rows, rows, rows, rows * n))
     r = TokenLogprobs(logprob, entropy, lse, torch.empty((rows, n), dtype=torch.int32, device=dev),
                       best.view(rows, n))
     st = lt_token_logprobs(_ptr(logits), dt, ld, rows, vocab, _ptr(tokens), scale, n, _ptr(r.logprob),
