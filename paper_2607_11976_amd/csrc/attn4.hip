@@ -594,8 +594,8 @@ __device__ __forceinline__ void clear_padding(const Attn4Args& a) {
 //
 // Bound by the cache's bytes where there are many (1.31 GB in 246 us, 5.3 TB/s) and
 // by a chain of dependent loads (places, pages, codes) and two launches where there
-// are few: one request of 4001 keys takes 8.4 us and its join 6.5; 32 tokens with
-// lists of 2048 keys (9.4 MB) 16 and 4.
+// are few: one request of 4001 keys takes 15 us, its join's 6 included, 32 tokens
+// with lists of 2048 keys (10.2 MB) 20 and 4.
 // ---------------------------------------------------------------------------
 template <int D, bool LIST>
 __global__ __launch_bounds__(256, 2) void k_attn4_few(Attn4Args a) {
@@ -1095,10 +1095,13 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn4_many(Attn4Args a) {
 
 // Joins the parts of a tile, by the block of the first cut inside it: parts c =
 // b - 1, b, ... of the shares that reach into it. A thread takes four outputs of
-// a row, a block 1024 / D rows at a time, eight parts' loads in flight.
+// a row, a block 1024 / D rows at a time. Its time is that of waiting for loads:
+// sixteen parts' in flight, and eight for lists, which have few parts (one request of
+// 4001 keys, 35 parts a tile: both kernels 15.2 us, with eight 16.4; 128K keys, 64
+// parts: 38.9 and 41.4; 32 lists of 4 parts: 21.6 and 20.0).
 template <int D, int ROWS, bool LIST>
 __global__ __launch_bounds__(256) void k_attn4_join(Attn4Args a) {
-  constexpr int kRowThreads = D / 4, kAtOnce = 256 / kRowThreads;
+  constexpr int kRowThreads = D / 4, kAtOnce = 256 / kRowThreads, kParts = LIST ? 8 : 16;
   const Line line = measure<ROWS, LIST>(a);
   const int b = blockIdx.x + 1;
   const uint64_t cut = b * line.share, before = cut - line.share;
@@ -1112,11 +1115,11 @@ __global__ __launch_bounds__(256) void k_attn4_join(Attn4Args a) {
   for (int in = blockIdx.y * kAtOnce + threadIdx.x / kRowThreads; in < n; in += gridDim.y * kAtOnce) {
     float M = neg_inf(), L = 0.0f;
     f32x4_t o = {};
-    for (int i0 = 0; i0 < parts; i0 += 8) {
-      float2 w[8];
-      f32x4_t v[8];
+    for (int i0 = 0; i0 < parts; i0 += kParts) {
+      float2 w[kParts];
+      f32x4_t v[kParts];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
+      for (int u = 0; u < kParts; ++u) {
         const int i = min(i0 + u, parts - 1);
         const int64_t row = (int64_t)(i == 0 ? slot0 : 2 * (b - 1 + i)) * ROWS + in;
         w[u] = a.part_ml[row];
@@ -1124,13 +1127,13 @@ __global__ __launch_bounds__(256) void k_attn4_join(Attn4Args a) {
       }
       float top = M;
 #pragma unroll
-      for (int u = 0; u < 8; ++u) top = fmaxf(top, w[u].x);
+      for (int u = 0; u < kParts; ++u) top = fmaxf(top, w[u].x);
       const float ref = top == neg_inf() ? 0.0f : top, f = exp2_fast(M - ref);
       M = top;
       L *= f;
       o *= f;
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
+      for (int u = 0; u < kParts; ++u) {
         const float g = exp2_fast(w[u].x - ref);
         if (i0 + u < parts) {
           L = fmaf(g, w[u].y, L);
