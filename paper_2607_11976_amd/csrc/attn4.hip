@@ -594,8 +594,8 @@ __device__ __forceinline__ void clear_padding(const Attn4Args& a) {
 //
 // Bound by the cache's bytes where there are many (1.31 GB in 246 us, 5.3 TB/s) and
 // by a chain of dependent loads (places, pages, codes) and two launches where there
-// are few: one request of 4001 keys takes 15 us, its join's 6 included, 32 tokens
-// with lists of 2048 keys (10.2 MB) 20 and 4.
+// are few: one request of 4001 keys takes 15 us and 32 tokens with lists of 2048
+// keys (10.2 MB) 20 us, the joins' 6 and 4 included.
 // ---------------------------------------------------------------------------
 template <int D, bool LIST>
 __global__ __launch_bounds__(256, 2) void k_attn4_few(Attn4Args a) {
