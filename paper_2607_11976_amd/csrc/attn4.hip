@@ -1096,12 +1096,13 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void k_attn4_many(Attn4Args a) {
 // Joins the parts of a tile, by the block of the first cut inside it: parts c =
 // b - 1, b, ... of the shares that reach into it. A thread takes four outputs of
 // a row, a block 1024 / D rows at a time. Its time is that of waiting for loads:
-// sixteen parts' in flight, and eight for lists, which have few parts (one request of
-// 4001 keys, 35 parts a tile: both kernels 15.2 us, with eight 16.4; 128K keys, 64
-// parts: 38.9 and 41.4; 32 lists of 4 parts: 21.6 and 20.0).
+// sixteen parts' in flight, and eight for lists and wide tiles, which mostly have few
+// parts (one request of 4001 keys, 35 parts a tile: both kernels 15.2 us, with eight
+// 16.4; 128K keys, 64 parts: 38.9 and 41.4; 32 lists of 4 parts: 21.6 and 20.0; the
+// join of a prefill of two requests 44 and 25).
 template <int D, int ROWS, bool LIST>
 __global__ __launch_bounds__(256) void k_attn4_join(Attn4Args a) {
-  constexpr int kRowThreads = D / 4, kAtOnce = 256 / kRowThreads, kParts = LIST ? 8 : 16;
+  constexpr int kRowThreads = D / 4, kAtOnce = 256 / kRowThreads, kParts = !LIST && ROWS == 16 ? 16 : 8;
   const Line line = measure<ROWS, LIST>(a);
   const int b = blockIdx.x + 1;
   const uint64_t cut = b * line.share, before = cut - line.share;
