@@ -573,16 +573,18 @@ __device__ __forceinline__ void add_values(const uint8_t* v, const bf16x8_t (&p)
   }
 }
 
-// Rows of tokens that belong to no request: zero, by all blocks of a launch.
+// Rows of tokens that belong to no request, those before cu[0] and from cu[R] on:
+// zero, by all blocks of a launch.
 template <int D>
 __device__ __forceinline__ void clear_padding(const Attn4Args& a) {
-  const int used = a.R > 0 ? min(max(a.cu[a.R], 0), a.T) : 0;
-  const int heads = a.hkv * a.group, per = heads * D / 2;
-  for (int t = used + blockIdx.x; t < a.T; t += gridDim.x) {
-    uint32_t* o = reinterpret_cast<uint32_t*>(a.out) + (int64_t)t * per;
-    for (int i = threadIdx.x; i < per; i += blockDim.x) o[i] = 0u;
+  const int first = a.R > 0 ? min(max(a.cu[0], 0), a.T) : 0, used = a.R > 0 ? min(max(a.cu[a.R], first), a.T) : 0;
+  const int heads = a.hkv * a.group, per = heads * D / 2, n = first + a.T - used;
+  for (int i = blockIdx.x; i < n; i += gridDim.x) {
+    const int64_t t = i < first ? i : used + (i - first);
+    uint32_t* o = reinterpret_cast<uint32_t*>(a.out) + t * per;
+    for (int j = threadIdx.x; j < per; j += blockDim.x) o[j] = 0u;
     if (a.lse)
-      for (int i = threadIdx.x; i < heads; i += blockDim.x) a.lse[(int64_t)t * heads + i] = neg_inf();
+      for (int j = threadIdx.x; j < heads; j += blockDim.x) a.lse[t * heads + j] = neg_inf();
   }
 }
 

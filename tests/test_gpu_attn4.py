@@ -430,3 +430,31 @@ def test_lists_of_many_tokens(lib, tokens, hq, hkv, d, k):
     assert torch.isnan(ref[0]).any() and not torch.isnan(ref[0]).all()
     _check(out, lse, ref)
     assert (out[tokens:] == 0).all() and (lse[tokens:] == NEG_INF).all()
+
+
+@pytest.mark.parametrize("hq,hkv,k", [(8, 2, 0), (64, 1, 0), (8, 2, 20), (64, 1, 20), (64, 1, 300)])
+@pytest.mark.parametrize("lead", [1, 4, 300])
+def test_tokens_before_the_first_request(lib, lead, hq, hkv, k):
+    """cu_tokens that starts above 0: the tokens before it belong to no request, like those past its end."""
+    total, new, tail = [90, 400, 7], [2, 40, 1], 3
+    codes, scales, table = _cache(total, 16, hkv, 64, seed=lead)
+    g = torch.Generator().manual_seed(lead + k)
+    cu = [lead]
+    for n in new:
+        cu.append(cu[-1] + n)
+    tokens = cu[-1] + tail
+    q = torch.randn(tokens, hq, 64, generator=g).to(torch.bfloat16)
+    kw = {}
+    if k:
+        sel = torch.zeros(tokens, k, dtype=torch.int32)
+        sel[lead:cu[-1]] = _lists(total, new, k, seed=k)
+        kw = dict(selected=sel)
+    # memory that the results are likely to get: not zeros
+    junk = [torch.full((tokens, hq, 64), 3.0, dtype=torch.bfloat16, device="cuda"),
+            torch.full((tokens, hq), 5.0, device="cuda")]
+    del junk
+    print("attn4 lead", lead, hq, hkv, k, flush=True)
+    out, lse = _run(q, codes, scales, table, cu, total, **kw)
+    _check(out, lse, orc.attention(q, codes, scales, table, cu, total, 64 ** -0.5, **kw))
+    for part in (slice(0, lead), slice(cu[-1], tokens)):
+        assert (out[part] == 0).all() and (lse[part] == NEG_INF).all()
