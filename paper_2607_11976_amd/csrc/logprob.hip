@@ -14,6 +14,8 @@
 // index), behind a threshold that the waves of a block share. Bound by reading
 // the logits: 2039 rows of 128001 in bfloat16 (0.52 GB) take 131 us, 4.0 TB/s;
 // more loads a thread or more blocks a CU lose.
+#include <algorithm>
+
 #include "internal.hpp"
 
 namespace lt {
@@ -517,51 +519,72 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_join(LogprobArgs a, Parti
 }
 
 // ---- gradient: one pass, bound by reading and writing the logits once ----
-// 2039 rows of 128001 in bfloat16 (1.04 GB) take 190 us, 5.5 TB/s.
-// p = w exp(scale (x - a) - b) with a = 0, b = lse, w = 1. Where lse is too large
-// for its last bit to be small (kFarLse and beyond; in earnest only rows whose
-// logits are all at their type's lowest value), a block first finds the row's own
-// maximum and sum again: a = max, b = 0, w = 1 / sum.
-constexpr float kFarLse = 1024.0f;
+// 2039 rows of 128001 in bfloat16 (1.04 GB) take 210 us, 5.0 TB/s, where rows of a
+// large lse (below), which are read twice, take 294; in float32 413 and 578.
+// p = w 2^((x - from) scale log2 e - minus log2 e), with from = 0, minus = lse and w = 1
+// where lse is near 0: half its last bit is then an error of at most 2^-21, common to
+// the row's p, as large as the exponential's own. That doubles with every power of two
+// of lse, though a softmax does not depend on a common offset. Rows of a larger lse
+// (kFarLse and beyond; -inf too, which may be a finite sum below float32's range) are
+// summed again, by one block that then writes the whole row: from = a logit near the
+// largest, minus = 0, w = 1 / sum.
+constexpr float kFarLse = 16.0f;
 
-template <class T>
-__global__ __launch_bounds__(kThreads) void k_logprobs_backward(const T* logits, int64_t ld, int vocab,
-                                                                const int64_t* tokens, float scale, const float* lse,
-                                                                const float* entropy, const float* g_lp,
-                                                                const float* g_ent, T* out, int64_t out_ld) {
-  constexpr int N = Vec<T>::N;
+template <class T, int THREADS>
+__global__ __launch_bounds__(THREADS, 2048 / THREADS) void k_logprobs_backward(
+    const T* logits, int64_t ld, int vocab, const int64_t* tokens, float scale, const float* lse, const float* entropy,
+    const float* g_lp, const float* g_ent, T* out, int64_t out_ld) {
+  constexpr int N = Vec<T>::N, kSpan = THREADS * N;
   const int row = blockIdx.x, t = threadIdx.x;
   const T* x = logits + (int64_t)row * ld;
   T* o = out + (int64_t)row * out_ld;
   const int64_t tok = tokens[row];
   const bool counts = tok >= 0 && tok < vocab;
   const float z = lse[row];
-  const bool none = z == ninf();
+  int first = blockIdx.y * kSpan + t * N, step = gridDim.y * kSpan;
+  bool none = false;
   float from = 0.0f, minus = z, w = 1.0f;
-  if (fabsf(z) >= kFarLse && !none) {
-    __shared__ float red[kWaves], red2[kWaves];
-    float top = ninf(), sum = 0.0f;
-    for (int i = t; i < vocab; i += kThreads) top = fmaxf(top, Vec<T>::one(x + i));
+  if (!(fabsf(z) < kFarLse)) {
+    if (blockIdx.y) return;
+    first = t * N;
+    step = kSpan;
+    __shared__ Sums wsum[THREADS / 64];
+    const float c = scale * kLog2e, slack = fminf(kSlack / c, 1.0e30f);
+    Sums s{kStart, 0.0f, 0.0f};
+    // a wave stops at the row's end: its lanes' elements lie side by side
+    for (int at = (t & ~63) * N; at < vocab; at += kUnroll * kSpan) {
+      uint4 raw[kUnroll];
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
-    if ((t & 63) == 0) red[t >> 6] = top;
-    __syncthreads();
-    for (int i = 0; i < kWaves; ++i) top = fmaxf(top, red[i]);
-    for (int i = t; i < vocab; i += kThreads)
-      sum += __builtin_amdgcn_exp2f((Vec<T>::one(x + i) - top) * scale * kLog2e);
+      for (int k = 0; k < kUnroll; ++k) raw[k] = fetch16<T>(x, at + k * kSpan + (t & 63) * N, vocab);
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
-    if ((t & 63) == 0) red2[t >> 6] = sum;
+      for (int k = 0; k < kUnroll; ++k) {
+        if (at + k * kSpan >= vocab) break;
+        float v[N], ss[2] = {};
+        Vec<T>::unpack(raw[k], v);
+        float top = v[0];
+#pragma unroll
+        for (int j = 1; j < N; ++j) top = fmaxf(top, v[j]);
+        if (__any(top > s.m + slack)) rebase(s, fmaxf(s.m, top), c);
+#pragma unroll
+        for (int j = 0; j < N; ++j) ss[j & 1] += __builtin_amdgcn_exp2f((v[j] - s.m) * c);
+        s.s += ss[0] + ss[1];
+      }
+    }
+    s = wave_join(s, c);
+    if ((t & 63) == 0) wsum[t >> 6] = s;
     __syncthreads();
-    from = top;
+    s = wsum[0];
+    for (int i = 1; i < THREADS / 64; ++i) s = join(s, wsum[i], c);
+    none = s.s == 0.0f;  // no value above -inf
+    from = s.m;
     minus = 0.0f;
-    w = 1.0f / ((red2[0] + red2[1]) + (red2[2] + red2[3]));
+    w = none ? 0.0f : 1.0f / s.s;
   }
   const float gl = counts && g_lp ? g_lp[row] * scale : 0.0f, gh = g_ent ? g_ent[row] * scale : 0.0f;
   // -g_lp p - g_H p (log p + H) = 2^d (k0 - k1w d), d = log2 (p / w)
   const float k1 = gh * kLn2;
   const float k0 = w * (-gl - gh * entropy[row] - k1 * __builtin_amdgcn_logf(w)), k1w = k1 * w;
-  for (int i = (blockIdx.y * kThreads + t) * N; i < vocab; i += gridDim.y * kThreads * N) {
+  for (int i = first; i < vocab; i += step) {
     const int n = min(N, vocab - i);
     float v[N];
     if (n == N) {
@@ -654,22 +677,29 @@ hipError_t launch_logprobs(LogprobArgs a, void* workspace, hipStream_t st) {
   return a.bf16 ? run_forward<uint16_t>(a, p, st) : run_forward<float>(a, p, st);
 }
 
+template <class T, int THREADS>
+static hipError_t run_backward(const void* logits, int64_t ld, int rows, int vocab, const int64_t* tokens, float scale,
+                               const float* lse, const float* entropy, const float* g_logprob, const float* g_entropy,
+                               void* out, int64_t out_ld, hipStream_t st) {
+  // up to 16384 waves, two rounds of the chip's
+  const int64_t span = THREADS * Vec<T>::N, most = ((int64_t)vocab + span - 1) / span;
+  const int64_t want = (4096 * 256 / THREADS + rows - 1) / rows;
+  const dim3 grid((unsigned)rows, (unsigned)std::min(most, want));
+  k_logprobs_backward<T, THREADS><<<grid, THREADS, 0, st>>>((const T*)logits, ld, vocab, tokens, scale, lse, entropy,
+                                                            g_logprob, g_entropy, (T*)out, out_ld);
+  return hipGetLastError();
+}
+
 hipError_t launch_logprobs_backward(const void* logits, int64_t ld, bool bf16, int rows, int vocab,
                                     const int64_t* tokens, float scale, const float* lse, const float* entropy,
                                     const float* g_logprob, const float* g_entropy, void* out, int64_t out_ld,
                                     hipStream_t st) {
-  const int unit = kThreads * (bf16 ? 8 : 4);
-  int64_t y = ((int64_t)vocab + unit - 1) / unit;
-  const int64_t want = (4096 + rows - 1) / rows;
-  y = y > want ? want : y;
-  const dim3 grid((unsigned)rows, (unsigned)(y < 1 ? 1 : y));
-  if (bf16)
-    k_logprobs_backward<uint16_t><<<grid, kThreads, 0, st>>>((const uint16_t*)logits, ld, vocab, tokens, scale, lse,
-                                                             entropy, g_logprob, g_entropy, (uint16_t*)out, out_ld);
-  else
-    k_logprobs_backward<float><<<grid, kThreads, 0, st>>>((const float*)logits, ld, vocab, tokens, scale, lse, entropy,
-                                                          g_logprob, g_entropy, (float*)out, out_ld);
-  return hipGetLastError();
+  // Wide blocks for long rows: 4096 rows of 32000 in bfloat16 take 101 us, 110 with
+  // narrow ones, of 18000 58 and 52; in float32 18000 take 113 and 121, 9000 57 and 50.
+  const bool wide = (int64_t)vocab * (bf16 ? 2 : 4) >= 56 * 1024;
+  auto run = bf16 ? wide ? run_backward<uint16_t, 1024> : run_backward<uint16_t, 256>
+                  : wide ? run_backward<float, 1024> : run_backward<float, 256>;
+  return run(logits, ld, rows, vocab, tokens, scale, lse, entropy, g_logprob, g_entropy, out, out_ld, st);
 }
 
 }  // namespace lt

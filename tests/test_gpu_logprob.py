@@ -252,3 +252,85 @@ def test_argument_errors_raise(lib):
         lt.token_logprobs(x, tok, scale=0.0)
     with pytest.raises(lt.LiteTopKError):
         lt.token_logprobs_backward(x, tok, x[0], x[1])
+
+
+def _gradient_and_formula(x, tok, scale, gl, gh):
+    """(the kernel's gradient, the formula's, log p, the entropy) of both gradients, in 64 bits on the CPU."""
+    xd, td = x.cuda(), tok.cuda()
+    print("gradient", tuple(x.shape), x.dtype, scale, flush=True)
+    r = lt.token_logprobs(xd, td, scale=scale)
+    got = lt.token_logprobs_backward(xd, td, r.lse, r.entropy, None if gl is None else gl.cuda(),
+                                     None if gh is None else gh.cuda(), scale=scale).cpu().double()
+    y = x.double() * scale
+    logp = y - y.amax(-1, keepdim=True)
+    logp = logp - torch.logsumexp(logp, -1, keepdim=True)
+    return got, orc.token_logprobs_backward(x, tok, scale, gl, gh), logp, -torch.special.xlogy(
+        torch.exp(logp), torch.exp(logp)).sum(-1, keepdim=True)
+
+
+@pytest.mark.parametrize("dtype", TYPES.values(), ids=TYPES.keys())
+@pytest.mark.parametrize("rows,vocab", [(1, 1), (6, 700), (5, 30011), (300, 515), (70, 4097)])
+@pytest.mark.parametrize("which", ["both", "logprob", "entropy"])
+def test_gradient_does_not_depend_on_an_offset(lib, rows, vocab, dtype, which):
+    """Rows moved by up to thousands, next to rows that are not. The distance to a logit near the row's
+    largest is exact to 2^-24, so p is off by at most e = 2^-20 + 2^-22 (8 + |log p|) relative (three
+    roundings of log p's size, the exponential, a sum of positive terms), whatever the offset."""
+    x, tok = _draw(rows, vocab, torch.float32, seed=rows + 3 * vocab)
+    shift = torch.tensor([300.0, 0.0, -700.0, 2000.0, 120.0, -65.0])[torch.arange(rows) % 6]
+    x = (x + shift[:, None]).to(dtype)
+    g = torch.Generator().manual_seed(9)
+    gl = torch.randn(rows, generator=g) if which != "entropy" else None
+    gh = torch.randn(rows, generator=g) if which != "logprob" else None
+    got, want, logp, h = _gradient_and_formula(x, tok, 1.0, gl, gh)
+    p, far = torch.exp(logp), logp.abs()
+    e = 2.0 ** -20 + 2.0 ** -22 * (8 + far)
+    tol = (2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -22) * want.abs() + 1e-30
+    if gl is not None:
+        tol = tol + gl.double().abs()[:, None] * e * p
+    if gh is not None:
+        tol = tol + gh.double().abs()[:, None] * 4 * e * p * (1 + far + h)
+    _near(got, want, tol)
+    if dtype == torch.float32 and which == "logprob":
+        # g (1 - sum p): the sums' 2^-20 and the entries' own rounding
+        assert (got.sum(-1).abs() <= 2.0 ** -19 * gl.double().abs()).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES.values(), ids=TYPES.keys())
+@pytest.mark.parametrize("rows", [3, 130])
+def test_gradient_at_a_low_temperature(lib, rows, dtype):
+    """scale 100: log sums of thousands from ordinary logits, rows that are not uniform, both gradients."""
+    g = torch.Generator().manual_seed(21)
+    x = 15 + (0.05 if dtype == torch.float32 else 0.3) * torch.randn(rows, 9001, generator=g)
+    x[1, 40] = 16.5
+    x = x.to(dtype)
+    tok = torch.randint(0, 9001, (rows,), generator=g)
+    tok[1] = 40
+    gl, gh = torch.randn(rows, generator=g), torch.randn(rows, generator=g)
+    got, want, logp, h = _gradient_and_formula(x, tok, 100.0, gl, gh)
+    p, far = torch.exp(logp), logp.abs()
+    e = 2.0 ** -20 + 2.0 ** -22 * (8 + far)
+    tol = (2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -22) * want.abs() + 1e-30
+    tol = tol + 100 * (gl.double().abs()[:, None] + 4 * gh.double().abs()[:, None] * (1 + far + h)) * e * p
+    _near(got, want, tol)
+
+
+@pytest.mark.parametrize("dtype", TYPES.values(), ids=TYPES.keys())
+@pytest.mark.parametrize("rows,vocab", [(2, 3001), (2, 40000)])
+def test_gradient_where_the_log_sum_leaves_float32(lib, rows, vocab, dtype):
+    """scale * logit beyond float32: lse is +-inf, but the row is uniform like any other of equal logits."""
+    x = torch.full((rows, vocab), torch.finfo(dtype).min).to(dtype)
+    x[1] = torch.finfo(dtype).max
+    tok = torch.tensor([7, vocab - 1])
+    r = lt.token_logprobs(x.cuda(), tok.cuda(), scale=1.4)
+    assert r.lse.tolist() == [NEG_INF, -NEG_INF]
+    gl, gh = torch.tensor([2.0, -3.0]), torch.tensor([1.0, -1.0])
+    got, want, logp, h = _gradient_and_formula(x, tok, 1.4, gl, gh)
+    p = torch.exp(logp)
+    e = 2.0 ** -20 + 2.0 ** -22 * (8 + logp.abs())
+    tol = (2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -22) * want.abs() + 1e-30
+    tol = tol + 1.4 * (gl.double().abs()[:, None] + 4 * gh.double().abs()[:, None] * (1 + logp.abs() + h)) * e * p
+    _near(got, want, tol)
+    x[0] = NEG_INF                                    # and a row of nothing still has none
+    r = lt.token_logprobs(x.cuda(), tok.cuda(), scale=1.4)
+    got = lt.token_logprobs_backward(x.cuda(), tok.cuda(), r.lse, r.entropy, gl.cuda(), gh.cuda(), scale=1.4)
+    assert (got[0] == 0).all() and torch.isfinite(got[1]).all()
