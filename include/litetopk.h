@@ -380,7 +380,8 @@ int lt_cache4_read(const uint8_t* codes, const uint8_t* scales, int64_t num_page
                    void* stream);
 
 /* Bytes of device workspace lt_cache4_attention needs; 0 for a shape that is
-   not supported. */
+   not supported. It also serves calls of fewer tokens or requests, and with
+   lists those of a shorter one. */
 size_t lt_cache4_attention_workspace_size(int32_t num_tokens, int32_t num_requests, int32_t num_heads,
                                           int32_t num_kv_heads, int32_t head_dim, int32_t selected_k);
 

@@ -1201,11 +1201,14 @@ hipError_t run_rows(const Attn4Args& a, hipStream_t st) {
   return run<D, 128, LIST>(a, st);
 }
 
+// Rows of a dense tile, for a request's mean of rows.
+int tile_rows(int64_t rows) { return rows <= 16 ? 16 : rows <= 64 ? 64 : 128; }
+
 // What depends on host values alone: the rows of a tile, and for lists, which are
 // all as long, the parts of a tile: none but where there are too few tiles.
 void shape_of(Attn4Args& a) {
   const int64_t rows = a.list_k > 0 ? a.group : ((int64_t)a.T * a.group + a.R - 1) / (a.R > 0 ? a.R : 1);
-  a.rows_per_tile = rows <= 16 ? 16 : rows <= 64 ? 64 : 128;
+  a.rows_per_tile = tile_rows(rows);
   if (a.list_k == 0) return;
   // few tokens: more, narrower tiles rather than more parts
   if ((int64_t)a.T * a.hkv < 256) a.rows_per_tile = 16;
@@ -1216,14 +1219,17 @@ void shape_of(Attn4Args& a) {
   a.list_parts = (int)(((int64_t)a.list_k + a.list_share - 1) / a.list_share);
 }
 
-// Rows of parts that may have to be kept. Lists: only narrow tiles have parts, 512
-// at most; as much for any list, so that a larger call's workspace serves a smaller.
-size_t kept_rows(const Attn4Args& a) { return 2 * (size_t)kShares * (a.list_k > 0 ? 16 : a.rows_per_tile); }
+// Rows of parts that may have to be kept, as many as a call of no more tokens and
+// requests may need, so that a larger call's workspace serves a smaller. Dense: the
+// same tokens in one request have the widest tiles. Lists: only narrow tiles have
+// parts, 512 at most.
+size_t kept_rows(const Attn4Args& a) {
+  return 2 * (size_t)kShares * (a.list_k > 0 ? 16 : tile_rows((int64_t)a.T * a.group));
+}
 
 }  // namespace
 
-size_t attn4_workspace_bytes(Attn4Args a) {
-  shape_of(a);
+size_t attn4_workspace_bytes(const Attn4Args& a) {
   return 256 + (((size_t)a.R + 1) * 8 + 255) / 256 * 256 +
          kept_rows(a) * ((size_t)a.d * 4 + 8);
 }

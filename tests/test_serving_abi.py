@@ -82,6 +82,20 @@ def test_attention_workspace_sizes():
     assert size(32, 32, 64, 1, 128, 2048) > 0 and size(32, 32, 64, 1, 128, -1) == 0
 
 
+@pytest.mark.parametrize("hq,hkv,d", [(64, 8, 128), (8, 8, 64), (64, 1, 128), (12, 4, 64)])
+def test_attention_workspace_serves_smaller_calls(hq, hkv, d):
+    size = lt.lt_cache4_attention_workspace_size
+    counts = [0, 1, 2, 3, 8, 15, 16, 17, 64, 65, 128, 129, 255, 256, 257, 2048, 70000]
+    for k in (0, 1, 130, 2048):
+        for r in range(len(counts) - 1):
+            for t in range(len(counts) - 1):
+                at = size(counts[t], counts[r], hq, hkv, d, k)
+                assert at > 0
+                assert at <= size(counts[t + 1], counts[r], hq, hkv, d, k)
+                assert at <= size(counts[t], counts[r + 1], hq, hkv, d, k)
+        assert k == 0 or size(256, 7, hq, hkv, d, k) <= size(256, 7, hq, hkv, d, 2 * k)
+
+
 def logprobs(**over):
     a = dict(x=P, dtype=lt.LT_BF16, ld=100, rows=3, vocab=100, tok=P, scale=1.0, top=5, lp=P, h=P, lse=P, ti=P, tl=P,
              ws=P, bytes=1 << 40, stream=None)
