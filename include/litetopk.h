@@ -421,7 +421,8 @@ int lt_cache4_attention(const void* q, int64_t q_stride, int32_t num_tokens, int
                         int64_t selected_ld, int32_t selected_k, const int32_t* selected_start, float scale,
                         void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
-/* Bytes of device workspace lt_token_logprobs needs; 0 for an unsupported shape. */
+/* Bytes of device workspace lt_token_logprobs needs; 0 for an unsupported shape.
+   It also serves calls of fewer rows, entries or alternatives. */
 size_t lt_token_logprobs_workspace_size(lt_dtype dtype, int32_t rows, int32_t vocab, int32_t top);
 
 /* What a model's logits say of given tokens. With y = scale * logits (scale =

@@ -270,7 +270,7 @@ struct LogprobArgs {
   bool parts;
 };
 void logprob_shape(LogprobArgs& a);
-size_t logprob_workspace_bytes(LogprobArgs a);
+size_t logprob_workspace_bytes(const LogprobArgs& a);
 hipError_t launch_logprobs(LogprobArgs a, void* workspace, hipStream_t st);
 hipError_t launch_logprobs_backward(const void* logits, int64_t ld, bool bf16, int rows, int vocab,
                                     const int64_t* tokens, float scale, const float* lse, const float* entropy,

@@ -344,6 +344,7 @@ __device__ __forceinline__ uint32_t nth_floor(uint32_t v, int n, uint32_t* mine)
 // entries than that (21 for 20, 73 for 64 of 4096 normal values), which go out in
 // any order. (More than kList: sorted lists as above.)
 constexpr int kHeld = 2;
+constexpr int64_t kMostParts = 2048;  // of all rows
 template <class T, bool TOP>
 __global__ __launch_bounds__(kThreads) void k_logprobs_part(LogprobArgs a, Partial part) {
   constexpr int N = Vec<T>::N;
@@ -639,12 +640,12 @@ hipError_t run_forward(const LogprobArgs& a, const Partial& p, hipStream_t st) {
 }  // namespace
 
 void logprob_shape(LogprobArgs& a) {
-  // Few rows: parts that a block holds in registers, eight blocks a CU at most
+  // Few rows: parts that a block holds in registers, eight blocks a CU at most (kMostParts)
   // (8 rows of 131072: 32 parts each). More rows are split until there are four
   // blocks a CU, down to one load a thread.
   const int n = a.bf16 ? 8 : 4, unit = kThreads * n;
   const int64_t parts = ((int64_t)a.vocab + kHeld * unit - 1) / (kHeld * unit);
-  a.parts = parts > 1 && parts * a.rows <= 2048;
+  a.parts = parts > 1 && parts * a.rows <= kMostParts;
   if (a.parts) {
     a.split_len = kHeld * unit;
     a.splits = (int)parts;
@@ -659,10 +660,14 @@ void logprob_shape(LogprobArgs& a) {
   a.splits = a.vocab > 0 ? (int)(((int64_t)a.vocab + a.split_len - 1) / a.split_len) : 1;
 }
 
-size_t logprob_workspace_bytes(LogprobArgs a) {
-  logprob_shape(a);
-  if (a.splits == 1) return 256;
-  const size_t n = (size_t)a.rows * a.splits;
+// As many splits as a call of no more rows and entries may have, so that a larger
+// call's workspace serves a smaller: up to kMostParts where parts are held in
+// registers, fewer than that (two a row at least) where rows are split to fill the
+// chip, none where one load a thread covers the row.
+size_t logprob_workspace_bytes(const LogprobArgs& a) {
+  const int64_t unit = kThreads * (a.bf16 ? 8 : 4), parts = ((int64_t)a.vocab + kHeld * unit - 1) / (kHeld * unit);
+  if (a.vocab <= unit) return 256;
+  const size_t n = (size_t)std::min(kMostParts, a.rows * std::max<int64_t>(parts, 2));
   return 256 + (n * sizeof(Sums) + 255) / 256 * 256 + (a.top > 0 ? n * kList * 8 : 0);
 }
 

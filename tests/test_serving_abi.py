@@ -129,3 +129,20 @@ def test_logprob_workspace_sizes():
     size = lt.lt_token_logprobs_workspace_size
     assert size(lt.LT_F32, 1, 100000, 20) > size(lt.LT_F32, 4096, 1000, 20) >= 256
     assert size(lt.LT_FP8_E4M3FN, 1, 10, 1) == 0 and size(lt.LT_F32, 1, 10, lt.LT_LOGPROB_MAX_TOP + 1) == 0
+
+
+@pytest.mark.parametrize("dtype", [lt.LT_F32, lt.LT_BF16])
+def test_logprob_workspace_serves_smaller_calls(dtype):
+    """Sizes rise with rows, entries and alternatives."""
+    size = lt.lt_token_logprobs_workspace_size
+    rows = [0, 1, 2, 3, 7, 8, 31, 32, 33, 64, 100, 500, 1000, 1023, 1024, 1025, 2039, 5000, 100000]
+    vocabs = [0, 1, 1000, 1024, 1025, 2048, 2049, 4096, 4097, 8192, 8193, 32000, 50257, 128001, 131072, 262144, 10**7,
+              2**30]
+    for top in (0, 1, 64):
+        for i in range(len(rows) - 1):
+            for j in range(len(vocabs) - 1):
+                at = size(dtype, rows[i], vocabs[j], top)
+                assert at >= 256
+                assert at <= size(dtype, rows[i + 1], vocabs[j], top)
+                assert at <= size(dtype, rows[i], vocabs[j + 1], top)
+                assert at <= size(dtype, rows[i], vocabs[j], 64)
