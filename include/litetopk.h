@@ -317,7 +317,8 @@ int lt_dsa_union(const int32_t* topk_idx, int64_t ld, int32_t num_queries, int32
 #define LT_MAX_PAGE_SIZE 4096       /* page sizes are powers of two up to this        */
 #define LT_PLAN_MAX_REQUESTS 16384  /* requests of one lt_paged_plan call             */
 #define LT_CACHE4_MAX_HEADS 1024    /* query and KV heads                             */
-#define LT_CACHE4_MAX_KEYS 0x7FFF0000  /* cached keys of a request that count          */
+#define LT_CACHE4_MAX_KEYS 0x7FFF0000  /* cached keys of a request that count, entries
+                                          of a token's list                           */
 #define LT_LOGPROB_MAX_TOP 64       /* alternatives of lt_token_logprobs              */
 #define LT_LOGPROB_MAX_VOCAB (1 << 30)
 

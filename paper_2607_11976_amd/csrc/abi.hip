@@ -689,7 +689,7 @@ static int attn4_shape(int32_t tokens, int32_t nreq, int32_t hq, int32_t hkv, in
                        Attn4Args* a) {
   if (tokens < 0 || nreq < 0 || hq < 1 || hkv < 1 || d < 1 || list_k < 0 || hq % hkv) return LT_EINVAL;
   if (d != 64 && d != 128) return LT_EUNSUPPORTED;
-  if (hkv > LT_CACHE4_MAX_HEADS || hq > LT_CACHE4_MAX_HEADS) return LT_EUNSUPPORTED;
+  if (hkv > LT_CACHE4_MAX_HEADS || hq > LT_CACHE4_MAX_HEADS || list_k > LT_CACHE4_MAX_KEYS) return LT_EUNSUPPORTED;
   if ((int64_t)tokens * hq > 0x3FFFFFFF) return LT_EUNSUPPORTED;
   *a = Attn4Args{};
   a->T = tokens;

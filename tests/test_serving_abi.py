@@ -146,3 +146,13 @@ def test_logprob_workspace_serves_smaller_calls(dtype):
                 assert at <= size(dtype, rows[i + 1], vocabs[j], top)
                 assert at <= size(dtype, rows[i], vocabs[j + 1], top)
                 assert at <= size(dtype, rows[i], vocabs[j], 64)
+
+
+def test_attention_lists_of_too_many_entries():
+    """Places in a list are 32-bit, and a step may look some way past its end."""
+    most = 0x7FFF0000
+    for k in (most + 1, 2**31 - 64, 2**31 - 1):
+        assert attention(k=k, sel=P, sel_ld=2**31) == lt.LT_EUNSUPPORTED
+        assert lt.lt_cache4_attention_workspace_size(5, 2, 16, 4, 128, k) == 0
+    assert lt.lt_cache4_attention_workspace_size(5, 2, 16, 4, 128, most) > 0
+    assert attention(k=most, sel=P, sel_ld=2**31, bytes=16) == lt.LT_EWORKSPACE
