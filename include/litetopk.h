@@ -321,6 +321,7 @@ int lt_dsa_union(const int32_t* topk_idx, int64_t ld, int32_t num_queries, int32
                                           of a token's list                           */
 #define LT_LOGPROB_MAX_TOP 64       /* alternatives of lt_token_logprobs              */
 #define LT_LOGPROB_MAX_VOCAB (1 << 30)
+#define LT_LOGPROB_MAX_ROWS 0xFFFFFF  /* a block a row: 2^32 threads a launch         */
 
 /* The plan of a serving step: pages for the step's new tokens, and where each
    token's key and value go. Request r holds context_lens[r] tokens and adds
@@ -368,8 +369,9 @@ int lt_paged_plan(const int32_t* context_lens, const int32_t* new_lens, int32_t 
    slots outside the cache are left out). The scale is the smallest 2^e with
    max|x| <= 7 * 2^e (never below 2^-127 nor above 2^125, whose 6 is the largest
    value there is), values round to the nearest code (halfway: the even code).
-   A block that holds a value that is not finite gets
-   the scale byte 255 and reads as NaN. */
+   A block that holds a value that is not finite gets the scale byte 255 and
+   reads as NaN. At most 2^35 - 2048 values of each in a call, here and in
+   lt_cache4_read. */
 int lt_cache4_append(const void* k, const void* v, lt_dtype dtype, int64_t k_stride, int64_t v_stride, int64_t rows,
                      uint8_t* codes, uint8_t* scales, int64_t num_pages, int32_t page_size, int32_t num_kv_heads,
                      int32_t head_dim, const int64_t* slots, void* stream);

@@ -299,6 +299,9 @@ Resolved resolve_scores(const lt_options* o, int nq, int nk, int k, bool split) 
 
 inline bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
 
+// A launch counts its threads in 32 bits.
+inline bool launches(int64_t blocks, int threads) { return blocks <= 0xFFFFFFFF / threads; }
+
 // page sizes of the serving cache: powers of two up to LT_MAX_PAGE_SIZE
 inline bool page_shift_ok(int p) { return p >= 1 && p <= LT_MAX_PAGE_SIZE && (p & (p - 1)) == 0; }
 inline int page_shift(int p) { return __builtin_ctz((unsigned)p); }
@@ -665,6 +668,7 @@ int lt_cache4_append(const void* k, const void* v, lt_dtype dtype, int64_t k_str
   if (dtype != LT_F32 && dtype != LT_BF16) return LT_EUNSUPPORTED;
   if (rows < 0 || rows > 0x7FFFFFFF) return LT_EINVAL;
   if (rows == 0 || num_pages == 0) return LT_OK;
+  if (!launches((rows * num_kv_heads * (d / 8) + 255) / 256, 256)) return LT_EUNSUPPORTED;
   const int64_t width = (int64_t)num_kv_heads * d, unit = dtype == LT_F32 ? 4 : 8;
   if (k_stride < width || v_stride < width || k_stride % unit || v_stride % unit) return LT_EINVAL;
   if (!k || !v || !slots || !aligned(k, 16) || !aligned(v, 16) || !aligned(slots, 8)) return LT_EINVAL;
@@ -680,6 +684,7 @@ int lt_cache4_read(const uint8_t* codes, const uint8_t* scales, int64_t num_page
   if (rc) return rc;
   if (rows < 0 || rows > 0x7FFFFFFF) return LT_EINVAL;
   if (rows == 0) return LT_OK;
+  if (!launches((rows * num_kv_heads * (d / 8) + 255) / 256, 256)) return LT_EUNSUPPORTED;
   if (!k || !v || !slots || !aligned(k, 16) || !aligned(v, 16) || !aligned(slots, 8)) return LT_EINVAL;
   return hip_status(launch_cache4_read(c, codes, scales, slots, rows, k, v, (hipStream_t)stream));
 }
@@ -698,6 +703,7 @@ static int attn4_shape(int32_t tokens, int32_t nreq, int32_t hq, int32_t hkv, in
   a->group = hq / hkv;
   a->d = d;
   a->list_k = list_k;
+  if (!launches(attn4_blocks(*a), 256)) return LT_EUNSUPPORTED;
   return LT_OK;
 }
 
@@ -756,7 +762,7 @@ static int check_logprobs(const void* logits, lt_dtype dtype, int64_t ld, int32_
                           const int64_t* tokens, float scale) {
   if (dtype != LT_F32 && dtype != LT_BF16) return LT_EUNSUPPORTED;
   if (rows < 0 || vocab < 0 || ld < vocab || !(scale > 0.0f) || !(scale <= 3.0e38f)) return LT_EINVAL;
-  if (vocab > LT_LOGPROB_MAX_VOCAB) return LT_EUNSUPPORTED;
+  if (vocab > LT_LOGPROB_MAX_VOCAB || rows > LT_LOGPROB_MAX_ROWS) return LT_EUNSUPPORTED;
   if (rows == 0) return LT_OK;
   if ((vocab > 0 && !logits) || !aligned(logits, dtype == LT_F32 ? 4 : 2)) return LT_EINVAL;
   if (!tokens || !aligned(tokens, 8)) return LT_EINVAL;
@@ -764,8 +770,8 @@ static int check_logprobs(const void* logits, lt_dtype dtype, int64_t ld, int32_
 }
 
 size_t lt_token_logprobs_workspace_size(lt_dtype dtype, int32_t rows, int32_t vocab, int32_t top) {
-  if ((dtype != LT_F32 && dtype != LT_BF16) || rows < 0 || vocab < 0 || vocab > LT_LOGPROB_MAX_VOCAB || top < 0 ||
-      top > LT_LOGPROB_MAX_TOP)
+  if ((dtype != LT_F32 && dtype != LT_BF16) || rows < 0 || rows > LT_LOGPROB_MAX_ROWS || vocab < 0 ||
+      vocab > LT_LOGPROB_MAX_VOCAB || top < 0 || top > LT_LOGPROB_MAX_TOP)
     return 0;
   LogprobArgs a{};
   a.bf16 = dtype == LT_BF16;

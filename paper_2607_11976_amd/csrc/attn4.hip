@@ -1166,10 +1166,15 @@ hipError_t run_many(const Attn4Args& a, dim3 grid, hipStream_t st) {
   return hipSuccess;
 }
 
+// Blocks of the first launch: a share of the line each.
+int64_t blocks_of(const Attn4Args& a) {
+  return a.list_k > 0 ? (int64_t)a.T * a.hkv * a.row_tiles * a.list_parts : kShares;
+}
+
 template <int D, int ROWS, bool LIST>
 hipError_t run(const Attn4Args& a, hipStream_t st) {
   if (!LIST && a.R > kInlineRequests) k_attn4_schedule<ROWS><<<1, 1024, 0, st>>>(a);
-  const unsigned shares = LIST ? (unsigned)((int64_t)a.T * a.hkv * a.row_tiles * a.list_parts) : kShares;
+  const unsigned shares = (unsigned)blocks_of(a);
   const dim3 grid(shares);
   if constexpr (ROWS == 16) {
     k_attn4_few<D, LIST><<<grid, 256, 0, st>>>(a);
@@ -1228,6 +1233,12 @@ size_t kept_rows(const Attn4Args& a) {
 }
 
 }  // namespace
+
+int64_t attn4_blocks(const Attn4Args& args) {
+  Attn4Args a = args;
+  shape_of(a);
+  return blocks_of(a);
+}
 
 size_t attn4_workspace_bytes(const Attn4Args& a) {
   return 256 + (((size_t)a.R + 1) * 8 + 255) / 256 * 256 +

@@ -252,6 +252,7 @@ struct Attn4Args {
   float* part_o;
   float2* part_ml;
 };
+int64_t attn4_blocks(const Attn4Args& a);  // of the largest launch
 size_t attn4_workspace_bytes(const Attn4Args& a);
 hipError_t launch_attn4(Attn4Args a, void* workspace, hipStream_t st);
 

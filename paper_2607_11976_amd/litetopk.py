@@ -40,6 +40,7 @@ LT_PLAN_MAX_REQUESTS = 16384
 LT_CACHE4_MAX_HEADS = 1024
 LT_LOGPROB_MAX_TOP = 64
 LT_LOGPROB_MAX_VOCAB = 1 << 30
+LT_LOGPROB_MAX_ROWS = 0xFFFFFF
 STAGES = ("sample", "range", "filter", "select", "fallback")
 
 EXPORTED = (

@@ -156,3 +156,19 @@ def test_attention_lists_of_too_many_entries():
         assert lt.lt_cache4_attention_workspace_size(5, 2, 16, 4, 128, k) == 0
     assert lt.lt_cache4_attention_workspace_size(5, 2, 16, 4, 128, most) > 0
     assert attention(k=most, sel=P, sel_ld=2**31, bytes=16) == lt.LT_EWORKSPACE
+
+
+def test_calls_of_more_threads_than_a_launch_counts():
+    """2^32 threads of a launch: refused on the host, the largest sizes below pass these checks."""
+    for n, code in ((2**25, lt.LT_EUNSUPPORTED), (2**25 - 2, lt.LT_EINVAL)):   # x 8 heads x 16 chunks of 8 values
+        assert append(rows=n, heads=8, ks=1024, vs=1024, slots=None) == code
+        assert lt.lt_cache4_read(P, P, 4, 16, 8, 128, None, n, P, P, None) == code
+    size = lt.lt_cache4_attention_workspace_size
+    assert size(2**24 - 1, 2, 1, 1, 64, 100) > 0 and size(2**24, 2, 1, 1, 64, 100) == 0    # a block a token
+    assert size(2**24, 2, 1, 1, 64, 0) > 0
+    assert attention(tokens=2**24, hq=1, hkv=1, k=4, sel=P, sel_ld=4) == lt.LT_EUNSUPPORTED
+    assert logprobs(rows=lt.LT_LOGPROB_MAX_ROWS + 1) == lt.LT_EUNSUPPORTED
+    assert logprobs(rows=lt.LT_LOGPROB_MAX_ROWS, bytes=0) == lt.LT_EWORKSPACE
+    assert lt.lt_token_logprobs_workspace_size(lt.LT_F32, lt.LT_LOGPROB_MAX_ROWS + 1, 100, 5) == 0
+    assert lt.lt_token_logprobs_backward(P, lt.LT_F32, 100, lt.LT_LOGPROB_MAX_ROWS + 1, 100, P, 1.0, P, P, P, None, P,
+                                         100, None) == lt.LT_EUNSUPPORTED
