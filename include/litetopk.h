@@ -414,7 +414,8 @@ size_t lt_cache4_attention_workspace_size(int32_t num_tokens, int32_t num_reques
    whatever they hold.
    out        bfloat16 [num_tokens, num_heads, head_dim], 16-byte aligned.
    lse        float32 [num_tokens, num_heads] or NULL.
-   scale      > 0 and finite.
+   scale      > 0, scale * log2 e finite; scaled scores have to stay within
+              float32 too.
    workspace  256-byte aligned; contents on entry do not matter. */
 int lt_cache4_attention(const void* q, int64_t q_stride, int32_t num_tokens, int32_t num_heads, int32_t head_dim,
                         const uint8_t* codes, const uint8_t* scales, int64_t num_pages, int32_t page_size,
@@ -436,6 +437,7 @@ size_t lt_token_logprobs_workspace_size(lt_dtype dtype, int32_t rows, int32_t vo
      logits; equal ones: lower index first) and their log probabilities.
    logits     float32 or bfloat16, ld >= vocab values between rows (no
               alignment beyond the elements').
+   scale      > 0, scale * log2 e finite.
    tokens     int64 [rows]; a token outside [0, vocab) is not counted: logprob 0.
    top        0..LT_LOGPROB_MAX_TOP; a vocabulary of fewer entries is padded with
               index -1 and log probability -inf.

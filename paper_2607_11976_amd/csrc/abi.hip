@@ -302,6 +302,9 @@ inline bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
 // A launch counts its threads in 32 bits.
 inline bool launches(int64_t blocks, int threads) { return blocks <= 0xFFFFFFFF / threads; }
 
+// Softmax scales, in powers of two on the device: scale * log2 e has to be finite too.
+inline bool scale_ok(float s) { return s > 0.0f && s * 1.44269504088896340736f <= 3.402823466e38f; }
+
 // page sizes of the serving cache: powers of two up to LT_MAX_PAGE_SIZE
 inline bool page_shift_ok(int p) { return p >= 1 && p <= LT_MAX_PAGE_SIZE && (p & (p - 1)) == 0; }
 inline int page_shift(int p) { return __builtin_ctz((unsigned)p); }
@@ -726,7 +729,7 @@ int lt_cache4_attention(const void* q, int64_t q_stride, int32_t tokens, int32_t
   int rc = attn4_shape(tokens, nreq, hq, hkv, d, list_k, &a);
   if (rc) return rc;
   if ((rc = check_cache4(codes, scales, num_pages, page_size, hkv, d, &c)) != LT_OK) return rc;
-  if (table_width < 0 || table_ld < table_width || !(scale > 0.0f) || !(scale <= 3.0e38f)) return LT_EINVAL;
+  if (table_width < 0 || table_ld < table_width || !scale_ok(scale)) return LT_EINVAL;
   if (list_k > 0 ? selected_ld < list_k : selected != nullptr) return LT_EINVAL;
   if (tokens == 0) return LT_OK;
   if (num_pages == 0 || !q || !out || !cu_tokens) return LT_EINVAL;
@@ -761,7 +764,7 @@ int lt_cache4_attention(const void* q, int64_t q_stride, int32_t tokens, int32_t
 static int check_logprobs(const void* logits, lt_dtype dtype, int64_t ld, int32_t rows, int32_t vocab,
                           const int64_t* tokens, float scale) {
   if (dtype != LT_F32 && dtype != LT_BF16) return LT_EUNSUPPORTED;
-  if (rows < 0 || vocab < 0 || ld < vocab || !(scale > 0.0f) || !(scale <= 3.0e38f)) return LT_EINVAL;
+  if (rows < 0 || vocab < 0 || ld < vocab || !scale_ok(scale)) return LT_EINVAL;
   if (vocab > LT_LOGPROB_MAX_VOCAB || rows > LT_LOGPROB_MAX_ROWS) return LT_EUNSUPPORTED;
   if (rows == 0) return LT_OK;
   if ((vocab > 0 && !logits) || !aligned(logits, dtype == LT_F32 ? 4 : 2)) return LT_EINVAL;

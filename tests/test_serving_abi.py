@@ -172,3 +172,13 @@ def test_calls_of_more_threads_than_a_launch_counts():
     assert lt.lt_token_logprobs_workspace_size(lt.LT_F32, lt.LT_LOGPROB_MAX_ROWS + 1, 100, 5) == 0
     assert lt.lt_token_logprobs_backward(P, lt.LT_F32, 100, lt.LT_LOGPROB_MAX_ROWS + 1, 100, P, 1.0, P, P, P, None, P,
                                          100, None) == lt.LT_EUNSUPPORTED
+
+
+@pytest.mark.parametrize("scale,code", [(3.0e38, lt.LT_EINVAL), (2.4e38, lt.LT_EINVAL), (2.3e38, lt.LT_EWORKSPACE),
+                                        (1e-45, lt.LT_EWORKSPACE)])
+def test_scales_times_log2_e_are_finite(scale, code):
+    """Scores are taken in powers of two: a scale that overflows there made every result NaN."""
+    assert attention(scale=scale, bytes=16) == code
+    assert logprobs(scale=scale, bytes=0) == code
+    none = lt.lt_token_logprobs_backward(P, lt.LT_F32, 100, 0, 100, P, scale, P, P, P, None, P, 100, None)
+    assert none == (lt.LT_OK if code == lt.LT_EWORKSPACE else lt.LT_EINVAL)
