@@ -343,11 +343,12 @@ int lt_dsa_union(const int32_t* topk_idx, int64_t ld, int32_t num_queries, int32
                  entries that are negative and rows past the step's tokens.
    positions     int32 [token_capacity]: position in the request, -1 past the
                  step's tokens.
-   free_used_out int32 [1]: *free_used plus the pages taken; must not be
-                 free_used itself.
+   free_used_out int32 [1]: *free_used plus the pages taken.
    status        int32 [num_requests]: 0 served, 1 the table is too narrow, 2
                  no free pages.
-   Tokens beyond token_capacity get no row. Prefix sums stop at 2^31 - 1. */
+   Tokens beyond token_capacity get no row. Prefix sums stop at 2^31 - 1. No
+   result may lie in the place of an input (seq_lens in that of context_lens,
+   free_used_out in that of free_used). */
 int lt_paged_plan(const int32_t* context_lens, const int32_t* new_lens, int32_t num_requests, int32_t page_size,
                   int32_t* block_table, int64_t table_ld, int32_t table_width, const int32_t* free_pages,
                   int32_t num_free_pages, const int32_t* free_used, int32_t token_capacity, int32_t* cu_tokens,

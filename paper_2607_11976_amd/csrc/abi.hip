@@ -624,11 +624,19 @@ int lt_paged_plan(const int32_t* context_lens, const int32_t* new_lens, int32_t 
   if (nreq < 0 || table_width < 0 || table_ld < table_width || num_free < 0 || token_capacity < 0) return LT_EINVAL;
   if (!page_shift_ok(page_size)) return LT_EINVAL;
   if (nreq > LT_PLAN_MAX_REQUESTS) return LT_EUNSUPPORTED;
-  if (!free_used || !free_used_out || free_used == free_used_out || !cu_tokens) return LT_EINVAL;
+  if (!free_used || !free_used_out || !cu_tokens) return LT_EINVAL;
   if (nreq > 0 && (!context_lens || !new_lens || !seq_lens || !status)) return LT_EINVAL;
   if (nreq > 0 && table_width > 0 && !block_table) return LT_EINVAL;
   if (num_free > 0 && !free_pages) return LT_EINVAL;
   if (token_capacity > 0 && (!slots || !positions || !aligned(slots, 8))) return LT_EINVAL;
+  // blocks read the inputs while others write: no result in an input's place
+  const void *in[] = {context_lens, new_lens, free_pages}, *out[] = {cu_tokens, seq_lens, status, positions, slots,
+                                                                      free_used_out};
+  for (const void* i : in)
+    for (const void* o : out)
+      if (i && i == o) return LT_EINVAL;
+  for (const void* o : out)
+    if (o == free_used) return LT_EINVAL;
   PlanArgs a{};
   a.context = context_lens;
   a.added = new_lens;

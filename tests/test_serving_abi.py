@@ -182,3 +182,13 @@ def test_scales_times_log2_e_are_finite(scale, code):
     assert logprobs(scale=scale, bytes=0) == code
     none = lt.lt_token_logprobs_backward(P, lt.LT_F32, 100, 0, 100, P, scale, P, P, P, None, P, 100, None)
     assert none == (lt.LT_OK if code == lt.LT_EWORKSPACE else lt.LT_EINVAL)
+
+
+@pytest.mark.parametrize("over", [dict(seq="ctx"), dict(status="new"), dict(cu="new"), dict(out="used"), dict(seq="used"),
+                                  dict(pos="free"), dict(slots="free"), dict(status="ctx")])
+def test_plan_results_in_place_of_inputs(over):
+    """Blocks read the lengths while others write results: a result there would be read as a length."""
+    names = ("ctx", "new", "table", "free", "used", "cu", "seq", "slots", "pos", "out", "status")
+    own = {n: (i + 1) << 20 for i, n in enumerate(names)}
+    own.update({n: own[o] for n, o in over.items()})
+    assert plan(**own) == lt.LT_EINVAL
