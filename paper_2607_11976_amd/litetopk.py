@@ -590,13 +590,30 @@ def _table(t: torch.Tensor, rows: int):
     return t.stride(0) if rows > 1 and s[1] > 0 else s[1], s[1]
 
 
+def _empty(shape, dtype, device, stream) -> torch.Tensor:
+    """Memory for work on `stream`, from that stream's own: what the current
+    stream's allocator hands out may still be read by work queued there."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _lent(stream, workspace: torch.Tensor):
+    """The caller's workspace, used on `stream`: its memory may belong to another."""
+    if stream is not None:
+        workspace.record_stream(stream)
+
+
 def _used_on(stream, *ts):
-    """Memory allocated here on the current stream and used on `stream`: keep
-    the allocator from handing it out before that work has run."""
-    if stream is not None and stream.cuda_stream != torch.cuda.current_stream().cuda_stream:
-        for t in ts:
-            if t is not None and t.numel():
-                t.record_stream(stream)
+    """Results on `stream`'s memory, which the caller goes on to use on the current
+    stream: keep the allocator from handing them out before that work has run."""
+    if stream is not None:
+        now = torch.cuda.current_stream()
+        if stream.cuda_stream != now.cuda_stream:
+            for t in ts:
+                if t is not None and t.numel():
+                    t.record_stream(now)
 
 
 class PagedPlan(NamedTuple):
@@ -625,9 +642,9 @@ def paged_plan(context_lens: torch.Tensor, new_lens: torch.Tensor, block_table: 
     ld, width = _table(block_table, n)
     dev = context_lens.device
     # the 32-bit results in one allocation
-    cu, seq, used, status, positions = torch.empty(
-        3 * n + 2 + token_capacity, dtype=torch.int32, device=dev).split_with_sizes((n + 1, n, 1, n, token_capacity))
-    p = PagedPlan(cu, seq, torch.empty(token_capacity, dtype=torch.int64, device=dev), positions, used, status)
+    cu, seq, used, status, positions = _empty(3 * n + 2 + token_capacity, torch.int32, dev, stream).split_with_sizes(
+        (n + 1, n, 1, n, token_capacity))
+    p = PagedPlan(cu, seq, _empty(token_capacity, torch.int64, dev, stream), positions, used, status)
     st = lt_paged_plan(_ptr(context_lens), _ptr(new_lens), n, page_size, _ptr(block_table), ld, width,
                        _ptr(free_pages), free_pages.numel(), _ptr(free_used), token_capacity, _ptr(p.cu_tokens),
                        _ptr(p.seq_lens), _ptr(p.slots), _ptr(p.positions), _ptr(p.free_used), _ptr(p.status),
@@ -689,8 +706,8 @@ def cache4_read(codes: torch.Tensor, scales: torch.Tensor, slots: torch.Tensor, 
     _on_gpu(slots)
     _need(slots.dtype == torch.int64 and slots.dim() == 1, "slots must be int64 [rows]")
     n = slots.numel()
-    k = torch.empty((n, heads, d), dtype=torch.bfloat16, device=slots.device)
-    v = torch.empty_like(k)
+    k = _empty((n, heads, d), torch.bfloat16, slots.device, stream)
+    v = _empty((n, heads, d), torch.bfloat16, slots.device, stream)
     st = lt_cache4_read(_ptr(codes), _ptr(scales), pages, page, heads, d, _ptr(slots), n, _ptr(k), _ptr(v),
                         _stream_of(stream, slots))
     _check(st, "lt_cache4_read")
@@ -731,19 +748,21 @@ def cache4_attention(q: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
               "selected must be an int32 [T, k] GPU matrix with unit column stride")
         k = selected.shape[1]
         sel_ld = selected.stride(0) if tokens > 1 else k
-    out = torch.empty((tokens, hq, d), dtype=torch.bfloat16, device=q.device)
-    lse = torch.empty((tokens, hq), dtype=torch.float32, device=q.device) if return_lse else None
+    out = _empty((tokens, hq, d), torch.bfloat16, q.device, stream)
+    lse = _empty((tokens, hq), torch.float32, q.device, stream) if return_lse else None
     need = lt_cache4_attention_workspace_size(tokens, n, hq, hkv, d, k)
     _need(need > 0, "unsupported shape for lt_cache4_attention")
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        workspace = _empty(need, torch.uint8, q.device, stream)
+    else:
+        _lent(stream, workspace)
     st = lt_cache4_attention(_ptr(q), qs, tokens, hq, d, _ptr(codes), _ptr(scales), pages, page, hkv,
                              _ptr(block_table), ld, width, _ptr(cu_tokens), _ptr(seq_lens), n, _ptr(visible_start),
                              _ptr(visible_end), _ptr(selected), sel_ld, k, _ptr(selected_start),
                              d ** -0.5 if scale is None else scale, _ptr(out), _ptr(lse), _ptr(workspace),
                              workspace.numel(), _stream_of(stream, q))
     _check(st, "lt_cache4_attention")
-    _used_on(stream, out, lse, workspace)
+    _used_on(stream, out, lse)
     return out, lse
 
 
@@ -778,17 +797,18 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0, sca
     need = lt_token_logprobs_workspace_size(dt, rows, vocab, top)
     _need(need > 0, "unsupported shape for lt_token_logprobs (top must be 0..%d)" % LT_LOGPROB_MAX_TOP)
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        workspace = _empty(need, torch.uint8, dev, stream)
+    else:
+        _lent(stream, workspace)
     n = min(top, vocab)
-    f = torch.empty(rows * (3 + n), dtype=torch.float32, device=dev)
+    f = _empty(rows * (3 + n), torch.float32, dev, stream)
     logprob, entropy, lse, best = f.split_with_sizes((rows, rows, rows, rows * n))
-    r = TokenLogprobs(logprob, entropy, lse, torch.empty((rows, n), dtype=torch.int32, device=dev),
-                      best.view(rows, n))
+    r = TokenLogprobs(logprob, entropy, lse, _empty((rows, n), torch.int32, dev, stream), best.view(rows, n))
     st = lt_token_logprobs(_ptr(logits), dt, ld, rows, vocab, _ptr(tokens), scale, n, _ptr(r.logprob),
                            _ptr(r.entropy), _ptr(r.lse), _ptr(r.top_index), _ptr(r.top_logprob), _ptr(workspace),
                            workspace.numel(), _stream_of(stream, logits))
     _check(st, "lt_token_logprobs")
-    _used_on(stream, f, r.top_index, r.top_logprob, workspace)
+    _used_on(stream, f, r.top_index)
     return r
 
 
@@ -805,7 +825,7 @@ def token_logprobs_backward(logits: torch.Tensor, tokens: torch.Tensor, lse: tor
               "lse, entropy and the gradients must be float32 [rows]")
     # rows start on a line: full-width stores whatever the vocabulary's size
     pad = (vocab + 63) // 64 * 64
-    out = torch.empty((rows, pad), dtype=logits.dtype, device=logits.device)[:, :vocab]
+    out = _empty((rows, pad), logits.dtype, logits.device, stream)[:, :vocab]
     st = lt_token_logprobs_backward(_ptr(logits), _dtype_code(logits), ld, rows, vocab, _ptr(tokens), scale, _ptr(lse),
                                     _ptr(entropy), _ptr(grad_logprob), _ptr(grad_entropy), _ptr(out), pad,
                                     _stream_of(stream, logits))

@@ -169,3 +169,30 @@ def test_argument_errors_raise(lib):
         lt.cache4_read(codes, scales[:1], slots)
     with pytest.raises(lt.LiteTopKError):
         lt.cache4_append(k.transpose(0, 1).contiguous().transpose(0, 1), k, codes, scales, slots)
+
+
+def test_results_on_another_stream_take_its_own_memory(lib):
+    """Memory that was freed here while work queued here still reads it is not written by a call on another stream."""
+    codes, scales = lt.cache4_empty(2, 16, 8, 128)
+    slots = torch.zeros(1 << 14, dtype=torch.int64, device="cuda")
+    zero = [torch.zeros(1, dtype=torch.int32, device="cuda") for _ in range(4)]
+    table = torch.zeros(1, 1, dtype=torch.int32, device="cuda")
+    ones = torch.ones(4096, 4096, device="cuda")
+    s = torch.cuda.Stream()
+    for call in (lambda: lt.cache4_read(codes, scales, slots, stream=s),
+                 lambda: [lt.paged_plan(zero[0], zero[1], table, zero[2], zero[3], 16, 1 << 22, stream=s).slots]):
+        a = torch.arange(1 << 23, dtype=torch.int32, device="cuda")     # 32 MiB, as large as a result
+        keep, want = torch.empty_like(a), a.cpu()
+        torch.cuda.synchronize()
+        x = ones
+        for _ in range(20):
+            x = torch.mm(x, ones)
+        keep.copy_(a)
+        lo, hi = a.data_ptr(), a.data_ptr() + a.numel() * 4
+        del a
+        for t in call():
+            p = t.data_ptr()
+            assert p + t.numel() * t.element_size() <= lo or p >= hi
+        s.synchronize()
+        torch.cuda.synchronize()
+        assert torch.equal(keep.cpu(), want)
