@@ -599,10 +599,16 @@ def _empty(shape, dtype, device, stream) -> torch.Tensor:
         return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _lent(stream, workspace: torch.Tensor):
-    """The caller's workspace, used on `stream`: its memory may belong to another."""
+def _workspace(t: Optional[torch.Tensor], need: int, device, stream) -> torch.Tensor:
+    """`need` bytes for work on `stream`, or the caller's (whose memory may belong to
+    another stream; its size is checked by the call)."""
+    if t is None:
+        return _empty(need, torch.uint8, device, stream)
+    if not (t.is_cuda and t.is_contiguous()):
+        raise LiteTopKError("workspace must be contiguous memory on the GPU")
     if stream is not None:
-        workspace.record_stream(stream)
+        t.record_stream(stream)
+    return t
 
 
 def _used_on(stream, *ts):
@@ -752,10 +758,7 @@ def cache4_attention(q: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
     lse = _empty((tokens, hq), torch.float32, q.device, stream) if return_lse else None
     need = lt_cache4_attention_workspace_size(tokens, n, hq, hkv, d, k)
     _need(need > 0, "unsupported shape for lt_cache4_attention")
-    if workspace is None:
-        workspace = _empty(need, torch.uint8, q.device, stream)
-    else:
-        _lent(stream, workspace)
+    workspace = _workspace(workspace, need, q.device, stream)
     st = lt_cache4_attention(_ptr(q), qs, tokens, hq, d, _ptr(codes), _ptr(scales), pages, page, hkv,
                              _ptr(block_table), ld, width, _ptr(cu_tokens), _ptr(seq_lens), n, _ptr(visible_start),
                              _ptr(visible_end), _ptr(selected), sel_ld, k, _ptr(selected_start),
@@ -796,10 +799,7 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0, sca
     dt, dev = _dtype_code(logits), logits.device
     need = lt_token_logprobs_workspace_size(dt, rows, vocab, top)
     _need(need > 0, "unsupported shape for lt_token_logprobs (top must be 0..%d)" % LT_LOGPROB_MAX_TOP)
-    if workspace is None:
-        workspace = _empty(need, torch.uint8, dev, stream)
-    else:
-        _lent(stream, workspace)
+    workspace = _workspace(workspace, need, dev, stream)
     n = min(top, vocab)
     f = _empty(rows * (3 + n), torch.float32, dev, stream)
     logprob, entropy, lse, best = f.split_with_sizes((rows, rows, rows, rows * n))

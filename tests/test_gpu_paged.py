@@ -196,3 +196,23 @@ def test_results_on_another_stream_take_its_own_memory(lib):
         s.synchronize()
         torch.cuda.synchronize()
         assert torch.equal(keep.cpu(), want)
+
+
+def test_workspaces_that_are_not_memory_of_their_size(lib):
+    """Host memory, and one byte that is expanded to a large size: neither is written."""
+    codes, scales = lt.cache4_empty(2, 16, 1, 64)
+    i = dict(dtype=torch.int32, device="cuda")
+    q = torch.zeros(1, 4, 64, dtype=torch.bfloat16, device="cuda")
+    args = (q, codes, scales, torch.zeros(1, 2, **i), torch.tensor([0, 1], **i), torch.tensor([5], **i))
+    x, tok = torch.zeros(2, 50000, device="cuda"), torch.zeros(2, dtype=torch.int64, device="cuda")
+    for bad in (torch.empty(1 << 24, dtype=torch.uint8), torch.zeros(1, dtype=torch.uint8, device="cuda").expand(1 << 24),
+                torch.zeros(1 << 24, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(lt.LiteTopKError):
+            lt.cache4_attention(*args, workspace=bad)
+        with pytest.raises(lt.LiteTopKError):
+            lt.token_logprobs(x, tok, top=5, workspace=bad)
+    own = torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
+    want = lt.cache4_attention(*args)
+    assert all(torch.equal(a, b) for a, b in zip(lt.cache4_attention(*args, workspace=own), want))
+    want = lt.token_logprobs(x, tok, top=5)
+    assert all(torch.equal(a, b) for a, b in zip(lt.token_logprobs(x, tok, top=5, workspace=own), want))
