@@ -61,6 +61,8 @@ class Decoder:
         """Logits after the last token of each sequence; tokens lie in sequence order."""
         w, x = self.w, self.w.embed[tokens]
         plan = lt.paged_plan(self.lens, new_lens, self.table, self.free, self.used, PAGE, tokens.numel())
+        if plan.status.any():
+            raise RuntimeError("no room for the new tokens of sequences %s" % plan.status.nonzero().flatten().tolist())
         lt.cache4_append((x @ w.k).view(-1, KV_HEADS, DIM), (x @ w.v).view(-1, KV_HEADS, DIM), self.codes, self.scales,
                          plan.slots)
         seq = torch.repeat_interleave(torch.arange(self.n, device="cuda"), new_lens)

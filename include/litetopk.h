@@ -345,7 +345,12 @@ int lt_dsa_union(const int32_t* topk_idx, int64_t ld, int32_t num_queries, int32
                  step's tokens.
    free_used_out int32 [1]: *free_used plus the pages taken.
    status        int32 [num_requests]: 0 served, 1 the table is too narrow, 2
-                 no free pages.
+                 no free pages. The tokens of a request that was not served
+                 stay in cu_tokens, without slots: lt_cache4_attention cannot
+                 tell, and by its causal default they would see the held keys
+                 as if they were the last of them. Look at the status first,
+                 or pass visible_end = positions + 1, 0 where the slot is -1
+                 (out = 0, lse = -inf).
    Tokens beyond token_capacity get no row. Prefix sums stop at 2^31 - 1. No
    result may lie in the place of an input (seq_lens in that of context_lens,
    free_used_out in that of free_used). */

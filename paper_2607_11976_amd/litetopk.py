@@ -638,7 +638,9 @@ def paged_plan(context_lens: torch.Tensor, new_lens: torch.Tensor, block_table: 
     """Block tables and slot maps of a step, built on the GPU from the
     requests' lengths (int32 [R] each): pages for the new tokens are taken from
     free_pages [free_used[0]:] in request order and entered into block_table
-    [R, W] (in place), and every new token gets its slot and position."""
+    [R, W] (in place), and every new token gets its slot and position. Look at
+    `status` before the step goes on: the tokens of a request that was not served
+    have no slots, but cache4_attention would still give them a result."""
     n = context_lens.numel()
     _int32(context_lens, None, "context_lens")
     _int32(new_lens, n, "new_lens")
