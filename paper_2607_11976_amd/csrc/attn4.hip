@@ -1194,8 +1194,10 @@ hipError_t run(const Attn4Args& a, hipStream_t st) {
     }
     if (e != hipSuccess) return e;
   }
-  if (!LIST || a.list_parts > 1)
-    k_attn4_join<D, ROWS, LIST><<<dim3(shares - 1, ROWS == 16 ? 2 : ROWS / 32), 256, 0, st>>>(a);
+  if constexpr (!LIST || ROWS == 16) {  // wide list tiles have one part
+    if (!LIST || a.list_parts > 1)
+      k_attn4_join<D, ROWS, LIST><<<dim3(shares - 1, ROWS == 16 ? 2 : ROWS / 32), 256, 0, st>>>(a);
+  }
   return hipGetLastError();
 }
 
