@@ -402,8 +402,8 @@ size_t lt_cache4_attention_workspace_size(int32_t num_tokens, int32_t num_reques
    q          bfloat16 [num_tokens, num_heads, head_dim], q_stride values
               between tokens (a multiple of 8), 16-byte aligned.
    cu_tokens  int32 [num_requests + 1], ascending: request r's tokens are
-              [cu[r], cu[r + 1]). Tokens from cu[num_requests] on belong to no
-              request (a padded batch).
+              [cu[r], cu[r + 1]). Tokens before cu[0] and from
+              cu[num_requests] on belong to no request (a padded batch).
    seq_lens   int32 [num_requests]: cached keys of the request, the step's own
               among them.
    Token t, the i-th of n of its request, sees the keys [s_t, e_t): e_t =
@@ -417,7 +417,10 @@ size_t lt_cache4_attention_workspace_size(int32_t num_tokens, int32_t num_reques
    twice. Keys whose page is not in the table or not in the cache do not count.
    A token that sees no key, or belongs to no request, gets out = 0 and lse =
    -inf. Keys and values that a token does not see never reach its result,
-   whatever they hold.
+   whatever they hold. num_pages >= 1 where there are tokens.
+   One call takes requests of any lengths, but without lists its tiles are as
+   wide as num_tokens * num_heads / num_kv_heads / num_requests asks for: a long
+   prompt beside many requests of one token is faster in a call of its own.
    out        bfloat16 [num_tokens, num_heads, head_dim], 16-byte aligned.
    lse        float32 [num_tokens, num_heads] or NULL.
    scale      > 0, scale * log2 e finite; scaled scores have to stay within

@@ -431,8 +431,9 @@ __device__ __forceinline__ uint32_t value_byte(const KeyRegs<D>& x, int part, bo
 }
 
 // Rows of decoded keys (k_attn4_many) and values (k_attn4_few) in LDS, in bytes.
-// 16 lanes that read 16 bytes of 16 key rows, and 32 that read 8 bytes of 8
-// value rows in fours, meet every bank once.
+// The padding spreads 16 lanes that read 16 bytes of 16 key rows, and 32 that read 8
+// bytes of 8 value rows in fours, over all banks. Conflicts are left, mostly by groups
+// of lanes other than these: 39% of LDS's busy cycles in a decode batch.
 template <int D>
 constexpr int kKRow = 2 * D + 16;
 template <int D>
@@ -872,8 +873,9 @@ struct Wide {
 };
 
 // Decoded values in LDS: rows of 2 D bytes whose 16-byte chunks are permuted by
-// the key, chunk ^ swizzle(key). Sixteen lanes that write a chunk of four keys'
-// quarters, and 32 that read 64 bytes of four keys, then meet every bank once.
+// the key, chunk ^ swizzle(key). It spreads sixteen lanes that write a chunk of four
+// keys' quarters, and 32 that read 64 bytes of four keys, over all banks; conflicts
+// still are 24% of LDS's busy cycles in a prefill and 32% with lists.
 template <int D>
 __device__ __forceinline__ int swizzle(int key) {
   return D == 128 ? 5 * (key & 3) : 5 * ((key >> 1) & 1);
@@ -1184,8 +1186,11 @@ hipError_t run(const Attn4Args& a, hipStream_t st) {
       e = run_many<D, 4, 1, LIST>(a, grid, st);
     } else if constexpr (LIST) {
       // Four waves a tile, 512 tiles at once, or two, 1024 at once, which has fewer
-      // starts: a round of lists of 2048 keys takes 53 us or 95 (1000 tokens 106 and
-      // 96, 1500 tokens 155 and 168, 512 tokens 57 and 80).
+      // starts: the rounds of lists of 2048 keys take 9 and 5. Two and four waves, us:
+      // 2048 keys, 512 tokens 78 and 57, 1000 98 and 105, 1500 164 and 156, 2000 189
+      // and 203; 1000 keys, the same tokens 45 and 34, 54 and 63, 93 and 91, 108 and
+      // 117; 256 keys 19 and 18, 26 and 33, 40 and 45, 56 and 58. So shorter lists lose
+      // up to 20% where the rule takes four waves for a third half-filled round.
       const int64_t tiles = grid.x;
       e = 9 * ((tiles + 1023) / 1024) <= 5 * ((tiles + 511) / 512) ? run_many<D, 2, 1, LIST>(a, grid, st)
                                                                    : run_many<D, 2, 2, LIST>(a, grid, st);
@@ -1217,7 +1222,12 @@ void shape_of(Attn4Args& a) {
   const int64_t rows = a.list_k > 0 ? a.group : ((int64_t)a.T * a.group + a.R - 1) / (a.R > 0 ? a.R : 1);
   a.rows_per_tile = tile_rows(rows);
   if (a.list_k == 0) return;
-  // few tokens: more, narrower tiles rather than more parts
+  // Few tokens: more, narrower tiles. Narrow and wide (of one part), lists of 2048 keys,
+  // us: 64 heads, 64 tokens 25 and 42, 128 33 and 43, 192 50 and 44, 256 61 and 45, 512
+  // 108 and 55; 32 heads, 128 25 and 42, 256 31 and 42, 320 48 and 51, 512 58 and 52. Of
+  // 256 keys, 64 heads: 64 tokens 9 and 12, 128 12 and 13, 192 18 and 13, 256 20 and 13.
+  // The line fits neither group exactly: 64 heads lose up to 15 us from 160 tokens on,
+  // 32 heads up to 11 from 256 to 320.
   if ((int64_t)a.T * a.hkv < 256) a.rows_per_tile = 16;
   a.row_tiles = (a.group + a.rows_per_tile - 1) / a.rows_per_tile;
   const int64_t tiles = (int64_t)a.T * a.hkv * a.row_tiles, most = ((int64_t)a.list_k + kMinShare - 1) / kMinShare;

@@ -11,9 +11,16 @@
 // H = (log2 s - u / s) ln 2, none with a large difference; logits at their type's
 // lowest value are values like any other. The best `top` entries are kept by each
 // wave, sorted over its lanes (one 64-bit key a lane: value, then the lower
-// index), behind a threshold that the waves of a block share. Bound by reading
-// the logits: 2039 rows of 128001 in bfloat16 (0.52 GB) take 131 us, 4.0 TB/s;
-// more loads a thread or more blocks a CU lose.
+// index), behind a threshold that the waves of a block share. Bound by reading the
+// logits where few are asked for: 2039 rows of 128001 in bfloat16 (0.52 GB) take 126 us
+// without, 134 with the best one, 4.2 and 3.9 TB/s, in float32 189 and 194, 5.5 and
+// 5.4; more loads a thread or more blocks a CU lose. More of the best are inserted one
+// by one before the threshold holds: with 5, 20 and 64 145, 194 and 351 us in bfloat16,
+// 198, 230 and 341 in float32.
+//
+// The entropy is a difference of two sums of up to kSlack, and where one entry holds
+// nearly all weight, of a sum near 1 and its rounding: its error, like the log
+// probabilities', is absolute, up to 1e-6 in rows of every kind tried, not relative.
 #include <algorithm>
 
 #include "internal.hpp"
@@ -520,8 +527,9 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_join(LogprobArgs a, Parti
 }
 
 // ---- gradient: one pass, bound by reading and writing the logits once ----
-// 2039 rows of 128001 in bfloat16 (1.04 GB) take 210 us, 5.0 TB/s, where rows of a
-// large lse (below), which are read twice, take 294; in float32 413 and 578.
+// 2039 rows of 128001 in bfloat16 (1.04 GB) take 183 us on one card and 210 on another,
+// 5.7 and 5.0 TB/s; on the latter rows of a large lse (below), which are read twice,
+// take 294, and in float32 413 and 578.
 // p = w 2^((x - from) scale log2 e - minus log2 e), with from = 0, minus = lse and w = 1
 // where lse is near 0: half its last bit is then an error of at most 2^-21, common to
 // the row's p, as large as the exponential's own. That doubles with every power of two

@@ -795,7 +795,9 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, top: int = 0, sca
     """Log probability of each row's token under softmax(scale * logits), the
     row's entropy, log normaliser and `top` best alternatives with their log
     probabilities (higher logit first, equal ones by index). A token outside the
-    vocabulary (-1) is not counted: its log probability is 0."""
+    vocabulary (-1) is not counted: its log probability is 0. The results are not
+    part of an autograd graph, whether or not the logits are: their gradient is
+    token_logprobs_backward's."""
     ld = _logits(logits, tokens)
     rows, vocab = logits.shape
     dt, dev = _dtype_code(logits), logits.device
@@ -818,7 +820,8 @@ def token_logprobs_backward(logits: torch.Tensor, tokens: torch.Tensor, lse: tor
                             grad_logprob: Optional[torch.Tensor] = None, grad_entropy: Optional[torch.Tensor] = None,
                             scale: float = 1.0, stream=None) -> torch.Tensor:
     """The logits' gradient (in their type) from those of token_logprobs'
-    logprob and entropy (float32 [rows], None = zero) and its lse and entropy."""
+    logprob and entropy (float32 [rows], None = zero) and its lse and entropy.
+    For a training step pass the result on: logits.backward(gradient)."""
     ld = _logits(logits, tokens)
     rows, vocab = logits.shape
     for t in (lse, entropy, grad_logprob, grad_entropy):
