@@ -467,6 +467,133 @@ int lt_token_logprobs_backward(const void* logits, lt_dtype dtype, int64_t ld, i
                                const float* grad_logprob, const float* grad_entropy, void* grad_logits,
                                int64_t grad_ld, void* stream);
 
+/* ---- rotary positions ----------------------------------------------------- */
+
+#define LT_ROTARY_INTERLEAVED 1u    /* pairs are values (2 i, 2 i + 1), else (i, i + num_pairs) */
+#define LT_ROTARY_INVERSE 2u        /* turned back: the gradient of the call without it        */
+#define LT_ROTARY_MAX_DIM 1024      /* values of a head                                        */
+
+/* Rotary positions. Of every head's values the part [rotary_start, rotary_start +
+   2 num_pairs) is turned, pair i of token t by the angle a = positions[t] *
+   inv_freq[i]:
+     y1 = x1 c - x2 s,  y2 = x2 c + x1 s,  c = amplitude cos a,  s = amplitude sin a;
+   other values pass as they are. The angle is taken in 64 bits (exact frequencies
+   stay exact at any position), c and s are rounded to float32, the products and sums
+   are float32 and each rounded.
+   x, out     [num_tokens, num_heads, head_dim], token_stride and head_stride values
+              apart; float32 or bfloat16, of out the same or bfloat16. No alignment
+              beyond the elements' (16-byte aligned rows whose part fills vectors of 8
+              are fastest). out may be x with the same type and strides; it must not
+              overlap x otherwise.
+   positions  DEVICE int32 [num_tokens]. A token of negative position (padding)
+              becomes zeros.
+   inv_freq   DEVICE float32 [num_pairs], in radians per position (not read for 0).
+   flags      LT_ROTARY_INTERLEAVED, LT_ROTARY_INVERSE. */
+int lt_rotary(const void* x, lt_dtype dtype, int64_t token_stride, int64_t head_stride, int32_t num_tokens,
+              int32_t num_heads, int32_t head_dim, const int32_t* positions, const float* inv_freq,
+              int32_t num_pairs, int32_t rotary_start, double amplitude, uint32_t flags, void* out,
+              lt_dtype out_dtype, int64_t out_token_stride, int64_t out_head_stride, void* stream);
+
+/* The same as fp8, as lt_indexer_topk reads queries and keys: codes E4M3FN
+   [num_tokens, num_heads, head_dim] contiguous and scales float32 [num_tokens,
+   num_heads]. The scale is the smallest power of two 2^e with max|y| <= 448 * 2^e
+   (never below 2^-126), values round to the nearest code (halfway: the even one). A
+   head that holds a value that is not finite gets the scale NaN and codes of 0. */
+int lt_rotary_fp8(const void* x, lt_dtype dtype, int64_t token_stride, int64_t head_stride, int32_t num_tokens,
+                  int32_t num_heads, int32_t head_dim, const int32_t* positions, const float* inv_freq,
+                  int32_t num_pairs, int32_t rotary_start, double amplitude, uint32_t flags, uint8_t* codes,
+                  float* scales, void* stream);
+
+/* lt_cache4_append with the keys rotated on the way (in float32, not rounded before
+   they are quantised), and a step's queries beside them: q [rows, num_heads,
+   head_dim] of the same type, q_stride values between rows, rotated into q_out
+   bfloat16 [rows, num_heads, head_dim], contiguous and 16-byte aligned, as
+   lt_cache4_attention reads it (q NULL: none; num_heads is then 0). positions int32
+   [rows]: a row of negative position writes nothing to the cache, and its query
+   becomes zeros. Other arguments as for lt_cache4_append and lt_rotary; flags:
+   LT_ROTARY_INTERLEAVED. q rows need no alignment. */
+int lt_cache4_append_rotary(const void* k, const void* v, lt_dtype dtype, int64_t k_stride, int64_t v_stride,
+                            int64_t rows, uint8_t* codes, uint8_t* scales, int64_t num_pages, int32_t page_size,
+                            int32_t num_kv_heads, int32_t head_dim, const int64_t* slots, const int32_t* positions,
+                            const float* inv_freq, int32_t num_pairs, int32_t rotary_start, double amplitude,
+                            uint32_t flags, const void* q, int64_t q_stride, int32_t num_heads, void* q_out,
+                            void* stream);
+
+/* ---- beam search ----------------------------------------------------------- */
+
+#define LT_BEAM_MAX_TOP 64          /* continuations of a request                     */
+#define LT_BEAM_MAX_BEAMS 1024      /* beams of a request in lt_beam_select           */
+#define LT_REORDER_MAX_GROUP 64     /* beams of a request in lt_paged_reorder         */
+
+/* Bytes of device workspace lt_beam_select needs; 0 for an unsupported shape. It also
+   serves calls of fewer requests, beams, entries or continuations. */
+size_t lt_beam_select_workspace_size(lt_dtype dtype, int32_t batch, int32_t beams, int32_t vocab, int32_t top);
+
+/* The best continuations of every request over its beams and the vocabulary: of the
+   candidates (w, v) with
+     score = cum[b, w] + scale * logits[b * beams + w, v] - lse[b, w],
+     lse = log sum_v exp(scale * logits),
+   the `top` of largest score. Scores are float32, rounded once; equal ones are ordered
+   by beam, then by logit (larger first), then by token.
+   logits     float32 or bfloat16 [batch * beams, vocab], ld >= vocab values between
+              rows (no alignment beyond the elements').
+   cum        float32 [batch, beams]: the beams' scores so far; -inf (or NaN): the beam
+              is not alive, its logits are not looked at.
+   scale      > 0, scale * log2 e finite.
+   out_score  float32 [batch, top], out_beam and out_token int32 [batch, top], best
+              first. Only scores above -inf are candidates (a logit of -inf is masked
+              out; a beam whose logits hold NaN or +inf has none); where there are
+              fewer than `top` of them, -inf, -1 and -1 follow. */
+int lt_beam_select(const void* logits, lt_dtype dtype, int64_t ld, int32_t batch, int32_t beams, int32_t vocab,
+                   const float* cum, double scale, int32_t top, float* out_score, int32_t* out_beam,
+                   int32_t* out_token, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of device workspace lt_paged_reorder needs (0 for a negative or too large
+   num_rows); it also serves fewer rows. */
+size_t lt_paged_reorder_workspace_size(int32_t num_rows);
+
+/* Rows of a paged cache (lt_paged_plan's block table and free list) go on as their
+   parents: after a step of beam search row r of a request takes the place of a child of
+   row parents[r]. Rows [g * group, (g + 1) * group) are the beams of request g;
+   parents[r] (DEVICE int32 [num_rows]) counts within the group, and anything outside
+   [0, group) ends the row. Row r held the pages block_table[r * table_ld + i], i <
+   ceil(seq_lens[r] / page_size) (at most table_width).
+   A child shares its parent's full pages; a partial page goes to the parent's first
+   child (lowest r), the other children get a page of the free list each, and a copy to
+   be made into it (lt_cache4_copy, for each layer's cache). Pages of a row without
+   children go back onto the free list, free_pages[used - 1, used - 2, ...] with used =
+   *free_used, in row order, unless a row that has children or lies before it in its
+   group holds them too; they are the first that copies take. keep_pages (int32
+   [num_rows] or NULL): so many first pages of a row are not given back (a prefix that
+   other groups share).
+   It relies on this: rows of a group that share pages share them from the first on (as
+   this call leaves them), partial pages are one row's alone, and the pages in the table
+   came from the list. Entries that are negative are neither given back nor copied.
+   new_table     int32 [num_rows, table_width], new_table_ld between rows: every entry is
+                 written, -1 behind a row's pages.
+   new_lens      int32 [num_rows]: the parent's length, 0 for a row that ends.
+   copies        int32 [num_rows, 2]: page to copy and page to write, or -1, -1.
+   free_used_out int32 [1].
+   status        int32 [num_rows]: 0 goes on, 1 ended by its parent, 2 ended because the
+                 list has no page for its copy.
+   The call is a function of its inputs and writes to free_pages only before *free_used:
+   calling it again with the same arguments gives the same result. No result may lie in
+   the place of an input (free_pages apart).
+   Limits: num_rows a multiple of group, at most LT_PLAN_MAX_REQUESTS; num_rows *
+   table_width < 2^31. workspace 256-byte aligned; contents on entry do not matter. */
+int lt_paged_reorder(const int32_t* block_table, int64_t table_ld, int32_t table_width, const int32_t* seq_lens,
+                     const int32_t* parents, int32_t num_rows, int32_t group, int32_t page_size,
+                     const int32_t* keep_pages, int32_t* free_pages, int32_t num_free_pages,
+                     const int32_t* free_used, int32_t* new_table, int64_t new_table_ld, int32_t* new_lens,
+                     int32_t* copies, int32_t* free_used_out, int32_t* status, void* workspace,
+                     size_t workspace_bytes, void* stream);
+
+/* Copies whole pages of a 4-bit cache: copies int32 [n, 2], page to copy and page to
+   write; pairs with a page outside the cache are left out. No page that is written may
+   occur twice or be copied in the same call (lt_paged_reorder's are such). */
+int lt_cache4_copy(uint8_t* codes, uint8_t* scales, int64_t num_pages, int32_t page_size, int32_t num_kv_heads,
+                   int32_t head_dim, const int32_t* copies, int32_t n, void* stream);
+
 /* ---- timing helpers ------------------------------------------------------- */
 
 /* Thin wrappers over hipEventCreateWithFlags / hipEventDestroy /

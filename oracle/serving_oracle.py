@@ -186,3 +186,94 @@ def token_logprobs_backward(logits, tokens, scale, g_logprob, g_entropy):
     if g_entropy is not None:
         g = g - g_entropy.double()[:, None] * (xlogx + p * entropy)
     return torch.where(none, torch.zeros_like(g), scale * g)
+
+
+# ---- rotary positions ------------------------------------------------------
+
+def rotary(x, positions, freq, start=0, interleaved=False, amplitude=1.0, inverse=False):
+    """x [tokens, heads, d] in 64 bits, token by token and pair by pair."""
+    y = x.double().clone()
+    n = len(freq)
+    f = freq.double()
+    for t, p in enumerate(positions.tolist()):
+        if p < 0:
+            y[t] = 0.0
+            continue
+        for i in range(n):
+            a, b = (start + 2 * i, start + 2 * i + 1) if interleaved else (start + i, start + n + i)
+            angle = float(f[i]) * p * (-1 if inverse else 1)
+            c, s = amplitude * math.cos(angle), amplitude * math.sin(angle)
+            u, v = x[t, :, a].double(), x[t, :, b].double()
+            y[t, :, a] = u * c - v * s
+            y[t, :, b] = v * c + u * s
+    return y
+
+
+def fp8_exponent(top: float) -> int:
+    """The smallest e >= -126 with top <= 448 * 2^e."""
+    e = -126
+    if top > 0:
+        e = max(e, math.frexp(top / 448)[1] - 2)
+        while top > math.ldexp(448.0, e):
+            e += 1
+    return e
+
+
+# ---- beam search -----------------------------------------------------------
+
+def beam_scores(logits, cum, scale=1.0):
+    """Scores [requests, beams, vocab] in 64 bits; -inf for what is no candidate."""
+    reqs, beams = cum.shape
+    x = logits.double().reshape(reqs, beams, -1) * scale
+    y = cum.double()[..., None] + (x - torch.logsumexp(x, -1, keepdim=True))
+    bad = ~torch.isfinite(x.masked_fill(x == -math.inf, 0.0)).all(-1) | ~(cum > -math.inf)
+    y[bad] = -math.inf
+    y[torch.isnan(y)] = -math.inf     # a row of nothing but -inf
+    return y
+
+
+# ---- rows that go on as their parents --------------------------------------
+
+def paged_reorder(table, lens, parents, group, page, free, used, keep=None):
+    """Row by row with sets of pages; lists in, a dict out."""
+    rows, width = len(table), len(table[0]) if table else 0
+    free = list(free)
+    used = min(max(used, 0), len(free))
+    held = [min(-(-max(n, 0) // page), width) for n in lens]
+    parent = [r // group * group + p if 0 <= p < group else -1 for r, p in enumerate(parents)]
+    alive = {p for p in parent if p >= 0}
+    in_use = {table[r][c] for r in alive for c in range(held[r])}
+    back = []
+    for r in range(rows):
+        if r in alive:
+            continue
+        for c in range(keep[r] if keep else 0, held[r]):
+            p = table[r][c]
+            if p >= 0 and p not in in_use and p not in back:
+                back.append(p)
+    for j, p in enumerate(back):
+        if used - 1 - j >= 0:
+            free[used - 1 - j] = p
+    mark = max(used - len(back), 0)
+    new, new_lens, copies, status, seen = [], [], [], [], set()
+    for r, p in enumerate(parent):
+        row, n, pair, st = [-1] * width, 0, [-1, -1], 0
+        if p < 0:
+            st = 1
+        else:
+            n = lens[p]
+            row[:held[p]] = table[p][:held[p]]
+            at = max(n, 0) // page
+            if p in seen and n > 0 and n % page and at < width and table[p][at] >= 0:
+                if mark < len(free):
+                    pair = [table[p][at], free[mark]]
+                    row[at] = free[mark]
+                    mark += 1
+                else:
+                    row, n, st = [-1] * width, 0, 2
+            seen.add(p)
+        new.append(row)
+        new_lens.append(n)
+        copies.append(pair)
+        status.append(st)
+    return dict(block_table=new, seq_lens=new_lens, copies=copies, free_used=[mark], status=status, free=free)

@@ -834,6 +834,251 @@ int lt_token_logprobs_backward(const void* logits, lt_dtype dtype, int64_t ld, i
                                              grad_logprob, grad_entropy, grad_logits, grad_ld, (hipStream_t)stream));
 }
 
+// The part that is turned, and what turns it.
+static int check_rotary(int32_t d, const float* freq, int32_t pairs, int32_t start, double amplitude, uint32_t flags,
+                        uint32_t allowed) {
+  if (d < 1 || pairs < 0 || start < 0 || (int64_t)start + 2 * (int64_t)pairs > d) return LT_EINVAL;
+  if (flags & ~allowed) return LT_EINVAL;
+  if (!(amplitude - amplitude == 0.0)) return LT_EINVAL;  // finite
+  if (pairs > 0 && (!freq || !aligned(freq, 4))) return LT_EINVAL;
+  return LT_OK;
+}
+
+// Checks of a rotary call; fills a, without its results' place.
+static int rotary_args(const void* x, lt_dtype dtype, int64_t token_stride, int64_t head_stride, int32_t tokens,
+                       int32_t heads, int32_t d, const int32_t* positions, const float* freq, int32_t pairs,
+                       int32_t start, double amplitude, uint32_t flags, RotaryArgs* a) {
+  if (dtype != LT_F32 && dtype != LT_BF16) return LT_EUNSUPPORTED;
+  if (tokens < 0 || heads < 0) return LT_EINVAL;
+  const int rc = check_rotary(d, freq, pairs, start, amplitude, flags, LT_ROTARY_INTERLEAVED | LT_ROTARY_INVERSE);
+  if (rc) return rc;
+  if (d > LT_ROTARY_MAX_DIM) return LT_EUNSUPPORTED;
+  *a = RotaryArgs{};
+  a->x = x;
+  a->x_token = token_stride;
+  a->x_head = head_stride;
+  a->positions = positions;
+  a->freq = freq;
+  a->amplitude = amplitude;
+  a->T = tokens;
+  a->H = heads;
+  a->d = d;
+  a->start = start;
+  a->pairs = pairs;
+  a->interleaved = flags & LT_ROTARY_INTERLEAVED;
+  a->inverse = flags & LT_ROTARY_INVERSE;
+  a->in_f32 = dtype == LT_F32;
+  if (tokens == 0 || heads == 0) return LT_OK;
+  if (!x || !positions || !aligned(x, a->in_f32 ? 4 : 2) || !aligned(positions, 4)) return LT_EINVAL;
+  if (token_stride < 0 || head_stride < 0) return LT_EINVAL;
+  return LT_OK;
+}
+
+int lt_rotary(const void* x, lt_dtype dtype, int64_t token_stride, int64_t head_stride, int32_t tokens, int32_t heads,
+              int32_t d, const int32_t* positions, const float* freq, int32_t pairs, int32_t start, double amplitude,
+              uint32_t flags, void* out, lt_dtype out_dtype, int64_t out_token_stride, int64_t out_head_stride,
+              void* stream) {
+  RotaryArgs a;
+  const int rc = rotary_args(x, dtype, token_stride, head_stride, tokens, heads, d, positions, freq, pairs, start,
+                             amplitude, flags, &a);
+  if (rc) return rc;
+  if (out_dtype != LT_BF16 && out_dtype != dtype) return LT_EUNSUPPORTED;
+  if (tokens == 0 || heads == 0) return LT_OK;
+  a.out = out;
+  a.out_f32 = out_dtype == LT_F32;
+  a.out_token = out_token_stride;
+  a.out_head = out_head_stride;
+  if (!out || !aligned(out, a.out_f32 ? 4 : 2)) return LT_EINVAL;
+  // rows of the result lie apart: heads inside tokens, or tokens inside heads
+  const int64_t ht = out_head_stride, tt = out_token_stride;
+  if ((heads > 1 && ht < d) || (tokens > 1 && tt < d)) return LT_EINVAL;
+  if (heads > 1 && tokens > 1 && tt < (int64_t)(heads - 1) * ht + d && ht < (int64_t)(tokens - 1) * tt + d)
+    return LT_EINVAL;
+  if (out == x && (out_dtype != dtype || (tokens > 1 && tt != token_stride) || (heads > 1 && ht != head_stride)))
+    return LT_EINVAL;
+  if (!launches(rotary_shape(a, false), 256)) return LT_EUNSUPPORTED;
+  return hip_status(launch_rotary(a, (hipStream_t)stream));
+}
+
+int lt_rotary_fp8(const void* x, lt_dtype dtype, int64_t token_stride, int64_t head_stride, int32_t tokens,
+                  int32_t heads, int32_t d, const int32_t* positions, const float* freq, int32_t pairs, int32_t start,
+                  double amplitude, uint32_t flags, uint8_t* codes, float* scales, void* stream) {
+  RotaryArgs a;
+  const int rc = rotary_args(x, dtype, token_stride, head_stride, tokens, heads, d, positions, freq, pairs, start,
+                             amplitude, flags, &a);
+  if (rc) return rc;
+  if (tokens == 0 || heads == 0) return LT_OK;
+  if (!codes || !scales || !aligned(scales, 4) || codes == x || (const void*)scales == x) return LT_EINVAL;
+  a.out = codes;
+  a.out_token = (int64_t)heads * d;
+  a.out_head = d;
+  a.scale = scales;
+  if (!launches(rotary_shape(a, true), 256)) return LT_EUNSUPPORTED;
+  return hip_status(launch_rotary(a, (hipStream_t)stream));
+}
+
+int lt_cache4_append_rotary(const void* k, const void* v, lt_dtype dtype, int64_t k_stride, int64_t v_stride,
+                            int64_t rows, uint8_t* codes, uint8_t* scales, int64_t num_pages, int32_t page_size,
+                            int32_t num_kv_heads, int32_t d, const int64_t* slots, const int32_t* positions,
+                            const float* freq, int32_t pairs, int32_t start, double amplitude, uint32_t flags,
+                            const void* q, int64_t q_stride, int32_t num_heads, void* q_out, void* stream) {
+  Cache4 c;
+  int rc = check_cache4(codes, scales, num_pages, page_size, num_kv_heads, d, &c);
+  if (rc) return rc;
+  if (dtype != LT_F32 && dtype != LT_BF16) return LT_EUNSUPPORTED;
+  if (rows < 0 || rows > 0x7FFFFFFF || num_heads < 0 || (q ? num_heads < 1 : num_heads != 0)) return LT_EINVAL;
+  if ((rc = check_rotary(d, freq, pairs, start, amplitude, flags, LT_ROTARY_INTERLEAVED)) != LT_OK) return rc;
+  if (num_heads > LT_CACHE4_MAX_HEADS) return LT_EUNSUPPORTED;
+  if (rows == 0 || (num_pages == 0 && !q)) return LT_OK;
+  const int64_t width = (int64_t)num_kv_heads * d, unit = dtype == LT_F32 ? 4 : 8;
+  if (k_stride < width || v_stride < width || k_stride % unit || v_stride % unit) return LT_EINVAL;
+  if (!k || !v || !slots || !aligned(k, 16) || !aligned(v, 16) || !aligned(slots, 8)) return LT_EINVAL;
+  if (!positions || !aligned(positions, 4)) return LT_EINVAL;
+  if (q && (!q_out || !aligned(q_out, 16) || !aligned(q, dtype == LT_F32 ? 4 : 2) || q == q_out ||
+            q_stride < (int64_t)num_heads * d))
+    return LT_EINVAL;
+  AppendRotaryArgs a{};
+  a.k = k;
+  a.v = v;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.rows = rows;
+  a.in_f32 = dtype == LT_F32;
+  a.positions = positions;
+  a.freq = freq;
+  a.amplitude = amplitude;
+  a.start = start;
+  a.pairs = pairs;
+  a.interleaved = flags & LT_ROTARY_INTERLEAVED;
+  a.codes = codes;
+  a.scales = scales;
+  a.slots = slots;
+  if (q) {
+    a.q.x = q;
+    a.q.x_token = q_stride;
+    a.q.x_head = d;
+    a.q.out = q_out;
+    a.q.out_token = (int64_t)num_heads * d;
+    a.q.out_head = d;
+    a.q.positions = positions;
+    a.q.freq = freq;
+    a.q.amplitude = amplitude;
+    a.q.T = (int)rows;
+    a.q.H = num_heads;
+    a.q.d = d;
+    a.q.start = start;
+    a.q.pairs = pairs;
+    a.q.interleaved = a.interleaved;
+    a.q.in_f32 = a.in_f32;
+  }
+  if (!launches(append_rotary_shape(a, c), 256)) return LT_EUNSUPPORTED;
+  return hip_status(launch_cache4_append_rotary(a, c, (hipStream_t)stream));
+}
+
+// The shape's part of a selection; an error where it is none that is built.
+static int beam_args(lt_dtype dtype, int32_t batch, int32_t beams, int32_t vocab, int32_t top, BeamArgs* a) {
+  if (batch < 0 || beams < 1 || vocab < 0 || top < 1) return LT_EINVAL;
+  if (dtype != LT_F32 && dtype != LT_BF16) return LT_EUNSUPPORTED;
+  if (beams > LT_BEAM_MAX_BEAMS || top > LT_BEAM_MAX_TOP || vocab > LT_LOGPROB_MAX_VOCAB ||
+      (int64_t)batch * beams > LT_LOGPROB_MAX_ROWS)
+    return LT_EUNSUPPORTED;
+  *a = BeamArgs{};
+  a->bf16 = dtype == LT_BF16;
+  a->batch = batch;
+  a->beams = beams;
+  a->vocab = vocab;
+  a->top = top;
+  return LT_OK;
+}
+
+size_t lt_beam_select_workspace_size(lt_dtype dtype, int32_t batch, int32_t beams, int32_t vocab, int32_t top) {
+  BeamArgs a;
+  return beam_args(dtype, batch, beams, vocab, top, &a) ? 0 : beam_workspace_bytes(a);
+}
+
+int lt_beam_select(const void* logits, lt_dtype dtype, int64_t ld, int32_t batch, int32_t beams, int32_t vocab,
+                   const float* cum, double scale, int32_t top, float* out_score, int32_t* out_beam,
+                   int32_t* out_token, void* workspace, size_t workspace_bytes, void* stream) {
+  BeamArgs a;
+  const int rc = beam_args(dtype, batch, beams, vocab, top, &a);
+  if (rc) return rc;
+  if (ld < vocab || !(scale >= 1.17549435e-38) || !scale_ok((float)scale)) return LT_EINVAL;
+  if (batch == 0) return LT_OK;
+  if ((vocab > 0 && !logits) || !aligned(logits, a.bf16 ? 2 : 4)) return LT_EINVAL;
+  if (!cum || !out_score || !out_beam || !out_token) return LT_EINVAL;
+  if (!aligned(cum, 4) || !aligned(out_score, 4) || !aligned(out_beam, 4) || !aligned(out_token, 4)) return LT_EINVAL;
+  if ((const float*)out_score == cum || (const void*)out_beam == cum || (const void*)out_token == cum) return LT_EINVAL;
+  if (!workspace || !aligned(workspace, 256)) return LT_EINVAL;
+  if (workspace_bytes < beam_workspace_bytes(a)) return LT_EWORKSPACE;
+  a.logits = logits;
+  a.ld = ld;
+  a.cum = cum;
+  a.scale = scale;
+  a.out_score = out_score;
+  a.out_beam = out_beam;
+  a.out_token = out_token;
+  return hip_status(launch_beam_select(a, workspace, (hipStream_t)stream));
+}
+
+size_t lt_paged_reorder_workspace_size(int32_t rows) {
+  return rows < 0 || rows > LT_PLAN_MAX_REQUESTS ? 0 : reorder_workspace_bytes(rows);
+}
+
+int lt_paged_reorder(const int32_t* block_table, int64_t table_ld, int32_t table_width, const int32_t* seq_lens,
+                     const int32_t* parents, int32_t rows, int32_t group, int32_t page_size, const int32_t* keep_pages,
+                     int32_t* free_pages, int32_t num_free, const int32_t* free_used, int32_t* new_table,
+                     int64_t new_table_ld, int32_t* new_lens, int32_t* copies, int32_t* free_used_out, int32_t* status,
+                     void* workspace, size_t workspace_bytes, void* stream) {
+  if (rows < 0 || group < 1 || rows % group || table_width < 0 || num_free < 0) return LT_EINVAL;
+  if (table_ld < table_width || new_table_ld < table_width || !page_shift_ok(page_size)) return LT_EINVAL;
+  if (rows > LT_PLAN_MAX_REQUESTS || group > LT_REORDER_MAX_GROUP) return LT_EUNSUPPORTED;
+  if ((int64_t)rows * table_width > 0x7FFFFFFF) return LT_EUNSUPPORTED;
+  if (!free_used || !free_used_out || (num_free > 0 && !free_pages)) return LT_EINVAL;
+  if (rows > 0 && (!seq_lens || !parents || !new_lens || !copies || !status)) return LT_EINVAL;
+  if (rows > 0 && table_width > 0 && (!block_table || !new_table)) return LT_EINVAL;
+  if (!workspace || !aligned(workspace, 256)) return LT_EINVAL;
+  if (workspace_bytes < reorder_workspace_bytes(rows)) return LT_EWORKSPACE;
+  // blocks read the inputs while others write: no result in an input's place
+  const void *in[] = {block_table, seq_lens, parents, keep_pages, free_used, free_pages},
+             *out[] = {new_table, new_lens, copies, free_used_out, status};
+  for (const void* i : in)
+    for (const void* o : out)
+      if (i && i == o) return LT_EINVAL;
+  if (free_pages == free_used) return LT_EINVAL;
+  ReorderArgs a{};
+  a.table = block_table;
+  a.lens = seq_lens;
+  a.parents = parents;
+  a.keep = keep_pages;
+  a.table_ld = table_ld;
+  a.R = rows;
+  a.group = group;
+  a.width = table_width;
+  a.shift = page_shift(page_size);
+  a.free_list = free_pages;
+  a.free_count = num_free;
+  a.free_used = free_used;
+  a.out_table = new_table;
+  a.out_ld = new_table_ld;
+  a.out_lens = new_lens;
+  a.copies = copies;
+  a.free_out = free_used_out;
+  a.status = status;
+  return hip_status(launch_paged_reorder(a, workspace, (hipStream_t)stream));
+}
+
+int lt_cache4_copy(uint8_t* codes, uint8_t* scales, int64_t num_pages, int32_t page_size, int32_t num_kv_heads,
+                   int32_t d, const int32_t* copies, int32_t n, void* stream) {
+  Cache4 c;
+  const int rc = check_cache4(codes, scales, num_pages, page_size, num_kv_heads, d, &c);
+  if (rc) return rc;
+  if (n < 0) return LT_EINVAL;
+  if (n == 0 || num_pages == 0) return LT_OK;
+  if (!copies || !aligned(copies, 4)) return LT_EINVAL;
+  if (!launches(cache4_copy_blocks(c, n), 256)) return LT_EUNSUPPORTED;
+  return hip_status(launch_cache4_copy(c, codes, scales, copies, n, (hipStream_t)stream));
+}
+
 int lt_event_create(void** ev) {
   if (!ev) return LT_EINVAL;
   // timing only: no system-scope fence when the event completes, so that

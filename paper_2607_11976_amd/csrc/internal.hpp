@@ -278,4 +278,80 @@ hipError_t launch_logprobs_backward(const void* logits, int64_t ld, bool bf16, i
                                     const float* g_logprob, const float* g_entropy, void* out, int64_t out_ld,
                                     hipStream_t st);
 
+// ---- rotary positions (rotary.hip) ----
+struct RotaryArgs {
+  const void* x;            // [T, H, d], strides in values; rows of a head are contiguous
+  int64_t x_token, x_head;
+  void* out;
+  int64_t out_token, out_head;
+  float* scale;             // [T, H]: fp8 output
+  const int32_t* positions;
+  const float* freq;        // [pairs]
+  double amplitude;
+  int T, H, d;
+  int start, pairs;
+  bool interleaved, inverse;
+  bool in_f32, out_f32;
+  // resolved by rotary_shape
+  int vec;                  // values of a vector: 8, 4, 2 or 1
+  int units;                // vector pairs of a head
+  int lanes_log2;           // lanes that share a head
+  int head_lanes;           // of a token: each takes every head_lanes-th head
+};
+// Fills in the resolved fields; the blocks of 256 threads that the launch takes.
+int64_t rotary_shape(RotaryArgs& a, bool fp8);
+hipError_t launch_rotary(const RotaryArgs& a, hipStream_t st);      // a.scale: fp8 codes out
+struct AppendRotaryArgs {
+  RotaryArgs q;             // T = 0 without queries
+  const void *k, *v;
+  int64_t k_stride, v_stride, rows;
+  bool in_f32;
+  const int32_t* positions;
+  const float* freq;
+  double amplitude;
+  int start, pairs;
+  bool interleaved;
+  uint8_t *codes, *scales;
+  const int64_t* slots;
+  // resolved by append_rotary_shape
+  int64_t q_blocks, k_blocks, v_blocks;
+  int head_lanes;
+  bool wide;
+};
+int64_t append_rotary_shape(AppendRotaryArgs& a, const Cache4& c);  // blocks of 256 threads
+hipError_t launch_cache4_append_rotary(const AppendRotaryArgs& a, const Cache4& c, hipStream_t st);
+
+// ---- beams: selection (beam.hip), pages of reordered rows (reorder.hip) ----
+struct BeamArgs {
+  const void* logits;       // [batch * beams, vocab], ld values between rows
+  int64_t ld;
+  bool bf16;
+  int batch, beams, vocab, top;
+  const float* cum;         // [batch, beams]
+  double scale;
+  float* out_score;         // [batch, top]
+  int32_t *out_beam, *out_token;
+  int splits, split_len;    // resolved by beam_shape
+};
+void beam_shape(BeamArgs& a);
+size_t beam_workspace_bytes(const BeamArgs& a);
+hipError_t launch_beam_select(BeamArgs a, void* workspace, hipStream_t st);
+
+struct ReorderArgs {
+  const int32_t *table, *lens, *parents, *keep;
+  int64_t table_ld;
+  int R, group, width, shift;
+  int32_t* free_list;
+  int free_count;
+  const int32_t* free_used;
+  int32_t* out_table;
+  int64_t out_ld;
+  int32_t *out_lens, *copies, *free_out, *status;
+};
+size_t reorder_workspace_bytes(int rows);
+hipError_t launch_paged_reorder(const ReorderArgs& a, void* workspace, hipStream_t st);
+hipError_t launch_cache4_copy(const Cache4& c, uint8_t* codes, uint8_t* scales, const int32_t* copies, int n,
+                              hipStream_t st);
+int64_t cache4_copy_blocks(const Cache4& c, int n);
+
 }  // namespace lt

@@ -1,0 +1,386 @@
+// Rotary positions of queries and keys (rotary.hpp): rotated in their type or as
+// fp8 codes with scales, and on the way into the 4-bit cache.
+#include <algorithm>
+
+#include "cache4.hpp"
+#include "internal.hpp"
+#include "rotary.hpp"
+
+namespace lt {
+namespace {
+
+constexpr int kThreads = 256;
+
+// What a unit of a head covers: two vectors of V values, V pairs in the rotated
+// part, which fill both in turn; elsewhere two vectors that pass as they are.
+struct Unit {
+  int a, b;    // offsets of the vectors; b < 0: there is none
+  int pair;    // first pair, < 0: not rotated
+};
+template <int V>
+__device__ __forceinline__ Unit unit_of(const RotaryArgs& r, int u) {
+  const int nr = r.pairs / V;
+  if (u < nr) {
+    if (r.interleaved) return Unit{r.start + 2 * u * V, r.start + (2 * u + 1) * V, u * V};
+    return Unit{r.start + u * V, r.start + r.pairs + u * V, u * V};
+  }
+  const int first = r.start / V, part = 2 * nr, count = r.d / V - part;  // vectors before, in, beside the part
+  const int i = 2 * (u - nr), a = i < first ? i : i + part, b = i + 1 < first ? i + 1 : i + 1 + part;
+  return Unit{a * V, i + 1 < count ? b * V : -1, -1};
+}
+
+template <int V>
+__device__ __forceinline__ void turns_of(const RotaryArgs& r, const Unit& u, int pos, float (&c)[V], float (&s)[V]) {
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const Turn t = turn_of((double)pos * turns_per(r.freq[u.pair + j]), r.amplitude);
+    c[j] = t.c;
+    s[j] = r.inverse ? -t.s : t.s;
+  }
+}
+
+// The unit's values x, y (of vectors a and b) turned in place.
+template <int V>
+__device__ __forceinline__ void turn_unit(const RotaryArgs& r, float (&x)[V], float (&y)[V], const float (&c)[V],
+                                          const float (&s)[V]) {
+  if (!r.interleaved) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const float u = x[j], v = y[j];
+      x[j] = turned(u, c[j], v, -s[j]);
+      y[j] = turned(v, c[j], u, s[j]);
+    }
+  } else if constexpr (V == 1) {
+    const float u = x[0], v = y[0];
+    x[0] = turned(u, c[0], v, -s[0]);
+    y[0] = turned(v, c[0], u, s[0]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; j += 2) {
+      float u = x[j], v = x[j + 1];
+      x[j] = turned(u, c[j / 2], v, -s[j / 2]);
+      x[j + 1] = turned(v, c[j / 2], u, s[j / 2]);
+      u = y[j], v = y[j + 1];
+      y[j] = turned(u, c[V / 2 + j / 2], v, -s[V / 2 + j / 2]);
+      y[j + 1] = turned(v, c[V / 2 + j / 2], u, s[V / 2 + j / 2]);
+    }
+  }
+}
+
+// Lanes of a head, one unit each (in turn where there are more units); a group of
+// them takes every head_lanes-th head of a token.
+template <class TI, class TO, int V>
+__device__ __forceinline__ void rotate_rows(const RotaryArgs& r, uint32_t block) {
+  const int lane = threadIdx.x & ((1 << r.lanes_log2) - 1);
+  const uint32_t item = block * (kThreads >> r.lanes_log2) + (threadIdx.x >> r.lanes_log2);
+  const uint32_t tok = item / (uint32_t)r.head_lanes;
+  if (tok >= (uint32_t)r.T) return;
+  const int h0 = (int)(item - tok * r.head_lanes), pos = r.positions[tok];
+  const TI* in = reinterpret_cast<const TI*>(r.x) + (int64_t)tok * r.x_token;
+  TO* out = reinterpret_cast<TO*>(r.out) + (int64_t)tok * r.out_token;
+  for (int u = lane; u < r.units; u += 1 << r.lanes_log2) {
+    const Unit w = unit_of<V>(r, u);
+    float c[V], s[V];
+    if (w.pair >= 0) turns_of<V>(r, w, pos, c, s);
+    for (int h = h0; h < r.H; h += r.head_lanes) {
+      float x[V] = {}, y[V] = {};
+      if (pos >= 0) {
+        load_values<V>(in + h * r.x_head + w.a, x);
+        if (w.b >= 0) load_values<V>(in + h * r.x_head + w.b, y);
+        if (w.pair >= 0) turn_unit<V>(r, x, y, c, s);
+      }
+      store_values<V>(out + h * r.out_head + w.a, x);
+      if (w.b >= 0) store_values<V>(out + h * r.out_head + w.b, y);
+    }
+  }
+}
+
+template <class TI, class TO, int V>
+__global__ __launch_bounds__(kThreads) void k_rotary(RotaryArgs r) {
+  rotate_rows<TI, TO, V>(r, blockIdx.x);
+}
+
+// ---- fp8 ----
+// Exponent byte of the smallest power of two 2^e with top <= 448 * 2^e, from the
+// bits of `top`: 448 = 1.75 * 2^8, so adding 0x1FFFFF carries where e has to be one
+// larger. Not below 2^-126; 255 (a NaN for the scale) where top is not finite.
+__device__ __forceinline__ uint32_t fp8_scale_byte(uint32_t top) {
+  if (top >= 0x7F800000u) return 255u;
+  const uint32_t e = (top + 0x1FFFFFu) >> 23;
+  return e > 9u ? e - 8u : 1u;
+}
+template <int V>
+__device__ __forceinline__ void store_fp8(uint8_t* p, const float (&x)[V], float by) {
+  if constexpr (V == 1) {
+    *p = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[0] * by, 0.0f, 0, false);
+  } else if constexpr (V == 2) {
+    *reinterpret_cast<uint16_t*>(p) = (uint16_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[0] * by, x[1] * by, 0, false);
+  } else {
+    uint32_t w[V / 4];
+#pragma unroll
+    for (int i = 0; i < V / 4; ++i) {
+      int v = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i] * by, x[4 * i + 1] * by, 0, false);
+      v = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i + 2] * by, x[4 * i + 3] * by, v, true);
+      w[i] = (uint32_t)v;
+    }
+    if constexpr (V == 8) *reinterpret_cast<uint2*>(p) = uint2{w[0], w[1]};
+    else *reinterpret_cast<uint32_t*>(p) = w[0];
+  }
+}
+template <int V>
+__device__ __forceinline__ uint32_t top_of(uint32_t top, const float (&x)[V]) {
+#pragma unroll
+  for (int j = 0; j < V; ++j) top = max(top, __float_as_uint(x[j]) & 0x7FFFFFFFu);
+  return top;
+}
+
+// A head's scale is known once all its units are turned. ONCE: a lane has one unit
+// and keeps it; else the units are turned a second time (rows that fill no vectors).
+template <class TI, int V, bool ONCE>
+__global__ __launch_bounds__(kThreads) void k_rotary_fp8(RotaryArgs r) {
+  const int lanes = 1 << r.lanes_log2, lane = threadIdx.x & (lanes - 1);
+  const uint32_t item = blockIdx.x * (kThreads >> r.lanes_log2) + (threadIdx.x >> r.lanes_log2);
+  const uint32_t tok = item / (uint32_t)r.head_lanes;
+  if (tok >= (uint32_t)r.T) return;  // whole groups of lanes
+  const int h0 = (int)(item - tok * r.head_lanes), pos = r.positions[tok];
+  const TI* in = reinterpret_cast<const TI*>(r.x) + (int64_t)tok * r.x_token;
+  uint8_t* out = reinterpret_cast<uint8_t*>(r.out) + (int64_t)tok * r.out_token;
+  float c[V], s[V];
+  Unit w{0, -1, -1};
+  auto prepare = [&](int u) {
+    w = unit_of<V>(r, u);
+    if (w.pair >= 0) turns_of<V>(r, w, pos, c, s);
+  };
+  auto values = [&](int h, float (&x)[V], float (&y)[V]) {
+    if (pos < 0) return;
+    load_values<V>(in + h * r.x_head + w.a, x);
+    if (w.b >= 0) load_values<V>(in + h * r.x_head + w.b, y);
+    if (w.pair >= 0) turn_unit<V>(r, x, y, c, s);
+  };
+  if (ONCE && lane < r.units) prepare(lane);
+  for (int h = h0; h < r.H; h += r.head_lanes) {
+    float x[V] = {}, y[V] = {};
+    uint32_t top = 0;
+    for (int u = lane; u < r.units; u += lanes) {
+      if (!ONCE) prepare(u);
+      values(h, x, y);
+      top = top_of<V>(top_of<V>(top, x), y);
+    }
+    for (int o = 1; o < lanes; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
+    const uint32_t e = fp8_scale_byte(top);
+    // a scale of NaN: codes of 0 (and no conversion of what is not finite)
+    const float by = e == 255u ? 0.0f : __uint_as_float((254u - e) << 23);
+    for (int u = lane; u < r.units; u += lanes) {
+      if (!ONCE) {
+        prepare(u);
+        values(h, x, y);
+      }
+      if (e == 255u) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[j] = y[j] = 0.0f;
+      }
+      store_fp8<V>(out + h * r.out_head + w.a, x, by);
+      if (w.b >= 0) store_fp8<V>(out + h * r.out_head + w.b, y, by);
+    }
+    if (lane == 0) r.scale[(int64_t)tok * r.H + h] = e == 255u ? __builtin_nanf("") : __uint_as_float(e << 23);
+  }
+}
+
+// ---- into the 4-bit cache ----
+// As k_cache4_append, a thread takes 8 consecutive values of a row and the four
+// threads of a block of 32 share its largest magnitude; a key's thread also reads
+// the 8 values that its own are paired with (from the cache: their own thread is in
+// the same wave). WIDE: they are a vector, or lie in the thread's own 8.
+__device__ __forceinline__ void put_codes(const float (&x)[8], int64_t row, int d, int which, int ch, uint8_t* codes,
+                                          uint8_t* scales) {
+  uint32_t top = top_of<8>(0u, x);  // NaN and infinity lie above every finite value
+  top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+  top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+  const uint32_t e = scale_byte(top);
+  const float s = __uint_as_float(e << 23);
+  uint32_t w = 0;
+  if (e != 255u) {
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], s, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], s, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], s, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], s, 3);
+  }
+  *reinterpret_cast<uint32_t*>(codes + row * d + which * (d / 2) + ch * 4) = w;
+  if ((ch & 3) == 0) scales[row * (d / 16) + which * (d / 32) + (ch >> 2)] = (uint8_t)e;
+}
+
+template <class T, bool WIDE>
+__device__ __forceinline__ void append_keys(const AppendRotaryArgs& a, const Cache4& c, uint32_t block) {
+  const int per_row = c.d / 8;  // lanes of a head: 8 or 16
+  const uint32_t item = (block * kThreads + threadIdx.x) / per_row;
+  const int ch = threadIdx.x & (per_row - 1);
+  const uint32_t tok = item / (uint32_t)a.head_lanes;
+  if (tok >= a.rows) return;  // whole heads
+  const int h0 = (int)(item - tok * a.head_lanes), pos = a.positions[tok];
+  const int64_t slot = a.slots[tok];
+  if (pos < 0 || slot < 0 || slot >= c.num_pages << c.shift) return;
+  // each value's partner (offset from its own), and its turn
+  int partner[8];
+  float cs[8], sn[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int i = ch * 8 + j - a.start;  // in the rotated part
+    partner[j] = 0;
+    cs[j] = 1.0f, sn[j] = 0.0f;
+    if (i < 0 || i >= 2 * a.pairs) continue;
+    const bool first = a.interleaved ? !(i & 1) : i < a.pairs;
+    const int pair = a.interleaved ? i >> 1 : first ? i : i - a.pairs;
+    partner[j] = a.interleaved ? (first ? 1 : -1) : first ? a.pairs : -a.pairs;
+    const Turn t = turn_of((double)pos * turns_per(a.freq[pair]), a.amplitude);
+    cs[j] = t.c;
+    sn[j] = first ? -t.s : t.s;
+  }
+  const T* in = reinterpret_cast<const T*>(a.k) + (int64_t)tok * a.k_stride + ch * 8;
+  for (int h = h0; h < c.hkv; h += a.head_lanes) {
+    const T* p = in + (int64_t)h * c.d;
+    float x[8], y[8], z[8];
+    load_values<8>(p, x);
+    if (WIDE && !a.interleaved) {
+      load_values<8>(p + partner[0], z);
+    } else if (WIDE) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) z[j] = x[j ^ 1];
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        float v[1];
+        load_values<1>(p + j + partner[j], v);
+        z[j] = v[0];
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) y[j] = partner[j] ? turned(x[j], cs[j], z[j], sn[j]) : x[j];
+    put_codes(y, c.row(slot, h), c.d, 0, ch, a.codes, a.scales);
+  }
+}
+
+template <class T>
+__device__ __forceinline__ void append_values(const AppendRotaryArgs& a, const Cache4& c, uint32_t block) {
+  const int per_row = c.d / 8, per_tok = c.hkv * per_row;
+  const uint32_t at = block * kThreads + threadIdx.x, tok = at / (uint32_t)per_tok;
+  if (tok >= a.rows) return;
+  const int in = (int)(at - tok * per_tok), h = in / per_row, ch = in - h * per_row;
+  const int64_t slot = a.slots[tok];
+  if (a.positions[tok] < 0 || slot < 0 || slot >= c.num_pages << c.shift) return;
+  float x[8];
+  load_values<8>(reinterpret_cast<const T*>(a.v) + (int64_t)tok * a.v_stride + in * 8, x);
+  put_codes(x, c.row(slot, h), c.d, 1, ch, a.codes, a.scales);
+}
+
+// One launch: blocks of queries, of keys and of values, side by side.
+template <class T, bool WIDE>
+__global__ __launch_bounds__(kThreads) void k_append_rotary(AppendRotaryArgs a, Cache4 c) {
+  const int64_t b = blockIdx.x;
+  if (b < a.k_blocks) append_keys<T, WIDE>(a, c, (uint32_t)b);
+  else if (b < a.k_blocks + a.v_blocks) append_values<T>(a, c, (uint32_t)(b - a.k_blocks));
+  else rotate_rows<T, uint16_t, WIDE ? 8 : 1>(a.q, (uint32_t)(b - a.k_blocks - a.v_blocks));
+}
+
+bool is_aligned(const void* p, int64_t n) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(n - 1)) == 0; }
+
+// Whether vectors of n values fit a side's address and strides.
+bool side_fits(const void* p, int64_t token, int64_t head, int T, int H, int n, int size) {
+  return is_aligned(p, std::min(n * size, 16)) && (H <= 1 || head % n == 0) && (T <= 1 || token % n == 0);
+}
+
+void lanes_of(RotaryArgs& a) {
+  const int V = a.vec;
+  const int beside = a.d / V - 2 * (a.pairs / V);  // vectors that pass
+  a.units = a.pairs / V + (beside + 1) / 2;
+  a.lanes_log2 = 0;
+  while (a.lanes_log2 < 6 && (1 << a.lanes_log2) < a.units) ++a.lanes_log2;
+}
+
+int64_t rotary_blocks(RotaryArgs& a) {
+  a.head_lanes = std::max(a.H, 1);
+  const int64_t items = (int64_t)a.T * a.head_lanes, per = kThreads >> a.lanes_log2;
+  return (items + per - 1) / per;
+}
+
+template <class TI, class TO>
+void run_rotary(const RotaryArgs& a, dim3 grid, hipStream_t st) {
+  switch (a.vec) {
+    case 8: k_rotary<TI, TO, 8><<<grid, kThreads, 0, st>>>(a); break;
+    case 4: k_rotary<TI, TO, 4><<<grid, kThreads, 0, st>>>(a); break;
+    case 2: k_rotary<TI, TO, 2><<<grid, kThreads, 0, st>>>(a); break;
+    default: k_rotary<TI, TO, 1><<<grid, kThreads, 0, st>>>(a); break;
+  }
+}
+template <class TI, int V>
+void run_fp8(const RotaryArgs& a, dim3 grid, hipStream_t st) {
+  if (a.units <= 1 << a.lanes_log2) k_rotary_fp8<TI, V, true><<<grid, kThreads, 0, st>>>(a);
+  else k_rotary_fp8<TI, V, false><<<grid, kThreads, 0, st>>>(a);
+}
+template <class TI>
+void run_rotary_fp8(const RotaryArgs& a, dim3 grid, hipStream_t st) {
+  switch (a.vec) {
+    case 8: k_rotary_fp8<TI, 8, true><<<grid, kThreads, 0, st>>>(a); break;  // units <= 64: d <= 1024
+    case 4: run_fp8<TI, 4>(a, grid, st); break;
+    case 2: run_fp8<TI, 2>(a, grid, st); break;
+    default: run_fp8<TI, 1>(a, grid, st); break;
+  }
+}
+
+}  // namespace
+
+// The widest vectors that the part's place, the head's size and both sides' strides
+// and addresses allow.
+int64_t rotary_shape(RotaryArgs& a, bool fp8) {
+  const int si = a.in_f32 ? 4 : 2, so = fp8 ? 1 : a.out_f32 ? 4 : 2;
+  for (a.vec = 8; a.vec > 1; a.vec /= 2)
+    if (a.d % a.vec == 0 && a.start % a.vec == 0 && a.pairs % a.vec == 0 &&
+        side_fits(a.x, a.x_token, a.x_head, a.T, a.H, a.vec, si) &&
+        side_fits(a.out, a.out_token, a.out_head, a.T, a.H, a.vec, so))
+      break;
+  lanes_of(a);
+  return rotary_blocks(a);
+}
+
+hipError_t launch_rotary(const RotaryArgs& r, hipStream_t st) {
+  RotaryArgs a = r;
+  const dim3 grid((unsigned)rotary_shape(a, a.scale != nullptr));
+  if (a.scale) {
+    if (a.in_f32) run_rotary_fp8<float>(a, grid, st);
+    else run_rotary_fp8<uint16_t>(a, grid, st);
+  } else if (a.in_f32 && a.out_f32) {
+    run_rotary<float, float>(a, grid, st);
+  } else if (a.in_f32) {
+    run_rotary<float, uint16_t>(a, grid, st);
+  } else {
+    run_rotary<uint16_t, uint16_t>(a, grid, st);
+  }
+  return hipGetLastError();
+}
+
+int64_t append_rotary_shape(AppendRotaryArgs& a, const Cache4& c) {
+  a.head_lanes = c.hkv;
+  a.k_blocks = a.v_blocks = (a.rows * c.hkv * (c.d / 8) + kThreads - 1) / kThreads;
+  // vectors of 8 that hold whole pairs, or face each other
+  a.wide = a.start % 8 == 0 && a.pairs % 8 == 0;
+  a.q_blocks = 0;
+  if (a.q.T > 0) {
+    a.wide = a.wide && side_fits(a.q.x, a.q.x_token, a.q.x_head, a.q.T, a.q.H, 8, a.in_f32 ? 4 : 2) &&
+             side_fits(a.q.out, a.q.out_token, a.q.out_head, a.q.T, a.q.H, 8, 2);
+    a.q.vec = a.wide ? 8 : 1;
+    lanes_of(a.q);
+    a.q_blocks = rotary_blocks(a.q);
+  }
+  return a.q_blocks + a.k_blocks + a.v_blocks;
+}
+
+hipError_t launch_cache4_append_rotary(const AppendRotaryArgs& r, const Cache4& c, hipStream_t st) {
+  AppendRotaryArgs a = r;
+  const dim3 grid((unsigned)append_rotary_shape(a, c));
+  if (a.in_f32 && a.wide) k_append_rotary<float, true><<<grid, kThreads, 0, st>>>(a, c);
+  else if (a.in_f32) k_append_rotary<float, false><<<grid, kThreads, 0, st>>>(a, c);
+  else if (a.wide) k_append_rotary<uint16_t, true><<<grid, kThreads, 0, st>>>(a, c);
+  else k_append_rotary<uint16_t, false><<<grid, kThreads, 0, st>>>(a, c);
+  return hipGetLastError();
+}
+
+}  // namespace lt

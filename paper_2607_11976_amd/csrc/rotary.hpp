@@ -1,0 +1,127 @@
+// Rotary positions. Pair i of a head's values [start, start + 2 n) is turned by
+// the angle position * f_i:
+//   y1 = x1 cos - x2 sin,  y2 = x2 cos + x1 sin,
+// the pair being values (i, i + n) of that part, or (2 i, 2 i + 1) interleaved.
+//
+// A position times a frequency passes float32's 24 bits long before a context of
+// 2^20 tokens ends (its error would be 0.06 rad there), so the angle is taken in
+// 64 bits, in quarter turns, and its sine and cosine are 64-bit Taylor sums over
+// |x| <= pi / 4 (remainder below 2^-41): about 20 fused multiply-adds a pair, which
+// a thread shares over the heads that it turns. They are rounded to float32 once,
+// after the amplitude; products and sums are float32, each rounded by itself, so
+// that a plain float32 program gets the same bits.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace lt {
+
+constexpr double kHalfPi = 1.57079632679489661923;
+// (pi / 2)^n / n!
+constexpr double turn_term(int n) {
+  double v = 1.0;
+  for (int i = 1; i <= n; ++i) v *= kHalfPi / i;
+  return v;
+}
+
+struct Turn {
+  float c, s;
+};
+// `turns` of 2 pi: cosine and sine, times the amplitude.
+__device__ __forceinline__ Turn turn_of(double turns, double amplitude) {
+  const double t = (turns - rint(turns)) * 4.0, q = rint(t), f = t - q, z = f * f;
+  double s = turn_term(13), c = turn_term(12);
+  s = fma(-z, s, turn_term(11));
+  s = fma(-z, s, turn_term(9));
+  s = fma(-z, s, turn_term(7));
+  s = fma(-z, s, turn_term(5));
+  s = fma(-z, s, turn_term(3));
+  s = fma(-z, s, turn_term(1)) * f;
+  c = fma(-z, c, turn_term(10));
+  c = fma(-z, c, turn_term(8));
+  c = fma(-z, c, turn_term(6));
+  c = fma(-z, c, turn_term(4));
+  c = fma(-z, c, turn_term(2));
+  c = fma(-z, c, turn_term(0));
+  const int k = (int)q;  // -2..2
+  const float fc = (float)(c * amplitude), fs = (float)(s * amplitude);
+  const float a = k & 1 ? fs : fc, b = k & 1 ? fc : fs;
+  // quarter k: cos = c, -s, -c, s; sin = s, c, -s, -c
+  return Turn{(k + 1) & 2 ? -a : a, k & 2 ? -b : b};
+}
+
+// Turns per position of a frequency in radians.
+__device__ __forceinline__ double turns_per(float f) { return (double)f * (0.25 / kHalfPi); }
+
+// x c + p s, each step rounded (never fused).
+__device__ __forceinline__ float turned(float x, float c, float p, float s) {
+#pragma clang fp contract(off)
+  const float a = x * c, b = p * s;
+  return a + b;
+}
+
+__device__ __forceinline__ float bf16_float(uint32_t h) { return __uint_as_float(h << 16); }
+// Nearest bfloat16, ties to even.
+__device__ __forceinline__ uint16_t float_bf16(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
+
+// N values at N * sizeof(T) alignment (16 bytes at most), as float32.
+template <int N>
+__device__ __forceinline__ void load_values(const float* p, float (&x)[N]) {
+  if constexpr (N >= 4) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      const float4 a = *reinterpret_cast<const float4*>(p + i);
+      x[i] = a.x, x[i + 1] = a.y, x[i + 2] = a.z, x[i + 3] = a.w;
+    }
+  } else if constexpr (N == 2) {
+    const float2 a = *reinterpret_cast<const float2*>(p);
+    x[0] = a.x, x[1] = a.y;
+  } else {
+    x[0] = *p;
+  }
+}
+template <int N>
+__device__ __forceinline__ void load_values(const uint16_t* p, float (&x)[N]) {
+  if constexpr (N == 8) {
+    const uint4 a = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[2 * i] = bf16_float(w[i]), x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+  } else if constexpr (N == 4) {
+    const uint2 a = *reinterpret_cast<const uint2*>(p);
+    x[0] = bf16_float(a.x), x[1] = __uint_as_float(a.x & 0xFFFF0000u);
+    x[2] = bf16_float(a.y), x[3] = __uint_as_float(a.y & 0xFFFF0000u);
+  } else if constexpr (N == 2) {
+    const uint32_t a = *reinterpret_cast<const uint32_t*>(p);
+    x[0] = bf16_float(a), x[1] = __uint_as_float(a & 0xFFFF0000u);
+  } else {
+    x[0] = bf16_float(*p);
+  }
+}
+template <int N>
+__device__ __forceinline__ void store_values(float* p, const float (&x)[N]) {
+  if constexpr (N >= 4) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) *reinterpret_cast<float4*>(p + i) = float4{x[i], x[i + 1], x[i + 2], x[i + 3]};
+  } else if constexpr (N == 2) {
+    *reinterpret_cast<float2*>(p) = float2{x[0], x[1]};
+  } else {
+    *p = x[0];
+  }
+}
+template <int N>
+__device__ __forceinline__ void store_values(uint16_t* p, const float (&x)[N]) {
+  if constexpr (N == 1) {
+    *p = float_bf16(x[0]);
+  } else {
+    uint32_t w[N / 2];
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) w[i] = (uint32_t)float_bf16(x[2 * i]) | (uint32_t)float_bf16(x[2 * i + 1]) << 16;
+    if constexpr (N == 8) *reinterpret_cast<uint4*>(p) = uint4{w[0], w[1], w[2], w[3]};
+    else if constexpr (N == 4) *reinterpret_cast<uint2*>(p) = uint2{w[0], w[1]};
+    else *reinterpret_cast<uint32_t*>(p) = w[0];
+  }
+}
+
+}  // namespace lt

@@ -15,6 +15,7 @@ Two layers:
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from typing import NamedTuple, Optional, Sequence
 
@@ -41,6 +42,11 @@ LT_CACHE4_MAX_HEADS = 1024
 LT_LOGPROB_MAX_TOP = 64
 LT_LOGPROB_MAX_VOCAB = 1 << 30
 LT_LOGPROB_MAX_ROWS = 0xFFFFFF
+LT_ROTARY_INTERLEAVED, LT_ROTARY_INVERSE = 1, 2
+LT_ROTARY_MAX_DIM = 1024
+LT_BEAM_MAX_TOP = 64
+LT_BEAM_MAX_BEAMS = 1024
+LT_REORDER_MAX_GROUP = 64
 STAGES = ("sample", "range", "filter", "select", "fallback")
 
 EXPORTED = (
@@ -50,6 +56,8 @@ EXPORTED = (
     "lt_sample_from_topk_workspace_size", "lt_sample_from_topk", "lt_dsa_union",
     "lt_paged_plan", "lt_cache4_append", "lt_cache4_read", "lt_cache4_attention_workspace_size",
     "lt_cache4_attention", "lt_token_logprobs_workspace_size", "lt_token_logprobs", "lt_token_logprobs_backward",
+    "lt_rotary", "lt_rotary_fp8", "lt_cache4_append_rotary", "lt_beam_select_workspace_size", "lt_beam_select",
+    "lt_paged_reorder_workspace_size", "lt_paged_reorder", "lt_cache4_copy",
     "lt_event_create",
     "lt_event_destroy", "lt_event_record", "lt_event_elapsed_ms", "lt_strerror",
 )
@@ -80,6 +88,8 @@ _I32 = ctypes.c_int32
 _I64 = ctypes.c_int64
 _SZ = ctypes.c_size_t
 _F32 = ctypes.c_float
+_F64 = ctypes.c_double
+_U32 = ctypes.c_uint32
 
 
 def load(path: str = LIB_PATH):
@@ -135,6 +145,26 @@ def load(path: str = LIB_PATH):
     lib.lt_token_logprobs_backward.argtypes = [_P, ctypes.c_int, _I64, _I32, _I32, _P, _F32, _P, _P, _P, _P, _P, _I64,
                                                _P]
     lib.lt_token_logprobs_backward.restype = ctypes.c_int
+    lib.lt_rotary.argtypes = [_P, ctypes.c_int, _I64, _I64, _I32, _I32, _I32, _P, _P, _I32, _I32, _F64, _U32, _P,
+                              ctypes.c_int, _I64, _I64, _P]
+    lib.lt_rotary.restype = ctypes.c_int
+    lib.lt_rotary_fp8.argtypes = [_P, ctypes.c_int, _I64, _I64, _I32, _I32, _I32, _P, _P, _I32, _I32, _F64, _U32, _P,
+                                  _P, _P]
+    lib.lt_rotary_fp8.restype = ctypes.c_int
+    lib.lt_cache4_append_rotary.argtypes = [_P, _P, ctypes.c_int, _I64, _I64, _I64, _P, _P, _I64, _I32, _I32, _I32, _P,
+                                            _P, _P, _I32, _I32, _F64, _U32, _P, _I64, _I32, _P, _P]
+    lib.lt_cache4_append_rotary.restype = ctypes.c_int
+    lib.lt_beam_select_workspace_size.argtypes = [ctypes.c_int, _I32, _I32, _I32, _I32]
+    lib.lt_beam_select_workspace_size.restype = _SZ
+    lib.lt_beam_select.argtypes = [_P, ctypes.c_int, _I64, _I32, _I32, _I32, _P, _F64, _I32, _P, _P, _P, _P, _SZ, _P]
+    lib.lt_beam_select.restype = ctypes.c_int
+    lib.lt_paged_reorder_workspace_size.argtypes = [_I32]
+    lib.lt_paged_reorder_workspace_size.restype = _SZ
+    lib.lt_paged_reorder.argtypes = [_P, _I64, _I32, _P, _P, _I32, _I32, _I32, _P, _P, _I32, _P, _P, _I64, _P, _P, _P,
+                                     _P, _P, _SZ, _P]
+    lib.lt_paged_reorder.restype = ctypes.c_int
+    lib.lt_cache4_copy.argtypes = [_P, _P, _I64, _I32, _I32, _I32, _P, _I32, _P]
+    lib.lt_cache4_copy.restype = ctypes.c_int
     lib.lt_event_create.argtypes = [ctypes.POINTER(ctypes.c_void_p)]
     lib.lt_event_create.restype = ctypes.c_int
     lib.lt_event_destroy.argtypes = [_P]
@@ -246,6 +276,38 @@ def lt_token_logprobs(*args) -> int:
 
 def lt_token_logprobs_backward(*args) -> int:
     return load().lt_token_logprobs_backward(*args)
+
+
+def lt_rotary(*args) -> int:
+    return load().lt_rotary(*args)
+
+
+def lt_rotary_fp8(*args) -> int:
+    return load().lt_rotary_fp8(*args)
+
+
+def lt_cache4_append_rotary(*args) -> int:
+    return load().lt_cache4_append_rotary(*args)
+
+
+def lt_beam_select_workspace_size(dtype, batch, beams, vocab, top) -> int:
+    return load().lt_beam_select_workspace_size(dtype, batch, beams, vocab, top)
+
+
+def lt_beam_select(*args) -> int:
+    return load().lt_beam_select(*args)
+
+
+def lt_paged_reorder_workspace_size(rows) -> int:
+    return load().lt_paged_reorder_workspace_size(rows)
+
+
+def lt_paged_reorder(*args) -> int:
+    return load().lt_paged_reorder(*args)
+
+
+def lt_cache4_copy(*args) -> int:
+    return load().lt_cache4_copy(*args)
 
 
 def lt_strerror(status: int) -> str:
@@ -837,3 +899,291 @@ def token_logprobs_backward(logits: torch.Tensor, tokens: torch.Tensor, lse: tor
     _check(st, "lt_token_logprobs_backward")
     _used_on(stream, out)
     return out
+
+
+# ---------------------------------------------------------------------------
+# rotary positions
+# ---------------------------------------------------------------------------
+
+class Rotary(NamedTuple):
+    """How positions turn a head: `inv_freq` (float32 [pairs] on the GPU, radians a
+    position) turns the values [start, start + 2 * pairs), paired (i, i + pairs) or
+    interleaved (2 i, 2 i + 1); sine and cosine are multiplied by `amplitude`."""
+    inv_freq: torch.Tensor
+    start: int = 0
+    interleaved: bool = False
+    amplitude: float = 1.0
+
+
+def rotary_frequencies(dim: int, base: float = 10000.0, method: str = "none", factor: float = 1.0,
+                       original_length: int = 0, low: Optional[float] = None, high: Optional[float] = None,
+                       start: int = 0, interleaved: bool = False, amplitude: Optional[float] = None,
+                       device=None) -> Rotary:
+    """The Rotary of frequencies f_i = base ** (-2 i / dim), i < dim / 2, scaled for
+    contexts `factor` times as long as the `original_length` positions trained on:
+
+    none      as they are
+    linear    f_i / factor: positions are interpolated
+    base      a base of base * factor ** (dim / (dim - 2)): the first frequency stays, the
+              last is divided by factor
+    ramp      f_i / factor below a ramp over the index i, f_i above it: the ramp ends where
+              a frequency turns `low` (1) and `high` (32) times over original_length;
+              amplitude 0.1 ln(factor) + 1
+    turns     the same with the ramp over the number of turns, from `low` (1) to `high` (4)
+
+    amplitude overrides the method's (1 but for ramp)."""
+    _need(dim >= 2 and dim % 2 == 0, "dim must be even and positive")
+    _need(base > 0.0 and factor > 0.0, "base and factor must be positive")
+    n = dim // 2
+    two_pi = 2.0 * math.pi
+    if method == "base":
+        _need(dim > 2, "method 'base' needs dim > 2")
+        base = base * factor ** (dim / (dim - 2.0))
+    f = [base ** (-2.0 * i / dim) for i in range(n)]
+    amp = 1.0
+    if method == "linear":
+        f = [x / factor for x in f]
+    elif method in ("ramp", "turns"):
+        _need(original_length > 0, "methods 'ramp' and 'turns' need original_length")
+        lo = 1.0 if low is None else float(low)
+        hi = (32.0 if method == "ramp" else 4.0) if high is None else float(high)
+        _need(0.0 < lo < hi, "need 0 < low < high")
+        if method == "turns":
+            keep = [(original_length * x / two_pi - lo) / (hi - lo) for x in f]
+        else:
+            _need(base > 1.0, "method 'ramp' needs base > 1")
+            # the (real) index whose frequency turns r times over original_length
+            at = [dim * math.log(original_length / (r * two_pi)) / (2.0 * math.log(base)) for r in (hi, lo)]
+            first, last = max(math.floor(at[0]), 0), min(math.ceil(at[1]), dim - 1)
+            keep = [1.0 - (i - first) / max(last - first, 1e-3) for i in range(n)]
+            amp = 0.1 * math.log(factor) + 1.0 if factor > 1.0 else 1.0
+        keep = [min(max(x, 0.0), 1.0) for x in keep]
+        f = [x * k + x / factor * (1.0 - k) for x, k in zip(f, keep)]
+    elif method not in ("none", "base"):
+        raise LiteTopKError("method must be 'none', 'linear', 'base', 'ramp' or 'turns'")
+    t = torch.tensor(f, dtype=torch.float64).float().to(device or "cuda")
+    return Rotary(t, start, interleaved, amp if amplitude is None else amplitude)
+
+
+def _here(dev, *ts):
+    """All tensors on one GPU, the current one (which launches go to)."""
+    if dev.type != "cuda":
+        raise LiteTopKError("tensors must be on the GPU")
+    for t in ts:
+        if t is not None and t.device != dev:
+            raise LiteTopKError("tensors must be on one GPU")
+    if dev.index != torch.cuda.current_device():
+        raise LiteTopKError("tensors are on %s, which is not the current device" % dev)
+
+
+def _heads(t: torch.Tensor, name: str):
+    """[tokens, heads, head_dim] in float32 or bfloat16, rows contiguous."""
+    if not (t.dim() == 3 and t.dtype in (torch.float32, torch.bfloat16)
+            and (t.numel() == 0 or t.shape[2] == 1 or t.stride(2) == 1)):
+        raise LiteTopKError("%s must be float32 or bfloat16 [tokens, heads, head_dim] with contiguous heads" % name)
+    return t.shape
+
+
+def _turn(rot: Rotary, d: int):
+    f = rot.inv_freq
+    if not (f.dtype is torch.float32 and f.dim() == 1 and f.is_contiguous()):
+        raise LiteTopKError("inv_freq must be a contiguous float32 vector on the GPU")
+    n = f.numel()
+    if rot.start < 0 or rot.start + 2 * n > d:
+        raise LiteTopKError("the rotated part [%d, %d) is not inside a head of %d" % (rot.start, rot.start + 2 * n, d))
+    return n
+
+
+def _rotate(x, positions, rot, out, out_dtype, flags, stream):
+    t, h, d = _heads(x, "x")
+    n = _turn(rot, d)
+    _here(x.device, positions, rot.inv_freq, out)
+    _int32(positions, t, "positions")
+    if out is None:
+        out = _empty((t, h, d), out_dtype or x.dtype, x.device, stream)
+        mine = out
+    else:
+        mine = None
+        _heads(out, "out")
+        _need(out.shape == x.shape, "out must have x's shape")
+        _need(out_dtype is None or out_dtype is out.dtype, "out is not of out_dtype")
+    st = lt_rotary(_ptr(x), _dtype_code(x), x.stride(0), x.stride(1), t, h, d, _ptr(positions), _ptr(rot.inv_freq), n,
+                   rot.start, rot.amplitude, flags | (LT_ROTARY_INTERLEAVED if rot.interleaved else 0), _ptr(out),
+                   _dtype_code(out), out.stride(0), out.stride(1), _stream_of(stream, x))
+    _check(st, "lt_rotary")
+    _used_on(stream, mine)
+    return out
+
+
+def rotary(x: torch.Tensor, positions: torch.Tensor, rot: Rotary, out: Optional[torch.Tensor] = None,
+           out_dtype: Optional[torch.dtype] = None, stream=None) -> torch.Tensor:
+    """x [T, heads, head_dim] (float32 or bfloat16, any strides between heads and
+    tokens: a slice of a common projection will do) with every head turned by its
+    token's position (int32 [T]; negative = padding, which becomes zeros). The result
+    has x's type, or is bfloat16 (out_dtype); `out` may be x. It is not part of an
+    autograd graph: its gradient is rotary_backward's."""
+    return _rotate(x, positions, rot, out, out_dtype, 0, stream)
+
+
+def rotary_backward(grad: torch.Tensor, positions: torch.Tensor, rot: Rotary, out: Optional[torch.Tensor] = None,
+                    stream=None) -> torch.Tensor:
+    """The gradient of rotary's x from that of its result: turned back, times the
+    amplitude in the rotated part."""
+    return _rotate(grad, positions, rot, out, None, LT_ROTARY_INVERSE, stream)
+
+
+def rotary_fp8(x: torch.Tensor, positions: torch.Tensor, rot: Rotary, out=None, stream=None):
+    """The same as fp8, for indexer_topk: (codes float8_e4m3fn [T, heads, head_dim],
+    scales float32 [T, heads]); scales are powers of two. For keys (one head) view them
+    as [T, head_dim] and [T]; `out` = (codes, scales) writes into an array of them."""
+    t, h, d = _heads(x, "x")
+    n = _turn(rot, d)
+    _int32(positions, t, "positions")
+    if out is None:
+        codes = _empty((t, h, d), torch.float8_e4m3fn, x.device, stream)
+        scales = _empty((t, h), torch.float32, x.device, stream)
+    else:
+        codes, scales = out
+        _on_gpu(codes, scales)
+        _need(codes.dtype in (torch.float8_e4m3fn, torch.uint8) and codes.shape == x.shape
+              and scales.dtype == torch.float32 and scales.shape == x.shape[:2],
+              "out must be codes float8_e4m3fn [T, heads, head_dim] and scales float32 [T, heads]")
+    _here(x.device, positions, rot.inv_freq, codes, scales)
+    st = lt_rotary_fp8(_ptr(x), _dtype_code(x), x.stride(0), x.stride(1), t, h, d, _ptr(positions),
+                       _ptr(rot.inv_freq), n, rot.start, rot.amplitude,
+                       LT_ROTARY_INTERLEAVED if rot.interleaved else 0, _ptr(codes), _ptr(scales),
+                       _stream_of(stream, x))
+    _check(st, "lt_rotary_fp8")
+    if out is None:
+        _used_on(stream, codes, scales)
+    return codes, scales
+
+
+def cache4_append_rotary(k: torch.Tensor, v: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
+                         slots: torch.Tensor, positions: torch.Tensor, rot: Rotary, q: Optional[torch.Tensor] = None,
+                         stream=None) -> Optional[torch.Tensor]:
+    """cache4_append with the keys turned by their positions (int32 [rows], as
+    paged_plan gives them) on the way. With q [rows, heads, head_dim] (of k's type) the
+    same launch turns the queries: returns them in bfloat16, for cache4_attention."""
+    pages, page, heads, d = _cache4(codes, scales)
+    ks, vs = _rows_of(k, heads, d, "k"), _rows_of(v, heads, d, "v")
+    rows = k.shape[0]
+    if not (k.dtype is v.dtype and k.dtype in (torch.float32, torch.bfloat16) and v.shape[0] == rows):
+        raise LiteTopKError("k and v must have as many rows of one type, float32 or bfloat16")
+    if not (slots.dtype is torch.int64 and slots.dim() == 1 and slots.is_contiguous() and slots.numel() == rows):
+        raise LiteTopKError("slots must be a contiguous int64 [rows]")
+    _int32(positions, rows, "positions")
+    n = _turn(rot, d)
+    _here(k.device, v, codes, scales, slots, positions, rot.inv_freq, q)
+    hq, qs, out = 0, 0, None
+    if q is not None:
+        if not (q.dtype is k.dtype and q.dim() == 3 and q.shape[0] == rows and q.shape[1] >= 1):
+            raise LiteTopKError("q must be [rows, heads, head_dim] of k's type")
+        hq = q.shape[1]
+        qs = _rows_of(q, hq, d, "q")
+        out = _empty((rows, hq, d), torch.bfloat16, k.device, stream)
+    st = lt_cache4_append_rotary(_ptr(k), _ptr(v), _dtype_code(k), ks, vs, rows, _ptr(codes), _ptr(scales), pages, page,
+                                 heads, d, _ptr(slots), _ptr(positions), _ptr(rot.inv_freq), n, rot.start,
+                                 rot.amplitude, LT_ROTARY_INTERLEAVED if rot.interleaved else 0,
+                                 _ptr(q) if rows else None, qs, hq if rows else 0, _ptr(out), _stream_of(stream, k))
+    _check(st, "lt_cache4_append_rotary")
+    _used_on(stream, out)
+    return out
+
+
+# ---------------------------------------------------------------------------
+# beam search
+# ---------------------------------------------------------------------------
+
+class BeamCandidates(NamedTuple):
+    """What beam_select returns, best first; see lt_beam_select in the header."""
+    score: torch.Tensor   # float32 [requests, top]; -inf behind the last candidate
+    beam: torch.Tensor    # int32 [requests, top], -1 there
+    token: torch.Tensor   # int32 [requests, top], -1 there
+
+
+def beam_select(logits: torch.Tensor, scores: torch.Tensor, top: int, scale: float = 1.0,
+                workspace: Optional[torch.Tensor] = None, stream=None) -> BeamCandidates:
+    """The `top` best continuations of every request over its beams and the
+    vocabulary: logits [requests * beams, vocab] (float32 or bfloat16), scores [requests,
+    beams] (float32: the beams' log probabilities so far, -inf for a beam that is not
+    alive, as all but one are in the first step). A program that lets beams finish asks
+    for more continuations than it has beams."""
+    _need(logits.dim() == 2 and logits.dtype in (torch.float32, torch.bfloat16)
+          and (logits.numel() == 0 or logits.shape[1] == 1 or logits.stride(1) == 1),
+          "logits must be a float32 or bfloat16 [requests * beams, vocab] GPU matrix with unit column stride")
+    _need(scores.dim() == 2 and scores.dtype is torch.float32 and scores.is_contiguous()
+          and scores.numel() == logits.shape[0], "scores must be float32 [requests, beams], contiguous")
+    dev = logits.device
+    _here(dev, scores, workspace)
+    reqs, beams = scores.shape
+    rows, vocab = logits.shape
+    dt = _dtype_code(logits)
+    need = lt_beam_select_workspace_size(dt, reqs, beams, vocab, top)
+    _need(need > 0, "unsupported shape for lt_beam_select (top must be 1..%d, beams 1..%d)"
+          % (LT_BEAM_MAX_TOP, LT_BEAM_MAX_BEAMS))
+    workspace = _workspace(workspace, need, dev, stream)
+    ints = _empty((2, reqs, top), torch.int32, dev, stream)
+    r = BeamCandidates(_empty((reqs, top), torch.float32, dev, stream), ints[0], ints[1])
+    ld = logits.stride(0) if rows > 1 and vocab > 0 else vocab
+    st = lt_beam_select(_ptr(logits), dt, ld, reqs, beams, vocab, _ptr(scores), scale, top, _ptr(r.score),
+                        _ptr(r.beam), _ptr(r.token), _ptr(workspace), workspace.numel(), _stream_of(stream, logits))
+    _check(st, "lt_beam_select")
+    _used_on(stream, r.score, ints)
+    return r
+
+
+class PagedReorder(NamedTuple):
+    """What paged_reorder returns; see lt_paged_reorder in the header."""
+    block_table: torch.Tensor  # int32 [rows, width]
+    seq_lens: torch.Tensor     # int32 [rows]
+    copies: torch.Tensor       # int32 [rows, 2]: page to copy, page to write (-1, -1: none)
+    free_used: torch.Tensor    # int32 [1]
+    status: torch.Tensor       # int32 [rows]: 0 goes on, 1 ended by its parent, 2 out of pages
+
+
+def paged_reorder(block_table: torch.Tensor, seq_lens: torch.Tensor, parents: torch.Tensor, group: int,
+                  free_pages: torch.Tensor, free_used: torch.Tensor, page_size: int,
+                  keep_pages: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                  stream=None) -> PagedReorder:
+    """Rows of a paged cache go on as their parents (int32 [rows], counted within each
+    group of `group` rows; outside [0, group): the row ends). Full pages are shared,
+    partial ones copied for all children but the first: pass `copies` to cache4_copy for
+    each layer. Pages that no row holds any more go back onto free_pages (in place,
+    before free_used). block_table [rows, width], seq_lens, free_pages and free_used are
+    paged_plan's."""
+    n = seq_lens.numel()
+    _int32(seq_lens, None, "seq_lens")
+    _int32(parents, n, "parents")
+    _int32(keep_pages, n, "keep_pages")
+    _int32(free_pages, None, "free_pages")
+    _int32(free_used, 1, "free_used")
+    ld, width = _table(block_table, n)
+    dev = block_table.device
+    _here(dev, seq_lens, parents, keep_pages, free_pages, free_used, workspace)
+    need = lt_paged_reorder_workspace_size(n)
+    _need(need > 0, "at most %d rows" % LT_PLAN_MAX_REQUESTS)
+    workspace = _workspace(workspace, need, dev, stream)
+    table, lens, copies, used, status = _empty(n * (width + 4) + 1, torch.int32, dev, stream).split_with_sizes(
+        (n * width, n, 2 * n, 1, n))
+    r = PagedReorder(table.view(n, width), lens, copies.view(n, 2), used, status)
+    st = lt_paged_reorder(_ptr(block_table), ld, width, _ptr(seq_lens), _ptr(parents), n, group, page_size,
+                          _ptr(keep_pages), _ptr(free_pages), free_pages.numel(), _ptr(free_used), _ptr(table), width,
+                          _ptr(lens), _ptr(copies), _ptr(used), _ptr(status), _ptr(workspace), workspace.numel(),
+                          _stream_of(stream, block_table))
+    _check(st, "lt_paged_reorder")
+    _used_on(stream, *r)
+    return r
+
+
+def cache4_copy(codes: torch.Tensor, scales: torch.Tensor, copies: torch.Tensor, stream=None) -> None:
+    """Copies whole pages of a 4-bit cache: copies int32 [n, 2], page to copy and page
+    to write, as paged_reorder gives them; pairs with a page outside the cache (-1) are
+    left out."""
+    pages, page, heads, d = _cache4(codes, scales)
+    if not (copies.dtype is torch.int32 and copies.dim() == 2 and copies.shape[1] == 2 and copies.is_contiguous()):
+        raise LiteTopKError("copies must be a contiguous int32 [n, 2] on the GPU")
+    _here(codes.device, scales, copies)
+    st = lt_cache4_copy(_ptr(codes), _ptr(scales), pages, page, heads, d, _ptr(copies), copies.shape[0],
+                        _stream_of(stream, codes))
+    _check(st, "lt_cache4_copy")
