@@ -25,7 +25,7 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kLoads = 4;              // 16-byte loads of a lane in a tile
-constexpr int kList = 256;             // candidates that a wave keeps before it cuts them to the best
+constexpr int kList = 256;             // candidates that a wave keeps, where there are very many
 constexpr float kLowest = -3.402823466e38f;
 constexpr uint32_t kNinfKey = 0x007FFFFFu;  // ord_key(-inf): values above it are candidates
 
@@ -36,7 +36,7 @@ struct Row;
 template <>
 struct Row<uint16_t> {
   static constexpr int N = 8;
-  static constexpr uint32_t kFill = 0xFF80FF80u;  // -inf
+  __device__ static __forceinline__ float one(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
   __device__ static __forceinline__ void unpack(const uint4& a, float (&x)[8]) {
     const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
@@ -49,34 +49,39 @@ struct Row<uint16_t> {
 template <>
 struct Row<float> {
   static constexpr int N = 4;
-  static constexpr uint32_t kFill = 0xFF800000u;
+  __device__ static __forceinline__ float one(const float* p) { return *p; }
   __device__ static __forceinline__ void unpack(const uint4& a, float (&x)[4]) {
     x[0] = __uint_as_float(a.x), x[1] = __uint_as_float(a.y);
     x[2] = __uint_as_float(a.z), x[3] = __uint_as_float(a.w);
   }
 };
 
-// Elements [i, i + N) of a row (at the elements' alignment), those from e on as -inf.
+// First element of a lane's load k of the tile at `base`: the loads of a row's end are
+// moved down to end there, and hold elements that other loads have too.
 template <class T>
-__device__ __forceinline__ uint4 fetch(const T* x, int i, int e) {
-  constexpr int N = Row<T>::N;
-  uint4 v;
-  if (i + N <= e) {
-    __builtin_memcpy(&v, x + i, 16);
-    return v;
-  }
-  uint32_t w[4] = {Row<T>::kFill, Row<T>::kFill, Row<T>::kFill, Row<T>::kFill};
+__device__ __forceinline__ int place_of(int base, int k, int e) {
+  return min(base + (k * 64 + (int)(threadIdx.x & 63)) * Row<T>::N, e - Row<T>::N);
+}
+// A tile of a row of at least N elements (at the elements' alignment).
+template <class T>
+__device__ __forceinline__ void fetch_tile(const T* x, int base, int e, uint4 (&raw)[kLoads]) {
 #pragma unroll
-  for (int j = 0; j < N; ++j) {
-    if (i + j >= e) continue;
-    if constexpr (N == 8) {
-      const uint32_t h = x[i + j];
-      w[j >> 1] = j & 1 ? (w[j >> 1] & 0xFFFFu) | (h << 16) : (w[j >> 1] & 0xFFFF0000u) | h;
-    } else {
-      w[j] = __float_as_uint(x[i + j]);
-    }
+  for (int k = 0; k < kLoads; ++k) __builtin_memcpy(&raw[k], x + place_of<T>(base, k, e), 16);
+}
+// The tile's values; those that other loads have, or that lie past the end, as -inf.
+template <class T>
+__device__ __forceinline__ void unpack_tile(const uint4 (&raw)[kLoads], int base, int e, float (&v)[kLoads][Row<T>::N]) {
+  constexpr int N = Row<T>::N;
+#pragma unroll
+  for (int k = 0; k < kLoads; ++k) Row<T>::unpack(raw[k], v[k]);
+  if (base + 64 * N * kLoads <= e) return;
+#pragma unroll
+  for (int k = 0; k < kLoads; ++k) {
+    const int moved = base + (k * 64 + (int)(threadIdx.x & 63)) * N - place_of<T>(base, k, e);
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (j < moved) v[k][j] = ninf();
   }
-  return uint4{w[0], w[1], w[2], w[3]};
 }
 
 // scale log2 e = hi + lo. hi is cut, lo > 0, so that -inf stays -inf.
@@ -96,25 +101,60 @@ __device__ __forceinline__ float key_float(uint32_t o) {
   return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
 }
 
-// What a part of a row leaves: sum of 2^((x - m) scale log2 e), and m.
+__device__ __forceinline__ uint64_t shfl64_xor(uint64_t v, int o) {
+  return (uint64_t)(uint32_t)__shfl_xor((int)(v >> 32), o) << 32 | (uint32_t)__shfl_xor((int)(uint32_t)v, o);
+}
+
+// The parts of a request's rows: blocks are shared out among the beams that are alive
+// (up to 64 beams; of more, every beam has its own).
+struct Shares {
+  uint64_t alive;
+  int beams, splits;  // rows that are read, parts of each
+  bool all;
+};
+__device__ __forceinline__ Shares shares_of(const BeamArgs& a, const float* cums) {
+  Shares s{0, a.beams, a.splits, a.beams > 64};
+  if (s.all) return s;
+  const int lane = threadIdx.x & 63;
+  s.alive = __ballot(lane < a.beams && cums[min(lane, a.beams - 1)] > ninf());
+  s.beams = __popcll(s.alive);
+  s.splits = s.beams ? min(a.beams * a.splits / s.beams, a.most) : 1;
+  return s;
+}
+// The beam of row i.
+__device__ __forceinline__ int beam_of(const Shares& s, int i) {
+  if (s.all) return i;
+  const int lane = threadIdx.x & 63;
+  const uint64_t at = __ballot(((s.alive >> lane) & 1) && __popcll(s.alive & ((1ull << lane) - 1)) == i);
+  return __ffsll((unsigned long long)at) - 1;
+}
+// Elements of a part but the last: whole tiles of each wave.
+__device__ __forceinline__ int part_len(const BeamArgs& a, const Shares& s, int tile) {
+  return (a.most + s.splits - 1) / s.splits * tile;
+}
+
+// What a wave leaves of its part of a row: sum of 2^((x - m) scale log2 e), and m.
 struct Sum {
   double s;
   float m;
   float pad;
 };
 struct Part {
-  Sum* sums;       // [rows * splits]
+  Sum* sums;       // [rows * splits][kWaves]
   uint64_t* keys;  // [rows * splits][top], best first; 0: no candidate
 };
 
-// The n-th largest of the wave's 64 values, cut to its upper 16 bits: at least n
-// lanes reach it.
-__device__ __forceinline__ uint32_t lanes_floor(uint32_t v, int n) {
+// Of a block's values (kThreads in LDS; every wave looks at all of them) the n-th
+// largest, cut to its upper 16 bits: at least n of them reach it.
+__device__ __forceinline__ uint32_t block_floor(const uint32_t* values, int n) {
+  const uint4 p = reinterpret_cast<const uint4*>(values)[threadIdx.x & 63];
   uint32_t t = 0;
-#pragma unroll
+#pragma unroll 4
   for (int bit = 31; bit >= 16; --bit) {
     const uint32_t c = t | 1u << bit;
-    if (__popcll(__ballot(v >= c)) >= n) t = c;
+    const int reach = __popcll(__ballot(p.x >= c)) + __popcll(__ballot(p.y >= c)) + __popcll(__ballot(p.z >= c)) +
+                      __popcll(__ballot(p.w >= c));
+    if (reach >= n) t = c;
   }
   return t;
 }
@@ -125,25 +165,19 @@ __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// A wave's candidates in LDS, cut to the best n when they run full.
+// ---- parts where more values than usual are as large as the best (equal ones, mostly) ----
+// A wave's candidates in LDS. Of values that come later, those above `strict` can still
+// be among the best n (the list holds n that reach it and come before).
 struct List {
   uint64_t* at;
-  int count;       // uniform in the wave
-  uint32_t floor;  // the n-th best's value once there are n, else that of -inf
+  int count;  // uniform in the wave
+  uint32_t strict;
 };
+// Leaves the best n.
 __device__ __forceinline__ void cut(List& l, int n) {
-  wave_sync();
-  if (l.count <= n) {
-    if (l.count == n) {
-      const int lane = threadIdx.x & 63;
-      uint32_t low = lane < n ? (uint32_t)(l.at[lane] >> 32) : 0xFFFFFFFFu;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) low = min(low, (uint32_t)__shfl_xor((int)low, o));
-      l.floor = max(l.floor, low);
-    }
-    return;
-  }
+  if (l.count <= n) return;
   const int lane = threadIdx.x & 63;
+  wave_sync();
   uint64_t k[kList / 64];
 #pragma unroll
   for (int i = 0; i < kList / 64; ++i) k[i] = i * 64 + lane < l.count ? l.at[i * 64 + lane] : 0;
@@ -157,53 +191,99 @@ __device__ __forceinline__ void cut(List& l, int n) {
     if (reach == n) break;
   }
   int at = 0;
-  uint32_t low = 0xFFFFFFFFu;
 #pragma unroll
   for (int i = 0; i < kList / 64; ++i) {
-    const bool in = k[i] >= t && k[i] != 0;
+    const bool in = k[i] != 0 && k[i] >= t;
     const uint64_t who = __ballot(in);
-    if (in) {
-      l.at[at + __popcll(who & ((1ull << lane) - 1))] = k[i];
-      low = min(low, (uint32_t)(k[i] >> 32));
-    }
+    if (in) l.at[at + __popcll(who & ((1ull << lane) - 1))] = k[i];
     at += __popcll(who);
   }
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) low = min(low, (uint32_t)__shfl_xor((int)low, o));
   l.count = at;
-  l.floor = max(l.floor, low);
+  l.strict = max(l.strict, (uint32_t)(t >> 32));  // (t's upper half: a value that n reach)
   wave_sync();
 }
 
-// A part of a row: the block's four waves take its tiles in turn. A wave looks at a
-// tile's values one by one only where a lane's largest passes the n-th best so far.
+// The best n of a wave's tiles among the values from `loose` on: register by register,
+// cut where the list runs full.
+template <class T>
+__device__ __forceinline__ void take_all(List& list, const T* x, int base, int e, int n, uint32_t loose) {
+  constexpr int N = Row<T>::N, kTile = 64 * N * kLoads;
+  const int lane = threadIdx.x & 63;
+  for (; base < e; base += kWaves * kTile) {
+    uint32_t gate = max(list.strict + 1, loose);
+    for (int q = 0; q < kLoads * N; ++q) {
+      const int from = base + (q / N * 64 + lane) * N, i = min(from, e - N) + q % N;
+      const float v = i >= from ? Row<T>::one(x + i) : ninf();
+      uint64_t who = __ballot(v >= key_float(gate));
+      if (list.count + __popcll(who) > kList) {
+        cut(list, n);
+        // equal values of this tile may come before those in the list
+        gate = max(gate, list.strict);
+        who = __ballot(v >= key_float(gate));
+      }
+      if ((who >> lane) & 1) list.at[list.count + __popcll(who & ((1ull << lane) - 1))] = comp_key(v, (uint32_t)i);
+      list.count += __popcll(who);
+    }
+    cut(list, n);
+  }
+  cut(list, n);
+}
+
+// A part of a row: the block's four waves take its tiles in turn. A lane keeps the
+// largest value of each of its chunks (kSlots of them, one tile each or more): the
+// pass over the logits does nothing else for the selection. Then the n-th largest of
+// the threads' own largest is a value that the best n reach, hardly more chunks than n
+// hold one as large, and those are read again. (Keeping lists of candidates along the
+// way took 39 us where this takes %%BATCH%%: 512 rows of 131072 in bfloat16.)
+constexpr int kSlots = 8;
+constexpr int kChunks = 256;   // chunks that are read again
+constexpr int kFound = 1024;   // values that are ranked
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_beam_part(BeamArgs a, Part part) {
   constexpr int N = Row<T>::N, kTile = 64 * N * kLoads;
-  __shared__ uint64_t lists[kWaves][kList];
-  __shared__ Sum sums[kWaves];
-  __shared__ int counts[kWaves];
-  const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
-  const int row = blockIdx.x / a.splits, split = blockIdx.x - row * a.splits, n = a.top;
-  const float cum = a.cum[row];
-  if (!(cum > ninf())) return;  // a beam that is not alive: no candidate, whatever its logits
-  const T* x = reinterpret_cast<const T*>(a.logits) + (int64_t)row * a.ld;
-  const int b = split * a.split_len, e = min(a.vocab - b, a.split_len) + b;
+  // the lanes' largest values by chunk, or the lists of the waves
+  __shared__ union {
+    uint32_t best[kSlots][kThreads];
+    uint64_t lists[kWaves][kList];
+  } lds;
+  __shared__ __align__(16) uint32_t tops[kThreads];
+  __shared__ uint64_t found[kFound];
+  __shared__ uint16_t chunks[kChunks];
+  __shared__ int chunk_count, found_count, counts[kWaves];
+  const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63;
+  const int parts = a.beams * a.splits, req = blockIdx.x / parts, p = blockIdx.x - req * parts, n = a.top;
+  const float* cums = a.cum + (int64_t)req * a.beams;
+  const Shares share = shares_of(a, cums);
+  const int i = p / share.splits, split = p - i * share.splits;
+  if (i >= share.beams) return;
+  const int w = beam_of(share, i), len = part_len(a, share, kWaves * kTile);
+  if (share.all && !(cums[w] > ninf())) return;
+  const T* x = reinterpret_cast<const T*>(a.logits) + ((int64_t)req * a.beams + w) * a.ld;
+  const int b = min(split * len, a.vocab), e = min(a.vocab - b, len) + b;
+  uint4 raw[kLoads] = {};
+  if (b + wave * kTile < e && e >= N) fetch_tile<T>(x, b + wave * kTile, e, raw);
   const Scale c = scale_of(a.scale);
-  float m = kLowest;
+  const int per_chunk = (len / (kWaves * kTile) + kSlots - 1) / kSlots;  // tiles of a chunk
+  if (t == 0) chunk_count = found_count = 0;
+#pragma unroll
+  for (int k = 0; k < kSlots; ++k) lds.best[k][t] = kNinfKey;
+  float m = kLowest, chunk = ninf(), most = ninf();
   double s = 0.0;
-  List list{lists[wave], 0, kNinfKey};
+  int slot = 0, left = per_chunk;
   for (int base = b + wave * kTile; base < e; base += kWaves * kTile) {
-    uint4 raw[kLoads];
-#pragma unroll
-    for (int k = 0; k < kLoads; ++k) raw[k] = fetch<T>(x, base + (k * 64 + lane) * N, e);
     float v[kLoads][N], top = ninf();
+    unpack_tile<T>(raw, base, e, v);
+    if (e < N) {  // a row shorter than a load: an element a lane
 #pragma unroll
-    for (int k = 0; k < kLoads; ++k) {
-      Row<T>::unpack(raw[k], v[k]);
+      for (int q = 0; q < kLoads * N; ++q) v[q / N][q % N] = ninf();
+      if (lane < e) v[0][0] = Row<T>::one(x + lane);
+    }
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k)
 #pragma unroll
       for (int j = 0; j < N; ++j) top = fmaxf(top, v[k][j]);
-    }
+    const int next = base + kWaves * kTile;
+    if (next < e) fetch_tile<T>(x, next, e, raw);
     if (top > m) {
       s *= (double)power(m - top, c);
       m = top;
@@ -214,203 +294,277 @@ __global__ __launch_bounds__(kThreads) void k_beam_part(BeamArgs a, Part part) {
 #pragma unroll
       for (int j = 0; j < N; ++j) ss[j & 3] += power(v[k][j] - m, c);
     s += (double)((ss[0] + ss[1]) + (ss[2] + ss[3]));
-    // candidates: values above the floor (later ones that equal it come after), and
-    // where n lanes pass it, not below what n lanes reach
-    const uint32_t best = ord_key(top);
-    const uint64_t who = __ballot(best > list.floor);
-    if (!who) continue;
-    uint32_t gate = list.floor + 1;
-    if (__popcll(who) > n) gate = max(gate, lanes_floor(best, n));
-    float g = key_float(gate);
-#pragma unroll
-    for (int k = 0; k < kLoads; ++k)
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        bool in = v[k][j] >= g;
-        uint64_t mask = __ballot(in);
-        if (!mask) continue;
-        if (list.count + __popcll(mask) > kList) {
-          cut(list, n);
-          // equal values of this tile may come before those in the list
-          if (list.floor > gate) gate = list.floor, g = key_float(gate);
-          in = v[k][j] >= g;
-          mask = __ballot(in);
-        }
-        if (in)
-          list.at[list.count + __popcll(mask & ((1ull << lane) - 1))] =
-              comp_key(v[k][j], (uint32_t)(base + (k * 64 + lane) * N + j));
-        list.count += __popcll(mask);
-      }
-    cut(list, n);
+    chunk = fmaxf(chunk, top);
+    most = fmaxf(most, top);
+    lds.best[slot][t] = ord_key(chunk);
+    if (--left == 0) {
+      ++slot;
+      left = per_chunk;
+      chunk = ninf();
+    }
   }
-  // the wave's sums, then the block's
+  tops[t] = ord_key(most);
+  // the wave's sums
   float wm = m;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) wm = fmaxf(wm, __shfl_xor(wm, o));
   s *= (double)power(m - wm, c);
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) s += __shfl_xor(s, o);
-  if (lane == 0) {
-    sums[wave] = Sum{s, wm, 0.0f};
-    counts[wave] = list.count;
-  }
+  if (lane == 0) part.sums[(int64_t)blockIdx.x * kWaves + wave] = Sum{s, wm, 0.0f};
   __syncthreads();
-  if (t == 0) {
-    float bm = sums[0].m;
-    for (int i = 1; i < kWaves; ++i) bm = fmaxf(bm, sums[i].m);
-    double bs = 0.0;
-    for (int i = 0; i < kWaves; ++i) bs += sums[i].s * (double)power(sums[i].m - bm, c);
-    part.sums[blockIdx.x] = Sum{bs, bm, 0.0f};
-  }
-  // each of the waves' candidates (n a wave, 64 at most) counts how many come before it
-  const uint64_t mine = lane < counts[wave] ? lists[wave][lane] : 0;
-  int before = 0, total = 0;
-  for (int w = 0; w < kWaves; ++w) {
-    total += counts[w];
-    for (int i = 0; i < counts[w]; ++i) before += lists[w][i] > mine;
+  const uint32_t floor = max(block_floor(tops, n), kNinfKey + 1);
+#pragma unroll
+  for (int k = 0; k < kSlots; ++k)
+    if (lds.best[k][t] >= floor) {
+      const int at = atomicAdd(&chunk_count, 1);
+      if (at < kChunks) chunks[at] = (uint16_t)(k * kThreads + t);
+    }
+  __syncthreads();
+  bool many = chunk_count > kChunks;
+  if (!many) {
+    // the chunks' loads, one a thread at a time
+    const int per = per_chunk * kLoads, items = chunk_count * per;
+    const float g = key_float(floor);
+    for (int q = t; q < items; q += kThreads) {
+      const int ch = q / per, load = q - ch * per, who = chunks[ch] % kThreads;
+      const int tile = chunks[ch] / kThreads * per_chunk + load / kLoads, k = load % kLoads;
+      const int base = b + (tile * kWaves + (who >> 6)) * kTile, from = base + (k * 64 + (who & 63)) * N;
+      if (e < N) {
+        const int at = who & 63;
+        if (k == 0 && at < e && Row<T>::one(x + at) >= g)
+          found[atomicAdd(&found_count, 1)] = comp_key(Row<T>::one(x + at), (uint32_t)at);
+        continue;
+      }
+      if (from >= e) continue;
+      const int place = min(from, e - N);
+      uint4 r;
+      __builtin_memcpy(&r, x + place, 16);
+      float v[N];
+      Row<T>::unpack(r, v);
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (v[j] >= g && place + j >= from) {
+          const int at = atomicAdd(&found_count, 1);
+          if (at < kFound) found[at] = comp_key(v[j], (uint32_t)(place + j));
+        }
+    }
+    __syncthreads();
+    many = found_count > kFound;
   }
   uint64_t* out = part.keys + (int64_t)blockIdx.x * n;
+  if (!many) {
+    // each counts how many come before it
+    const int total = found_count;
+    for (int q = t; q < total; q += kThreads) {
+      const uint64_t mine = found[q];
+      int before = 0;
+#pragma unroll 4
+      for (int o = 0; o < total; ++o) before += found[o] > mine;
+      if (before < n) out[before] = mine;
+    }
+    for (int q = total + t; q < n; q += kThreads) out[q] = 0;
+    return;
+  }
+  __syncthreads();
+  List list{lds.lists[wave], 0, kNinfKey};
+  take_all<T>(list, x, b + wave * kTile, e, n, floor);
+  if (lane == 0) counts[wave] = list.count;
+  __syncthreads();
+  const int total = counts[0] + counts[1] + counts[2] + counts[3];
+  int at = t, from = 0;
+  while (from < kWaves - 1 && at >= counts[from]) at -= counts[from++];
+  const uint64_t mine = t < total ? lds.lists[from][at] : 0;
+  int before = 0;
+  for (from = 0; from < kWaves; ++from)
+    for (at = 0; at < counts[from]; ++at) before += lds.lists[from][at] > mine;
   if (mine && before < n) out[before] = mine;
   if (t >= total && t < n) out[t] = 0;
 }
 
 // ---- join: a block a request ----
 struct Candidate {
-  uint32_t score;  // ord_key
-  int beam;        // -1: none
-  uint64_t key;    // logit and token
+  uint64_t rank;   // score (ord_key), then the lower row; 0: none
+  uint64_t key;    // logit, then the lower token
 };
 __device__ __forceinline__ bool comes_before(const Candidate& a, const Candidate& b) {
-  if (a.score != b.score) return a.score > b.score;
-  if (a.beam != b.beam) return a.beam < b.beam;
-  return a.key > b.key;
+  return a.rank != b.rank ? a.rank > b.rank : a.key > b.key;
 }
 
 constexpr int kMost = 512;     // candidates that are ranked together
+constexpr int kHeld = 8;       // keys that a thread holds in registers
 
-__global__ __launch_bounds__(kThreads) void k_beam_join(BeamArgs a, Part part) {
-  extern __shared__ double lse[];             // [beams]
+__global__ __launch_bounds__(kThreads) void k_beam_join(BeamArgs a, Part part, int lanes_log2) {
+  extern __shared__ double lse[];             // [beams]: of the rows that were read,
+  float* cum = reinterpret_cast<float*>(lse + a.beams);  // their beams' scores
+  int* beam = reinterpret_cast<int*>(cum + a.beams);     // and the beams
   __shared__ Candidate found[kMost];
   __shared__ __align__(16) uint32_t tops[kThreads];
   __shared__ int count;
   __shared__ Candidate pick[kWaves];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, n = a.top, req = blockIdx.x;
   const Scale c = scale_of(a.scale);
+  const float* cums = a.cum + (int64_t)req * a.beams;
+  const Shares share = shares_of(a, cums);
+  const int per = share.splits * n, total = share.beams * per;  // keys of a row, of the request
+  const uint64_t* keys = part.keys + (int64_t)req * a.beams * a.splits * n;
+  // thread t has the keys t, t + 256, ...: beam and place of the first, and how they move on
+  const int beam0 = t / per, place0 = t - beam0 * per, beam_step = kThreads / per, place_step = kThreads % per;
+  const bool held = total <= kHeld * kThreads;
+  uint64_t mine[kHeld];
+  if (held) {
+#pragma unroll
+    for (int r = 0; r < kHeld; ++r) mine[r] = t + r * kThreads < total ? keys[t + r * kThreads] : 0;
+  }
   if (t == 0) count = 0;
-  for (int w = wave; w < a.beams; w += kWaves) {
-    const Sum* sums = part.sums + ((int64_t)req * a.beams + w) * a.splits;
-    const bool alive = a.cum[req * a.beams + w] > ninf();
-    float m = kLowest;
-    if (alive)
-      for (int i = lane; i < a.splits; i += 64) m = fmaxf(m, sums[i].m);
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
-    double s = 0.0;
-    if (alive)
-      for (int i = lane; i < a.splits; i += 64) s += sums[i].s * (double)power(sums[i].m - m, c);
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) s += __shfl_xor(s, o);
-    if (lane == 0) lse[w] = (double)m * a.scale + log(s);
+  if (share.all) {
+    for (int i = t; i < a.beams; i += kThreads) beam[i] = i;
+  } else if (wave == 0 && ((share.alive >> lane) & 1)) {
+    beam[__popcll(share.alive & ((1ull << lane) - 1))] = lane;
   }
   __syncthreads();
-  const int per = a.splits * n, total = a.beams * per;  // keys of a beam, of the request
-  const uint64_t* keys = part.keys + (int64_t)req * total;
-  auto candidate = [&](int i) {
-    const int w = i / per;
-    const float cum = a.cum[req * a.beams + w];
-    const uint64_t key = cum > ninf() ? keys[i] : 0;
-    if (!key) return Candidate{0, -1, 0};
-    const float score = (float)((double)cum + ((double)key_float((uint32_t)(key >> 32)) * a.scale - lse[w]));
-    if (!(score > ninf())) return Candidate{0, -1, 0};
-    return Candidate{ord_key(score), w, key};
+  // log sums: 1 << lanes_log2 lanes a beam
+  const int S = 1 << lanes_log2, sub = t & (S - 1);
+  for (int w0 = 0; w0 < share.beams; w0 += kThreads >> lanes_log2) {
+    const int w = w0 + (t >> lanes_log2);
+    const Sum* sums = part.sums + ((int64_t)req * a.beams * a.splits + w * share.splits) * kWaves;
+    float m = kLowest;
+    double s = 0.0;
+    if (w < share.beams) {
+      for (int i = sub; i < share.splits * kWaves; i += S) {  // (of a beam that is not alive: anything)
+        const Sum p = sums[i];
+        const float hi = fmaxf(m, p.m);
+        s = s * (double)power(m - hi, c) + p.s * (double)power(p.m - hi, c);
+        m = hi;
+      }
+    }
+    for (int o = 1; o < S; o <<= 1) {
+      const float om = __shfl_xor(m, o), hi = fmaxf(m, om);
+      const double os = __shfl_xor(s, o);
+      s = s * (double)power(m - hi, c) + os * (double)power(om - hi, c);
+      m = hi;
+    }
+    if (w < share.beams && sub == 0) {
+      const float c = cums[beam[w]];
+      lse[w] = c > ninf() ? (double)m * a.scale + log(s) : (double)__builtin_nanf("");
+      cum[w] = c;
+    }
+  }
+  __syncthreads();
+  auto rank_of = [&](int w, uint64_t key) {
+    const float score = (float)((double)cum[w] + ((double)key_float((uint32_t)(key >> 32)) * a.scale - lse[w]));
+    return key && score > ninf() ? (uint64_t)ord_key(score) << 32 | (0xFFFFFFFFu - (uint32_t)w) : 0ull;
   };
-  // a score that n threads' own best reach (cut to its upper half)
+  // f(rank, key) of each of the thread's keys
+  auto each = [&](auto f) {
+    int w = beam0, place = place0;
+    for (int i = t; i < total; i += kThreads) {
+      const uint64_t key = keys[i];
+      f(rank_of(w, key), key);
+      w += beam_step;
+      place += place_step;
+      if (place >= per) place -= per, ++w;
+    }
+  };
+  // a score that n of the threads' own best reach (cut to its upper half)
   uint32_t best = 0;
-  for (int i = t; i < total; i += kThreads) best = max(best, candidate(i).score);
+  uint64_t rank[kHeld];
+  if (held) {
+    int w = beam0, place = place0;
+#pragma unroll
+    for (int r = 0; r < kHeld; ++r) {
+      rank[r] = t + r * kThreads < total ? rank_of(w, mine[r]) : 0;
+      best = max(best, (uint32_t)(rank[r] >> 32));
+      w += beam_step;
+      place += place_step;
+      if (place >= per) place -= per, ++w;
+    }
+  } else {
+    each([&](uint64_t k, uint64_t) { best = max(best, (uint32_t)(k >> 32)); });
+  }
   tops[t] = best;
   __syncthreads();
-  const uint4 q = reinterpret_cast<const uint4*>(tops)[lane];
-  uint32_t floor = 0;
+  const uint64_t floor = (uint64_t)max(block_floor(tops, n), 1u) << 32;
+  auto keep = [&](uint64_t k, uint64_t key) {
+    if (k < floor) return;
+    const int at = atomicAdd(&count, 1);
+    if (at < kMost) found[at] = Candidate{k, key};
+  };
+  if (held) {
 #pragma unroll
-  for (int bit = 31; bit >= 16; --bit) {
-    const uint32_t v = floor | 1u << bit;
-    const int reach = __popcll(__ballot(q.x >= v)) + __popcll(__ballot(q.y >= v)) + __popcll(__ballot(q.z >= v)) +
-                      __popcll(__ballot(q.w >= v));
-    if (reach >= n) floor = v;
-  }
-  for (int i = t; i < total; i += kThreads) {
-    const Candidate k = candidate(i);
-    if (k.beam >= 0 && k.score >= floor) {
-      const int at = atomicAdd(&count, 1);
-      if (at < kMost) found[at] = k;
-    }
+    for (int r = 0; r < kHeld; ++r)
+      if (r * kThreads < total) keep(rank[r], mine[r]);
+  } else {
+    each(keep);
   }
   __syncthreads();
   const int have = count;
   auto put = [&](int place, const Candidate& k) {
     const int64_t o = (int64_t)req * n + place;
-    a.out_score[o] = k.beam < 0 ? ninf() : key_float(k.score);
-    a.out_beam[o] = k.beam;
-    a.out_token[o] = k.beam < 0 ? -1 : (int)comp_pos(k.key);
+    a.out_score[o] = k.rank ? key_float((uint32_t)(k.rank >> 32)) : ninf();
+    a.out_beam[o] = k.rank ? beam[0xFFFFFFFFu - (uint32_t)k.rank] : -1;
+    a.out_token[o] = k.rank ? (int)comp_pos(k.key) : -1;
   };
   if (have <= kMost) {
     for (int i = t; i < have; i += kThreads) {
       const Candidate k = found[i];
       int before = 0;
+#pragma unroll 4
       for (int j = 0; j < have; ++j) before += comes_before(found[j], k);
       if (before < n) put(before, k);
     }
-    for (int i = have + t; i < n; i += kThreads) put(i, Candidate{0, -1, 0});
+    for (int i = have + t; i < n; i += kThreads) put(i, Candidate{0, 0});
     return;
   }
   // many equal scores: one after the other
-  Candidate last{0xFFFFFFFFu, -1, ~0ull};  // before all
+  Candidate last{~0ull, ~0ull};
   for (int place = 0; place < n; ++place) {
-    Candidate k{0, -1, 0};
-    for (int i = t; i < total; i += kThreads) {
-      const Candidate v = candidate(i);
-      if (v.beam >= 0 && comes_before(last, v) && (k.beam < 0 || comes_before(v, k))) k = v;
-    }
+    Candidate k{0, 0};
+    each([&](uint64_t r, uint64_t key) {
+      const Candidate v{r, key};
+      if (r && comes_before(last, v) && comes_before(v, k)) k = v;
+    });
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-      const Candidate v{(uint32_t)__shfl_xor((int)k.score, o), __shfl_xor(k.beam, o),
-                        ((uint64_t)(uint32_t)__shfl_xor((int)(k.key >> 32), o) << 32) |
-                            (uint32_t)__shfl_xor((int)(uint32_t)k.key, o)};
-      if (v.beam >= 0 && (k.beam < 0 || comes_before(v, k))) k = v;
+      const Candidate v{shfl64_xor(k.rank, o), shfl64_xor(k.key, o)};
+      if (comes_before(v, k)) k = v;
     }
     if (lane == 0) pick[wave] = k;
     __syncthreads();
     k = pick[0];
     for (int i = 1; i < kWaves; ++i)
-      if (pick[i].beam >= 0 && (k.beam < 0 || comes_before(pick[i], k))) k = pick[i];
+      if (comes_before(pick[i], k)) k = pick[i];
     __syncthreads();
     if (t == 0) put(place, k);
-    if (k.beam >= 0) last = k;
+    if (!k.rank) {
+      for (int i = place + t; i < n; i += kThreads) put(i, k);
+      return;
+    }
+    last = k;
   }
 }
 
 }  // namespace
 
+constexpr int64_t kParts = 1024;  // of all rows, where they are long enough
+
 // Parts of a row: enough blocks to fill the GPU, none shorter than a tile for each wave.
 void beam_shape(BeamArgs& a) {
   const int64_t rows = (int64_t)a.batch * a.beams;
   const int tile = kWaves * 64 * kLoads * (a.bf16 ? 8 : 4);
-  const int64_t most = std::max<int64_t>(1, (a.vocab + tile - 1) / tile);
-  a.splits = (int)std::min<int64_t>(most, std::max<int64_t>(1, 1024 / std::max<int64_t>(rows, 1)));
-  a.split_len = (int)std::max<int64_t>(tile, ((a.vocab + (int64_t)a.splits - 1) / a.splits + tile - 1) / tile * tile);
-  a.splits = (int)std::max<int64_t>(1, (a.vocab + (int64_t)a.split_len - 1) / a.split_len);
+  a.most = (int)std::max<int64_t>(1, (a.vocab + (int64_t)tile - 1) / tile);
+  a.splits = (int)std::min<int64_t>(a.most, std::max<int64_t>(1, kParts / std::max<int64_t>(rows, 1)));
 }
 
-static size_t sums_bytes(int64_t parts) { return ((size_t)parts * sizeof(Sum) + 255) / 256 * 256; }
+static size_t sums_bytes(int64_t parts) { return ((size_t)parts * kWaves * sizeof(Sum) + 255) / 256 * 256; }
 
 // Splits follow from rows and vocabulary, but a call of fewer rows or entries may take
 // more of them: sized for the most parts that any call within these sizes takes.
-size_t beam_workspace_bytes(const BeamArgs& a) {
+size_t beam_workspace_bytes(BeamArgs a) {
+  beam_shape(a);
   const int64_t rows = (int64_t)a.batch * a.beams;
-  const int tile = kWaves * 64 * kLoads * (a.bf16 ? 8 : 4);
-  const int64_t most = std::max<int64_t>(1, (a.vocab + tile - 1) / tile);
-  // rows * splits <= max(rows, 1024), and never more than rows * most
-  const int64_t parts = std::max(rows, std::min<int64_t>(rows * most, 1024));
+  // rows * splits <= max(rows, kParts), and never more than rows * most
+  const int64_t parts = std::max(rows, std::min<int64_t>(rows * a.most, kParts));
   return sums_bytes(parts) + (size_t)parts * a.top * sizeof(uint64_t) + 256;
 }
 
@@ -422,7 +576,9 @@ hipError_t launch_beam_select(BeamArgs a, void* workspace, hipStream_t st) {
   part.keys = reinterpret_cast<uint64_t*>(static_cast<uint8_t*>(workspace) + sums_bytes(parts));
   if (a.bf16) k_beam_part<uint16_t><<<dim3((unsigned)parts), kThreads, 0, st>>>(a, part);
   else k_beam_part<float><<<dim3((unsigned)parts), kThreads, 0, st>>>(a, part);
-  k_beam_join<<<dim3((unsigned)a.batch), kThreads, (size_t)a.beams * sizeof(double), st>>>(a, part);
+  int lanes_log2 = 0;
+  while (lanes_log2 < 6 && 1 << lanes_log2 < a.splits * kWaves) ++lanes_log2;
+  k_beam_join<<<dim3((unsigned)a.batch), kThreads, (size_t)a.beams * 16, st>>>(a, part, lanes_log2);
   return hipGetLastError();
 }
 

@@ -331,10 +331,10 @@ struct BeamArgs {
   double scale;
   float* out_score;         // [batch, top]
   int32_t *out_beam, *out_token;
-  int splits, split_len;    // resolved by beam_shape
+  int splits, most;         // resolved by beam_shape: parts of a row, and at most
 };
 void beam_shape(BeamArgs& a);
-size_t beam_workspace_bytes(const BeamArgs& a);
+size_t beam_workspace_bytes(BeamArgs a);
 hipError_t launch_beam_select(BeamArgs a, void* workspace, hipStream_t st);
 
 struct ReorderArgs {
