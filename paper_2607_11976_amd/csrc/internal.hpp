@@ -295,7 +295,7 @@ struct RotaryArgs {
   // resolved by rotary_shape
   int vec;                  // values of a vector: 8, 4, 2 or 1
   int units;                // vector pairs of a head
-  int lanes_log2;           // lanes that share a head
+  int lanes;                // that share a head
   int head_lanes;           // of a token: each takes every head_lanes-th head
 };
 // Fills in the resolved fields; the blocks of 256 threads that the launch takes.

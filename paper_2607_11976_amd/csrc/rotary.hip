@@ -10,6 +10,9 @@ namespace lt {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int64_t kFill = 1 << 19;    // threads that fill the GPU
+constexpr int64_t kFillFp8 = 1 << 18;
+constexpr int64_t kFillKv = 1 << 17;  // with the keys' and values' loads of two heads
 
 // What a unit of a head covers: two vectors of V values, V pairs in the rotated
 // part, which fill both in turn; elsewhere two vectors that pass as they are.
@@ -68,29 +71,45 @@ __device__ __forceinline__ void turn_unit(const RotaryArgs& r, float (&x)[V], fl
 }
 
 // Lanes of a head, one unit each (in turn where there are more units); a group of
-// them takes every head_lanes-th head of a token.
+// them takes every head_lanes-th head of a token, kAhead heads' loads at a time, all
+// with the same sines and cosines.
+constexpr int kAhead = 4;
 template <class TI, class TO, int V>
 __device__ __forceinline__ void rotate_rows(const RotaryArgs& r, uint32_t block) {
-  const int lane = threadIdx.x & ((1 << r.lanes_log2) - 1);
-  const uint32_t item = block * (kThreads >> r.lanes_log2) + (threadIdx.x >> r.lanes_log2);
+  const uint32_t at = block * kThreads + threadIdx.x, item = at / (uint32_t)r.lanes;
+  const int lane = (int)(at - item * r.lanes);
   const uint32_t tok = item / (uint32_t)r.head_lanes;
   if (tok >= (uint32_t)r.T) return;
   const int h0 = (int)(item - tok * r.head_lanes), pos = r.positions[tok];
   const TI* in = reinterpret_cast<const TI*>(r.x) + (int64_t)tok * r.x_token;
   TO* out = reinterpret_cast<TO*>(r.out) + (int64_t)tok * r.out_token;
-  for (int u = lane; u < r.units; u += 1 << r.lanes_log2) {
+  for (int u = lane; u < r.units; u += r.lanes) {
     const Unit w = unit_of<V>(r, u);
     float c[V], s[V];
-    if (w.pair >= 0) turns_of<V>(r, w, pos, c, s);
-    for (int h = h0; h < r.H; h += r.head_lanes) {
-      float x[V] = {}, y[V] = {};
+    for (int h = h0; h < r.H; h += kAhead * r.head_lanes) {
+      Raw<TI, V> x[kAhead], y[kAhead];
       if (pos >= 0) {
-        load_values<V>(in + h * r.x_head + w.a, x);
-        if (w.b >= 0) load_values<V>(in + h * r.x_head + w.b, y);
-        if (w.pair >= 0) turn_unit<V>(r, x, y, c, s);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          const int g = min(h + k * r.head_lanes, r.H - 1);
+          x[k].load(in + g * r.x_head + w.a);
+          if (w.b >= 0) y[k].load(in + g * r.x_head + w.b);
+        }
       }
-      store_values<V>(out + h * r.out_head + w.a, x);
-      if (w.b >= 0) store_values<V>(out + h * r.out_head + w.b, y);
+      if (h == h0 && w.pair >= 0) turns_of<V>(r, w, pos, c, s);  // while the first loads are on their way
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int g = h + k * r.head_lanes;
+        if (g >= r.H) break;
+        float a[V] = {}, b[V] = {};
+        if (pos >= 0) {
+          x[k].unpack(a);
+          y[k].unpack(b);
+          if (w.pair >= 0) turn_unit<V>(r, a, b, c, s);
+        }
+        store_values<V>(out + g * r.out_head + w.a, a);
+        if (w.b >= 0) store_values<V>(out + g * r.out_head + w.b, b);
+      }
     }
   }
 }
@@ -134,63 +153,92 @@ __device__ __forceinline__ uint32_t top_of(uint32_t top, const float (&x)[V]) {
   return top;
 }
 
-// A head's scale is known once all its units are turned. ONCE: a lane has one unit
-// and keeps it; else the units are turned a second time (rows that fill no vectors).
+// A head's scale is known once all its units are turned. ONCE: a lane has one unit and
+// keeps it, and has kAhead heads' loads on their way; else the units are turned a second
+// time (rows that fill no vectors).
 template <class TI, int V, bool ONCE>
 __global__ __launch_bounds__(kThreads) void k_rotary_fp8(RotaryArgs r) {
-  const int lanes = 1 << r.lanes_log2, lane = threadIdx.x & (lanes - 1);
-  const uint32_t item = blockIdx.x * (kThreads >> r.lanes_log2) + (threadIdx.x >> r.lanes_log2);
+  const int lanes = r.lanes, lane = threadIdx.x & (lanes - 1);  // a power of two
+  const uint32_t item = (blockIdx.x * kThreads + threadIdx.x) / (uint32_t)lanes;
   const uint32_t tok = item / (uint32_t)r.head_lanes;
   if (tok >= (uint32_t)r.T) return;  // whole groups of lanes
   const int h0 = (int)(item - tok * r.head_lanes), pos = r.positions[tok];
   const TI* in = reinterpret_cast<const TI*>(r.x) + (int64_t)tok * r.x_token;
   uint8_t* out = reinterpret_cast<uint8_t*>(r.out) + (int64_t)tok * r.out_token;
   float c[V], s[V];
-  Unit w{0, -1, -1};
-  auto prepare = [&](int u) {
-    w = unit_of<V>(r, u);
-    if (w.pair >= 0) turns_of<V>(r, w, pos, c, s);
-  };
-  auto values = [&](int h, float (&x)[V], float (&y)[V]) {
-    if (pos < 0) return;
-    load_values<V>(in + h * r.x_head + w.a, x);
-    if (w.b >= 0) load_values<V>(in + h * r.x_head + w.b, y);
-    if (w.pair >= 0) turn_unit<V>(r, x, y, c, s);
-  };
-  if (ONCE && lane < r.units) prepare(lane);
-  for (int h = h0; h < r.H; h += r.head_lanes) {
-    float x[V] = {}, y[V] = {};
-    uint32_t top = 0;
-    for (int u = lane; u < r.units; u += lanes) {
-      if (!ONCE) prepare(u);
-      values(h, x, y);
-      top = top_of<V>(top_of<V>(top, x), y);
-    }
+  // the head's scale from its lanes' largest magnitudes; what values are multiplied by
+  auto scale_head = [&](int h, uint32_t top) {
     for (int o = 1; o < lanes; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
     const uint32_t e = fp8_scale_byte(top);
-    // a scale of NaN: codes of 0 (and no conversion of what is not finite)
-    const float by = e == 255u ? 0.0f : __uint_as_float((254u - e) << 23);
-    for (int u = lane; u < r.units; u += lanes) {
-      if (!ONCE) {
-        prepare(u);
-        values(h, x, y);
-      }
-      if (e == 255u) {
-#pragma unroll
-        for (int j = 0; j < V; ++j) x[j] = y[j] = 0.0f;
-      }
-      store_fp8<V>(out + h * r.out_head + w.a, x, by);
-      if (w.b >= 0) store_fp8<V>(out + h * r.out_head + w.b, y, by);
-    }
     if (lane == 0) r.scale[(int64_t)tok * r.H + h] = e == 255u ? __builtin_nanf("") : __uint_as_float(e << 23);
+    return e == 255u ? 0.0f : __uint_as_float((254u - e) << 23);
+  };
+  auto put = [&](const Unit& w, int h, float by, float (&x)[V], float (&y)[V]) {
+    if (by == 0.0f) {  // not finite: codes of 0 (and no conversion of what is not finite)
+#pragma unroll
+      for (int j = 0; j < V; ++j) x[j] = y[j] = 0.0f;
+    }
+    store_fp8<V>(out + h * r.out_head + w.a, x, by);
+    if (w.b >= 0) store_fp8<V>(out + h * r.out_head + w.b, y, by);
+  };
+  if constexpr (ONCE) {
+    const bool mine = lane < r.units;
+    const Unit w = unit_of<V>(r, mine ? lane : 0);
+    for (int h = h0; h < r.H; h += kAhead * r.head_lanes) {
+      Raw<TI, V> p[kAhead], q[kAhead];
+      if (pos >= 0) {
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          const int g = min(h + k * r.head_lanes, r.H - 1);
+          p[k].load(in + g * r.x_head + w.a);
+          if (w.b >= 0) q[k].load(in + g * r.x_head + w.b);
+        }
+      }
+      if (h == h0 && w.pair >= 0) turns_of<V>(r, w, pos, c, s);
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int g = h + k * r.head_lanes;
+        if (g >= r.H) break;  // whole groups of lanes
+        float x[V] = {}, y[V] = {};
+        if (pos >= 0) {
+          p[k].unpack(x);
+          if (w.b >= 0) q[k].unpack(y);
+          if (w.pair >= 0) turn_unit<V>(r, x, y, c, s);
+        }
+        const float by = scale_head(g, mine ? top_of<V>(top_of<V>(0u, x), y) : 0u);
+        if (mine) put(w, g, by, x, y);
+      }
+    }
+  } else {
+    auto values = [&](const Unit& w, int h, float (&x)[V], float (&y)[V]) {
+      if (pos < 0) return;
+      load_values<V>(in + h * r.x_head + w.a, x);
+      if (w.b >= 0) load_values<V>(in + h * r.x_head + w.b, y);
+      if (w.pair < 0) return;
+      turns_of<V>(r, w, pos, c, s);
+      turn_unit<V>(r, x, y, c, s);
+    };
+    for (int h = h0; h < r.H; h += r.head_lanes) {
+      uint32_t top = 0;
+      for (int u = lane; u < r.units; u += lanes) {
+        float x[V] = {}, y[V] = {};
+        values(unit_of<V>(r, u), h, x, y);
+        top = top_of<V>(top_of<V>(top, x), y);
+      }
+      const float by = scale_head(h, top);
+      for (int u = lane; u < r.units; u += lanes) {
+        float x[V] = {}, y[V] = {};
+        const Unit w = unit_of<V>(r, u);
+        values(w, h, x, y);
+        put(w, h, by, x, y);
+      }
+    }
   }
 }
 
 // ---- into the 4-bit cache ----
-// As k_cache4_append, a thread takes 8 consecutive values of a row and the four
-// threads of a block of 32 share its largest magnitude; a key's thread also reads
-// the 8 values that its own are paired with (from the cache: their own thread is in
-// the same wave). WIDE: they are a vector, or lie in the thread's own 8.
+// As in k_cache4_append, four threads share a block of 32 values and its largest
+// magnitude, 8 consecutive values each.
 __device__ __forceinline__ void put_codes(const float (&x)[8], int64_t row, int d, int which, int ch, uint8_t* codes,
                                           uint8_t* scales) {
   uint32_t top = top_of<8>(0u, x);  // NaN and infinity lie above every finite value
@@ -209,16 +257,117 @@ __device__ __forceinline__ void put_codes(const float (&x)[8], int64_t row, int 
   if ((ch & 3) == 0) scales[row * (d / 16) + which * (d / 32) + (ch >> 2)] = (uint8_t)e;
 }
 
-template <class T, bool WIDE>
+// A token's slot, or -1 where nothing is written.
+__device__ __forceinline__ int64_t slot_of(const AppendRotaryArgs& a, const Cache4& c, uint32_t tok) {
+  const int64_t slot = a.slots[tok];
+  return a.positions[tok] < 0 || slot < 0 || slot >= c.num_pages << c.shift ? -1 : slot;
+}
+
+// Parts made of whole blocks of 32 (or of whole vectors, interleaved): a thread takes
+// two vectors of 8 of a head, those that face each other where halves are paired, of the
+// key and of the value, and every head_lanes-th head with the same sines and cosines. So
+// a slot's key and value are written side by side, a line at a time. 16381 tokens of 8
+// heads of 128 in bfloat16: %%KV%%.
+constexpr int kAheadKv = 1;
+template <class T>
+__device__ __forceinline__ void append_pairs(const AppendRotaryArgs& a, const Cache4& c, uint32_t block) {
+  const int units = c.d / 16;  // lanes of a head: 4 or 8
+  const uint32_t item = (block * kThreads + threadIdx.x) / units;
+  const int u = threadIdx.x & (units - 1);
+  const uint32_t tok = item / (uint32_t)a.head_lanes;
+  if (tok >= a.rows) return;  // whole heads
+  const int64_t slot = slot_of(a, c, tok);
+  if (slot < 0) return;
+  const int h0 = (int)(item - tok * a.head_lanes), pos = a.positions[tok];
+  // the thread's vectors, and whether (and as which pairs) they are turned
+  int va, vb, pair[2] = {-1, -1};
+  if (a.interleaved) {
+    va = u, vb = u + units;
+    const int first = a.start / 8, last = first + a.pairs / 4;
+    if (va >= first && va < last) pair[0] = (va - first) * 4;
+    if (vb >= first && vb < last) pair[1] = (vb - first) * 4;
+  } else {
+    const int n = a.pairs / 8, first = a.start / 8;
+    if (u < n) {
+      va = first + u, vb = va + n;
+      pair[0] = u * 8, pair[1] = pair[0] + 4;
+    } else {  // blocks that pass, two at a time
+      const int i = (u - n) / 4 * 8 + (u & 3);
+      va = i < first ? i : i + 2 * n;
+      vb = i + 4 < first ? i + 4 : i + 4 + 2 * n;
+    }
+  }
+  const T* kin = reinterpret_cast<const T*>(a.k) + (int64_t)tok * a.k_stride;
+  const T* vin = reinterpret_cast<const T*>(a.v) + (int64_t)tok * a.v_stride;
+  float cs[8], sn[8];
+  for (int h = h0; h < c.hkv; h += kAheadKv * a.head_lanes) {
+    Raw<T, 8> raw[kAheadKv][4];
+#pragma unroll
+    for (int k = 0; k < kAheadKv; ++k) {
+      const int g = min(h + k * a.head_lanes, c.hkv - 1) * c.d;
+      raw[k][0].load(kin + g + va * 8);
+      raw[k][1].load(kin + g + vb * 8);
+      raw[k][2].load(vin + g + va * 8);
+      raw[k][3].load(vin + g + vb * 8);
+    }
+    if (h == h0) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int p = pair[j / 4];
+        if (p < 0) continue;
+        const Turn t = turn_of((double)pos * turns_per(a.freq[p + j % 4]), a.amplitude);
+        cs[j] = t.c, sn[j] = t.s;
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kAheadKv; ++k) {
+      const int g = h + k * a.head_lanes;
+      if (g >= c.hkv) break;  // whole heads
+      const int64_t row = c.row(slot, g);
+      float x[8], y[8];
+      raw[k][0].unpack(x);
+      raw[k][1].unpack(y);
+      if (!a.interleaved) {
+        if (pair[0] >= 0) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float p = x[j], q = y[j];
+            x[j] = turned(p, cs[j], q, -sn[j]);
+            y[j] = turned(q, cs[j], p, sn[j]);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float p = x[2 * j], q = x[2 * j + 1];
+          if (pair[0] >= 0) x[2 * j] = turned(p, cs[j], q, -sn[j]), x[2 * j + 1] = turned(q, cs[j], p, sn[j]);
+          p = y[2 * j], q = y[2 * j + 1];
+          if (pair[1] >= 0)
+            y[2 * j] = turned(p, cs[4 + j], q, -sn[4 + j]), y[2 * j + 1] = turned(q, cs[4 + j], p, sn[4 + j]);
+        }
+      }
+      put_codes(x, row, c.d, 0, va, a.codes, a.scales);
+      put_codes(y, row, c.d, 0, vb, a.codes, a.scales);
+      raw[k][2].unpack(x);
+      raw[k][3].unpack(y);
+      put_codes(x, row, c.d, 1, va, a.codes, a.scales);
+      put_codes(y, row, c.d, 1, vb, a.codes, a.scales);
+    }
+  }
+}
+
+// Any other part: a thread takes 8 consecutive values of a key and reads each one's
+// partner by itself.
+template <class T>
 __device__ __forceinline__ void append_keys(const AppendRotaryArgs& a, const Cache4& c, uint32_t block) {
   const int per_row = c.d / 8;  // lanes of a head: 8 or 16
   const uint32_t item = (block * kThreads + threadIdx.x) / per_row;
   const int ch = threadIdx.x & (per_row - 1);
   const uint32_t tok = item / (uint32_t)a.head_lanes;
   if (tok >= a.rows) return;  // whole heads
+  const int64_t slot = slot_of(a, c, tok);
+  if (slot < 0) return;
   const int h0 = (int)(item - tok * a.head_lanes), pos = a.positions[tok];
-  const int64_t slot = a.slots[tok];
-  if (pos < 0 || slot < 0 || slot >= c.num_pages << c.shift) return;
   // each value's partner (offset from its own), and its turn
   int partner[8];
   float cs[8], sn[8];
@@ -238,23 +387,14 @@ __device__ __forceinline__ void append_keys(const AppendRotaryArgs& a, const Cac
   const T* in = reinterpret_cast<const T*>(a.k) + (int64_t)tok * a.k_stride + ch * 8;
   for (int h = h0; h < c.hkv; h += a.head_lanes) {
     const T* p = in + (int64_t)h * c.d;
-    float x[8], y[8], z[8];
+    float x[8], y[8];
     load_values<8>(p, x);
-    if (WIDE && !a.interleaved) {
-      load_values<8>(p + partner[0], z);
-    } else if (WIDE) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) z[j] = x[j ^ 1];
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        float v[1];
-        load_values<1>(p + j + partner[j], v);
-        z[j] = v[0];
-      }
+    for (int j = 0; j < 8; ++j) {
+      float z[1];
+      load_values<1>(p + j + partner[j], z);
+      y[j] = partner[j] ? turned(x[j], cs[j], z[0], sn[j]) : x[j];
     }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) y[j] = partner[j] ? turned(x[j], cs[j], z[j], sn[j]) : x[j];
     put_codes(y, c.row(slot, h), c.d, 0, ch, a.codes, a.scales);
   }
 }
@@ -265,22 +405,27 @@ __device__ __forceinline__ void append_values(const AppendRotaryArgs& a, const C
   const uint32_t at = block * kThreads + threadIdx.x, tok = at / (uint32_t)per_tok;
   if (tok >= a.rows) return;
   const int in = (int)(at - tok * per_tok), h = in / per_row, ch = in - h * per_row;
-  const int64_t slot = a.slots[tok];
-  if (a.positions[tok] < 0 || slot < 0 || slot >= c.num_pages << c.shift) return;
+  const int64_t slot = slot_of(a, c, tok);
+  if (slot < 0) return;
   float x[8];
   load_values<8>(reinterpret_cast<const T*>(a.v) + (int64_t)tok * a.v_stride + in * 8, x);
   put_codes(x, c.row(slot, h), c.d, 1, ch, a.codes, a.scales);
 }
 
-// One launch: blocks of queries, of keys and of values, side by side.
+// One launch: blocks of keys and values and of queries, side by side (two kernels one after
+// the other take 83 us where this takes %%ALL%%: 32 query heads beside the above).
 template <class T, bool WIDE>
 __global__ __launch_bounds__(kThreads) void k_append_rotary(AppendRotaryArgs a, Cache4 c) {
   const int64_t b = blockIdx.x;
-  if (b < a.k_blocks) append_keys<T, WIDE>(a, c, (uint32_t)b);
-  else if (b < a.k_blocks + a.v_blocks) append_values<T>(a, c, (uint32_t)(b - a.k_blocks));
-  else rotate_rows<T, uint16_t, WIDE ? 8 : 1>(a.q, (uint32_t)(b - a.k_blocks - a.v_blocks));
+  if (b < a.k_blocks) {
+    if constexpr (WIDE) append_pairs<T>(a, c, (uint32_t)b);
+    else append_keys<T>(a, c, (uint32_t)b);
+  } else if (!WIDE && b < a.k_blocks + a.v_blocks) {
+    append_values<T>(a, c, (uint32_t)(b - a.k_blocks));
+  } else {
+    rotate_rows<T, uint16_t, WIDE ? 8 : 1>(a.q, (uint32_t)(b - a.k_blocks - a.v_blocks));
+  }
 }
-
 bool is_aligned(const void* p, int64_t n) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(n - 1)) == 0; }
 
 // Whether vectors of n values fit a side's address and strides.
@@ -288,18 +433,25 @@ bool side_fits(const void* p, int64_t token, int64_t head, int T, int H, int n, 
   return is_aligned(p, std::min(n * size, 16)) && (H <= 1 || head % n == 0) && (T <= 1 || token % n == 0);
 }
 
-void lanes_of(RotaryArgs& a) {
+// Lanes of a head: one a unit, 64 at most; where they exchange values a power of two.
+void lanes_of(RotaryArgs& a, bool power) {
   const int V = a.vec;
   const int beside = a.d / V - 2 * (a.pairs / V);  // vectors that pass
   a.units = a.pairs / V + (beside + 1) / 2;
-  a.lanes_log2 = 0;
-  while (a.lanes_log2 < 6 && (1 << a.lanes_log2) < a.units) ++a.lanes_log2;
+  a.lanes = std::min(std::max(a.units, 1), 64);
+  if (power)
+    while (a.lanes & (a.lanes - 1)) ++a.lanes;
 }
 
-int64_t rotary_blocks(RotaryArgs& a) {
-  a.head_lanes = std::max(a.H, 1);
-  const int64_t items = (int64_t)a.T * a.head_lanes, per = kThreads >> a.lanes_log2;
-  return (items + per - 1) / per;
+// Groups of lanes of a token: as few as fill the GPU, so that each has several heads.
+int lanes_for(int64_t threads, int heads, int64_t fill) {  // threads with one group a token
+  return (int)std::min<int64_t>(std::max(heads, 1), (fill + std::max<int64_t>(threads, 1) - 1) / std::max<int64_t>(threads, 1));
+}
+
+int64_t rotary_blocks(RotaryArgs& a, int64_t fill = kFill) {
+  const int64_t threads = (int64_t)a.T * a.lanes;
+  a.head_lanes = lanes_for(threads, a.H, fill);
+  return (threads * a.head_lanes + kThreads - 1) / kThreads;
 }
 
 template <class TI, class TO>
@@ -313,7 +465,7 @@ void run_rotary(const RotaryArgs& a, dim3 grid, hipStream_t st) {
 }
 template <class TI, int V>
 void run_fp8(const RotaryArgs& a, dim3 grid, hipStream_t st) {
-  if (a.units <= 1 << a.lanes_log2) k_rotary_fp8<TI, V, true><<<grid, kThreads, 0, st>>>(a);
+  if (a.units <= a.lanes) k_rotary_fp8<TI, V, true><<<grid, kThreads, 0, st>>>(a);
   else k_rotary_fp8<TI, V, false><<<grid, kThreads, 0, st>>>(a);
 }
 template <class TI>
@@ -337,8 +489,8 @@ int64_t rotary_shape(RotaryArgs& a, bool fp8) {
         side_fits(a.x, a.x_token, a.x_head, a.T, a.H, a.vec, si) &&
         side_fits(a.out, a.out_token, a.out_head, a.T, a.H, a.vec, so))
       break;
-  lanes_of(a);
-  return rotary_blocks(a);
+  lanes_of(a, fp8);
+  return rotary_blocks(a, fp8 ? kFillFp8 : kFill);
 }
 
 hipError_t launch_rotary(const RotaryArgs& r, hipStream_t st) {
@@ -358,16 +510,17 @@ hipError_t launch_rotary(const RotaryArgs& r, hipStream_t st) {
 }
 
 int64_t append_rotary_shape(AppendRotaryArgs& a, const Cache4& c) {
-  a.head_lanes = c.hkv;
-  a.k_blocks = a.v_blocks = (a.rows * c.hkv * (c.d / 8) + kThreads - 1) / kThreads;
-  // vectors of 8 that hold whole pairs, or face each other
-  a.wide = a.start % 8 == 0 && a.pairs % 8 == 0;
+  a.wide = a.interleaved ? a.start % 8 == 0 && a.pairs % 4 == 0 : a.start % 32 == 0 && a.pairs % 32 == 0;
+  if (a.q.T > 0)
+    a.wide = a.wide && a.pairs % 8 == 0 && side_fits(a.q.x, a.q.x_token, a.q.x_head, a.q.T, a.q.H, 8, a.in_f32 ? 4 : 2);
+  const int lanes = c.d / (a.wide ? 16 : 8);
+  a.head_lanes = lanes_for(a.rows * lanes, c.hkv, kFillKv);
+  a.k_blocks = (a.rows * a.head_lanes * lanes + kThreads - 1) / kThreads;
+  a.v_blocks = a.wide ? 0 : (a.rows * c.hkv * lanes + kThreads - 1) / kThreads;
   a.q_blocks = 0;
   if (a.q.T > 0) {
-    a.wide = a.wide && side_fits(a.q.x, a.q.x_token, a.q.x_head, a.q.T, a.q.H, 8, a.in_f32 ? 4 : 2) &&
-             side_fits(a.q.out, a.q.out_token, a.q.out_head, a.q.T, a.q.H, 8, 2);
     a.q.vec = a.wide ? 8 : 1;
-    lanes_of(a.q);
+    lanes_of(a.q, false);
     a.q_blocks = rotary_blocks(a.q);
   }
   return a.q_blocks + a.k_blocks + a.v_blocks;
@@ -375,7 +528,8 @@ int64_t append_rotary_shape(AppendRotaryArgs& a, const Cache4& c) {
 
 hipError_t launch_cache4_append_rotary(const AppendRotaryArgs& r, const Cache4& c, hipStream_t st) {
   AppendRotaryArgs a = r;
-  const dim3 grid((unsigned)append_rotary_shape(a, c));
+  const int64_t blocks = append_rotary_shape(a, c);
+  const dim3 grid((unsigned)blocks);
   if (a.in_f32 && a.wide) k_append_rotary<float, true><<<grid, kThreads, 0, st>>>(a, c);
   else if (a.in_f32) k_append_rotary<float, false><<<grid, kThreads, 0, st>>>(a, c);
   else if (a.wide) k_append_rotary<uint16_t, true><<<grid, kThreads, 0, st>>>(a, c);

@@ -65,39 +65,43 @@ __device__ __forceinline__ float bf16_float(uint32_t h) { return __uint_as_float
 // Nearest bfloat16, ties to even.
 __device__ __forceinline__ uint16_t float_bf16(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
 
-// N values at N * sizeof(T) alignment (16 bytes at most), as float32.
-template <int N>
-__device__ __forceinline__ void load_values(const float* p, float (&x)[N]) {
-  if constexpr (N >= 4) {
+// N values as they lie in memory, loaded at N * sizeof(T) alignment (16 bytes at most),
+// and as float32.
+template <class T, int N>
+struct Raw {
+  static constexpr int kBytes = N * (int)sizeof(T);
+  uint32_t w[(kBytes + 3) / 4];
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (kBytes >= 16) {
 #pragma unroll
-    for (int i = 0; i < N; i += 4) {
-      const float4 a = *reinterpret_cast<const float4*>(p + i);
-      x[i] = a.x, x[i + 1] = a.y, x[i + 2] = a.z, x[i + 3] = a.w;
+      for (int i = 0; i < kBytes / 16; ++i) {
+        const uint4 a = reinterpret_cast<const uint4*>(p)[i];
+        w[4 * i] = a.x, w[4 * i + 1] = a.y, w[4 * i + 2] = a.z, w[4 * i + 3] = a.w;
+      }
+    } else if constexpr (kBytes == 8) {
+      const uint2 a = *reinterpret_cast<const uint2*>(p);
+      w[0] = a.x, w[1] = a.y;
+    } else if constexpr (kBytes == 4) {
+      w[0] = *reinterpret_cast<const uint32_t*>(p);
+    } else {
+      w[0] = *reinterpret_cast<const uint16_t*>(p);
     }
-  } else if constexpr (N == 2) {
-    const float2 a = *reinterpret_cast<const float2*>(p);
-    x[0] = a.x, x[1] = a.y;
-  } else {
-    x[0] = *p;
   }
-}
-template <int N>
-__device__ __forceinline__ void load_values(const uint16_t* p, float (&x)[N]) {
-  if constexpr (N == 8) {
-    const uint4 a = *reinterpret_cast<const uint4*>(p);
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+  __device__ __forceinline__ void unpack(float (&x)[N]) const {
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[2 * i] = bf16_float(w[i]), x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-  } else if constexpr (N == 4) {
-    const uint2 a = *reinterpret_cast<const uint2*>(p);
-    x[0] = bf16_float(a.x), x[1] = __uint_as_float(a.x & 0xFFFF0000u);
-    x[2] = bf16_float(a.y), x[3] = __uint_as_float(a.y & 0xFFFF0000u);
-  } else if constexpr (N == 2) {
-    const uint32_t a = *reinterpret_cast<const uint32_t*>(p);
-    x[0] = bf16_float(a), x[1] = __uint_as_float(a & 0xFFFF0000u);
-  } else {
-    x[0] = bf16_float(*p);
+      for (int i = 0; i < N; ++i) x[i] = __uint_as_float(w[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] = i & 1 ? __uint_as_float(w[i / 2] & 0xFFFF0000u) : bf16_float(w[i / 2]);
+    }
   }
+};
+template <int N, class T>
+__device__ __forceinline__ void load_values(const T* p, float (&x)[N]) {
+  Raw<T, N> r;
+  r.load(p);
+  r.unpack(x);
 }
 template <int N>
 __device__ __forceinline__ void store_values(float* p, const float (&x)[N]) {
