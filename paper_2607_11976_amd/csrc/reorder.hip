@@ -46,10 +46,9 @@ __device__ __forceinline__ uint64_t or_lanes(uint64_t v) {
   return v;
 }
 
-__global__ __launch_bounds__(kThreads) void k_reorder_find(ReorderArgs a, RowInfo* info, int lanes_log2) {
+// Row r's, by a whole wave.
+__device__ __forceinline__ RowInfo find_row(const ReorderArgs& a, int r, int lanes_log2) {
   const int lane = threadIdx.x & 63;
-  const int r = blockIdx.x * kWaves + (threadIdx.x >> 6);
-  if (r >= a.R) return;
   const int g = r / a.group * a.group, w = r - g;
   int par = -1;
   if (lane < a.group) {
@@ -96,12 +95,21 @@ __global__ __launch_bounds__(kThreads) void k_reorder_find(ReorderArgs a, RowInf
     from = min(from, held);
     for (int c = from; c < held; c += 64) give += __popcll(__ballot(c + lane < held && row[min(c + lane, held - 1)] >= 0));
   }
-  if (lane == 0) info[r] = RowInfo{parent, take, from, give};
+  return RowInfo{parent, take, from, give};
+}
+
+__global__ __launch_bounds__(kThreads) void k_reorder_find(ReorderArgs a, RowInfo* info, int lanes_log2) {
+  const int r = blockIdx.x * kWaves + (threadIdx.x >> 6);
+  if (r >= a.R) return;
+  const RowInfo me = find_row(a, r, lanes_log2);
+  if ((threadIdx.x & 63) == 0) info[r] = me;
 }
 
 // In-place exclusive prefix sums of two arrays of n entries, the totals at [n].
+template <int THREADS>
 __device__ __forceinline__ void sums_of(uint32_t* x, uint32_t* y, int n, uint32_t* part) {
-  const int t = threadIdx.x, per = (n + kThreads - 1) / kThreads, lane = t & 63, w = t >> 6;
+  constexpr int kParts = THREADS / 64;
+  const int t = threadIdx.x, per = (n + THREADS - 1) / THREADS, lane = t & 63, w = t >> 6;
   const int b = min(t * per, n), e = min(b + per, n);
   uint32_t sx = 0, sy = 0;
   for (int i = b; i < e; ++i) sx += x[i], sy += y[i];
@@ -111,16 +119,16 @@ __device__ __forceinline__ void sums_of(uint32_t* x, uint32_t* y, int n, uint32_
     const uint32_t ux = __shfl_up(ix, o), uy = __shfl_up(iy, o);
     if (lane >= o) ix += ux, iy += uy;
   }
-  if (lane == 63) part[w] = ix, part[kWaves + w] = iy;
+  if (lane == 63) part[w] = ix, part[kParts + w] = iy;
   __syncthreads();
   uint32_t bx = ix - sx, by = iy - sy;
-  for (int i = 0; i < w; ++i) bx += part[i], by += part[kWaves + i];
+  for (int i = 0; i < w; ++i) bx += part[i], by += part[kParts + i];
   for (int i = b; i < e; ++i) {
     const uint32_t vx = x[i], vy = y[i];
     x[i] = bx, y[i] = by;
     bx += vx, by += vy;
   }
-  if (t == kThreads - 1) x[n] = bx, y[n] = by;
+  if (t == THREADS - 1) x[n] = bx, y[n] = by;
   __syncthreads();
 }
 
@@ -139,78 +147,114 @@ __device__ __forceinline__ int nth_page(const int32_t* row, int c, int held, int
   return -1;
 }
 
+// What the sums over the rows say of the list.
+struct Marks {
+  int used, mark;   // the list's mark before, and with the pages given back
+  uint32_t room;    // pages behind it
+};
+__device__ __forceinline__ Marks marks_of(const ReorderArgs& a, int used, const uint32_t* taken, const uint32_t* given) {
+  const uint32_t back = given[a.R];
+  const int mark = back < (uint32_t)used ? used - (int)back : 0;  // pages past the list's start are not kept
+  const Marks m{used, mark, (uint32_t)(a.free_count - mark)};
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.free_out = mark + (int)min(taken[a.R], m.room);
+  return m;
+}
+
+// Row r's results and the pages that it gives back, by a whole wave; the sums over the
+// rows before each row (R + 1 entries) and all rows' infos.
+__device__ __forceinline__ void write_row(const ReorderArgs& a, int r, const RowInfo* info, const uint32_t* taken,
+                                          const uint32_t* given, const Marks& m) {
+  const int lane = threadIdx.x & 63;
+  const RowInfo me = info[r];
+  if (me.give > 0) {
+    const int32_t* row = a.table + (int64_t)r * a.table_ld;
+    const int held = pages_held(a, a.lens[r]);
+    int64_t at = (int64_t)m.used - 1 - given[r];
+    for (int c = me.from; c < held; c += 64) {
+      const int page = c + lane < held ? row[c + lane] : -1;
+      const uint64_t in = __ballot(page >= 0);
+      const int64_t place = at - __popcll(in & ((1ull << lane) - 1));
+      if (page >= 0 && place >= 0) a.free_list[place] = page;
+      at -= __popcll(in);
+    }
+  }
+  // the page of a copy: the list from its mark on, where the pages given back come first
+  int source = -1, target = -1, status = me.parent < 0 ? 1 : 0;
+  const int len = me.parent < 0 ? 0 : a.lens[me.parent];
+  const int32_t* from = a.table + (int64_t)max(me.parent, 0) * a.table_ld;
+  const int cut = len > 0 ? len >> a.shift : 0;  // column of the partial page
+  if (me.take) {
+    const uint32_t n = taken[r];
+    if (n >= m.room) {
+      status = 2;
+    } else {
+      const int at = m.mark + (int)n;
+      source = from[cut];
+      if (at >= m.used) {
+        target = a.free_list[at];
+      } else {
+        const uint32_t j = (uint32_t)(m.used - 1 - at);  // of the pages given back
+        int lo = 0, hi = a.R;                            // given[lo] <= j < given[hi]
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (given[mid] <= j) lo = mid;
+          else hi = mid;
+        }
+        const int32_t* row = a.table + (int64_t)lo * a.table_ld;
+        const int c = nth_page(row, info[lo].from, pages_held(a, a.lens[lo]), (int)(j - given[lo]));
+        if (c >= 0) target = row[c];
+      }
+    }
+  }
+  const int held = status ? 0 : pages_held(a, len);
+  int32_t* out = a.out_table + (int64_t)r * a.out_ld;
+  for (int c = lane; c < a.width; c += 64) {
+    int page = c < held ? from[c] : -1;
+    if (me.take && c == cut && c < held) page = target;
+    out[c] = page;
+  }
+  if (lane == 0) {
+    a.out_lens[r] = status ? 0 : len;
+    a.status[r] = status;
+    a.copies[2 * (int64_t)r] = source;
+    a.copies[2 * (int64_t)r + 1] = target;
+  }
+}
+
 __global__ __launch_bounds__(kThreads) void k_reorder_write(ReorderArgs a, const RowInfo* info) {
   extern __shared__ uint32_t lds[];
   __shared__ uint32_t part[2 * kWaves];
   uint32_t* taken = lds;                // [R + 1] prefix sums of the copies
   uint32_t* given = lds + a.R + 1;      // [R + 1] and of the pages given back
-  const int t = threadIdx.x, lane = t & 63;
+  const int t = threadIdx.x;
   for (int r = t; r < a.R; r += kThreads) taken[r] = (uint32_t)info[r].take, given[r] = (uint32_t)info[r].give;
   const int used = min(max(*a.free_used, 0), a.free_count);
   __syncthreads();
-  sums_of(taken, given, a.R, part);
-  const uint32_t back = given[a.R];
-  const int mark = back < (uint32_t)used ? used - (int)back : 0;  // pages past the list's start are not kept
-  const uint32_t room = (uint32_t)(a.free_count - mark);
-  if (blockIdx.x == 0 && t == 0) *a.free_out = mark + (int)min(taken[a.R], room);
+  sums_of<kThreads>(taken, given, a.R, part);
+  const Marks m = marks_of(a, used, taken, given);
   const int waves = gridDim.x * kWaves;
-  for (int r = blockIdx.x * kWaves + (t >> 6); r < a.R; r += waves) {
-    const RowInfo me = info[r];
-    // pages of a row that ends
-    if (me.give > 0) {
-      const int32_t* row = a.table + (int64_t)r * a.table_ld;
-      const int held = pages_held(a, a.lens[r]);
-      int64_t at = (int64_t)used - 1 - given[r];
-      for (int c = me.from; c < held; c += 64) {
-        const int page = c + lane < held ? row[c + lane] : -1;
-        const uint64_t in = __ballot(page >= 0);
-        const int64_t place = at - __popcll(in & ((1ull << lane) - 1));
-        if (page >= 0 && place >= 0) a.free_list[place] = page;
-        at -= __popcll(in);
-      }
-    }
-    // the page of a copy: the list from its mark on, where the pages given back come first
-    int source = -1, target = -1, status = me.parent < 0 ? 1 : 0;
-    const int len = me.parent < 0 ? 0 : a.lens[me.parent];
-    const int32_t* from = a.table + (int64_t)max(me.parent, 0) * a.table_ld;
-    const int cut = len > 0 ? len >> a.shift : 0;  // column of the partial page
-    if (me.take) {
-      const uint32_t n = taken[r];
-      if (n >= room) {
-        status = 2;
-      } else {
-        const int at = mark + (int)n;
-        source = from[cut];
-        if (at >= used) {
-          target = a.free_list[at];
-        } else {
-          const uint32_t j = (uint32_t)(used - 1 - at);  // of the pages given back
-          int lo = 0, hi = a.R;                          // given[lo] <= j < given[hi]
-          while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (given[mid] <= j) lo = mid;
-            else hi = mid;
-          }
-          const int32_t* row = a.table + (int64_t)lo * a.table_ld;
-          const int c = nth_page(row, info[lo].from, pages_held(a, a.lens[lo]), (int)(j - given[lo]));
-          if (c >= 0) target = row[c];
-        }
-      }
-    }
-    const int held = status ? 0 : pages_held(a, len);
-    int32_t* out = a.out_table + (int64_t)r * a.out_ld;
-    for (int c = lane; c < a.width; c += 64) {
-      int page = c < held ? from[c] : -1;
-      if (me.take && c == cut && c < held) page = target;
-      out[c] = page;
-    }
-    if (lane == 0) {
-      a.out_lens[r] = status ? 0 : len;
-      a.status[r] = status;
-      a.copies[2 * (int64_t)r] = source;
-      a.copies[2 * (int64_t)r + 1] = target;
+  for (int r = blockIdx.x * kWaves + (t >> 6); r < a.R; r += waves) write_row(a, r, info, taken, given, m);
+}
+
+// Few rows: all in one block, one launch (a request of 4 beams and 4001 tokens: %%STEP%%).
+constexpr int kFewRows = 32, kFewThreads = 1024;
+__global__ __launch_bounds__(kFewThreads) void k_reorder_few(ReorderArgs a, int lanes_log2) {
+  __shared__ uint32_t part[2 * kFewThreads / 64], taken[kFewRows + 1], given[kFewRows + 1];
+  __shared__ RowInfo info[kFewRows];
+  const int wave = threadIdx.x >> 6, waves = kFewThreads / 64;
+  const int used = min(max(*a.free_used, 0), a.free_count);
+  for (int r = wave; r < a.R; r += waves) {
+    const RowInfo me = find_row(a, r, lanes_log2);
+    if ((threadIdx.x & 63) == 0) {
+      info[r] = me;
+      taken[r] = (uint32_t)me.take;
+      given[r] = (uint32_t)me.give;
     }
   }
+  __syncthreads();
+  sums_of<kFewThreads>(taken, given, a.R, part);
+  const Marks m = marks_of(a, used, taken, given);
+  for (int r = wave; r < a.R; r += waves) write_row(a, r, info, taken, given, m);
 }
 
 // ---- copies of whole pages ----
@@ -251,11 +295,13 @@ hipError_t launch_paged_reorder(const ReorderArgs& a, void* workspace, hipStream
   RowInfo* info = static_cast<RowInfo*>(workspace);
   int lanes_log2 = 6;
   while (a.group << lanes_log2 > 64) --lanes_log2;
-  if (a.R > 0) {
-    k_reorder_find<<<dim3((unsigned)((a.R + kWaves - 1) / kWaves)), kThreads, 0, st>>>(a, info, lanes_log2);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+  if (a.R <= kFewRows) {
+    k_reorder_few<<<1, kFewThreads, 0, st>>>(a, lanes_log2);
+    return hipGetLastError();
   }
+  k_reorder_find<<<dim3((unsigned)((a.R + kWaves - 1) / kWaves)), kThreads, 0, st>>>(a, info, lanes_log2);
+  const hipError_t found = hipGetLastError();
+  if (found != hipSuccess) return found;
   const size_t lds = 8 * ((size_t)a.R + 1);
   if (lds > 64 * 1024) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_reorder_write),
@@ -263,7 +309,7 @@ hipError_t launch_paged_reorder(const ReorderArgs& a, void* workspace, hipStream
     if (e != hipSuccess) return e;
   }
   // every block sums all rows: no more blocks than fill the GPU
-  const int blocks = std::min(std::max((a.R + kWaves - 1) / kWaves, 1), 512);
+  const int blocks = std::min((a.R + kWaves - 1) / kWaves, 512);
   k_reorder_write<<<dim3((unsigned)blocks), kThreads, lds, st>>>(a, info);
   return hipGetLastError();
 }

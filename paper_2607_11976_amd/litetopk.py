@@ -965,30 +965,36 @@ def rotary_frequencies(dim: int, base: float = 10000.0, method: str = "none", fa
     return Rotary(t, start, interleaved, amp if amplitude is None else amplitude)
 
 
-def _here(dev, *ts):
-    """All tensors on one GPU, the current one (which launches go to)."""
-    if dev.type != "cuda":
-        raise LiteTopKError("tensors must be on the GPU")
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _here(*ts):
+    """All tensors on one GPU, the current one (which launches go to). Its index is read
+    off the tensors without making a device object of any."""
+    i = ts[0].get_device()
     for t in ts:
-        if t is not None and t.device != dev:
+        if t is not None and t.get_device() != i:
             raise LiteTopKError("tensors must be on one GPU")
-    if dev.index != torch.cuda.current_device():
-        raise LiteTopKError("tensors are on %s, which is not the current device" % dev)
+    if i < 0:
+        raise LiteTopKError("tensors must be on the GPU")
+    if i != _current_device():
+        raise LiteTopKError("tensors are on GPU %d, which is not the current device" % i)
 
 
 def _heads(t: torch.Tensor, name: str):
-    """[tokens, heads, head_dim] in float32 or bfloat16, rows contiguous."""
-    if not (t.dim() == 3 and t.dtype in (torch.float32, torch.bfloat16)
-            and (t.numel() == 0 or t.shape[2] == 1 or t.stride(2) == 1)):
+    """Shape of [tokens, heads, head_dim] in float32 or bfloat16, rows contiguous."""
+    s = t.shape
+    if not (len(s) == 3 and (t.dtype is torch.bfloat16 or t.dtype is torch.float32)
+            and (t.is_contiguous() or s[2] == 1 or t.stride(2) == 1 or t.numel() == 0)):
         raise LiteTopKError("%s must be float32 or bfloat16 [tokens, heads, head_dim] with contiguous heads" % name)
-    return t.shape
+    return s
 
 
 def _turn(rot: Rotary, d: int):
     f = rot.inv_freq
     if not (f.dtype is torch.float32 and f.dim() == 1 and f.is_contiguous()):
         raise LiteTopKError("inv_freq must be a contiguous float32 vector on the GPU")
-    n = f.numel()
+    n = f.shape[0]
     if rot.start < 0 or rot.start + 2 * n > d:
         raise LiteTopKError("the rotated part [%d, %d) is not inside a head of %d" % (rot.start, rot.start + 2 * n, d))
     return n
@@ -997,21 +1003,33 @@ def _turn(rot: Rotary, d: int):
 def _rotate(x, positions, rot, out, out_dtype, flags, stream):
     t, h, d = _heads(x, "x")
     n = _turn(rot, d)
-    _here(x.device, positions, rot.inv_freq, out)
+    f = rot.inv_freq
     _int32(positions, t, "positions")
-    if out is None:
-        out = _empty((t, h, d), out_dtype or x.dtype, x.device, stream)
-        mine = out
+    _here(x, positions, f, out)
+    fresh = out is None
+    kind = x.dtype
+    if fresh:
+        out_kind = out_dtype or kind
+        out = x.new_empty((t, h, d), dtype=out_kind) if stream is None else _empty((t, h, d), out_kind, x.device, stream)
+        ot, oh = h * d, d
     else:
-        mine = None
-        _heads(out, "out")
-        _need(out.shape == x.shape, "out must have x's shape")
-        _need(out_dtype is None or out_dtype is out.dtype, "out is not of out_dtype")
-    st = lt_rotary(_ptr(x), _dtype_code(x), x.stride(0), x.stride(1), t, h, d, _ptr(positions), _ptr(rot.inv_freq), n,
-                   rot.start, rot.amplitude, flags | (LT_ROTARY_INTERLEAVED if rot.interleaved else 0), _ptr(out),
-                   _dtype_code(out), out.stride(0), out.stride(1), _stream_of(stream, x))
-    _check(st, "lt_rotary")
-    _used_on(stream, mine)
+        out_kind = out.dtype
+        if not (_heads(out, "out") == x.shape and (out_dtype is None or out_dtype is out_kind)):
+            raise LiteTopKError("out must have x's shape, and out_dtype if that is given")
+        ot, oh = out.stride(0), out.stride(1)
+    xt, xh = x.stride(0), x.stride(1)
+    if out_kind is torch.bfloat16:
+        out_code = LT_BF16
+    else:
+        out_code = _dtype_code(out)
+    st = load().lt_rotary(x.data_ptr(), LT_BF16 if kind is torch.bfloat16 else LT_F32, xt, xh, t, h, d,
+                          positions.data_ptr(), f.data_ptr(), n, rot.start, rot.amplitude,
+                          flags | 1 if rot.interleaved else flags, out.data_ptr(), out_code, ot, oh,
+                          _stream_of(stream, x))
+    if st:
+        _check(st, "lt_rotary")
+    if fresh and stream is not None:
+        _used_on(stream, out)
     return out
 
 
@@ -1039,6 +1057,7 @@ def rotary_fp8(x: torch.Tensor, positions: torch.Tensor, rot: Rotary, out=None, 
     t, h, d = _heads(x, "x")
     n = _turn(rot, d)
     _int32(positions, t, "positions")
+    _here(x, positions, rot.inv_freq)
     if out is None:
         codes = _empty((t, h, d), torch.float8_e4m3fn, x.device, stream)
         scales = _empty((t, h), torch.float32, x.device, stream)
@@ -1048,7 +1067,7 @@ def rotary_fp8(x: torch.Tensor, positions: torch.Tensor, rot: Rotary, out=None, 
         _need(codes.dtype in (torch.float8_e4m3fn, torch.uint8) and codes.shape == x.shape
               and scales.dtype == torch.float32 and scales.shape == x.shape[:2],
               "out must be codes float8_e4m3fn [T, heads, head_dim] and scales float32 [T, heads]")
-    _here(x.device, positions, rot.inv_freq, codes, scales)
+        _here(x, codes, scales)
     st = lt_rotary_fp8(_ptr(x), _dtype_code(x), x.stride(0), x.stride(1), t, h, d, _ptr(positions),
                        _ptr(rot.inv_freq), n, rot.start, rot.amplitude,
                        LT_ROTARY_INTERLEAVED if rot.interleaved else 0, _ptr(codes), _ptr(scales),
@@ -1074,7 +1093,7 @@ def cache4_append_rotary(k: torch.Tensor, v: torch.Tensor, codes: torch.Tensor, 
         raise LiteTopKError("slots must be a contiguous int64 [rows]")
     _int32(positions, rows, "positions")
     n = _turn(rot, d)
-    _here(k.device, v, codes, scales, slots, positions, rot.inv_freq, q)
+    _here(k, v, codes, scales, slots, positions, rot.inv_freq, q)
     hq, qs, out = 0, 0, None
     if q is not None:
         if not (q.dtype is k.dtype and q.dim() == 3 and q.shape[0] == rows and q.shape[1] >= 1):
@@ -1082,7 +1101,7 @@ def cache4_append_rotary(k: torch.Tensor, v: torch.Tensor, codes: torch.Tensor, 
         hq = q.shape[1]
         qs = _rows_of(q, hq, d, "q")
         out = _empty((rows, hq, d), torch.bfloat16, k.device, stream)
-    st = lt_cache4_append_rotary(_ptr(k), _ptr(v), _dtype_code(k), ks, vs, rows, _ptr(codes), _ptr(scales), pages, page,
+    st = load().lt_cache4_append_rotary(_ptr(k), _ptr(v), _dtype_code(k), ks, vs, rows, _ptr(codes), _ptr(scales), pages, page,
                                  heads, d, _ptr(slots), _ptr(positions), _ptr(rot.inv_freq), n, rot.start,
                                  rot.amplitude, LT_ROTARY_INTERLEAVED if rot.interleaved else 0,
                                  _ptr(q) if rows else None, qs, hq if rows else 0, _ptr(out), _stream_of(stream, k))
@@ -1109,27 +1128,34 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, top: int, scale: flo
     beams] (float32: the beams' log probabilities so far, -inf for a beam that is not
     alive, as all but one are in the first step). A program that lets beams finish asks
     for more continuations than it has beams."""
-    _need(logits.dim() == 2 and logits.dtype in (torch.float32, torch.bfloat16)
-          and (logits.numel() == 0 or logits.shape[1] == 1 or logits.stride(1) == 1),
-          "logits must be a float32 or bfloat16 [requests * beams, vocab] GPU matrix with unit column stride")
-    _need(scores.dim() == 2 and scores.dtype is torch.float32 and scores.is_contiguous()
-          and scores.numel() == logits.shape[0], "scores must be float32 [requests, beams], contiguous")
+    if not (logits.dim() == 2 and (logits.dtype is torch.bfloat16 or logits.dtype is torch.float32)
+            and (logits.is_contiguous() or logits.shape[1] == 1 or logits.stride(1) == 1 or logits.numel() == 0)):
+        raise LiteTopKError("logits must be a float32 or bfloat16 [requests * beams, vocab] GPU matrix with unit "
+                            "column stride")
+    if not (scores.dim() == 2 and scores.dtype is torch.float32 and scores.is_contiguous()
+            and scores.numel() == logits.shape[0]):
+        raise LiteTopKError("scores must be float32 [requests, beams], contiguous")
+    _here(logits, scores, workspace)
     dev = logits.device
-    _here(dev, scores, workspace)
     reqs, beams = scores.shape
     rows, vocab = logits.shape
-    dt = _dtype_code(logits)
-    need = lt_beam_select_workspace_size(dt, reqs, beams, vocab, top)
-    _need(need > 0, "unsupported shape for lt_beam_select (top must be 1..%d, beams 1..%d)"
-          % (LT_BEAM_MAX_TOP, LT_BEAM_MAX_BEAMS))
+    dt = LT_BF16 if logits.dtype is torch.bfloat16 else LT_F32
+    lib = load()
+    need = lib.lt_beam_select_workspace_size(dt, reqs, beams, vocab, top)
+    if need == 0:
+        raise LiteTopKError("unsupported shape for lt_beam_select (top must be 1..%d, beams 1..%d)"
+                            % (LT_BEAM_MAX_TOP, LT_BEAM_MAX_BEAMS))
     workspace = _workspace(workspace, need, dev, stream)
-    ints = _empty((2, reqs, top), torch.int32, dev, stream)
-    r = BeamCandidates(_empty((reqs, top), torch.float32, dev, stream), ints[0], ints[1])
-    ld = logits.stride(0) if rows > 1 and vocab > 0 else vocab
-    st = lt_beam_select(_ptr(logits), dt, ld, reqs, beams, vocab, _ptr(scores), scale, top, _ptr(r.score),
-                        _ptr(r.beam), _ptr(r.token), _ptr(workspace), workspace.numel(), _stream_of(stream, logits))
-    _check(st, "lt_beam_select")
-    _used_on(stream, r.score, ints)
+    # the results in one allocation
+    score, beam, token = _empty((3, reqs, top), torch.int32, dev, stream).unbind(0)
+    r = BeamCandidates(score.view(torch.float32), beam, token)
+    st = lib.lt_beam_select(logits.data_ptr(), dt, logits.stride(0) if rows > 1 and vocab > 0 else vocab, reqs, beams,
+                            vocab, scores.data_ptr(), scale, top, score.data_ptr(), beam.data_ptr(), token.data_ptr(),
+                            workspace.data_ptr(), workspace.numel(), _stream_of(stream, logits))
+    if st:
+        _check(st, "lt_beam_select")
+    if stream is not None:
+        _used_on(stream, *r)
     return r
 
 
@@ -1159,20 +1185,26 @@ def paged_reorder(block_table: torch.Tensor, seq_lens: torch.Tensor, parents: to
     _int32(free_pages, None, "free_pages")
     _int32(free_used, 1, "free_used")
     ld, width = _table(block_table, n)
+    _here(block_table, seq_lens, parents, keep_pages, free_pages, free_used, workspace)
     dev = block_table.device
-    _here(dev, seq_lens, parents, keep_pages, free_pages, free_used, workspace)
-    need = lt_paged_reorder_workspace_size(n)
-    _need(need > 0, "at most %d rows" % LT_PLAN_MAX_REQUESTS)
+    lib = load()
+    need = lib.lt_paged_reorder_workspace_size(n)
+    if need == 0:
+        raise LiteTopKError("at most %d rows" % LT_PLAN_MAX_REQUESTS)
     workspace = _workspace(workspace, need, dev, stream)
+    # the results in one allocation
     table, lens, copies, used, status = _empty(n * (width + 4) + 1, torch.int32, dev, stream).split_with_sizes(
         (n * width, n, 2 * n, 1, n))
     r = PagedReorder(table.view(n, width), lens, copies.view(n, 2), used, status)
-    st = lt_paged_reorder(_ptr(block_table), ld, width, _ptr(seq_lens), _ptr(parents), n, group, page_size,
-                          _ptr(keep_pages), _ptr(free_pages), free_pages.numel(), _ptr(free_used), _ptr(table), width,
-                          _ptr(lens), _ptr(copies), _ptr(used), _ptr(status), _ptr(workspace), workspace.numel(),
-                          _stream_of(stream, block_table))
-    _check(st, "lt_paged_reorder")
-    _used_on(stream, *r)
+    st = lib.lt_paged_reorder(block_table.data_ptr(), ld, width, seq_lens.data_ptr(), parents.data_ptr(), n, group,
+                              page_size, _ptr(keep_pages), free_pages.data_ptr(), free_pages.numel(),
+                              free_used.data_ptr(), table.data_ptr(), width, lens.data_ptr(), copies.data_ptr(),
+                              used.data_ptr(), status.data_ptr(), workspace.data_ptr(), workspace.numel(),
+                              _stream_of(stream, block_table))
+    if st:
+        _check(st, "lt_paged_reorder")
+    if stream is not None:
+        _used_on(stream, *r)
     return r
 
 
@@ -1183,7 +1215,7 @@ def cache4_copy(codes: torch.Tensor, scales: torch.Tensor, copies: torch.Tensor,
     pages, page, heads, d = _cache4(codes, scales)
     if not (copies.dtype is torch.int32 and copies.dim() == 2 and copies.shape[1] == 2 and copies.is_contiguous()):
         raise LiteTopKError("copies must be a contiguous int32 [n, 2] on the GPU")
-    _here(codes.device, scales, copies)
+    _here(codes, scales, copies)
     st = lt_cache4_copy(_ptr(codes), _ptr(scales), pages, page, heads, d, _ptr(copies), copies.shape[0],
                         _stream_of(stream, codes))
     _check(st, "lt_cache4_copy")
