@@ -23,7 +23,7 @@
 namespace lt {
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kThreads = 256, kWaves = kThreads / 64;  // of a part's block, where rows are long
 constexpr int kLoads = 4;              // 16-byte loads of a lane in a tile
 constexpr int kList = 256;             // candidates that a wave keeps, where there are very many
 constexpr float kLowest = -3.402823466e38f;
@@ -140,20 +140,25 @@ struct Sum {
   float pad;
 };
 struct Part {
-  Sum* sums;       // [rows * splits][kWaves]
+  Sum* sums;       // [rows * splits][waves]
   uint64_t* keys;  // [rows * splits][top], best first; 0: no candidate
 };
 
-// Of a block's values (kThreads in LDS; every wave looks at all of them) the n-th
+// Of a block's values (VALUES in LDS; every wave looks at all of them) the n-th
 // largest, cut to its upper 16 bits: at least n of them reach it.
+template <int VALUES>
 __device__ __forceinline__ uint32_t block_floor(const uint32_t* values, int n) {
-  const uint4 p = reinterpret_cast<const uint4*>(values)[threadIdx.x & 63];
+  constexpr int kEach = VALUES / 64;
+  uint32_t p[kEach];
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) p[i] = values[i * 64 + (threadIdx.x & 63)];
   uint32_t t = 0;
-#pragma unroll 4
+#pragma unroll 1
   for (int bit = 31; bit >= 16; --bit) {
     const uint32_t c = t | 1u << bit;
-    const int reach = __popcll(__ballot(p.x >= c)) + __popcll(__ballot(p.y >= c)) + __popcll(__ballot(p.z >= c)) +
-                      __popcll(__ballot(p.w >= c));
+    int reach = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) reach += __popcll(__ballot(p[i] >= c));
     if (reach >= n) t = c;
   }
   return t;
@@ -205,12 +210,22 @@ __device__ __forceinline__ void cut(List& l, int n) {
 
 // The best n of a wave's tiles among the values from `loose` on: register by register,
 // cut where the list runs full.
-template <class T>
+template <class T, int WAVES>
 __device__ __forceinline__ void take_all(List& list, const T* x, int base, int e, int n, uint32_t loose) {
   constexpr int N = Row<T>::N, kTile = 64 * N * kLoads;
   const int lane = threadIdx.x & 63;
-  for (; base < e; base += kWaves * kTile) {
+  for (; base < e; base += WAVES * kTile) {
     uint32_t gate = max(list.strict + 1, loose);
+    uint4 raw[kLoads];
+    fetch_tile<T>(x, base, e, raw);
+    float v[kLoads][N], top = ninf();
+    unpack_tile<T>(raw, base, e, v);
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k)
+#pragma unroll
+      for (int j = 0; j < N; ++j) top = fmaxf(top, v[k][j]);
+    if (!__any(ord_key(top) >= gate)) continue;
+#pragma unroll 1
     for (int q = 0; q < kLoads * N; ++q) {
       const int from = base + (q / N * 64 + lane) * N, i = min(from, e - N) + q % N;
       const float v = i >= from ? Row<T>::one(x + i) : ninf();
@@ -237,40 +252,40 @@ __device__ __forceinline__ void take_all(List& list, const T* x, int base, int e
 // way took 39 us where this takes %%BATCH%%: 512 rows of 131072 in bfloat16.)
 constexpr int kSlots = 8;
 constexpr int kChunks = 256;   // chunks that are read again
-constexpr int kFound = 1024;   // values that are ranked
-template <class T>
-__global__ __launch_bounds__(kThreads) void k_beam_part(BeamArgs a, Part part) {
+template <class T, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void k_beam_part(BeamArgs a, Part part) {
+  constexpr int kThreads = 64 * WAVES, kFound = 256 * WAVES;  // values that are ranked
   constexpr int N = Row<T>::N, kTile = 64 * N * kLoads;
   // the lanes' largest values by chunk, or the lists of the waves
   __shared__ union {
     uint32_t best[kSlots][kThreads];
-    uint64_t lists[kWaves][kList];
+    uint64_t lists[WAVES][kList];
   } lds;
   __shared__ __align__(16) uint32_t tops[kThreads];
   __shared__ uint64_t found[kFound];
   __shared__ uint16_t chunks[kChunks];
-  __shared__ int chunk_count, found_count, counts[kWaves];
+  __shared__ int chunk_count, found_count, counts[WAVES];
   const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63;
   const int parts = a.beams * a.splits, req = blockIdx.x / parts, p = blockIdx.x - req * parts, n = a.top;
   const float* cums = a.cum + (int64_t)req * a.beams;
   const Shares share = shares_of(a, cums);
   const int i = p / share.splits, split = p - i * share.splits;
   if (i >= share.beams) return;
-  const int w = beam_of(share, i), len = part_len(a, share, kWaves * kTile);
+  const int w = beam_of(share, i), len = part_len(a, share, WAVES * kTile);
   if (share.all && !(cums[w] > ninf())) return;
   const T* x = reinterpret_cast<const T*>(a.logits) + ((int64_t)req * a.beams + w) * a.ld;
   const int b = min(split * len, a.vocab), e = min(a.vocab - b, len) + b;
   uint4 raw[kLoads] = {};
   if (b + wave * kTile < e && e >= N) fetch_tile<T>(x, b + wave * kTile, e, raw);
   const Scale c = scale_of(a.scale);
-  const int per_chunk = (len / (kWaves * kTile) + kSlots - 1) / kSlots;  // tiles of a chunk
+  const int per_chunk = (len / (WAVES * kTile) + kSlots - 1) / kSlots;  // tiles of a chunk
   if (t == 0) chunk_count = found_count = 0;
 #pragma unroll
   for (int k = 0; k < kSlots; ++k) lds.best[k][t] = kNinfKey;
   float m = kLowest, chunk = ninf(), most = ninf();
   double s = 0.0;
   int slot = 0, left = per_chunk;
-  for (int base = b + wave * kTile; base < e; base += kWaves * kTile) {
+  for (int base = b + wave * kTile; base < e; base += WAVES * kTile) {
     float v[kLoads][N], top = ninf();
     unpack_tile<T>(raw, base, e, v);
     if (e < N) {  // a row shorter than a load: an element a lane
@@ -282,7 +297,7 @@ __global__ __launch_bounds__(kThreads) void k_beam_part(BeamArgs a, Part part) {
     for (int k = 0; k < kLoads; ++k)
 #pragma unroll
       for (int j = 0; j < N; ++j) top = fmaxf(top, v[k][j]);
-    const int next = base + kWaves * kTile;
+    const int next = base + WAVES * kTile;
     if (next < e) fetch_tile<T>(x, next, e, raw);
     if (top > m) {
       s *= (double)power(m - top, c);
@@ -311,9 +326,9 @@ __global__ __launch_bounds__(kThreads) void k_beam_part(BeamArgs a, Part part) {
   s *= (double)power(m - wm, c);
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) s += __shfl_xor(s, o);
-  if (lane == 0) part.sums[(int64_t)blockIdx.x * kWaves + wave] = Sum{s, wm, 0.0f};
+  if (lane == 0) part.sums[(int64_t)blockIdx.x * WAVES + wave] = Sum{s, wm, 0.0f};
   __syncthreads();
-  const uint32_t floor = max(block_floor(tops, n), kNinfKey + 1);
+  const uint32_t floor = max(block_floor<kThreads>(tops, n), kNinfKey + 1);
 #pragma unroll
   for (int k = 0; k < kSlots; ++k)
     if (lds.best[k][t] >= floor) {
@@ -329,7 +344,7 @@ __global__ __launch_bounds__(kThreads) void k_beam_part(BeamArgs a, Part part) {
     for (int q = t; q < items; q += kThreads) {
       const int ch = q / per, load = q - ch * per, who = chunks[ch] % kThreads;
       const int tile = chunks[ch] / kThreads * per_chunk + load / kLoads, k = load % kLoads;
-      const int base = b + (tile * kWaves + (who >> 6)) * kTile, from = base + (k * 64 + (who & 63)) * N;
+      const int base = b + (tile * WAVES + (who >> 6)) * kTile, from = base + (k * 64 + (who & 63)) * N;
       if (e < N) {
         const int at = who & 63;
         if (k == 0 && at < e && Row<T>::one(x + at) >= g)
@@ -368,15 +383,15 @@ __global__ __launch_bounds__(kThreads) void k_beam_part(BeamArgs a, Part part) {
   }
   __syncthreads();
   List list{lds.lists[wave], 0, kNinfKey};
-  take_all<T>(list, x, b + wave * kTile, e, n, floor);
+  take_all<T, WAVES>(list, x, b + wave * kTile, e, n, floor);
   if (lane == 0) counts[wave] = list.count;
   __syncthreads();
-  const int total = counts[0] + counts[1] + counts[2] + counts[3];
-  int at = t, from = 0;
-  while (from < kWaves - 1 && at >= counts[from]) at -= counts[from++];
+  int total = 0, at = t, from = 0;
+  for (int q = 0; q < WAVES; ++q) total += counts[q];
+  while (from < WAVES - 1 && at >= counts[from]) at -= counts[from++];
   const uint64_t mine = t < total ? lds.lists[from][at] : 0;
   int before = 0;
-  for (from = 0; from < kWaves; ++from)
+  for (from = 0; from < WAVES; ++from)
     for (at = 0; at < counts[from]; ++at) before += lds.lists[from][at] > mine;
   if (mine && before < n) out[before] = mine;
   if (t >= total && t < n) out[t] = 0;
@@ -393,45 +408,50 @@ __device__ __forceinline__ bool comes_before(const Candidate& a, const Candidate
 
 constexpr int kMost = 512;     // candidates that are ranked together
 constexpr int kHeld = 8;       // keys that a thread holds in registers
+constexpr int kManyKeys = 2048, kManyThreads = 1024;  // a request of more keys takes a larger block
 
-__global__ __launch_bounds__(kThreads) void k_beam_join(BeamArgs a, Part part, int lanes_log2) {
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void k_beam_join(BeamArgs a, Part part, int lanes_log2) {
+  constexpr int kJoinWaves = THREADS / 64;
   extern __shared__ double lse[];             // [beams]: of the rows that were read,
   float* cum = reinterpret_cast<float*>(lse + a.beams);  // their beams' scores
   int* beam = reinterpret_cast<int*>(cum + a.beams);     // and the beams
   __shared__ Candidate found[kMost];
-  __shared__ __align__(16) uint32_t tops[kThreads];
+  __shared__ __align__(16) uint32_t tops[THREADS];
   __shared__ int count;
-  __shared__ Candidate pick[kWaves];
+  __shared__ Candidate pick[kJoinWaves];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, n = a.top, req = blockIdx.x;
   const Scale c = scale_of(a.scale);
   const float* cums = a.cum + (int64_t)req * a.beams;
   const Shares share = shares_of(a, cums);
   const int per = share.splits * n, total = share.beams * per;  // keys of a row, of the request
   const uint64_t* keys = part.keys + (int64_t)req * a.beams * a.splits * n;
-  // thread t has the keys t, t + 256, ...: beam and place of the first, and how they move on
-  const int beam0 = t / per, place0 = t - beam0 * per, beam_step = kThreads / per, place_step = kThreads % per;
-  const bool held = total <= kHeld * kThreads;
+  // A thread's r-th key. The keys of a part are sorted: a thread that took every
+  // THREADS-th one would have the same place in all parts, and few threads all that count.
+  auto place_of_key = [&](int r) { return r * THREADS + ((t + 29 * r) & (THREADS - 1)); };
+  const int rounds = (total + THREADS - 1) / THREADS;
+  const bool held = rounds <= kHeld;
   uint64_t mine[kHeld];
   if (held) {
 #pragma unroll
-    for (int r = 0; r < kHeld; ++r) mine[r] = t + r * kThreads < total ? keys[t + r * kThreads] : 0;
+    for (int r = 0; r < kHeld; ++r) mine[r] = place_of_key(r) < total ? keys[place_of_key(r)] : 0;
   }
   if (t == 0) count = 0;
   if (share.all) {
-    for (int i = t; i < a.beams; i += kThreads) beam[i] = i;
+    for (int i = t; i < a.beams; i += THREADS) beam[i] = i;
   } else if (wave == 0 && ((share.alive >> lane) & 1)) {
     beam[__popcll(share.alive & ((1ull << lane) - 1))] = lane;
   }
   __syncthreads();
   // log sums: 1 << lanes_log2 lanes a beam
   const int S = 1 << lanes_log2, sub = t & (S - 1);
-  for (int w0 = 0; w0 < share.beams; w0 += kThreads >> lanes_log2) {
+  for (int w0 = 0; w0 < share.beams; w0 += THREADS >> lanes_log2) {
     const int w = w0 + (t >> lanes_log2);
-    const Sum* sums = part.sums + ((int64_t)req * a.beams * a.splits + w * share.splits) * kWaves;
+    const Sum* sums = part.sums + ((int64_t)req * a.beams * a.splits + w * share.splits) * a.waves;
     float m = kLowest;
     double s = 0.0;
     if (w < share.beams) {
-      for (int i = sub; i < share.splits * kWaves; i += S) {  // (of a beam that is not alive: anything)
+      for (int i = sub; i < share.splits * a.waves; i += S) {  // (of a beam that is not alive: anything)
         const Sum p = sums[i];
         const float hi = fmaxf(m, p.m);
         s = s * (double)power(m - hi, c) + p.s * (double)power(p.m - hi, c);
@@ -445,46 +465,41 @@ __global__ __launch_bounds__(kThreads) void k_beam_join(BeamArgs a, Part part, i
       m = hi;
     }
     if (w < share.beams && sub == 0) {
-      const float c = cums[beam[w]];
-      lse[w] = c > ninf() ? (double)m * a.scale + log(s) : (double)__builtin_nanf("");
-      cum[w] = c;
+      const float f = cums[beam[w]];
+      lse[w] = f > ninf() ? (double)m * a.scale + log(s) : (double)__builtin_nanf("");
+      cum[w] = f;
     }
   }
   __syncthreads();
-  auto rank_of = [&](int w, uint64_t key) {
+  auto rank_of = [&](int i, uint64_t key) {
+    if (!key) return 0ull;
+    const int w = (uint32_t)i / (uint32_t)per;
     const float score = (float)((double)cum[w] + ((double)key_float((uint32_t)(key >> 32)) * a.scale - lse[w]));
-    return key && score > ninf() ? (uint64_t)ord_key(score) << 32 | (0xFFFFFFFFu - (uint32_t)w) : 0ull;
+    return score > ninf() ? (unsigned long long)ord_key(score) << 32 | (0xFFFFFFFFu - (uint32_t)w) : 0ull;
   };
   // f(rank, key) of each of the thread's keys
   auto each = [&](auto f) {
-    int w = beam0, place = place0;
-    for (int i = t; i < total; i += kThreads) {
-      const uint64_t key = keys[i];
-      f(rank_of(w, key), key);
-      w += beam_step;
-      place += place_step;
-      if (place >= per) place -= per, ++w;
+    for (int r = 0; r < rounds; ++r) {
+      const int i = place_of_key(r);
+      const uint64_t key = i < total ? keys[i] : 0;
+      f(rank_of(i, key), key);
     }
   };
   // a score that n of the threads' own best reach (cut to its upper half)
   uint32_t best = 0;
   uint64_t rank[kHeld];
   if (held) {
-    int w = beam0, place = place0;
 #pragma unroll
     for (int r = 0; r < kHeld; ++r) {
-      rank[r] = t + r * kThreads < total ? rank_of(w, mine[r]) : 0;
+      rank[r] = rank_of(place_of_key(r), mine[r]);
       best = max(best, (uint32_t)(rank[r] >> 32));
-      w += beam_step;
-      place += place_step;
-      if (place >= per) place -= per, ++w;
     }
   } else {
     each([&](uint64_t k, uint64_t) { best = max(best, (uint32_t)(k >> 32)); });
   }
   tops[t] = best;
   __syncthreads();
-  const uint64_t floor = (uint64_t)max(block_floor(tops, n), 1u) << 32;
+  const uint64_t floor = (uint64_t)max(block_floor<THREADS>(tops, n), 1u) << 32;
   auto keep = [&](uint64_t k, uint64_t key) {
     if (k < floor) return;
     const int at = atomicAdd(&count, 1);
@@ -492,8 +507,7 @@ __global__ __launch_bounds__(kThreads) void k_beam_join(BeamArgs a, Part part, i
   };
   if (held) {
 #pragma unroll
-    for (int r = 0; r < kHeld; ++r)
-      if (r * kThreads < total) keep(rank[r], mine[r]);
+    for (int r = 0; r < kHeld; ++r) keep(rank[r], mine[r]);
   } else {
     each(keep);
   }
@@ -506,14 +520,14 @@ __global__ __launch_bounds__(kThreads) void k_beam_join(BeamArgs a, Part part, i
     a.out_token[o] = k.rank ? (int)comp_pos(k.key) : -1;
   };
   if (have <= kMost) {
-    for (int i = t; i < have; i += kThreads) {
+    for (int i = t; i < have; i += THREADS) {
       const Candidate k = found[i];
       int before = 0;
 #pragma unroll 4
       for (int j = 0; j < have; ++j) before += comes_before(found[j], k);
       if (before < n) put(before, k);
     }
-    for (int i = have + t; i < n; i += kThreads) put(i, Candidate{0, 0});
+    for (int i = have + t; i < n; i += THREADS) put(i, Candidate{0, 0});
     return;
   }
   // many equal scores: one after the other
@@ -532,39 +546,47 @@ __global__ __launch_bounds__(kThreads) void k_beam_join(BeamArgs a, Part part, i
     if (lane == 0) pick[wave] = k;
     __syncthreads();
     k = pick[0];
-    for (int i = 1; i < kWaves; ++i)
+    for (int i = 1; i < kJoinWaves; ++i)
       if (comes_before(pick[i], k)) k = pick[i];
     __syncthreads();
     if (t == 0) put(place, k);
     if (!k.rank) {
-      for (int i = place + t; i < n; i += kThreads) put(i, k);
+      for (int i = place + t; i < n; i += THREADS) put(i, k);
       return;
     }
     last = k;
   }
 }
 
+int wave_tile(const BeamArgs& a) { return 64 * kLoads * (a.bf16 ? 8 : 4); }
+
 }  // namespace
 
-constexpr int64_t kParts = 1024;  // of all rows, where they are long enough
+constexpr int64_t kParts = 1024;   // of all rows, where they are long enough
+constexpr int64_t kMostKeys = 8192;  // of a request's parts
+constexpr int64_t kNarrowRows = 2048;
 
-// Parts of a row: enough blocks to fill the GPU, none shorter than a tile for each wave.
+// Parts of a row: enough blocks to fill the GPU, none shorter than a tile for each wave,
+// and no more keys of a request than its join's block holds. Rows of one tile take a
+// wave, and so do short ones of which there are many (%%NARROW%%).
 void beam_shape(BeamArgs& a) {
   const int64_t rows = (int64_t)a.batch * a.beams;
-  const int tile = kWaves * 64 * kLoads * (a.bf16 ? 8 : 4);
-  a.most = (int)std::max<int64_t>(1, (a.vocab + (int64_t)tile - 1) / tile);
-  a.splits = (int)std::min<int64_t>(a.most, std::max<int64_t>(1, kParts / std::max<int64_t>(rows, 1)));
+  const int64_t tiles = (a.vocab + (int64_t)wave_tile(a) - 1) / wave_tile(a);
+  a.waves = a.top <= 32 && (tiles <= 1 || (tiles <= 4 && rows >= kNarrowRows)) ? 1 : kWaves;
+  a.most = (int)std::max<int64_t>(1, (tiles + a.waves - 1) / a.waves);
+  const int64_t keys = std::max<int64_t>(1, kMostKeys / ((int64_t)a.beams * a.top));
+  a.splits = (int)std::min({(int64_t)a.most, std::max<int64_t>(1, kParts / std::max<int64_t>(rows, 1)), keys});
 }
 
 static size_t sums_bytes(int64_t parts) { return ((size_t)parts * kWaves * sizeof(Sum) + 255) / 256 * 256; }
 
 // Splits follow from rows and vocabulary, but a call of fewer rows or entries may take
 // more of them: sized for the most parts that any call within these sizes takes.
-size_t beam_workspace_bytes(BeamArgs a) {
-  beam_shape(a);
+size_t beam_workspace_bytes(const BeamArgs& a) {
   const int64_t rows = (int64_t)a.batch * a.beams;
+  const int64_t most = std::max<int64_t>(1, (a.vocab + (int64_t)wave_tile(a) - 1) / wave_tile(a));
   // rows * splits <= max(rows, kParts), and never more than rows * most
-  const int64_t parts = std::max(rows, std::min<int64_t>(rows * a.most, kParts));
+  const int64_t parts = std::max(rows, std::min<int64_t>(rows * most, kParts));
   return sums_bytes(parts) + (size_t)parts * a.top * sizeof(uint64_t) + 256;
 }
 
@@ -574,11 +596,19 @@ hipError_t launch_beam_select(BeamArgs a, void* workspace, hipStream_t st) {
   Part part;
   part.sums = static_cast<Sum*>(workspace);
   part.keys = reinterpret_cast<uint64_t*>(static_cast<uint8_t*>(workspace) + sums_bytes(parts));
-  if (a.bf16) k_beam_part<uint16_t><<<dim3((unsigned)parts), kThreads, 0, st>>>(a, part);
-  else k_beam_part<float><<<dim3((unsigned)parts), kThreads, 0, st>>>(a, part);
+  const dim3 all((unsigned)parts);
+  if (a.bf16 && a.waves == 1) k_beam_part<uint16_t, 1><<<all, 64, 0, st>>>(a, part);
+  else if (a.bf16) k_beam_part<uint16_t, kWaves><<<all, kThreads, 0, st>>>(a, part);
+  else if (a.waves == 1) k_beam_part<float, 1><<<all, 64, 0, st>>>(a, part);
+  else k_beam_part<float, kWaves><<<all, kThreads, 0, st>>>(a, part);
   int lanes_log2 = 0;
-  while (lanes_log2 < 6 && 1 << lanes_log2 < a.splits * kWaves) ++lanes_log2;
-  k_beam_join<<<dim3((unsigned)a.batch), kThreads, (size_t)a.beams * 16, st>>>(a, part, lanes_log2);
+  while (lanes_log2 < 6 && 1 << lanes_log2 < a.splits * a.waves) ++lanes_log2;
+  const dim3 grid((unsigned)a.batch);
+  const size_t lds = (size_t)a.beams * 16;
+  if ((int64_t)a.beams * a.splits * a.top > kManyKeys)
+    k_beam_join<kManyThreads><<<grid, kManyThreads, lds, st>>>(a, part, lanes_log2);
+  else
+    k_beam_join<kThreads><<<grid, kThreads, lds, st>>>(a, part, lanes_log2);
   return hipGetLastError();
 }
 

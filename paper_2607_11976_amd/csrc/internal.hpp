@@ -331,10 +331,10 @@ struct BeamArgs {
   double scale;
   float* out_score;         // [batch, top]
   int32_t *out_beam, *out_token;
-  int splits, most;         // resolved by beam_shape: parts of a row, and at most
+  int splits, most, waves;  // resolved by beam_shape: parts of a row, at most; a part's waves
 };
 void beam_shape(BeamArgs& a);
-size_t beam_workspace_bytes(BeamArgs a);
+size_t beam_workspace_bytes(const BeamArgs& a);
 hipError_t launch_beam_select(BeamArgs a, void* workspace, hipStream_t st);
 
 struct ReorderArgs {

@@ -68,7 +68,8 @@ def _cum(reqs, beams, seed):
 
 @pytest.mark.parametrize("reqs,beams,vocab,top", [
     (1, 1, 1, 1), (2, 3, 1, 5), (3, 2, 7, 4), (1, 4, 32000, 8), (5, 5, 1001, 10), (2, 16, 5003, 32), (1, 64, 777, 64),
-    (1, 2, 131072, 64), (3, 8, 8192, 16), (2, 4, 8193, 8), (40, 8, 2047, 16), (300, 4, 1500, 8), (1, 1, 200001, 2), (1, 200, 50, 64)])
+    (1, 2, 131072, 64), (3, 8, 8192, 16), (2, 4, 8193, 8), (40, 8, 2047, 16), (300, 4, 1500, 8), (1, 1, 200001, 2), (1, 200, 50, 64),
+    (600, 4, 5000, 8), (2, 32, 20000, 64), (70, 16, 2048, 32)])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_matches_definition(lib, reqs, beams, vocab, top, dtype):
     _check(_draw(reqs * beams, vocab, dtype, 1), _cum(reqs, beams, 2), top)
