@@ -153,7 +153,7 @@ __device__ __forceinline__ uint32_t block_floor(const uint32_t* values, int n) {
 #pragma unroll
   for (int i = 0; i < kEach; ++i) p[i] = values[i * 64 + (threadIdx.x & 63)];
   uint32_t t = 0;
-#pragma unroll 1
+#pragma unroll 4
   for (int bit = 31; bit >= 16; --bit) {
     const uint32_t c = t | 1u << bit;
     int reach = 0;
@@ -408,18 +408,15 @@ __device__ __forceinline__ bool comes_before(const Candidate& a, const Candidate
 
 constexpr int kMost = 512;     // candidates that are ranked together
 constexpr int kHeld = 8;       // keys that a thread holds in registers
-constexpr int kManyKeys = 2048, kManyThreads = 1024;  // a request of more keys takes a larger block
 
-template <int THREADS>
-__global__ __launch_bounds__(THREADS) void k_beam_join(BeamArgs a, Part part, int lanes_log2) {
-  constexpr int kJoinWaves = THREADS / 64;
+__global__ __launch_bounds__(kThreads) void k_beam_join(BeamArgs a, Part part, int lanes_log2) {
   extern __shared__ double lse[];             // [beams]: of the rows that were read,
   float* cum = reinterpret_cast<float*>(lse + a.beams);  // their beams' scores
   int* beam = reinterpret_cast<int*>(cum + a.beams);     // and the beams
   __shared__ Candidate found[kMost];
-  __shared__ __align__(16) uint32_t tops[THREADS];
+  __shared__ __align__(16) uint32_t tops[kThreads];
   __shared__ int count;
-  __shared__ Candidate pick[kJoinWaves];
+  __shared__ Candidate pick[kWaves];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, n = a.top, req = blockIdx.x;
   const Scale c = scale_of(a.scale);
   const float* cums = a.cum + (int64_t)req * a.beams;
@@ -427,9 +424,9 @@ __global__ __launch_bounds__(THREADS) void k_beam_join(BeamArgs a, Part part, in
   const int per = share.splits * n, total = share.beams * per;  // keys of a row, of the request
   const uint64_t* keys = part.keys + (int64_t)req * a.beams * a.splits * n;
   // A thread's r-th key. The keys of a part are sorted: a thread that took every
-  // THREADS-th one would have the same place in all parts, and few threads all that count.
-  auto place_of_key = [&](int r) { return r * THREADS + ((t + 29 * r) & (THREADS - 1)); };
-  const int rounds = (total + THREADS - 1) / THREADS;
+  // kThreads-th one would have the same place in all parts, and few threads all that count.
+  auto place_of_key = [&](int r) { return r * kThreads + ((t + 29 * r) & (kThreads - 1)); };
+  const int rounds = (total + kThreads - 1) / kThreads;
   const bool held = rounds <= kHeld;
   uint64_t mine[kHeld];
   if (held) {
@@ -438,14 +435,14 @@ __global__ __launch_bounds__(THREADS) void k_beam_join(BeamArgs a, Part part, in
   }
   if (t == 0) count = 0;
   if (share.all) {
-    for (int i = t; i < a.beams; i += THREADS) beam[i] = i;
+    for (int i = t; i < a.beams; i += kThreads) beam[i] = i;
   } else if (wave == 0 && ((share.alive >> lane) & 1)) {
     beam[__popcll(share.alive & ((1ull << lane) - 1))] = lane;
   }
   __syncthreads();
   // log sums: 1 << lanes_log2 lanes a beam
   const int S = 1 << lanes_log2, sub = t & (S - 1);
-  for (int w0 = 0; w0 < share.beams; w0 += THREADS >> lanes_log2) {
+  for (int w0 = 0; w0 < share.beams; w0 += kThreads >> lanes_log2) {
     const int w = w0 + (t >> lanes_log2);
     const Sum* sums = part.sums + ((int64_t)req * a.beams * a.splits + w * share.splits) * a.waves;
     float m = kLowest;
@@ -499,7 +496,7 @@ __global__ __launch_bounds__(THREADS) void k_beam_join(BeamArgs a, Part part, in
   }
   tops[t] = best;
   __syncthreads();
-  const uint64_t floor = (uint64_t)max(block_floor<THREADS>(tops, n), 1u) << 32;
+  const uint64_t floor = (uint64_t)max(block_floor<kThreads>(tops, n), 1u) << 32;
   auto keep = [&](uint64_t k, uint64_t key) {
     if (k < floor) return;
     const int at = atomicAdd(&count, 1);
@@ -520,14 +517,14 @@ __global__ __launch_bounds__(THREADS) void k_beam_join(BeamArgs a, Part part, in
     a.out_token[o] = k.rank ? (int)comp_pos(k.key) : -1;
   };
   if (have <= kMost) {
-    for (int i = t; i < have; i += THREADS) {
+    for (int i = t; i < have; i += kThreads) {
       const Candidate k = found[i];
       int before = 0;
 #pragma unroll 4
       for (int j = 0; j < have; ++j) before += comes_before(found[j], k);
       if (before < n) put(before, k);
     }
-    for (int i = have + t; i < n; i += THREADS) put(i, Candidate{0, 0});
+    for (int i = have + t; i < n; i += kThreads) put(i, Candidate{0, 0});
     return;
   }
   // many equal scores: one after the other
@@ -546,12 +543,12 @@ __global__ __launch_bounds__(THREADS) void k_beam_join(BeamArgs a, Part part, in
     if (lane == 0) pick[wave] = k;
     __syncthreads();
     k = pick[0];
-    for (int i = 1; i < kJoinWaves; ++i)
+    for (int i = 1; i < kWaves; ++i)
       if (comes_before(pick[i], k)) k = pick[i];
     __syncthreads();
     if (t == 0) put(place, k);
     if (!k.rank) {
-      for (int i = place + t; i < n; i += THREADS) put(i, k);
+      for (int i = place + t; i < n; i += kThreads) put(i, k);
       return;
     }
     last = k;
@@ -562,8 +559,8 @@ int wave_tile(const BeamArgs& a) { return 64 * kLoads * (a.bf16 ? 8 : 4); }
 
 }  // namespace
 
-constexpr int64_t kParts = 1024;   // of all rows, where they are long enough
-constexpr int64_t kMostKeys = 8192;  // of a request's parts
+constexpr int64_t kParts = 512;   // of all rows, where they are long enough
+constexpr int64_t kMostKeys = kHeld * kThreads;  // of a request's parts
 constexpr int64_t kNarrowRows = 2048;
 
 // Parts of a row: enough blocks to fill the GPU, none shorter than a tile for each wave,
@@ -603,12 +600,7 @@ hipError_t launch_beam_select(BeamArgs a, void* workspace, hipStream_t st) {
   else k_beam_part<float, kWaves><<<all, kThreads, 0, st>>>(a, part);
   int lanes_log2 = 0;
   while (lanes_log2 < 6 && 1 << lanes_log2 < a.splits * a.waves) ++lanes_log2;
-  const dim3 grid((unsigned)a.batch);
-  const size_t lds = (size_t)a.beams * 16;
-  if ((int64_t)a.beams * a.splits * a.top > kManyKeys)
-    k_beam_join<kManyThreads><<<grid, kManyThreads, lds, st>>>(a, part, lanes_log2);
-  else
-    k_beam_join<kThreads><<<grid, kThreads, lds, st>>>(a, part, lanes_log2);
+  k_beam_join<<<dim3((unsigned)a.batch), kThreads, (size_t)a.beams * 16, st>>>(a, part, lanes_log2);
   return hipGetLastError();
 }
 
