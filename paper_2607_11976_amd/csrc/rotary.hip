@@ -14,29 +14,42 @@ constexpr int64_t kFill = 1 << 19;    // threads that fill the GPU
 constexpr int64_t kFillFp8 = 1 << 18;
 constexpr int64_t kFillKv = 1 << 17;  // with the keys' and values' loads of two heads
 
-// What a unit of a head covers: two vectors of V values, V pairs in the rotated
-// part, which fill both in turn; elsewhere two vectors that pass as they are.
+// What a unit of a head covers: two vectors of V values. Halves: in the rotated part
+// two vectors whose values are paired, elsewhere two that pass as they are. Interleaved,
+// with pairs inside a vector (V > 1): neighbours, each of which is turned or passes.
 struct Unit {
-  int a, b;    // offsets of the vectors; b < 0: there is none
-  int pair;    // first pair, < 0: not rotated
+  int a, b;      // offsets of the vectors; b < 0: there is none
+  int pa, pb;    // their first pairs, < 0: not rotated (halves: pb = pa)
 };
 template <int V>
 __device__ __forceinline__ Unit unit_of(const RotaryArgs& r, int u) {
+  if (V > 1 && r.interleaved) {
+    const int a = 2 * u * V, b = a + V, end = r.start + 2 * r.pairs;
+    return Unit{a, b < r.d ? b : -1, a >= r.start && a < end ? (a - r.start) / 2 : -1,
+                b >= r.start && b < end ? (b - r.start) / 2 : -1};
+  }
   const int nr = r.pairs / V;
   if (u < nr) {
-    if (r.interleaved) return Unit{r.start + 2 * u * V, r.start + (2 * u + 1) * V, u * V};
-    return Unit{r.start + u * V, r.start + r.pairs + u * V, u * V};
+    if (r.interleaved) return Unit{r.start + 2 * u, r.start + 2 * u + 1, u, u};
+    return Unit{r.start + u * V, r.start + r.pairs + u * V, u * V, u * V};
   }
   const int first = r.start / V, part = 2 * nr, count = r.d / V - part;  // vectors before, in, beside the part
   const int i = 2 * (u - nr), a = i < first ? i : i + part, b = i + 1 < first ? i + 1 : i + 1 + part;
-  return Unit{a * V, i + 1 < count ? b * V : -1, -1};
+  return Unit{a * V, i + 1 < count ? b * V : -1, -1, -1};
 }
 
+// Sines and cosines: of pairs pa ..., or interleaved of V / 2 pairs of either vector (of
+// any pairs where one of the two passes).
 template <int V>
 __device__ __forceinline__ void turns_of(const RotaryArgs& r, const Unit& u, int pos, float (&c)[V], float (&s)[V]) {
+  if (u.pa < 0 && u.pb < 0) return;
+  const float *fa = r.freq + max(u.pa, 0), *fb = V > 1 && r.interleaved ? r.freq + max(u.pb, 0) : fa + V / 2;
+  float f[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) f[j] = j < (V + 1) / 2 ? fa[j] : fb[j - (V + 1) / 2];
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    const Turn t = turn_of((double)pos * turns_per(r.freq[u.pair + j]), r.amplitude);
+    const Turn t = turn_of((double)pos * turns_per(f[j]), r.amplitude);
     c[j] = t.c;
     s[j] = r.inverse ? -t.s : t.s;
   }
@@ -44,28 +57,33 @@ __device__ __forceinline__ void turns_of(const RotaryArgs& r, const Unit& u, int
 
 // The unit's values x, y (of vectors a and b) turned in place.
 template <int V>
-__device__ __forceinline__ void turn_unit(const RotaryArgs& r, float (&x)[V], float (&y)[V], const float (&c)[V],
-                                          const float (&s)[V]) {
-  if (!r.interleaved) {
+__device__ __forceinline__ void turn_unit(const RotaryArgs& r, const Unit& w, float (&x)[V], float (&y)[V],
+                                          const float (&c)[V], const float (&s)[V]) {
+  if (V == 1 || !r.interleaved) {
+    if (w.pa < 0) return;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       const float u = x[j], v = y[j];
       x[j] = turned(u, c[j], v, -s[j]);
       y[j] = turned(v, c[j], u, s[j]);
     }
-  } else if constexpr (V == 1) {
-    const float u = x[0], v = y[0];
-    x[0] = turned(u, c[0], v, -s[0]);
-    y[0] = turned(v, c[0], u, s[0]);
-  } else {
+    return;
+  }
+  constexpr int H = V > 1 ? V / 2 : 1;
+  if (w.pa >= 0) {
 #pragma unroll
-    for (int j = 0; j < V; j += 2) {
-      float u = x[j], v = x[j + 1];
+    for (int j = 0; j + 1 < V; j += 2) {
+      const float u = x[j], v = x[j + 1];
       x[j] = turned(u, c[j / 2], v, -s[j / 2]);
       x[j + 1] = turned(v, c[j / 2], u, s[j / 2]);
-      u = y[j], v = y[j + 1];
-      y[j] = turned(u, c[V / 2 + j / 2], v, -s[V / 2 + j / 2]);
-      y[j + 1] = turned(v, c[V / 2 + j / 2], u, s[V / 2 + j / 2]);
+    }
+  }
+  if (w.pb >= 0) {
+#pragma unroll
+    for (int j = 0; j + 1 < V; j += 2) {
+      const float u = y[j], v = y[j + 1];
+      y[j] = turned(u, c[H + j / 2], v, -s[H + j / 2]);
+      y[j + 1] = turned(v, c[H + j / 2], u, s[H + j / 2]);
     }
   }
 }
@@ -96,7 +114,7 @@ __device__ __forceinline__ void rotate_rows(const RotaryArgs& r, uint32_t block)
           if (w.b >= 0) y[k].load(in + g * r.x_head + w.b);
         }
       }
-      if (h == h0 && w.pair >= 0) turns_of<V>(r, w, pos, c, s);  // while the first loads are on their way
+      if (h == h0) turns_of<V>(r, w, pos, c, s);  // while the first loads are on their way
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
         const int g = h + k * r.head_lanes;
@@ -104,8 +122,8 @@ __device__ __forceinline__ void rotate_rows(const RotaryArgs& r, uint32_t block)
         float a[V] = {}, b[V] = {};
         if (pos >= 0) {
           x[k].unpack(a);
-          y[k].unpack(b);
-          if (w.pair >= 0) turn_unit<V>(r, a, b, c, s);
+          if (w.b >= 0) y[k].unpack(b);
+          turn_unit<V>(r, w, a, b, c, s);
         }
         store_values<V>(out + g * r.out_head + w.a, a);
         if (w.b >= 0) store_values<V>(out + g * r.out_head + w.b, b);
@@ -194,7 +212,7 @@ __global__ __launch_bounds__(kThreads) void k_rotary_fp8(RotaryArgs r) {
           if (w.b >= 0) q[k].load(in + g * r.x_head + w.b);
         }
       }
-      if (h == h0 && w.pair >= 0) turns_of<V>(r, w, pos, c, s);
+      if (h == h0) turns_of<V>(r, w, pos, c, s);
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
         const int g = h + k * r.head_lanes;
@@ -203,7 +221,7 @@ __global__ __launch_bounds__(kThreads) void k_rotary_fp8(RotaryArgs r) {
         if (pos >= 0) {
           p[k].unpack(x);
           if (w.b >= 0) q[k].unpack(y);
-          if (w.pair >= 0) turn_unit<V>(r, x, y, c, s);
+          turn_unit<V>(r, w, x, y, c, s);
         }
         const float by = scale_head(g, mine ? top_of<V>(top_of<V>(0u, x), y) : 0u);
         if (mine) put(w, g, by, x, y);
@@ -214,9 +232,8 @@ __global__ __launch_bounds__(kThreads) void k_rotary_fp8(RotaryArgs r) {
       if (pos < 0) return;
       load_values<V>(in + h * r.x_head + w.a, x);
       if (w.b >= 0) load_values<V>(in + h * r.x_head + w.b, y);
-      if (w.pair < 0) return;
       turns_of<V>(r, w, pos, c, s);
-      turn_unit<V>(r, x, y, c, s);
+      turn_unit<V>(r, w, x, y, c, s);
     };
     for (int h = h0; h < r.H; h += r.head_lanes) {
       uint32_t top = 0;
@@ -423,7 +440,10 @@ __global__ __launch_bounds__(kThreads) void k_append_rotary(AppendRotaryArgs a, 
   } else if (!WIDE && b < a.k_blocks + a.v_blocks) {
     append_values<T>(a, c, (uint32_t)(b - a.k_blocks));
   } else {
-    rotate_rows<T, uint16_t, WIDE ? 8 : 1>(a.q, (uint32_t)(b - a.k_blocks - a.v_blocks));
+    const uint32_t q = (uint32_t)(b - a.k_blocks - a.v_blocks);
+    if constexpr (WIDE) rotate_rows<T, uint16_t, 8>(a.q, q);
+    else if (a.q.vec == 2) rotate_rows<T, uint16_t, 2>(a.q, q);
+    else rotate_rows<T, uint16_t, 1>(a.q, q);
   }
 }
 bool is_aligned(const void* p, int64_t n) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(n - 1)) == 0; }
@@ -437,7 +457,7 @@ bool side_fits(const void* p, int64_t token, int64_t head, int T, int H, int n, 
 void lanes_of(RotaryArgs& a, bool power) {
   const int V = a.vec;
   const int beside = a.d / V - 2 * (a.pairs / V);  // vectors that pass
-  a.units = a.pairs / V + (beside + 1) / 2;
+  a.units = V > 1 && a.interleaved ? (a.d / V + 1) / 2 : a.pairs / V + (beside + 1) / 2;
   a.lanes = std::min(std::max(a.units, 1), 64);
   if (power)
     while (a.lanes & (a.lanes - 1)) ++a.lanes;
@@ -482,13 +502,16 @@ void run_rotary_fp8(const RotaryArgs& a, dim3 grid, hipStream_t st) {
 
 // The widest vectors that the part's place, the head's size and both sides' strides
 // and addresses allow.
-int64_t rotary_shape(RotaryArgs& a, bool fp8) {
+static void choose_vec(RotaryArgs& a, bool fp8) {
   const int si = a.in_f32 ? 4 : 2, so = fp8 ? 1 : a.out_f32 ? 4 : 2;
   for (a.vec = 8; a.vec > 1; a.vec /= 2)
-    if (a.d % a.vec == 0 && a.start % a.vec == 0 && a.pairs % a.vec == 0 &&
+    if (a.d % a.vec == 0 && a.start % a.vec == 0 && (a.interleaved ? 2 * a.pairs : a.pairs) % a.vec == 0 &&
         side_fits(a.x, a.x_token, a.x_head, a.T, a.H, a.vec, si) &&
         side_fits(a.out, a.out_token, a.out_head, a.T, a.H, a.vec, so))
       break;
+}
+int64_t rotary_shape(RotaryArgs& a, bool fp8) {
+  choose_vec(a, fp8);
   lanes_of(a, fp8);
   return rotary_blocks(a, fp8 ? kFillFp8 : kFill);
 }
@@ -511,15 +534,17 @@ hipError_t launch_rotary(const RotaryArgs& r, hipStream_t st) {
 
 int64_t append_rotary_shape(AppendRotaryArgs& a, const Cache4& c) {
   a.wide = a.interleaved ? a.start % 8 == 0 && a.pairs % 4 == 0 : a.start % 32 == 0 && a.pairs % 32 == 0;
-  if (a.q.T > 0)
-    a.wide = a.wide && a.pairs % 8 == 0 && side_fits(a.q.x, a.q.x_token, a.q.x_head, a.q.T, a.q.H, 8, a.in_f32 ? 4 : 2);
+  if (a.q.T > 0) {
+    choose_vec(a.q, false);
+    a.wide = a.wide && a.q.vec == 8;
+    if (!a.wide) a.q.vec = std::min(a.q.vec, 2);
+  }
   const int lanes = c.d / (a.wide ? 16 : 8);
   a.head_lanes = lanes_for(a.rows * lanes, c.hkv, kFillKv);
   a.k_blocks = (a.rows * a.head_lanes * lanes + kThreads - 1) / kThreads;
   a.v_blocks = a.wide ? 0 : (a.rows * c.hkv * lanes + kThreads - 1) / kThreads;
   a.q_blocks = 0;
   if (a.q.T > 0) {
-    a.q.vec = a.wide ? 8 : 1;
     lanes_of(a.q, false);
     a.q_blocks = rotary_blocks(a.q);
   }

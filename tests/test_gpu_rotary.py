@@ -65,6 +65,7 @@ def _rot(n, start=0, interleaved=False, amplitude=1.0):
 SHAPES = [  # tokens, heads, d, pairs, start: vectors of 8, 4, 2 and 1, whole heads and parts
     (1, 1, 128, 64, 0), (5, 3, 128, 32, 64), (3, 2, 64, 16, 16), (7, 8, 80, 20, 0), (4, 5, 80, 10, 2), (9, 1, 96, 48, 0),
     (2, 3, 6, 3, 0), (3, 1, 7, 2, 1), (2, 2, 1024, 512, 0), (2, 1, 1016, 100, 8), (3, 2, 1001, 77, 500), (5, 2, 192, 32, 128),
+    (3, 2, 80, 27, 0), (5, 3, 80, 20, 40), (2, 2, 96, 12, 8), (2, 2, 64, 5, 2), (3, 1, 72, 36, 0), (2, 3, 40, 1, 36),
     (1, 64, 128, 64, 0), (130, 1, 128, 64, 0), (3, 2, 64, 0, 0), (2, 1, 1, 0, 0), (67, 40, 128, 64, 0), (33, 20, 256, 128, 0)]
 
 
@@ -224,7 +225,7 @@ def _append_case(rows, heads, d, dtype, page, hq=0, seed=20):
 
 @pytest.mark.parametrize("rows,heads,d,page,n,start", [
     (1, 1, 128, 16, 64, 0), (64, 8, 128, 64, 64, 0), (77, 2, 64, 16, 32, 0), (50, 4, 128, 1, 32, 64), (33, 1, 64, 64, 8, 32),
-    (40, 3, 128, 16, 20, 0), (21, 2, 64, 16, 5, 3), (9, 2, 128, 16, 0, 0), (300, 8, 64, 128, 16, 16), (18, 5, 128, 64, 63, 1)])
+    (40, 3, 128, 16, 20, 0), (21, 2, 64, 16, 5, 3), (31, 2, 128, 16, 36, 8), (26, 2, 64, 16, 12, 40), (17, 4, 128, 16, 39, 50), (9, 2, 128, 16, 0, 0), (300, 8, 64, 128, 16, 16), (18, 5, 128, 64, 63, 1)])
 @pytest.mark.parametrize("interleaved", [False, True])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_append_is_rotation_then_append(lib, rows, heads, d, page, n, start, interleaved, dtype):
