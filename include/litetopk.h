@@ -472,6 +472,7 @@ int lt_token_logprobs_backward(const void* logits, lt_dtype dtype, int64_t ld, i
 #define LT_ROTARY_INTERLEAVED 1u    /* pairs are values (2 i, 2 i + 1), else (i, i + num_pairs) */
 #define LT_ROTARY_INVERSE 2u        /* turned back: the gradient of the call without it        */
 #define LT_ROTARY_MAX_DIM 1024      /* values of a head                                        */
+#define LT_ROTARY_MAX_HEADS (1 << 20)
 
 /* Rotary positions. Of every head's values the part [rotary_start, rotary_start +
    2 num_pairs) is turned, pair i of token t by the angle a = positions[t] *
@@ -481,7 +482,7 @@ int lt_token_logprobs_backward(const void* logits, lt_dtype dtype, int64_t ld, i
    stay exact at any position), c and s are rounded to float32, the products and sums
    are float32 and each rounded.
    x, out     [num_tokens, num_heads, head_dim], token_stride and head_stride values
-              apart; float32 or bfloat16, of out the same or bfloat16. No alignment
+              apart (2^31 at most); float32 or bfloat16, of out the same or bfloat16. No alignment
               beyond the elements' (16-byte aligned rows whose part fills vectors of 8
               are fastest). out may be x with the same type and strides; it must not
               overlap x otherwise.

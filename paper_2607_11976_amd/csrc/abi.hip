@@ -834,6 +834,8 @@ int lt_token_logprobs_backward(const void* logits, lt_dtype dtype, int64_t ld, i
                                              grad_logprob, grad_entropy, grad_logits, grad_ld, (hipStream_t)stream));
 }
 
+constexpr int64_t kMaxStride = 1LL << 31;  // of rotary calls: 2^31 of them are within 64 bits
+
 // The part that is turned, and what turns it.
 static int check_rotary(int32_t d, const float* freq, int32_t pairs, int32_t start, double amplitude, uint32_t flags,
                         uint32_t allowed) {
@@ -852,7 +854,7 @@ static int rotary_args(const void* x, lt_dtype dtype, int64_t token_stride, int6
   if (tokens < 0 || heads < 0) return LT_EINVAL;
   const int rc = check_rotary(d, freq, pairs, start, amplitude, flags, LT_ROTARY_INTERLEAVED | LT_ROTARY_INVERSE);
   if (rc) return rc;
-  if (d > LT_ROTARY_MAX_DIM) return LT_EUNSUPPORTED;
+  if (d > LT_ROTARY_MAX_DIM || heads > LT_ROTARY_MAX_HEADS) return LT_EUNSUPPORTED;
   *a = RotaryArgs{};
   a->x = x;
   a->x_token = token_stride;
@@ -870,7 +872,7 @@ static int rotary_args(const void* x, lt_dtype dtype, int64_t token_stride, int6
   a->in_f32 = dtype == LT_F32;
   if (tokens == 0 || heads == 0) return LT_OK;
   if (!x || !positions || !aligned(x, a->in_f32 ? 4 : 2) || !aligned(positions, 4)) return LT_EINVAL;
-  if (token_stride < 0 || head_stride < 0) return LT_EINVAL;
+  if (token_stride < 0 || head_stride < 0 || token_stride > kMaxStride || head_stride > kMaxStride) return LT_EINVAL;
   return LT_OK;
 }
 
@@ -888,7 +890,8 @@ int lt_rotary(const void* x, lt_dtype dtype, int64_t token_stride, int64_t head_
   a.out_f32 = out_dtype == LT_F32;
   a.out_token = out_token_stride;
   a.out_head = out_head_stride;
-  if (!out || !aligned(out, a.out_f32 ? 4 : 2)) return LT_EINVAL;
+  if (!out || !aligned(out, a.out_f32 ? 4 : 2) || out == positions || out == freq) return LT_EINVAL;
+  if (out_token_stride > kMaxStride || out_head_stride > kMaxStride) return LT_EINVAL;
   // rows of the result lie apart: heads inside tokens, or tokens inside heads
   const int64_t ht = out_head_stride, tt = out_token_stride;
   if ((heads > 1 && ht < d) || (tokens > 1 && tt < d)) return LT_EINVAL;
@@ -908,7 +911,11 @@ int lt_rotary_fp8(const void* x, lt_dtype dtype, int64_t token_stride, int64_t h
                              amplitude, flags, &a);
   if (rc) return rc;
   if (tokens == 0 || heads == 0) return LT_OK;
-  if (!codes || !scales || !aligned(scales, 4) || codes == x || (const void*)scales == x) return LT_EINVAL;
+  if (!codes || !scales || !aligned(scales, 4)) return LT_EINVAL;
+  const void *in[] = {x, positions, freq};
+  for (const void* i : in)
+    if (codes == i || scales == i) return LT_EINVAL;
+  if ((const void*)scales == codes) return LT_EINVAL;
   a.out = codes;
   a.out_token = (int64_t)heads * d;
   a.out_head = d;
@@ -1044,7 +1051,9 @@ int lt_paged_reorder(const int32_t* block_table, int64_t table_ld, int32_t table
   for (const void* i : in)
     for (const void* o : out)
       if (i && i == o) return LT_EINVAL;
-  if (free_pages == free_used) return LT_EINVAL;
+  const void* kept[] = {block_table, seq_lens, parents, keep_pages, free_used};
+  for (const void* i : kept)
+    if (i && i == free_pages) return LT_EINVAL;
   ReorderArgs a{};
   a.table = block_table;
   a.lens = seq_lens;

@@ -44,6 +44,7 @@ LT_LOGPROB_MAX_VOCAB = 1 << 30
 LT_LOGPROB_MAX_ROWS = 0xFFFFFF
 LT_ROTARY_INTERLEAVED, LT_ROTARY_INVERSE = 1, 2
 LT_ROTARY_MAX_DIM = 1024
+LT_ROTARY_MAX_HEADS = 1 << 20
 LT_BEAM_MAX_TOP = 64
 LT_BEAM_MAX_BEAMS = 1024
 LT_REORDER_MAX_GROUP = 64

@@ -33,7 +33,11 @@ def rotary(**over):
     (dict(ots=127), lt.LT_EINVAL), (dict(ots=1023), lt.LT_EINVAL), (dict(ots=128, ohs=128), lt.LT_EINVAL),
     (dict(out=P, ts=2048), lt.LT_EINVAL), (dict(out=P, hs=256, ts=2048, ots=2048), lt.LT_EINVAL),
     (dict(out=P, dtype=lt.LT_F32), lt.LT_EINVAL), (dict(tokens=0), lt.LT_OK), (dict(heads=0), lt.LT_OK),
-    (dict(tokens=0x7FFFFFFF, heads=1024, ts=1 << 20, ots=1 << 20), lt.LT_EUNSUPPORTED)])
+    (dict(tokens=0x7FFFFFFF, heads=1024, ts=1 << 20, ots=1 << 20), lt.LT_EUNSUPPORTED),
+    (dict(heads=lt.LT_ROTARY_MAX_HEADS + 1, ts=1 << 28, ots=1 << 28), lt.LT_EUNSUPPORTED),
+    (dict(ts=(1 << 31) + 1), lt.LT_EINVAL), (dict(hs=1 << 40), lt.LT_EINVAL), (dict(ots=1 << 62), lt.LT_EINVAL),
+    (dict(ohs=1 << 62, tokens=1 << 30), lt.LT_EINVAL), (dict(out=3 * P, pos=3 * P), lt.LT_EINVAL),
+    (dict(out=3 * P, freq=3 * P), lt.LT_EINVAL)])
 def test_rotary_refusals(over, code):
     assert rotary(**over) == code
 
@@ -41,7 +45,9 @@ def test_rotary_refusals(over, code):
 @pytest.mark.parametrize("over,code", [
     (dict(dtype=lt.LT_FP8_E4M3FN), lt.LT_EUNSUPPORTED), (dict(flags=4), lt.LT_EINVAL), (dict(codes=None), lt.LT_EINVAL),
     (dict(scales=None), lt.LT_EINVAL), (dict(scales=P + 2), lt.LT_EINVAL), (dict(codes=P), lt.LT_EINVAL),
-    (dict(start=120), lt.LT_EINVAL), (dict(d=2000, pairs=0), lt.LT_EUNSUPPORTED), (dict(tokens=0), lt.LT_OK)])
+    (dict(start=120), lt.LT_EINVAL), (dict(d=2000, pairs=0), lt.LT_EUNSUPPORTED), (dict(tokens=0), lt.LT_OK),
+    (dict(scales=P), lt.LT_EINVAL), (dict(scales=2 * P), lt.LT_EINVAL), (dict(pos=2 * P), lt.LT_EINVAL),
+    (dict(freq=3 * P), lt.LT_EINVAL)])
 def test_rotary_fp8_refusals(over, code):
     a = dict(x=P, dtype=lt.LT_BF16, ts=1024, hs=128, tokens=3, heads=8, d=128, pos=P, freq=P, pairs=64, start=0, amp=1.0,
              flags=0, codes=2 * P, scales=3 * P, stream=None)
@@ -111,6 +117,7 @@ def test_beam_workspace_sizes():
     (dict(status=None), lt.LT_EINVAL), (dict(copies=None), lt.LT_EINVAL), (dict(new_lens=None), lt.LT_EINVAL),
     (dict(new_table=P), lt.LT_EINVAL), (dict(new_lens=2 * P), lt.LT_EINVAL), (dict(used_out=5 * P), lt.LT_EINVAL),
     (dict(status=3 * P), lt.LT_EINVAL), (dict(copies=6 * P), lt.LT_EINVAL), (dict(free=6 * P), lt.LT_EINVAL),
+    (dict(free=P), lt.LT_EINVAL), (dict(free=2 * P), lt.LT_EINVAL), (dict(keep=5 * P), lt.LT_EINVAL),
     (dict(ws=None), lt.LT_EINVAL), (dict(ws=P + 8), lt.LT_EINVAL), (dict(bytes=16), lt.LT_EWORKSPACE),
     (dict(width=1 << 28, ld=1 << 28, new_ld=1 << 28), lt.LT_EUNSUPPORTED)])
 def test_reorder_refusals(over, code):
