@@ -10,9 +10,14 @@ namespace lt {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int64_t kFill = 1 << 19;    // threads that fill the GPU
+// Threads that fill the GPU; a thread takes more heads where there are more tokens than
+// that. 16384 tokens of 40 heads of 128 in bfloat16 (335 MB): 67 us with 2^19, 71 with 2^18,
+// 65 with 2^20, which costs 5003 tokens of 12 heads of 80 12 us where the others take 10.
+constexpr int64_t kFill = 1 << 19;
+// As fp8 (4096 tokens of 64 heads of 128, 101 MB): 22 us with 2^18, 25 with 2^19, 27 with 2^17.
 constexpr int64_t kFillFp8 = 1 << 18;
-constexpr int64_t kFillKv = 1 << 17;  // with the keys' and values' loads of two heads
+// Into the cache: 25 us with 2^17 (below), 29 with 2^18.
+constexpr int64_t kFillKv = 1 << 17;
 
 // What a unit of a head covers: two vectors of V values. Halves: in the rotated part
 // two vectors whose values are paired, elsewhere two that pass as they are. Interleaved,
@@ -90,7 +95,7 @@ __device__ __forceinline__ void turn_unit(const RotaryArgs& r, const Unit& w, fl
 
 // Lanes of a head, one unit each (in turn where there are more units); a group of
 // them takes every head_lanes-th head of a token, kAhead heads' loads at a time, all
-// with the same sines and cosines.
+// with the same sines and cosines (two at a time: 71 us where four take 67).
 constexpr int kAhead = 4;
 template <class TI, class TO, int V>
 __device__ __forceinline__ void rotate_rows(const RotaryArgs& r, uint32_t block) {
@@ -284,8 +289,8 @@ __device__ __forceinline__ int64_t slot_of(const AppendRotaryArgs& a, const Cach
 // two vectors of 8 of a head, those that face each other where halves are paired, of the
 // key and of the value, and every head_lanes-th head with the same sines and cosines. So
 // a slot's key and value are written side by side, a line at a time. 16381 tokens of 8
-// heads of 128 in bfloat16: %%KV%%.
-constexpr int kAheadKv = 1;
+// heads of 128 in bfloat16 (85 MB): 25 us, where k_cache4_append alone takes 27. (Loads of
+// two heads ahead: 3 us more, of four 5.)
 template <class T>
 __device__ __forceinline__ void append_pairs(const AppendRotaryArgs& a, const Cache4& c, uint32_t block) {
   const int units = c.d / 16;  // lanes of a head: 4 or 8
@@ -317,16 +322,12 @@ __device__ __forceinline__ void append_pairs(const AppendRotaryArgs& a, const Ca
   const T* kin = reinterpret_cast<const T*>(a.k) + (int64_t)tok * a.k_stride;
   const T* vin = reinterpret_cast<const T*>(a.v) + (int64_t)tok * a.v_stride;
   float cs[8], sn[8];
-  for (int h = h0; h < c.hkv; h += kAheadKv * a.head_lanes) {
-    Raw<T, 8> raw[kAheadKv][4];
-#pragma unroll
-    for (int k = 0; k < kAheadKv; ++k) {
-      const int g = min(h + k * a.head_lanes, c.hkv - 1) * c.d;
-      raw[k][0].load(kin + g + va * 8);
-      raw[k][1].load(kin + g + vb * 8);
-      raw[k][2].load(vin + g + va * 8);
-      raw[k][3].load(vin + g + vb * 8);
-    }
+  for (int h = h0; h < c.hkv; h += a.head_lanes) {
+    Raw<T, 8> raw[4];
+    raw[0].load(kin + h * c.d + va * 8);
+    raw[1].load(kin + h * c.d + vb * 8);
+    raw[2].load(vin + h * c.d + va * 8);
+    raw[3].load(vin + h * c.d + vb * 8);
     if (h == h0) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -336,40 +337,35 @@ __device__ __forceinline__ void append_pairs(const AppendRotaryArgs& a, const Ca
         cs[j] = t.c, sn[j] = t.s;
       }
     }
+    const int64_t row = c.row(slot, h);
+    float x[8], y[8];
+    raw[0].unpack(x);
+    raw[1].unpack(y);
+    if (!a.interleaved) {
+      if (pair[0] >= 0) {
 #pragma unroll
-    for (int k = 0; k < kAheadKv; ++k) {
-      const int g = h + k * a.head_lanes;
-      if (g >= c.hkv) break;  // whole heads
-      const int64_t row = c.row(slot, g);
-      float x[8], y[8];
-      raw[k][0].unpack(x);
-      raw[k][1].unpack(y);
-      if (!a.interleaved) {
-        if (pair[0] >= 0) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float p = x[j], q = y[j];
-            x[j] = turned(p, cs[j], q, -sn[j]);
-            y[j] = turned(q, cs[j], p, sn[j]);
-          }
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float p = x[2 * j], q = x[2 * j + 1];
-          if (pair[0] >= 0) x[2 * j] = turned(p, cs[j], q, -sn[j]), x[2 * j + 1] = turned(q, cs[j], p, sn[j]);
-          p = y[2 * j], q = y[2 * j + 1];
-          if (pair[1] >= 0)
-            y[2 * j] = turned(p, cs[4 + j], q, -sn[4 + j]), y[2 * j + 1] = turned(q, cs[4 + j], p, sn[4 + j]);
+        for (int j = 0; j < 8; ++j) {
+          const float p = x[j], q = y[j];
+          x[j] = turned(p, cs[j], q, -sn[j]);
+          y[j] = turned(q, cs[j], p, sn[j]);
         }
       }
-      put_codes(x, row, c.d, 0, va, a.codes, a.scales);
-      put_codes(y, row, c.d, 0, vb, a.codes, a.scales);
-      raw[k][2].unpack(x);
-      raw[k][3].unpack(y);
-      put_codes(x, row, c.d, 1, va, a.codes, a.scales);
-      put_codes(y, row, c.d, 1, vb, a.codes, a.scales);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float p = x[2 * j], q = x[2 * j + 1];
+        if (pair[0] >= 0) x[2 * j] = turned(p, cs[j], q, -sn[j]), x[2 * j + 1] = turned(q, cs[j], p, sn[j]);
+        p = y[2 * j], q = y[2 * j + 1];
+        if (pair[1] >= 0)
+          y[2 * j] = turned(p, cs[4 + j], q, -sn[4 + j]), y[2 * j + 1] = turned(q, cs[4 + j], p, sn[4 + j]);
+      }
     }
+    put_codes(x, row, c.d, 0, va, a.codes, a.scales);
+    put_codes(y, row, c.d, 0, vb, a.codes, a.scales);
+    raw[2].unpack(x);
+    raw[3].unpack(y);
+    put_codes(x, row, c.d, 1, va, a.codes, a.scales);
+    put_codes(y, row, c.d, 1, vb, a.codes, a.scales);
   }
 }
 
@@ -430,7 +426,7 @@ __device__ __forceinline__ void append_values(const AppendRotaryArgs& a, const C
 }
 
 // One launch: blocks of keys and values and of queries, side by side (two kernels one after
-// the other take 83 us where this takes %%ALL%%: 32 query heads beside the above).
+// the other take 83 us where this takes 75: 32 query heads beside the above).
 template <class T, bool WIDE>
 __global__ __launch_bounds__(kThreads) void k_append_rotary(AppendRotaryArgs a, Cache4 c) {
   const int64_t b = blockIdx.x;

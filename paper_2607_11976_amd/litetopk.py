@@ -1180,27 +1180,32 @@ def paged_reorder(block_table: torch.Tensor, seq_lens: torch.Tensor, parents: to
     before free_used). block_table [rows, width], seq_lens, free_pages and free_used are
     paged_plan's."""
     n = seq_lens.numel()
-    _int32(seq_lens, None, "seq_lens")
-    _int32(parents, n, "parents")
-    _int32(keep_pages, n, "keep_pages")
-    _int32(free_pages, None, "free_pages")
-    _int32(free_used, 1, "free_used")
+    for t, size, name in ((seq_lens, n, "seq_lens"), (parents, n, "parents"), (free_pages, None, "free_pages"),
+                          (free_used, 1, "free_used"), (keep_pages, n, "keep_pages")):
+        _int32(t, size, name)
     ld, width = _table(block_table, n)
-    _here(block_table, seq_lens, parents, keep_pages, free_pages, free_used, workspace)
+    _here(block_table, seq_lens, parents, free_pages, free_used, keep_pages, workspace)
     dev = block_table.device
     lib = load()
     need = lib.lt_paged_reorder_workspace_size(n)
     if need == 0:
         raise LiteTopKError("at most %d rows" % LT_PLAN_MAX_REQUESTS)
-    workspace = _workspace(workspace, need, dev, stream)
-    # the results in one allocation
-    table, lens, copies, used, status = _empty(n * (width + 4) + 1, torch.int32, dev, stream).split_with_sizes(
-        (n * width, n, 2 * n, 1, n))
+    # the results in one allocation, and behind them the workspace (16 bytes a row)
+    many = n * (width + 4) + 1
+    if workspace is None:
+        pad = -many % 64
+        table, lens, copies, used, status, _, workspace = _empty(
+            many + pad + need // 4, torch.int32, dev, stream).split_with_sizes((n * width, n, 2 * n, 1, n, pad, need // 4))
+    else:
+        workspace = _workspace(workspace, need, dev, stream)
+        need = workspace.numel() * workspace.element_size()
+        table, lens, copies, used, status = _empty(many, torch.int32, dev, stream).split_with_sizes(
+            (n * width, n, 2 * n, 1, n))
     r = PagedReorder(table.view(n, width), lens, copies.view(n, 2), used, status)
     st = lib.lt_paged_reorder(block_table.data_ptr(), ld, width, seq_lens.data_ptr(), parents.data_ptr(), n, group,
                               page_size, _ptr(keep_pages), free_pages.data_ptr(), free_pages.numel(),
                               free_used.data_ptr(), table.data_ptr(), width, lens.data_ptr(), copies.data_ptr(),
-                              used.data_ptr(), status.data_ptr(), workspace.data_ptr(), workspace.numel(),
+                              used.data_ptr(), status.data_ptr(), workspace.data_ptr(), need,
                               _stream_of(stream, block_table))
     if st:
         _check(st, "lt_paged_reorder")
