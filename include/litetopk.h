@@ -540,7 +540,7 @@ size_t lt_beam_select_workspace_size(lt_dtype dtype, int32_t batch, int32_t beam
               rows (no alignment beyond the elements').
    cum        float32 [batch, beams]: the beams' scores so far; -inf (or NaN): the beam
               is not alive, its logits are not looked at.
-   scale      > 0, scale * log2 e finite.
+   scale      2^-100 or more, scale * log2 e finite.
    out_score  float32 [batch, top], out_beam and out_token int32 [batch, top], best
               first. Only scores above -inf are candidates (a logit of -inf is masked
               out; a beam whose logits hold NaN or +inf has none); where there are

@@ -1009,7 +1009,7 @@ int lt_beam_select(const void* logits, lt_dtype dtype, int64_t ld, int32_t batch
   BeamArgs a;
   const int rc = beam_args(dtype, batch, beams, vocab, top, &a);
   if (rc) return rc;
-  if (ld < vocab || !(scale >= 1.17549435e-38) || !scale_ok((float)scale)) return LT_EINVAL;
+  if (ld < vocab || !(scale >= 0x1p-100) || !scale_ok((float)scale)) return LT_EINVAL;
   if (batch == 0) return LT_OK;
   if ((vocab > 0 && !logits) || !aligned(logits, a.bf16 ? 2 : 4)) return LT_EINVAL;
   if (!cum || !out_score || !out_beam || !out_token) return LT_EINVAL;

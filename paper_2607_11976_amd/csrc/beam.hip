@@ -231,15 +231,15 @@ __device__ __forceinline__ void take_all(List& list, const T* x, int base, int e
 #pragma unroll 1
     for (int q = 0; q < kLoads * N; ++q) {
       const int from = base + (q / N * 64 + lane) * N, i = min(from, e - N) + q % N;
-      const float v = i >= from ? Row<T>::one(x + i) : ninf();
-      uint64_t who = __ballot(v >= key_float(gate));
+      const float u = i >= from ? Row<T>::one(x + i) : ninf();
+      uint64_t who = __ballot(u >= key_float(gate));
       if (list.count + __popcll(who) > kList) {
         cut(list, n);
         // equal values of this tile may come before those in the list
         gate = max(gate, list.strict);
-        who = __ballot(v >= key_float(gate));
+        who = __ballot(u >= key_float(gate));
       }
-      if ((who >> lane) & 1) list.at[list.count + __popcll(who & ((1ull << lane) - 1))] = comp_key(v, (uint32_t)i);
+      if ((who >> lane) & 1) list.at[list.count + __popcll(who & ((1ull << lane) - 1))] = comp_key(u, (uint32_t)i);
       list.count += __popcll(who);
     }
     cut(list, n);

@@ -80,7 +80,7 @@ def test_append_rotary_refusals(over, code):
     (dict(beams=1025), lt.LT_EUNSUPPORTED), (dict(vocab=lt.LT_LOGPROB_MAX_VOCAB + 1, ld=1 << 40), lt.LT_EUNSUPPORTED),
     (dict(batch=1 << 20, beams=64), lt.LT_EUNSUPPORTED), (dict(ld=999), lt.LT_EINVAL), (dict(scale=0.0), lt.LT_EINVAL),
     (dict(scale=-1.0), lt.LT_EINVAL), (dict(scale=NAN), lt.LT_EINVAL), (dict(scale=INF), lt.LT_EINVAL),
-    (dict(scale=3e38), lt.LT_EINVAL), (dict(scale=1e300), lt.LT_EINVAL), (dict(scale=1e-40), lt.LT_EINVAL),
+    (dict(scale=3e38), lt.LT_EINVAL), (dict(scale=1e300), lt.LT_EINVAL), (dict(scale=7e-31), lt.LT_EINVAL),
     (dict(logits=None), lt.LT_EINVAL),
     (dict(logits=P + 1), lt.LT_EINVAL), (dict(cum=None), lt.LT_EINVAL), (dict(score=None), lt.LT_EINVAL),
     (dict(beam=None), lt.LT_EINVAL), (dict(token=None), lt.LT_EINVAL), (dict(score=P), lt.LT_EINVAL),
