@@ -483,9 +483,9 @@ int lt_token_logprobs_backward(const void* logits, lt_dtype dtype, int64_t ld, i
    are float32 and each rounded.
    x, out     [num_tokens, num_heads, head_dim], token_stride and head_stride values
               apart (2^31 at most); float32 or bfloat16, of out the same or bfloat16. No alignment
-              beyond the elements' (16-byte aligned rows whose part fills vectors of 8
-              are fastest). out may be x with the same type and strides; it must not
-              overlap x otherwise.
+              beyond the elements' (fastest: 16-byte aligned rows; in place, parts that
+              vectors of 8 fill). out may be x with the same type and strides; it must
+              not overlap x otherwise.
    positions  DEVICE int32 [num_tokens]. A token of negative position (padding)
               becomes zeros.
    inv_freq   DEVICE float32 [num_pairs], in radians per position (not read for 0).

@@ -294,7 +294,8 @@ struct RotaryArgs {
   bool in_f32, out_f32;
   // resolved by rotary_shape
   int vec;                  // values of a vector: 8, 4, 2 or 1
-  int units;                // vector pairs of a head
+  int front, part, back;    // vectors before, in and behind the rotated part (halves: of a half)
+  int units;                // of a head: two vectors each
   int lanes;                // that share a head
   int head_lanes;           // of a token: each takes every head_lanes-th head
 };

@@ -65,8 +65,8 @@ __device__ __forceinline__ float bf16_float(uint32_t h) { return __uint_as_float
 // Nearest bfloat16, ties to even.
 __device__ __forceinline__ uint16_t float_bf16(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
 
-// N values as they lie in memory, loaded at N * sizeof(T) alignment (16 bytes at most),
-// and as float32.
+// N values as they lie in memory, at their own alignment (the hardware takes wide loads
+// and stores at any), and as float32.
 template <class T, int N>
 struct Raw {
   static constexpr int kBytes = N * (int)sizeof(T);
@@ -75,14 +75,16 @@ struct Raw {
     if constexpr (kBytes >= 16) {
 #pragma unroll
       for (int i = 0; i < kBytes / 16; ++i) {
-        const uint4 a = reinterpret_cast<const uint4*>(p)[i];
+        uint4 a;
+        __builtin_memcpy(&a, p + i * (16 / sizeof(T)), 16);
         w[4 * i] = a.x, w[4 * i + 1] = a.y, w[4 * i + 2] = a.z, w[4 * i + 3] = a.w;
       }
     } else if constexpr (kBytes == 8) {
-      const uint2 a = *reinterpret_cast<const uint2*>(p);
+      uint2 a;
+      __builtin_memcpy(&a, p, 8);
       w[0] = a.x, w[1] = a.y;
     } else if constexpr (kBytes == 4) {
-      w[0] = *reinterpret_cast<const uint32_t*>(p);
+      __builtin_memcpy(&w[0], p, 4);
     } else {
       w[0] = *reinterpret_cast<const uint16_t*>(p);
     }
@@ -107,11 +109,12 @@ template <int N>
 __device__ __forceinline__ void store_values(float* p, const float (&x)[N]) {
   if constexpr (N >= 4) {
 #pragma unroll
-    for (int i = 0; i < N; i += 4) *reinterpret_cast<float4*>(p + i) = float4{x[i], x[i + 1], x[i + 2], x[i + 3]};
-  } else if constexpr (N == 2) {
-    *reinterpret_cast<float2*>(p) = float2{x[0], x[1]};
+    for (int i = 0; i < N; i += 4) {
+      const float4 a = {x[i], x[i + 1], x[i + 2], x[i + 3]};
+      __builtin_memcpy(p + i, &a, 16);
+    }
   } else {
-    *p = x[0];
+    __builtin_memcpy(p, x, 4 * N);
   }
 }
 template <int N>
@@ -122,9 +125,15 @@ __device__ __forceinline__ void store_values(uint16_t* p, const float (&x)[N]) {
     uint32_t w[N / 2];
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) w[i] = (uint32_t)float_bf16(x[2 * i]) | (uint32_t)float_bf16(x[2 * i + 1]) << 16;
-    if constexpr (N == 8) *reinterpret_cast<uint4*>(p) = uint4{w[0], w[1], w[2], w[3]};
-    else if constexpr (N == 4) *reinterpret_cast<uint2*>(p) = uint2{w[0], w[1]};
-    else *reinterpret_cast<uint32_t*>(p) = w[0];
+    if constexpr (N == 8) {
+      const uint4 a = {w[0], w[1], w[2], w[3]};
+      __builtin_memcpy(p, &a, 16);
+    } else if constexpr (N == 4) {
+      const uint2 a = {w[0], w[1]};
+      __builtin_memcpy(p, &a, 8);
+    } else {
+      __builtin_memcpy(p, &w[0], 4);
+    }
   }
 }
 

@@ -328,3 +328,29 @@ def test_argument_errors_raise(lib):
         with pytest.raises(lt.LiteTopKError):
             call()
             print("call %d was taken" % i)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("d,n,start", [(64, 13, 0), (80, 27, 0), (64, 13, 9), (33, 9, 8), (1024, 505, 14), (1023, 501, 10),
+                                       (17, 4, 0), (18, 8, 1), (40, 12, 16), (19, 5, 9)])
+def test_parts_that_fill_no_vectors(lib, dtype, interleaved, d, n, start):
+    """Vectors may cover the end of a length twice, in a result of its own: equal to the
+    rotation in place, which covers it once, and to that of the same rows at an odd address."""
+    tokens, heads = 37, 5
+    x, pos, rot = _x(tokens, heads, d, dtype, 21).cuda(), _pos(tokens, 4000, 22), _rot(n, start, interleaved, 0.75)
+    got = lt.rotary(x, pos.cuda(), rot)
+    _check(got, x.cpu(), pos, rot)
+    room = torch.full((tokens * heads * d + 3,), 7.0, dtype=x.dtype, device="cuda")
+    odd = room[1:-2].view(tokens, heads, d)
+    odd.copy_(x)
+    assert torch.equal(lt.rotary(odd, pos.cuda(), rot), got)
+    codes, scales = lt.rotary_fp8(x, pos.cuda(), rot)
+    lt.rotary(odd, pos.cuda(), rot, out=odd)
+    assert torch.equal(odd, got) and torch.all(room[:1] == 7.0) and torch.all(room[-2:] == 7.0)
+    # fp8: half a step of the float32 rotation, whose own error is in _limit
+    want = orc.rotary(x.cpu(), pos, rot.inv_freq.cpu(), rot.start, rot.interleaved, rot.amplitude, False)
+    wide = scales.double().cpu()[..., None]
+    err = (codes.cpu().view(torch.float8_e4m3fn).double() * wide - want).abs()
+    lim = _limit(x.cpu(), rot, n) * (1 + 2 ** -4) + torch.maximum(2.0 ** -4 * want.abs(), 2.0 ** -10 * wide)
+    assert torch.all(err <= lim)
