@@ -499,7 +499,8 @@ int lt_rotary(const void* x, lt_dtype dtype, int64_t token_stride, int64_t head_
    [num_tokens, num_heads, head_dim] contiguous and scales float32 [num_tokens,
    num_heads]. The scale is the smallest power of two 2^e with max|y| <= 448 * 2^e
    (never below 2^-126), values round to the nearest code (halfway: the even one). A
-   head that holds a value that is not finite gets the scale NaN and codes of 0. */
+   head that holds a value that is not finite gets the scale NaN and codes of 0. The
+   results must not overlap the inputs. */
 int lt_rotary_fp8(const void* x, lt_dtype dtype, int64_t token_stride, int64_t head_stride, int32_t num_tokens,
                   int32_t num_heads, int32_t head_dim, const int32_t* positions, const float* inv_freq,
                   int32_t num_pairs, int32_t rotary_start, double amplitude, uint32_t flags, uint8_t* codes,
