@@ -224,8 +224,8 @@ def fp8_exponent(top: float) -> int:
 def beam_scores(logits, cum, scale=1.0):
     """Scores [requests, beams, vocab] in 64 bits; -inf for what is no candidate."""
     reqs, beams = cum.shape
-    x = logits.double().reshape(reqs, beams, -1) * scale
-    y = cum.double()[..., None] + (x - torch.logsumexp(x, -1, keepdim=True))
+    x = logits.double().reshape(reqs, beams, -1)
+    y = cum.double()[..., None] + _log_softmax(x, scale)[1]
     bad = ~torch.isfinite(x.masked_fill(x == -math.inf, 0.0)).all(-1) | ~(cum > -math.inf)
     y[bad] = -math.inf
     y[torch.isnan(y)] = -math.inf     # a row of nothing but -inf

@@ -1,7 +1,11 @@
 // Beam search's selection: of a request's beams w, each with a score c_w and a row
 // of logits x_w, the `top` best continuations by
 //
-//   score(w, v) = c_w + scale x_wv - lse_w,   lse_w = log sum_v exp(scale x_wv).
+//   score(w, v) = c_w + scale x_wv - lse_w,   lse_w = log sum_v exp(scale x_wv),
+//
+// computed from the row's largest logit m as c_w + (scale (x_wv - m_w) - log s_w) with
+// s_w = sum_v exp(scale (x_wv - m_w)): scale m_w may be so large (a mask of the type's
+// lowest value) that log s_w is lost beside it.
 //
 // Order: larger score (float32) first; equal ones by beam, then by logit, then by
 // token. Within a beam the score rises with the logit, so a beam's best `top` logits
@@ -12,7 +16,7 @@
 // Scores of different beams lie close together (a step of float32 at 20 is 2e-6), and
 // their order is the result, so the sums are kept better than float32: a lane adds
 // up 2^((x - m) scale log2 e) relative to its own largest logit m in short float32
-// chains, those in float64; scale log2 e is two float32 numbers, and lse and score
+// chains, those in float64; scale log2 e is two float32 numbers, and log s and score
 // are float64 until the score's one rounding.
 //
 // Bound by reading the logits: 512 rows of 131072 in bfloat16 (134 MB), 16 of 8 beams:
@@ -413,9 +417,10 @@ constexpr int kMost = 512;     // candidates that are ranked together
 constexpr int kHeld = 8;       // keys that a thread holds in registers
 
 __global__ __launch_bounds__(kThreads) void k_beam_join(BeamArgs a, Part part, int lanes_log2) {
-  extern __shared__ double lse[];             // [beams]: of the rows that were read,
-  float* cum = reinterpret_cast<float*>(lse + a.beams);  // their beams' scores
-  int* beam = reinterpret_cast<int*>(cum + a.beams);     // and the beams
+  extern __shared__ double logs[];            // [beams]: of the rows that were read log s,
+  float* tip = reinterpret_cast<float*>(logs + a.beams);  // m,
+  float* cum = tip + a.beams;                             // their beams' scores
+  int* beam = reinterpret_cast<int*>(cum + a.beams);      // and the beams
   __shared__ Candidate found[kMost];
   __shared__ __align__(16) uint32_t tops[kThreads];
   __shared__ int count;
@@ -466,7 +471,8 @@ __global__ __launch_bounds__(kThreads) void k_beam_join(BeamArgs a, Part part, i
     }
     if (w < share.beams && sub == 0) {
       const float f = cums[beam[w]];
-      lse[w] = f > ninf() ? (double)m * a.scale + log(s) : (double)__builtin_nanf("");
+      logs[w] = f > ninf() ? log(s) : (double)__builtin_nanf("");
+      tip[w] = m;
       cum[w] = f;
     }
   }
@@ -474,7 +480,8 @@ __global__ __launch_bounds__(kThreads) void k_beam_join(BeamArgs a, Part part, i
   auto rank_of = [&](int i, uint64_t key) {
     if (!key) return 0ull;
     const int w = (uint32_t)i / (uint32_t)per;
-    const float score = (float)((double)cum[w] + ((double)key_float((uint32_t)(key >> 32)) * a.scale - lse[w]));
+    const double below = (double)key_float((uint32_t)(key >> 32)) - (double)tip[w];
+    const float score = (float)((double)cum[w] + (below * a.scale - logs[w]));
     return score > ninf() ? (unsigned long long)ord_key(score) << 32 | (0xFFFFFFFFu - (uint32_t)w) : 0ull;
   };
   // f(rank, key) of each of the thread's keys
@@ -609,7 +616,7 @@ hipError_t launch_beam_select(BeamArgs a, void* workspace, hipStream_t st) {
   else k_beam_part<float, kWaves><<<all, kThreads, 0, st>>>(a, part);
   int lanes_log2 = 0;
   while (lanes_log2 < 6 && 1 << lanes_log2 < a.splits * a.waves) ++lanes_log2;
-  k_beam_join<<<dim3((unsigned)a.batch), kThreads, (size_t)a.beams * 16, st>>>(a, part, lanes_log2);
+  k_beam_join<<<dim3((unsigned)a.batch), kThreads, (size_t)a.beams * 20, st>>>(a, part, lanes_log2);
   return hipGetLastError();
 }
 

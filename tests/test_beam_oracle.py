@@ -61,6 +61,16 @@ def test_beam_scores_by_hand():
     assert torch.allclose(y, torch.tensor([want], dtype=torch.float64))
 
 
+@pytest.mark.parametrize("low", [-1e30, torch.finfo(torch.float32).min, torch.finfo(torch.bfloat16).min, 1e30])
+def test_beam_scores_of_far_rows(low):
+    """Where a row lies does not matter: equal values share the probability, however large they are."""
+    x = torch.tensor([[low] * 4, [low] * 2 + [-math.inf] * 2, [2.0 * low if low < -1e38 else -abs(low)] * 4], dtype=torch.float64)
+    cum = torch.tensor([[-3.0, -1.0, -2.0]])
+    y = orc.beam_scores(x, cum)[0]
+    want = [[-3.0 - math.log(4)] * 4, [-1.0 - math.log(2)] * 2 + [-math.inf] * 2, [-2.0 - math.log(4)] * 4]
+    assert torch.allclose(y, torch.tensor(want, dtype=torch.float64), rtol=0, atol=1e-12)
+
+
 def test_reorder_by_hand():
     # two rows share page 4; row 0 has 5, row 1 has 6; three tokens a... page of 2: lengths 3
     table, lens = [[4, 5, -1], [4, 6, -1]], [3, 3]

@@ -125,6 +125,54 @@ def test_masks_and_beams_that_are_not_alive(lib, dtype, vocab):
     _check(x, cum, top)
 
 
+def _alike(cum, n):
+    """What n equal logits score, and how far off a float32 may be: the terms are 1, their sum exact, the logarithm
+    a few 2^-52 of itself; then one rounding."""
+    want = cum - math.log(n)
+    return want, 2.0 ** -24 * abs(want) + 1e-13
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab", [7, 300, 30011])
+@pytest.mark.parametrize("scale", [1.0, 0.7, 100.0])
+def test_rows_of_the_lowest_values(lib, dtype, vocab, scale):
+    """By hand: a row of one value gives every token cum - log(vocab), a mask's lowest value or any other,
+    and so does what a row keeps of a mask that leaves n equal ones."""
+    low = torch.finfo(TYPES[dtype]).min
+    values = [low, -low, -1e30, 1e30, 1e15, -1e12, 0.0]
+    top, beams = 6, 2
+    x = torch.zeros(len(values), beams, vocab, dtype=TYPES[dtype])
+    for r, v in enumerate(values):
+        x[r, 0] = v
+        x[r, 1], x[r, 1, 1:6] = low, max(v, -1e30)     # five equal ones above a mask
+    cum = torch.tensor([[-3.0, -3.0 - 2 * math.log(vocab)]]).repeat(len(values), 1)
+    r = lt.beam_select(x.view(-1, vocab).cuda(), cum.cuda(), top, scale=scale)
+    want, tol = _alike(-3.0, vocab)
+    n = min(top, vocab)
+    assert torch.all((r.score[:, :n].cpu().double() - want).abs() <= tol)
+    assert torch.all(r.beam[:, :n] == 0) and torch.equal(r.token[:, :n].cpu(), torch.arange(n).int().repeat(len(values), 1))
+    # the second beam alone
+    cum[:, 0], cum[:, 1] = -INF, -2.0
+    r = lt.beam_select(x.view(-1, vocab).cuda(), cum.cuda(), 5, scale=scale)
+    want, tol = _alike(-2.0, 5)
+    assert torch.all((r.score.cpu().double() - want).abs() <= tol)
+    assert torch.all(r.beam == 1) and torch.equal(r.token.cpu(), torch.arange(1, 6).int().repeat(len(values), 1))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_row_of_the_lowest_values_beside_others(lib, dtype):
+    """It takes its place among its request's beams, not before them, and so does a row of one large value
+    (in the second request)."""
+    reqs, beams, vocab = 2, 4, 5003
+    x, cum = _draw(reqs * beams, vocab, dtype, 21), torch.full((reqs, beams), -4.0)
+    rows = x.view(reqs, beams, vocab)
+    rows[:, 2] = torch.finfo(rows.dtype).min
+    rows[1, 3] = 3e38
+    r = lt.beam_select(x.cuda(), cum.cuda(), 1)
+    assert torch.all(r.beam != 2) and r.beam[1, 0] != 3
+    _check(x, cum, 40)
+
+
 @pytest.mark.parametrize("dtype,pad,shift", [("bf16", 1, 0), ("bf16", 0, 3), ("f32", 5, 1), ("f32", 0, 0)])
 def test_strided_and_unaligned_rows(lib, dtype, pad, shift):
     reqs, beams, vocab, top = 3, 3, 4999, 7
