@@ -513,7 +513,8 @@ int lt_rotary_fp8(const void* x, lt_dtype dtype, int64_t token_stride, int64_t h
    lt_cache4_attention reads it (q NULL: none; num_heads is then 0). positions int32
    [rows]: a row of negative position writes nothing to the cache, and its query
    becomes zeros. Other arguments as for lt_cache4_append and lt_rotary; flags:
-   LT_ROTARY_INTERLEAVED. q rows need no alignment. */
+   LT_ROTARY_INTERLEAVED. q rows need no alignment. q_out must not overlap any other
+   argument. */
 int lt_cache4_append_rotary(const void* k, const void* v, lt_dtype dtype, int64_t k_stride, int64_t v_stride,
                             int64_t rows, uint8_t* codes, uint8_t* scales, int64_t num_pages, int32_t page_size,
                             int32_t num_kv_heads, int32_t head_dim, const int64_t* slots, const int32_t* positions,

@@ -941,9 +941,13 @@ int lt_cache4_append_rotary(const void* k, const void* v, lt_dtype dtype, int64_
   if (k_stride < width || v_stride < width || k_stride % unit || v_stride % unit) return LT_EINVAL;
   if (!k || !v || !slots || !aligned(k, 16) || !aligned(v, 16) || !aligned(slots, 8)) return LT_EINVAL;
   if (!positions || !aligned(positions, 4)) return LT_EINVAL;
-  if (q && (!q_out || !aligned(q_out, 16) || !aligned(q, dtype == LT_F32 ? 4 : 2) || q == q_out ||
+  if (q && (!q_out || !aligned(q_out, 16) || !aligned(q, dtype == LT_F32 ? 4 : 2) ||
             q_stride < (int64_t)num_heads * d))
     return LT_EINVAL;
+  // blocks of queries run beside those that read the rest and write the cache
+  const void* others[] = {q, k, v, slots, positions, pairs > 0 ? freq : nullptr, codes, scales};
+  for (const void* o : others)
+    if (q && q_out == o) return LT_EINVAL;
   AppendRotaryArgs a{};
   a.k = k;
   a.v = v;

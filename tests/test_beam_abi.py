@@ -74,6 +74,16 @@ def test_append_rotary_refusals(over, code):
     assert lt.lt_cache4_append_rotary(*a.values()) == code
 
 
+@pytest.mark.parametrize("name", ["k", "v", "slots", "pos", "freq", "codes", "scales", "q"])
+def test_append_rotary_refuses_queries_in_the_place_of_another_argument(name):
+    """Blocks of one launch write the queries while others read the rest, or write the cache."""
+    a = dict(k=P, v=2 * P, dtype=lt.LT_BF16, ks=256, vs=256, rows=3, codes=3 * P, scales=4 * P, pages=4, page=16, heads=2,
+             d=128, slots=5 * P, pos=6 * P, freq=7 * P, pairs=64, start=0, amp=1.0, flags=0, q=8 * P, qs=1024, hq=8,
+             q_out=9 * P, stream=None)
+    a["q_out"] = a[name]
+    assert lt.lt_cache4_append_rotary(*a.values()) == lt.LT_EINVAL
+
+
 @pytest.mark.parametrize("over,code", [
     (dict(dtype=lt.LT_FP8_E4M3FN), lt.LT_EUNSUPPORTED), (dict(batch=-1), lt.LT_EINVAL), (dict(beams=0), lt.LT_EINVAL),
     (dict(top=0), lt.LT_EINVAL), (dict(top=65), lt.LT_EUNSUPPORTED), (dict(vocab=-1), lt.LT_EINVAL),
