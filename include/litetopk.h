@@ -546,7 +546,8 @@ size_t lt_beam_select_workspace_size(lt_dtype dtype, int32_t batch, int32_t beam
    out_score  float32 [batch, top], out_beam and out_token int32 [batch, top], best
               first. Only scores above -inf are candidates (a logit of -inf is masked
               out; a beam whose logits hold NaN or +inf has none); where there are
-              fewer than `top` of them, -inf, -1 and -1 follow. */
+              fewer than `top` of them, -inf, -1 and -1 follow.
+   Results and workspace must not overlap each other or an input. */
 int lt_beam_select(const void* logits, lt_dtype dtype, int64_t ld, int32_t batch, int32_t beams, int32_t vocab,
                    const float* cum, double scale, int32_t top, float* out_score, int32_t* out_beam,
                    int32_t* out_token, void* workspace, size_t workspace_bytes, void* stream);

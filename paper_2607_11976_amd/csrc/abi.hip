@@ -1018,9 +1018,13 @@ int lt_beam_select(const void* logits, lt_dtype dtype, int64_t ld, int32_t batch
   if ((vocab > 0 && !logits) || !aligned(logits, a.bf16 ? 2 : 4)) return LT_EINVAL;
   if (!cum || !out_score || !out_beam || !out_token) return LT_EINVAL;
   if (!aligned(cum, 4) || !aligned(out_score, 4) || !aligned(out_beam, 4) || !aligned(out_token, 4)) return LT_EINVAL;
-  if ((const float*)out_score == cum || (const void*)out_beam == cum || (const void*)out_token == cum) return LT_EINVAL;
   if (!workspace || !aligned(workspace, 256)) return LT_EINVAL;
   if (workspace_bytes < beam_workspace_bytes(a)) return LT_EWORKSPACE;
+  // blocks write the workspace and their request's results while others still read
+  const void* places[] = {out_score, out_beam, out_token, workspace, cum, vocab > 0 ? logits : nullptr};
+  for (int i = 0; i < 4; ++i)
+    for (int j = i + 1; j < 6; ++j)
+      if (places[i] == places[j]) return LT_EINVAL;
   a.logits = logits;
   a.ld = ld;
   a.cum = cum;

@@ -103,6 +103,18 @@ def test_beam_refusals(over, code):
     assert lt.lt_beam_select(*a.values()) == code
 
 
+@pytest.mark.parametrize("one,other", [
+    ("score", "beam"), ("score", "token"), ("beam", "token"), ("score", "logits"), ("beam", "logits"), ("token", "logits"),
+    ("score", "cum"), ("beam", "cum"), ("token", "cum"), ("score", "ws"), ("beam", "ws"), ("token", "ws"),
+    ("ws", "logits"), ("ws", "cum")])
+def test_beam_refuses_results_in_the_place_of_another_argument(one, other):
+    """A request's block writes its results while others read theirs."""
+    a = dict(logits=P, dtype=lt.LT_BF16, ld=1000, batch=3, beams=4, vocab=1000, cum=2 * P, scale=1.0, top=8, score=3 * P,
+             beam=4 * P, token=5 * P, ws=6 * P, bytes=1 << 40, stream=None)
+    a[one] = a[other]
+    assert lt.lt_beam_select(*a.values()) == lt.LT_EINVAL
+
+
 def test_beam_workspace_sizes():
     size = lt.lt_beam_select_workspace_size
     assert size(lt.LT_BF16, 3, 4, 1000, 65) == 0 and size(lt.LT_FP8_E4M3FN, 3, 4, 1000, 8) == 0
