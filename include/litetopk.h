@@ -582,7 +582,8 @@ size_t lt_paged_reorder_workspace_size(int32_t num_rows);
                  list has no page for its copy.
    The call is a function of its inputs and writes to free_pages only before *free_used:
    calling it again with the same arguments gives the same result. No result may lie in
-   the place of an input (free_pages apart).
+   the place of an input (free_pages apart) or of another result, and the workspace in
+   neither's.
    Limits: num_rows a multiple of group, at most LT_PLAN_MAX_REQUESTS; num_rows *
    table_width < 2^31. workspace 256-byte aligned; contents on entry do not matter. */
 int lt_paged_reorder(const int32_t* block_table, int64_t table_ld, int32_t table_width, const int32_t* seq_lens,

@@ -1062,6 +1062,17 @@ int lt_paged_reorder(const int32_t* block_table, int64_t table_ld, int32_t table
   const void* kept[] = {block_table, seq_lens, parents, keep_pages, free_used};
   for (const void* i : kept)
     if (i && i == free_pages) return LT_EINVAL;
+  // nor in another's, and the workspace apart from both (empty ones may lie anywhere)
+  const bool any = rows > 0, pages = any && table_width > 0;
+  const void* apart[] = {pages ? new_table : nullptr, any ? new_lens : nullptr, any ? copies : nullptr, free_used_out,
+                         any ? status : nullptr};
+  for (int i = 0; i < 5; ++i)
+    for (int j = i + 1; j < 5; ++j)
+      if (apart[i] && apart[i] == apart[j]) return LT_EINVAL;
+  for (const void* o : apart)
+    if (workspace == o) return LT_EINVAL;
+  for (const void* i : in)
+    if (workspace == i) return LT_EINVAL;
   ReorderArgs a{};
   a.table = block_table;
   a.lens = seq_lens;

@@ -150,6 +150,20 @@ def test_reorder_refusals(over, code):
     assert lt.lt_paged_reorder(*a.values()) == code
 
 
+RESULTS = ["new_table", "new_lens", "copies", "used_out", "status"]
+READ = ["table", "lens", "parents", "keep", "used", "free"]
+
+
+@pytest.mark.parametrize("one,other", [(o, r) for i, o in enumerate(RESULTS) for r in RESULTS[i + 1:]]
+                         + [("ws", n) for n in RESULTS + READ])
+def test_reorder_refuses_results_in_the_place_of_another_argument(one, other):
+    a = dict(table=P, ld=9, width=9, lens=2 * P, parents=3 * P, rows=8, group=4, page=16, keep=4 * P, free=5 * P,
+             nfree=50, used=6 * P, new_table=7 * P, new_ld=9, new_lens=8 * P, copies=9 * P, used_out=10 * P,
+             status=11 * P, ws=12 * P, bytes=1 << 40, stream=None)
+    a[one] = a[other]
+    assert lt.lt_paged_reorder(*a.values()) == lt.LT_EINVAL
+
+
 def test_reorder_workspace_sizes():
     size = lt.lt_paged_reorder_workspace_size
     assert size(-1) == 0 and size(lt.LT_PLAN_MAX_REQUESTS + 1) == 0
