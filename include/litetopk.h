@@ -478,9 +478,9 @@ int lt_token_logprobs_backward(const void* logits, lt_dtype dtype, int64_t ld, i
    2 num_pairs) is turned, pair i of token t by the angle a = positions[t] *
    inv_freq[i]:
      y1 = x1 c - x2 s,  y2 = x2 c + x1 s,  c = amplitude cos a,  s = amplitude sin a;
-   other values pass as they are. The angle is taken in 64 bits (exact frequencies
-   stay exact at any position), c and s are rounded to float32, the products and sums
-   are float32 and each rounded.
+   other values pass as they are. The angle is taken in 64 bits, off by 2^-51 of itself
+   at most (less than float32's 2^-24 up to 2^27 rad), c and s are rounded to float32,
+   the products and sums are float32 and each rounded.
    x, out     [num_tokens, num_heads, head_dim], token_stride and head_stride values
               apart (2^31 at most); float32 or bfloat16, of out the same or bfloat16. No alignment
               beyond the elements' (fastest: 16-byte aligned rows; in place, parts that

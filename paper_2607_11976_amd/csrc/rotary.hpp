@@ -5,11 +5,13 @@
 //
 // A position times a frequency passes float32's 24 bits long before a context of
 // 2^20 tokens ends (its error would be 0.06 rad there), so the angle is taken in
-// 64 bits, in quarter turns, and its sine and cosine are 64-bit Taylor sums over
+// 64 bits, in quarter turns (four roundings of 2^-53 at most, together less than
+// 2^-51 of the angle), and its sine and cosine are 64-bit Taylor sums over
 // |x| <= pi / 4 (remainder below 2^-41): about 20 fused multiply-adds a pair, which
 // a thread shares over the heads that it turns. They are rounded to float32 once,
 // after the amplitude; products and sums are float32, each rounded by itself, so
-// that a plain float32 program gets the same bits.
+// that a plain float32 program gets the same bits (but where a sine lies within 2^-41
+// of a border between two float32 numbers).
 #pragma once
 
 #include <hip/hip_runtime.h>

@@ -7,6 +7,8 @@ are better than 2^-35), then a product and a sum each (2^-24): of y = x1 c - x2 
 products, below 2^-46. Written as bfloat16 half a step more (2^-8 of the value), as e4m3
 2^-4 of the value or half the smallest step (2^-10 times the scale)."""
 import math
+from decimal import Decimal
+from fractions import Fraction
 
 import numpy as np
 import pytest
@@ -94,6 +96,26 @@ def test_far_positions(lib, far):
     a = x.double().abs()
     both = torch.cat([a[..., :64] + a[..., 64:]] * 2, -1)
     assert torch.all((got.cpu().double() - want).abs() <= both * (3.01 * STEP + far * 2.0 ** -51))
+
+
+@pytest.mark.parametrize("far", [1 << 20, 1 << 27, 0x7FFFFFFF])
+@pytest.mark.parametrize("inverse", [False, True])
+def test_far_angles_pair_by_pair(lib, far, inverse):
+    """Against exact angles: pi / 2 as a 64-bit number is off by 2^-54 of itself, its quotient, the frequency's product
+    and the position's by 2^-53 each, so an angle by 2^-51 of itself at most; c and s and the products as above."""
+    pi = Fraction(Decimal("3.14159265358979323846264338327950288419716939937510582097494"))
+    x, rot = _x(6, 2, 128, "f32", 4), _rot(64)
+    pos = [far, far - 1, far - 12345, far // 3, 65537, 1]
+    call = lt.rotary_backward if inverse else lt.rotary
+    got = call(x.cuda(), torch.tensor(pos, dtype=torch.int32, device="cuda"), rot).cpu().double()
+    for t, p in enumerate(pos):
+        for i, f in enumerate(rot.inv_freq.tolist()):
+            a = Fraction(f) * p
+            r = float(a - 2 * pi * round(a / (2 * pi))) * (-1 if inverse else 1)
+            u, v = x[t, :, i].double(), x[t, :, 64 + i].double()
+            lim = (u.abs() + v.abs()) * (3.01 * STEP + float(a) * 2.0 ** -51)
+            assert torch.all((got[t, :, i] - (u * math.cos(r) - v * math.sin(r))).abs() <= lim), (p, i)
+            assert torch.all((got[t, :, 64 + i] - (v * math.cos(r) + u * math.sin(r))).abs() <= lim), (p, i)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
