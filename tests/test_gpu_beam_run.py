@@ -46,6 +46,23 @@ def test_one_beam_is_greedy(lib):
         assert logits.argmax(-1).item() == tokens[r, 0, 0].item()
 
 
+def test_one_beam_is_greedy_at_every_step(lib):
+    """Decoded on with the search's own tokens, in the same batch and without selecting or reordering rows, every
+    step's best logit is the token that the search took next, and its score is the sum of their log probabilities:
+    each step adds the log sum's error and rounds a score of this size once."""
+    prompts, steps = _prompts((13, 30)), 6
+    tokens, scores = ex.beam_search(prompts, 1, steps)
+    dec = ex.BeamDecoder(ex.weights(0), len(prompts), 1, max(len(p) for p in prompts) + steps)
+    logits, one = dec.prompt(prompts), torch.ones(len(prompts), dtype=torch.int32, device="cuda")
+    total = torch.zeros(len(prompts), dtype=torch.float64, device="cuda")
+    for i in range(steps):
+        assert torch.equal(logits.argmax(-1), tokens[:, 0, i])
+        total += torch.log_softmax(logits.double(), -1).amax(-1)
+        logits = dec.step(tokens[:, 0, i], one)
+    slack = (2 * math.log(ex.VOCAB) + 2 * (ex.VOCAB // 1024 + 41) + 10) * 2.0 ** -24    # as in test_log_sums
+    assert torch.all((scores[:, 0].double() - total).abs() <= steps * (slack + 2.0 ** -24 * total.abs()))
+
+
 def test_pages_come_back(lib):
     """Beams that are given up return their pages: after a long search as many are in use as the
     surviving rows hold."""
