@@ -173,6 +173,36 @@ def test_a_row_of_the_lowest_values_beside_others(lib, dtype):
     _check(x, cum, 40)
 
 
+def _upper(score):
+    """The upper half of a score's float32 as it is ordered (no score is above 0)."""
+    return -(score.float().view(torch.int32) & 0x7FFFFFFF) >> 16
+
+
+@pytest.mark.parametrize("kind,reqs,beams,vocab,top,cum", [
+    ("equal", 2, 16, 20011, 64, -3.0), ("equal", 1, 64, 5000, 64, -3.0), ("equal", 2, 200, 50, 64, -3.0),
+    ("few", 2, 16, 9000, 64, -3.0), ("random", 2, 32, 20000, 64, -600.0), ("random", 1, 16, 128000, 64, -1000.0),
+    ("random", 1, 100, 2000, 40, -5000.0), ("dead", 2, 100, 300, 50, -3.0), ("dead", 3, 64, 700, 64, -900.0)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_joins_of_many(lib, kind, reqs, beams, vocab, top, cum, dtype):
+    """More than 512 of the beams' best reach what the n-th best has in its upper 16 bits: equal scores, or
+    different ones far from 0, where those bits tell them apart by 4 and more. The join takes them one by one."""
+    x = _draw(reqs * beams, vocab, dtype, 41)
+    if kind in ("equal", "dead"):
+        x[:] = 1.5
+    elif kind == "few":
+        x = (x > 2.0).to(x.dtype)
+    c = torch.full((reqs, beams), cum)
+    if kind == "random":
+        c -= 3 * torch.rand(reqs, beams, generator=torch.Generator().manual_seed(42))
+    if kind == "dead":
+        c[:, 3::5], c[0, 1] = -INF, math.nan
+    y = orc.beam_scores(x, c)
+    mine = y.topk(min(top, vocab), -1).values.flatten(1)
+    mine = torch.where(mine > -INF, mine, -3e38)
+    assert torch.all((_upper(mine) >= _upper(mine.topk(top, -1).values[:, -1:])).sum(-1) > 520)
+    _check(x, c, top)
+
+
 @pytest.mark.parametrize("dtype,pad,shift", [("bf16", 1, 0), ("bf16", 0, 3), ("f32", 5, 1), ("f32", 0, 0)])
 def test_strided_and_unaligned_rows(lib, dtype, pad, shift):
     reqs, beams, vocab, top = 3, 3, 4999, 7
