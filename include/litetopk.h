@@ -536,8 +536,11 @@ size_t lt_beam_select_workspace_size(lt_dtype dtype, int32_t batch, int32_t beam
    candidates (w, v) with
      score = cum[b, w] + scale * logits[b * beams + w, v] - lse[b, w],
      lse = log sum_v exp(scale * logits),
-   the `top` of largest score. Scores are float32, rounded once; equal ones are ordered
-   by beam, then by logit (larger first), then by token.
+   the `top` of largest score. Scores are rounded to float32 once, from 64 bits in which
+   the log sum's terms are float32: it is off by (2 H + 2 j + 12) 2^-24 at most, H the
+   row's entropy and j how often a sum is brought to a larger maximum (2e-7 at most in
+   rows of 1000 to 260000; exact terms where all logits are equal). Equal scores are
+   ordered by beam, then by logit (larger first), then by token.
    logits     float32 or bfloat16 [batch * beams, vocab], ld >= vocab values between
               rows (no alignment beyond the elements').
    cum        float32 [batch, beams]: the beams' scores so far; -inf (or NaN): the beam

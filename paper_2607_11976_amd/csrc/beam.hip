@@ -17,7 +17,11 @@
 // their order is the result, so the sums are kept better than float32: a lane adds
 // up 2^((x - m) scale log2 e) relative to its own largest logit m in short float32
 // chains, those in float64; scale log2 e is two float32 numbers, and log s and score
-// are float64 until the score's one rounding.
+// are float64 until the score's one rounding. What is float32, the distances, exponents
+// and powers, makes log s wrong by (2 H + 2 j + 12) 2^-24 at most: 2 H for the first two,
+// H the row's entropy (it bounds the mean distance to the largest logit), 2 for every
+// power, of which there are 1 + j where a sum is brought j times to a larger m, 10 for
+// the chains. Measured: 2e-7 at most over rows of 1000 to 260000, 1e-8 in the mean.
 //
 // Bound by reading the logits: 512 rows of 131072 in bfloat16 (134 MB), 16 of 8 beams:
 // 27 us for the parts, 5.0 TB/s, and 5 for the join; 496 of 50001 in float32, 32 of 16

@@ -173,6 +173,34 @@ def test_a_row_of_the_lowest_values_beside_others(lib, dtype):
     _check(x, cum, 40)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["random", "rising", "falling", "equal"])
+@pytest.mark.parametrize("rows,vocab,scale", [(8, 32000, 1.0), (512, 1001, 0.7), (3, 131072, 1.4), (600, 20011, 1.0)])
+def test_log_sums(lib, dtype, kind, rows, vocab, scale):
+    """The log sum's own error: the beam's score so far is minus its best log probability, so that the result
+    lies near 0, where float32 resolves it. A term's distance and its exponent are rounded (2^-24 of the distance
+    each; weighted over the row at most 2 H, H its entropy, and what rescaling adds to a term's distance makes up
+    its distance to the row's largest), its power of two is off by 2^-23, and so is every factor that brings a
+    sum to a larger maximum: at most one a tile of 1024 (bf16: 2048) logits and 40 in the joins; chains and
+    their joining round ten times. Terms of equal logits are 1 and their sums exact."""
+    x = _draw(rows, vocab, dtype, 31)
+    if kind == "equal":
+        x[:] = 3.0
+    elif kind != "random":
+        x = x.sort(-1, descending=kind == "falling").values
+    logp = torch.log_softmax(x.double() * scale, -1)
+    best = logp.amax(-1, keepdim=True)
+    r = lt.beam_select(x.cuda(), (-best).float().cuda(), 1, scale=scale)
+    off = (r.score.cpu().double() - ((-best).float().double() + best)).abs()
+    p = logp.exp()
+    entropy = -torch.special.xlogy(p, p).sum(-1, keepdim=True)
+    moved = vocab // (2048 if dtype == "bf16" else 1024) + 40
+    if kind == "equal":
+        assert torch.all(off <= 1e-12)
+    else:
+        assert torch.all(off <= (2 * entropy + 2 * (1 + moved) + 10) * 1.01 * 2.0 ** -24)
+
+
 def _upper(score):
     """The upper half of a score's float32 as it is ordered (no score is above 0)."""
     return -(score.float().view(torch.int32) & 0x7FFFFFFF) >> 16
