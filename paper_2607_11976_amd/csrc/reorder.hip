@@ -238,8 +238,13 @@ __global__ __launch_bounds__(kThreads) void k_reorder_write(ReorderArgs a, const
   for (int r = blockIdx.x * kWaves + (t >> 6); r < a.R; r += waves) write_row(a, r, info, taken, given, m);
 }
 
-// Few rows: all in one block, one launch (a request of 4 beams and 4001 tokens:
-// 6.6 us, where the two kernels above take 6 each).
+// Few rows: all in one block, one launch, which saves the host's 4 us for another: with
+// cache4_copy from a program's loop a step takes 19.3 us where two launches take 23.5, with
+// tables 63 to 512 pages wide; with 2048 pages 32 rows take 25.1 and 23.3. On the GPU alone
+// (us in a graph, tables 63, 512, 2048 and 8192 wide): 4 rows 6.3, 7.6, 10.9, 24.8, by two
+// kernels 6.9, 8.1, 11.4, 25.0; 16 rows 9.0, 10.1, 14.6, 30.7 and 8.8, 10.1, 13.9, 28.2; 32
+// rows, two a wave, 11.7, 14.0, 22.4, 54 and 8.3, 9.8, 13.7, 28: the rule costs where tables
+// are long or the calls are in a graph; 64 rows take 20 and 8.5.
 constexpr int kFewRows = 32, kFewThreads = 1024;
 __global__ __launch_bounds__(kFewThreads) void k_reorder_few(ReorderArgs a, int lanes_log2) {
   __shared__ uint32_t part[2 * kFewThreads / 64], taken[kFewRows + 1], given[kFewRows + 1];

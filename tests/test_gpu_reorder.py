@@ -70,6 +70,19 @@ def test_matches_definition(lib, reqs, group, page, width, spare, few):
             assert got[name] == want[name], (seed, name)
 
 
+@pytest.mark.parametrize("reqs,group", [(1, 15), (15, 1), (4, 4), (2, 8), (1, 16), (17, 1), (1, 17), (6, 3), (31, 1), (2, 16),
+                                        (8, 4), (33, 1)])
+@pytest.mark.parametrize("page,width", [(16, 63), (4, 513)])
+def test_rows_of_one_launch_and_of_two(lib, reqs, group, page, width):
+    for seed in range(2):
+        table, lens, free, used, rng = _tree(reqs, group, page, width, 100 + seed, 7)
+        parents = [rng.choice(list(range(-1, group)) + [0, 0]) for _ in lens]
+        want = orc.paged_reorder(table, lens, parents, group, page, free, used)
+        got = _run(table, lens, parents, group, page, free, used)
+        for name in want:
+            assert got[name] == want[name], (seed, name)
+
+
 def test_no_pages_left(lib):
     # prompts in the first row of each group; all rows go on as it: copies beyond the list end
     group, page, width = 4, 16, 3
