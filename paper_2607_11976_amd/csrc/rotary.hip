@@ -393,7 +393,8 @@ __device__ __forceinline__ void append_pairs(const AppendRotaryArgs& a, const Ca
 }
 
 // Any other part: a thread takes 8 consecutive values of a key and reads each one's
-// partner by itself.
+// partner by itself. The same rows with 32 of 128 values turned in halves: 33 us, 20 where
+// whole blocks are.
 template <class T>
 __device__ __forceinline__ void append_keys(const AppendRotaryArgs& a, const Cache4& c, uint32_t block) {
   const int per_row = c.d / 8;  // lanes of a head: 8 or 16
@@ -490,7 +491,9 @@ void lanes_of(RotaryArgs& a, bool power) {
     while (a.lanes & (a.lanes - 1)) ++a.lanes;
 }
 
-// Groups of lanes of a token: as few as fill the GPU, so that each has several heads.
+// Groups of lanes of a token: as few as fill the GPU, so that each has several heads. (Few
+// heads get a group each, which takes the sines and cosines again: 48887 tokens of 3 heads
+// of 64 in bfloat16, 38 MB, 14 us, where the memory takes 7.6.)
 int lanes_for(int64_t threads, int heads, int64_t fill) {  // threads with one group a token
   return (int)std::min<int64_t>(std::max(heads, 1), (fill + std::max<int64_t>(threads, 1) - 1) / std::max<int64_t>(threads, 1));
 }

@@ -932,6 +932,10 @@ def rotary_frequencies(dim: int, base: float = 10000.0, method: str = "none", fa
               amplitude 0.1 ln(factor) + 1
     turns     the same with the ramp over the number of turns, from `low` (1) to `high` (4)
 
+    These are published methods: linear is position interpolation (Chen et al. 2023,
+    arXiv 2306.15595), ramp with its amplitude and the ramp over turns are those of Peng et
+    al. 2023 (YaRN, arXiv 2309.00071, which also describes the scaled base).
+
     amplitude overrides the method's (1 but for ramp)."""
     _need(dim >= 2 and dim % 2 == 0, "dim must be even and positive")
     _need(base > 0.0 and factor > 0.0, "base and factor must be positive")
